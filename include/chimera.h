@@ -509,6 +509,76 @@ int chimera_head_loss(int dtype, int tokens, int hidden, int vocab, const void* 
                       float* d_dlnf_b, float* d_dw_head, float* d_loss, void* d_workspace,
                       size_t workspace_bytes, void* hip_stream);
 
+/* The vocabulary projection and its cross-entropy without the logits: nothing of size [tokens, vocab] is kept or
+ * written.  h [tokens, hidden] with rows ldh apart, W [hidden, vocab] with rows ldw apart (ldw >= vocab; the columns between may hold anything), both
+ * in the given dtype; z = h W.  vocab is any number; hidden and the leading dimensions are multiples of 8, leading dimensions below 2^23, tokens up
+ * to 2^22, hidden to 2^16, vocab to 2^22; tensors 16-byte, the workspace 256-byte aligned.  A target outside [0, vocab) marks a token that does
+ * not count (padding): its loss is 0 and it takes no part in any gradient, whatever its hidden state holds.
+ *
+ * Forward (evaluation, scoring, or the first half of training):
+ *   d_lse[t] = logsumexp(z[t]),  d_loss_rows[t] = scale * (d_lse[t] - z[t, target[t]]),  d_loss[0] += their sum (d_loss may be NULL).
+ * Backward, given d_lse, with coef[t] = scale * d_dloss[t] (d_dloss NULL: scale), dz[t, v] = coef[t] * (exp(z[t, v] - d_lse[t]) - [v == target[t]]):
+ *   d_dh [tokens, hidden] (dtype, rows lddh apart) = dz W^T,  d_dw [hidden, vocab] (float, rows lddw apart, columns from vocab on left as they are)
+ *   += h^T dz, or = with overwrite != 0.  Either may be NULL, not both.  z is formed again, `piece` columns of the vocabulary at a time (rounded up to
+ *   a multiple of 256; 0: the library's choice); the workspace grows with it.
+ * bf16: dh is formed from dz rounded to bf16 (2^-8 a term), dW from dz in 22 bits, so that it is as exact as a sum of floats; the products' sums are float.
+ * All sums have a fixed order.  ENOMEM if the workspace is too small (a function of the same sizes; 0 for sizes that the calls refuse). */
+size_t chimera_op_linear_xent_fwd_workspace_bytes(int dtype, int tokens, int hidden, int vocab);
+int chimera_op_linear_xent_fwd(int dtype, int tokens, int hidden, int vocab, const void* d_h, int ldh, const void* d_w, int ldw,
+                               const int32_t* d_targets, float scale, float* d_loss_rows, float* d_lse, float* d_loss,
+                               void* d_workspace, size_t workspace_bytes, void* hip_stream);
+size_t chimera_op_linear_xent_bwd_workspace_bytes(int dtype, int tokens, int hidden, int vocab, int piece);
+int chimera_op_linear_xent_bwd(int dtype, int tokens, int hidden, int vocab, const void* d_h, int ldh, const void* d_w, int ldw,
+                               const int32_t* d_targets, const float* d_lse, float scale, const float* d_dloss, void* d_dh, int lddh,
+                               float* d_dw, int lddw, int overwrite, int piece, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+/* chimera_head_loss on these two: the same results (tokens whose target lies outside [0, vocab) do not count here; their rows of y
+ * still have to be finite) without its [tokens, vocab] workspace, for any vocab.  d_w_head and d_dw_head have rows ldw apart.  It forms z twice and dW from a
+ * finer dz, two thirds more work on the matrix cores, so where the logits fit chimera_head_loss is the faster one. */
+size_t chimera_head_pieces_workspace_bytes(int dtype, int tokens, int hidden, int vocab, int piece);
+int chimera_head_loss_pieces(int dtype, int tokens, int hidden, int vocab, const void* d_y, const int32_t* d_targets, const void* d_lnf_g,
+                             const void* d_lnf_b, const void* d_w_head, int ldw, float scale, void* d_dy, float* d_dlnf_g, float* d_dlnf_b,
+                             float* d_dw_head, float* d_loss, int piece, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* ------------------------------------------------------- from gradients to weights
+ * Norm of `count` float gradient tensors taken as one vector: d_out[0] = sqrt(sum of all squares), d_out[1] = the factor that brings it down to
+ * max_norm, min(1, max_norm / norm); NaN where the norm is no finite float.  Squares are summed in double, in a fixed order.  h_n: element
+ * counts (0 is fine), h_grad: device pointers; both host arrays, read before the call returns, as below.  The workspace is 8-byte aligned. */
+size_t chimera_op_grad_norm_workspace_bytes(int count, const int64_t* h_n);
+int chimera_op_grad_norm(int count, const int64_t* h_n, const float* const* h_grad, float max_norm, float* d_out,
+                         void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* One AdamW step over `count` tensors, some tens of them a launch:
+ *   g' = factor g,  m = beta1 m + (1 - beta1) g',  v = beta2 v + (1 - beta2) g'^2,
+ *   p = p (1 - lr decay) - lr / (1 - beta1^step) m / (sqrt(v) / sqrt(1 - beta2^step) + eps),
+ * factor = d_grad_scale[0] (NULL: 1); where that is not finite the call changes nothing, so a step behind a gradient norm that overflowed is left out.
+ * h_param: the weights in `dtype`.  CHIMERA_BF16: h_master holds them in float as well; the step updates those and rounds.  h_grad: float.
+ * h_decay: one float per tensor (NULL: none decays).  Weights of two tensors must not overlap (EINVAL).
+ * state_bits 32: h_m, h_v point to floats, the moments above; h_scale is not used.
+ * state_bits 8: h_m and h_v point to one byte per element, e4m3 numbers (4 exponent bits, bias 7, 3 of mantissa, no infinities) that hold m and
+ * sqrt(v) as multiples of a float scale for each 256 elements of a tensor; h_scale to the pairs (m's, sqrt(v)'s), ceil(n / 256) of them.  Zeros are the
+ * state before the first step in either width.  Codes are rounded up or down at random, with the right mean, by a hash of seed, step and the
+ * element's number in the call (tensors counted in whole blocks of 256): the same call on the same state gives the same bits.
+ * Tensors are aligned to their elements.  d_hyper (may be NULL): device memory of CHIMERA_ADAMW_HYPER_BYTES bytes, 16-byte aligned, that begins with a
+ * chimera_adamw_hyper to be used in place of h_hyper, so that a recorded call can be replayed for further steps; its values are the caller's to
+ * check, the bytes behind the struct the call's, and calls that overlap need one each. */
+typedef struct {
+    double lr, beta1, beta2, eps;
+    int64_t step;          /* 1 for the first */
+    uint64_t seed;         /* of the rounding of 8-bit moments */
+} chimera_adamw_hyper;
+#define CHIMERA_ADAMW_HYPER_BYTES 128
+int chimera_op_adamw(int dtype, int state_bits, int count, const int64_t* h_n, void* const* h_param, float* const* h_master,
+                     const float* const* h_grad, void* const* h_m, void* const* h_v, float* const* h_scale, const float* h_decay,
+                     const chimera_adamw_hyper* h_hyper, void* d_hyper, const float* d_grad_scale, void* hip_stream);
+/* The same for a stage: d_weights (the buffer the stage is bound to, or another in its layout) from the stage's gradients, on the stage's stream.
+ * d_state: chimera_stage_adamw_state_bytes bytes, 256-byte aligned, laid out by chimera_stage_adamw_init (master weights from d_weights, moments zero).
+ * `decay` applies to the four matrices of a block, not to biases and LayerNorm parameters.  ESTATE: stage not bound, or micro-batches in flight (their
+ * backward reads the weights). */
+size_t chimera_stage_adamw_state_bytes(const chimera_stage* st, int state_bits);
+int chimera_stage_adamw_init(chimera_stage* st, const void* d_weights, void* d_state, int state_bits);
+int chimera_stage_adamw_step(chimera_stage* st, void* d_weights, void* d_state, int state_bits, float decay, const chimera_adamw_hyper* h_hyper,
+                             void* d_hyper, const float* d_grad_scale);
+
 /* ------------------------------------------------------------ measured ceilings
  * What the device sustains, to set beside the published peaks when the stage kernels'
  * rates are reported (measurement only; the hot path never calls them).

@@ -91,6 +91,18 @@ _SIGNATURES = {
     "chimera_op_softmax_xent": (_i, [_i, _i, _i, _p, _p, C.c_float, _p, _p, _p]),
     "chimera_head_workspace_bytes": (_sz, [_i, _i, _i, _i]),
     "chimera_head_loss": (_i, [_i] * 4 + [_p] * 5 + [C.c_float] + [_p] * 6 + [_sz, _p]),
+    "chimera_op_linear_xent_fwd_workspace_bytes": (_sz, [_i] * 4),
+    "chimera_op_linear_xent_fwd": (_i, [_i] * 4 + [_p, _i, _p, _i, _p, C.c_float] + [_p] * 4 + [_sz, _p]),
+    "chimera_op_linear_xent_bwd_workspace_bytes": (_sz, [_i] * 5),
+    "chimera_op_linear_xent_bwd": (_i, [_i] * 4 + [_p, _i, _p, _i, _p, _p, C.c_float, _p, _p, _i, _p, _i, _i, _i, _p, _sz, _p]),
+    "chimera_head_pieces_workspace_bytes": (_sz, [_i] * 5),
+    "chimera_head_loss_pieces": (_i, [_i] * 4 + [_p] * 5 + [_i, C.c_float] + [_p] * 5 + [_i, _p, _sz, _p]),
+    "chimera_op_grad_norm_workspace_bytes": (_sz, [_i, _p]),
+    "chimera_op_grad_norm": (_i, [_i, _p, _p, C.c_float, _p, _p, _sz, _p]),
+    "chimera_op_adamw": (_i, [_i, _i, _i] + [_p] * 11),
+    "chimera_stage_adamw_state_bytes": (_sz, [_p, _i]),
+    "chimera_stage_adamw_init": (_i, [_p, _p, _p, _i]),
+    "chimera_stage_adamw_step": (_i, [_p, _p, _p, _i, C.c_float, _p, _p, _p]),
     "chimera_probe_mfma_bf16": (_i, [_p, _i, C.POINTER(C.c_double), _p]),
     "chimera_probe_copy": (_i, [_p, _p, _sz, C.POINTER(C.c_double), _p]),
 }
@@ -276,6 +288,19 @@ class Stage:
         out = np.empty(self.grads.numel(), dtype=np.float32)
         check(lib().chimera_stage_read_grads(self.handle, out.ctypes.data_as(C.c_void_p), out.nbytes))
         return out
+
+    def adamw_init(self, state_bits=32):
+        """Allocates and initialises the state of AdamW steps over the stage's weights."""
+        n = lib().chimera_stage_adamw_state_bytes(self.handle, state_bits)
+        self.adamw_state = self.torch.empty(n, dtype=self.torch.uint8, device=self.device)
+        self.adamw_bits = state_bits
+        check(lib().chimera_stage_adamw_init(self.handle, _ptr(self.weights), _ptr(self.adamw_state), state_bits))
+
+    def adamw_step(self, lr, step, beta1=0.9, beta2=0.95, eps=1e-8, decay=0.0, seed=0, grad_scale=None, d_hyper=None):
+        """One step from the stage's gradients; grad_scale: device float (what chimera_op_grad_norm leaves in its second place)."""
+        h = AdamWHyper(lr, beta1, beta2, eps, step, seed)
+        check(lib().chimera_stage_adamw_step(self.handle, _ptr(self.weights), _ptr(self.adamw_state), self.adamw_bits, decay, C.byref(h),
+                                             _ptr(d_hyper), _ptr(grad_scale)))
 
     def close(self):
         if self.handle:
@@ -506,3 +531,99 @@ def chimera_head_loss(y, targets, lnf_g, lnf_b, w_head, scale, dy, dlnf_g, dlnf_
                                   _ptr(lnf_b), _ptr(w_head), scale, _ptr(dy), _ptr(dlnf_g), _ptr(dlnf_b), _ptr(dw_head),
                                   _ptr(loss), _ptr(ws), ws.numel(), _stream(y)))
     return ws
+
+
+def chimera_op_linear_xent_fwd(h, w, targets, scale, loss_rows, lse, loss=None, workspace=None):
+    """h [tokens, hidden], w [hidden, vocab] (rows may lie further apart than they are long), targets int32; fills loss_rows and lse
+    (float, [tokens]) and adds to loss.  Allocates the workspace (a torch uint8 tensor) unless one is given, and returns it."""
+    import torch
+    (tokens, hidden), vocab = h.shape, w.shape[1]
+    if workspace is None:
+        workspace = torch.empty(lib().chimera_op_linear_xent_fwd_workspace_bytes(_dt(h), tokens, hidden, vocab), dtype=torch.uint8, device=h.device)
+    check(lib().chimera_op_linear_xent_fwd(_dt(h), tokens, hidden, vocab, _ptr(h), h.stride(0), _ptr(w), w.stride(0), _ptr(targets), scale,
+                                           _ptr(loss_rows), _ptr(lse), _ptr(loss), _ptr(workspace), workspace.numel(), _stream(h)))
+    return workspace
+
+
+def chimera_op_linear_xent_bwd(h, w, targets, lse, scale, dh=None, dw=None, dloss=None, overwrite=False, piece=0, workspace=None):
+    """dh [tokens, hidden] (type of h) and dw [hidden, vocab] (float) are tensors to be filled, or None; dloss float [tokens] or None."""
+    import torch
+    (tokens, hidden), vocab = h.shape, w.shape[1]
+    if workspace is None:
+        workspace = torch.empty(lib().chimera_op_linear_xent_bwd_workspace_bytes(_dt(h), tokens, hidden, vocab, piece), dtype=torch.uint8, device=h.device)
+    check(lib().chimera_op_linear_xent_bwd(_dt(h), tokens, hidden, vocab, _ptr(h), h.stride(0), _ptr(w), w.stride(0), _ptr(targets), _ptr(lse),
+                                           scale, _ptr(dloss), _ptr(dh), 0 if dh is None else dh.stride(0), _ptr(dw),
+                                           0 if dw is None else dw.stride(0), int(overwrite), piece, _ptr(workspace), workspace.numel(), _stream(h)))
+    return workspace
+
+
+def chimera_head_loss_pieces(y, targets, lnf_g, lnf_b, w_head, scale, dy, dlnf_g, dlnf_b, dw_head, loss, piece=0, workspace=None):
+    """w_head [hidden, vocab]; dw_head has the same row stride.  Allocates the workspace unless one is given, and returns it."""
+    import torch
+    tokens, hidden, vocab = y.shape[0], y.shape[1], w_head.shape[1]
+    assert dw_head.stride(0) == w_head.stride(0)
+    if workspace is None:
+        workspace = torch.empty(lib().chimera_head_pieces_workspace_bytes(_dt(y), tokens, hidden, vocab, piece), dtype=torch.uint8, device=y.device)
+    check(lib().chimera_head_loss_pieces(_dt(y), tokens, hidden, vocab, _ptr(y), _ptr(targets), _ptr(lnf_g), _ptr(lnf_b), _ptr(w_head),
+                                         w_head.stride(0), scale, _ptr(dy), _ptr(dlnf_g), _ptr(dlnf_b), _ptr(dw_head), _ptr(loss), piece,
+                                         _ptr(workspace), workspace.numel(), _stream(y)))
+    return workspace
+
+
+# ---------------------------------------------------- from gradients to weights
+class AdamWHyper(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("step", C.c_int64), ("seed", C.c_uint64)]
+
+
+ADAMW_HYPER_BYTES = 128
+
+
+def _pointers(tensors):
+    return None if tensors is None else (C.c_void_p * len(tensors))(*[t.data_ptr() for t in tensors])
+
+
+def _counts(tensors):
+    return (C.c_int64 * len(tensors))(*[t.numel() for t in tensors])
+
+
+def chimera_op_grad_norm(grads, max_norm, out, workspace=None):
+    """grads: float tensors (contiguous); out: float [2], the norm and the factor that brings it down to max_norm."""
+    import torch
+    n = _counts(grads)
+    if workspace is None:
+        workspace = torch.empty(lib().chimera_op_grad_norm_workspace_bytes(len(grads), n), dtype=torch.uint8, device=out.device)
+    check(lib().chimera_op_grad_norm(len(grads), n, _pointers(grads), max_norm, _ptr(out), _ptr(workspace), workspace.numel(), _stream(out)))
+    return workspace
+
+
+class AdamW:
+    """The argument arrays of chimera_op_adamw for a list of tensors, kept from step to step.
+
+    params: float32, or bfloat16 with float32 `masters`; grads: float32.  32-bit moments: ms, vs float32 and scales None; 8-bit: ms, vs
+    float8_e4m3fn (or uint8) and scales float32, a pair for each 256 elements of a tensor.  decay: a number per tensor, or None."""
+
+    def __init__(self, params, grads, ms, vs, masters=None, scales=None, decay=None, beta1=0.9, beta2=0.95, eps=1e-8):
+        lists = [params, grads, ms, vs] + [x for x in (masters, scales, decay) if x is not None]
+        if any(len(x) != len(params) for x in lists):
+            raise ValueError("one entry per tensor expected")
+        for x in (params, grads, ms, vs, masters or [], scales or []):
+            if not all(t.is_contiguous() for t in x):
+                raise ValueError("tensors must be contiguous")
+        for x in (grads, ms, vs, masters or []):
+            if any(a.numel() != p.numel() for a, p in zip(x, params)):
+                raise ValueError("tensors of one entry must have one size")
+        if scales is not None and any(a.numel() != 2 * ((p.numel() + 255) // 256) for a, p in zip(scales, params)):
+            raise ValueError("scales: a pair for each 256 elements")
+        self.tensors = lists                               # the library borrows them
+        self.dtype, self.bits, self.count = _dt(params[0]), 32 if scales is None else 8, len(params)
+        self.n, self.param, self.grad, self.m, self.v = _counts(params), _pointers(params), _pointers(grads), _pointers(ms), _pointers(vs)
+        self.master, self.scale = _pointers(masters), _pointers(scales)
+        self.decay = None if decay is None else (C.c_float * len(decay))(*decay)
+        self.hyper = AdamWHyper(0.0, beta1, beta2, eps, 0, 0)
+
+    def step(self, lr, step, seed=0, grad_scale=None, d_hyper=None):
+        """grad_scale: device float or None; d_hyper: device copy of an AdamWHyper in ADAMW_HYPER_BYTES bytes, used in place of lr, step and seed."""
+        h = self.hyper
+        h.lr, h.step, h.seed = lr, step, seed
+        check(lib().chimera_op_adamw(self.dtype, self.bits, self.count, self.n, self.param, self.master, self.grad, self.m, self.v, self.scale,
+                                     self.decay, C.byref(h), _ptr(d_hyper), _ptr(grad_scale), _stream(self.tensors[0][0])))

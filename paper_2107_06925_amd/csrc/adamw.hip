@@ -1,0 +1,409 @@
+// The step from gradients to weights, over many tensors at once: the norm of all gradients with the factor that clips them, and
+// AdamW with moments in 32 or in 8 bits.
+//   g' = factor g,  m = b1 m + (1 - b1) g',  v = b2 v + (1 - b2) g'^2,  r = sqrt(v)
+//   p = p (1 - lr decay) - lr / (1 - b1^t) m / (r / sqrt(1 - b2^t) + eps)
+// What bounds both is memory: a value's 28 bytes (float), 30 (bf16 with a float master weight) or 18 (the same with 8-bit moments), and 4 for the norm.
+// The tensors' addresses travel as a kernel argument, so a launch takes some tens of them and nothing has to be laid out in device memory.
+//
+// 8-bit moments: m and r are held as e4m3 numbers times a float scale for each 256 values, the largest of which becomes 448.  r and not v: its
+// range is the root of v's, and a code's range of 2^17.8 then spans one of 2^35 in v.  Codes are rounded at random (up with the probability that
+// keeps the expectation): a step moves r by less than a thousandth, a code is 6 to 12 % wide, and rounding to nearest would leave r where it is for good.
+// The random bits are a hash of (seed, step, the value's number), so a step's result is a function of its arguments.  A value whose r is
+// not zero keeps a code above zero, whatever the bits: its m would otherwise be divided by eps.
+#include "device.h"
+
+#include <algorithm>
+#include <climits>
+#include <cmath>
+#include <new>
+
+namespace chimera {
+namespace {
+
+constexpr int STEP_THREADS = 256, STEP_CHUNK = 4096, MOMENT_BLOCK = 256;
+static_assert(MOMENT_BLOCK == 4 * WAVE, "a wavefront holds one block of moments, four values a lane");
+constexpr float CODE_TOP = 448.0f, CODE_LEAST = 1e-30f;      // largest e4m3 number; blocks whose largest value is below this hold zeros
+
+// Tensors need not be aligned to more than their elements.
+typedef float f4_t __attribute__((ext_vector_type(4)));
+typedef f4_t f4_u __attribute__((aligned(4)));
+typedef bf16_t b4_t __attribute__((ext_vector_type(4)));
+typedef b4_t b4_u __attribute__((aligned(2)));
+typedef unsigned u32_u __attribute__((aligned(1)));
+
+struct Scalars { float b1, w1, b2, w2, eps, lr, rate, root; unsigned key; };     // w = 1 - b, rate = lr / (1 - b1^t), root = 1 / sqrt(1 - b2^t)
+__host__ __device__ Scalars scalars_of(const chimera_adamw_hyper& h) {
+    Scalars s;
+    s.b1 = (float)h.beta1; s.w1 = (float)(1.0 - h.beta1); s.b2 = (float)h.beta2; s.w2 = (float)(1.0 - h.beta2);
+    s.eps = (float)h.eps; s.lr = (float)h.lr;
+    s.rate = (float)(h.lr / (1.0 - pow(h.beta1, (double)h.step)));
+    s.root = (float)(1.0 / sqrt(1.0 - pow(h.beta2, (double)h.step)));
+    s.key = (unsigned)h.seed * 0x243F6A89u + (unsigned)h.step * 0xB7E15163u;     // (pi and e, as odd numbers; below the golden ratio and the roots of 2 and 3)
+    return s;
+}
+struct DeviceHyper { chimera_adamw_hyper given; Scalars derived; };
+static_assert(sizeof(DeviceHyper) <= CHIMERA_ADAMW_HYPER_BYTES, "room for what a call derives");
+__global__ void adamw_derive_kernel(DeviceHyper* h) { h->derived = scalars_of(h->given); }
+
+constexpr int STEP_TENSORS = 48;
+struct StepTensor {
+    void *p, *m, *v;
+    float *master, *scale;
+    const float* g;
+    long long n;
+    long long block0;            // number of the tensor's first block of 256 values in the call
+    float decay;
+};
+struct StepLaunch {
+    StepTensor t[STEP_TENSORS];
+    int first[STEP_TENSORS];     // a tensor's first chunk (INT_MAX behind the last tensor)
+    Scalars s;
+    const DeviceHyper* device;   // null: s
+    const float* factor;
+};
+static_assert(sizeof(StepLaunch) <= 4096, "kernel arguments");
+
+// Number of the last tensor that begins at or before `chunk` (lanes ask for 64 beginnings at once).
+template <int N> __device__ __forceinline__ int tensor_of(const int (&first)[N], int chunk) {
+    static_assert(N <= WAVE, "one lane a tensor");
+    const int lane = threadIdx.x % WAVE;
+    const bool at = lane < N && first[min(lane, N - 1)] <= chunk;
+    return __builtin_amdgcn_readfirstlane(__popcll(__ballot(at)) - 1);
+}
+
+__device__ __forceinline__ unsigned random_bits(unsigned long long i, unsigned key) {
+    unsigned x = (unsigned)i * 0x9E3779B1u + (unsigned)(i >> 32) * 0x6A09E667u + key;
+    x = (x ^ (x >> 15)) * 0x6A09E667u;
+    x = (x ^ (x >> 13)) * 0xBB67AE85u;
+    return x ^ (x >> 16);
+}
+// |x| / top as an e4m3 code: its bits follow from the float's, whose exponent is moved so that e4m3's smallest normal number becomes the float's.
+__device__ __forceinline__ unsigned encode(float x, float inv, unsigned bits16, bool keep) {
+#pragma clang fp contract(off)
+    const float y = fabsf(x) * inv;
+    if (y != y) return 0x7f;                                  // not a number stays one
+    unsigned code = min((__float_as_uint(y * 0x1p-120f) + bits16 * 16u + 8u) >> 20, 126u);
+    if (keep && x > 0.f) code = max(code, 1u);
+    return x < 0.f ? code | 0x80u : code;
+}
+__device__ __forceinline__ float decode(unsigned code, float scale) {
+    const float v = __uint_as_float((code & 0x7f) << 20) * 0x1p120f;
+    return ((code & 0x7f) == 0x7f ? __builtin_nanf("") : code & 0x80 ? -v : v) * scale;
+}
+
+// Every operation is rounded by itself (no contraction), so that a step of the same numbers is the same everywhere, the choice of codes included.
+template <typename T, int BITS>
+__global__ __launch_bounds__(STEP_THREADS) void adamw_kernel(StepLaunch L) {
+#pragma clang fp contract(off)
+    const float factor = L.factor ? *L.factor : 1.0f;
+    if (!(fabsf(factor) <= 3.4028235e38f)) return;            // not finite: nothing changes
+    const Scalars s = L.device ? L.device->derived : L.s;
+    const int k = tensor_of(L.first, (int)blockIdx.x);
+    const StepTensor& t = L.t[k];
+    const long long n = t.n, begin = (long long)((int)blockIdx.x - L.first[k]) * STEP_CHUNK, end = min(begin + STEP_CHUNK, n);
+    const float keep = 1.0f - t.decay * s.lr;
+    T* __restrict__ const param = (T*)t.p;
+    float* __restrict__ const weight = sizeof(T) == 4 ? (float*)t.p : t.master;
+    const float* __restrict__ const grad = t.g;
+    const int lane = threadIdx.x % WAVE;
+    for (long long i0 = begin + threadIdx.x / WAVE * MOMENT_BLOCK; i0 < end; i0 += STEP_THREADS / WAVE * MOMENT_BLOCK) {
+        const long long i = i0 + lane * 4;
+        const int have = (int)max(0ll, min(4ll, n - i));     // of this lane's four values
+        f4_t g = {0.f, 0.f, 0.f, 0.f}, w = g, m = g, v = g, r;
+        auto get = [&](const float* from, f4_t& to) {
+            if (have == 4) to = *reinterpret_cast<const f4_u*>(from + i);
+            else
+#pragma unroll
+                for (int e = 0; e < 3; ++e)
+                    if (e < have) to[e] = from[i + e];
+        };
+        auto put = [&](float* to, const f4_t& x) {
+            if (have == 4) *reinterpret_cast<f4_u*>(to + i) = x;
+            else
+#pragma unroll
+                for (int e = 0; e < 3; ++e)
+                    if (e < have) to[i + e] = x[e];
+        };
+        auto get_codes = [&](const void* from) {
+            const unsigned char* c = (const unsigned char*)from + i;
+            unsigned q = 0;
+            if (have == 4) q = *reinterpret_cast<const u32_u*>(c);
+            else
+#pragma unroll
+                for (int e = 0; e < 3; ++e)
+                    if (e < have) q |= (unsigned)c[e] << (8 * e);
+            return q;
+        };
+        auto put_codes = [&](void* to, unsigned q) {
+            unsigned char* c = (unsigned char*)to + i;
+            if (have == 4) *reinterpret_cast<u32_u*>(c) = q;
+            else
+#pragma unroll
+                for (int e = 0; e < 3; ++e)
+                    if (e < have) c[e] = (unsigned char)(q >> (8 * e));
+        };
+        get(grad, g);
+        get(weight, w);
+        if constexpr (BITS == 32) {
+            get((const float*)t.m, m);
+            get((const float*)t.v, v);
+        } else {
+            const unsigned qm = get_codes(t.m), qv = get_codes(t.v);
+            const float sm = t.scale[i0 / MOMENT_BLOCK * 2], sv = t.scale[i0 / MOMENT_BLOCK * 2 + 1];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                m[e] = decode(qm >> (8 * e) & 0xff, sm);
+                const float root = decode(qv >> (8 * e) & 0xff, sv);
+                v[e] = root * root;
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float x = g[e] * factor;
+            m[e] = m[e] * s.b1 + x * s.w1;
+            v[e] = v[e] * s.b2 + (x * x) * s.w2;
+            r[e] = __fsqrt_rn(v[e]);
+            w[e] = w[e] * keep - __fdiv_rn(m[e] * s.rate, r[e] * s.root + s.eps);
+        }
+        put(weight, w);
+        if constexpr (sizeof(T) == 2) {
+            if (have == 4) *reinterpret_cast<b4_u*>(param + i) = b4_t{(bf16_t)w[0], (bf16_t)w[1], (bf16_t)w[2], (bf16_t)w[3]};
+            else
+#pragma unroll
+                for (int e = 0; e < 3; ++e)
+                    if (e < have) param[i + e] = (bf16_t)w[e];
+        }
+        if constexpr (BITS == 32) {
+            put((float*)t.m, m);
+            put((float*)t.v, v);
+        } else {
+            float tm = 0.f, tv = 0.f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (e < have) { tm = fmaxf(tm, fabsf(m[e])); tv = fmaxf(tv, r[e]); }
+            tm = wave_max(tm);
+            tv = wave_max(tv);
+            const float im = tm > CODE_LEAST ? __fdiv_rn(CODE_TOP, tm) : 0.f, iv = tv > CODE_LEAST ? __fdiv_rn(CODE_TOP, tv) : 0.f;
+            unsigned qm = 0, qv = 0;
+            const unsigned long long number = (unsigned long long)(t.block0 * MOMENT_BLOCK + i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const unsigned bits = random_bits(number + e, s.key);
+                qm |= encode(m[e], im, bits & 0xffff, false) << (8 * e);
+                qv |= encode(r[e], iv, bits >> 16, iv > 0.f) << (8 * e);
+            }
+            put_codes(t.m, qm);
+            put_codes(t.v, qv);
+            if (lane == 0) {
+                t.scale[i0 / MOMENT_BLOCK * 2] = tm > CODE_LEAST ? __fdiv_rn(tm, CODE_TOP) : 0.f;
+                t.scale[i0 / MOMENT_BLOCK * 2 + 1] = tv > CODE_LEAST ? __fdiv_rn(tv, CODE_TOP) : 0.f;
+            }
+        }
+    }
+}
+
+// ---- sum of squares: a double per workgroup, in a fixed order; one workgroup adds them.  (Squares of floats reach beyond the floats' range.)
+constexpr int NORM_TENSORS = 64;
+struct NormLaunch {
+    const float* g[NORM_TENSORS];
+    long long n[NORM_TENSORS];
+    int first[NORM_TENSORS];
+    long long chunk;
+    double* partial;
+};
+__device__ __forceinline__ double wave_sum_double(double v) {
+#pragma unroll
+    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o, WAVE);
+    return v;
+}
+__global__ __launch_bounds__(STEP_THREADS) void grad_square_kernel(NormLaunch L) {
+    __shared__ double part[STEP_THREADS / WAVE];
+    const int k = tensor_of(L.first, (int)blockIdx.x);
+    const float* g = L.g[k];
+    const long long begin = (long long)((int)blockIdx.x - L.first[k]) * L.chunk, end = min(begin + L.chunk, L.n[k]);
+    double sum[4] = {0, 0, 0, 0};
+    constexpr int FLY = 4, STRIDE = STEP_THREADS * 4;
+    long long i = begin + threadIdx.x * 4;
+    for (; i + (FLY - 1) * STRIDE + 4 <= end; i += FLY * STRIDE) {
+        f4_t x[FLY];
+#pragma unroll
+        for (int u = 0; u < FLY; ++u) x[u] = *reinterpret_cast<const f4_u*>(g + i + u * STRIDE);
+#pragma unroll
+        for (int u = 0; u < FLY; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[e] += (double)x[u][e] * x[u][e];
+    }
+    for (; i < end; i += STRIDE)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (i + e < end) { const double x = g[i + e]; sum[e] += x * x; }
+    const double s = wave_sum_double((sum[0] + sum[1]) + (sum[2] + sum[3]));
+    if (threadIdx.x % WAVE == 0) part[threadIdx.x / WAVE] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) L.partial[blockIdx.x] = (part[0] + part[1]) + (part[2] + part[3]);
+}
+__global__ __launch_bounds__(1024) void grad_norm_kernel(const double* __restrict__ partial, int n, float max_norm, float* __restrict__ out) {
+    __shared__ double part[1024 / WAVE];
+    double s = 0;
+    for (int i = threadIdx.x; i < n; i += 1024) s += partial[i];
+    s = wave_sum_double(s);
+    if (threadIdx.x % WAVE == 0) part[threadIdx.x / WAVE] = s;
+    __syncthreads();
+    if (threadIdx.x) return;
+    s = 0;
+    for (int i = 0; i < 1024 / WAVE; ++i) s += part[i];
+    const double norm = sqrt(s);
+    out[0] = (float)norm;
+    out[1] = !(norm <= 3.4028235e38) ? __builtin_nanf("") : norm > max_norm ? (float)(max_norm / norm) : 1.0f;
+}
+
+// Values per workgroup: some eight workgroups a CU, pieces of 4096 to 65536.
+struct NormPlan { long long chunk, chunks; };
+bool norm_plan(int count, const int64_t* h_n, NormPlan& p) {
+    long long total = 0;
+    for (int i = 0; i < count; ++i) {
+        if (h_n[i] < 0 || h_n[i] > 1ll << 40) return false;
+        total += h_n[i];
+    }
+    p.chunk = std::clamp((total / 2048 + 4095) / 4096 * 4096, 4096ll, 65536ll);
+    p.chunks = 0;
+    for (int i = 0; i < count; ++i) p.chunks += (h_n[i] + p.chunk - 1) / p.chunk;
+    return p.chunks < 1 << 22;
+}
+
+int check_hyper(const chimera_adamw_hyper& h) {
+    if (!(h.lr >= 0) || !std::isfinite(h.lr)) return fail(CHIMERA_EINVAL, "lr must be finite and not negative");
+    if (!(h.beta1 >= 0 && h.beta1 < 1) || !(h.beta2 >= 0 && h.beta2 < 1)) return fail(CHIMERA_EINVAL, "beta1 and beta2 must lie in [0, 1)");
+    if (!(h.eps > 0) || !std::isfinite(h.eps)) return fail(CHIMERA_EINVAL, "eps must be finite and positive");
+    if (h.step < 1) return fail(CHIMERA_EINVAL, "step=%lld: the first step is 1", (long long)h.step);
+    return CHIMERA_OK;
+}
+
+}  // namespace
+
+int adamw_step(int dtype, int bits, int count, const AdamwTensor* t, const chimera_adamw_hyper* h_hyper, void* d_hyper, const float* d_factor, void* stream) {
+    hipStream_t s = (hipStream_t)stream;
+    StepLaunch L{};
+    L.factor = d_factor;
+    L.device = (const DeviceHyper*)d_hyper;
+    if (d_hyper) {
+        hipLaunchKernelGGL(adamw_derive_kernel, dim3(1), dim3(1), 0, s, (DeviceHyper*)d_hyper);
+        CHIMERA_LAUNCH_CHECK("AdamW");
+    } else {
+        L.s = scalars_of(*h_hyper);
+    }
+    long long block = 0;
+    for (int i = 0; i < count;) {
+        std::fill(std::begin(L.first), std::end(L.first), INT_MAX);
+        long long chunks = 0;
+        int used = 0;
+        for (; i < count && used < STEP_TENSORS && chunks + (t[i].n + STEP_CHUNK - 1) / STEP_CHUNK < 1 << 23; ++i) {
+            if (!t[i].n) continue;
+            L.t[used] = {t[i].p, t[i].m, t[i].v, t[i].master, t[i].scale, t[i].g, (long long)t[i].n, block, t[i].decay};
+            L.first[used++] = (int)chunks;
+            chunks += (t[i].n + STEP_CHUNK - 1) / STEP_CHUNK;
+            block += (t[i].n + MOMENT_BLOCK - 1) / MOMENT_BLOCK;
+        }
+        if (!used) continue;
+        const dim3 grid((unsigned)chunks), threads(STEP_THREADS);
+        if (dtype == CHIMERA_F32 && bits == 32) hipLaunchKernelGGL((adamw_kernel<float, 32>), grid, threads, 0, s, L);
+        else if (dtype == CHIMERA_F32) hipLaunchKernelGGL((adamw_kernel<float, 8>), grid, threads, 0, s, L);
+        else if (bits == 32) hipLaunchKernelGGL((adamw_kernel<bf16_t, 32>), grid, threads, 0, s, L);
+        else hipLaunchKernelGGL((adamw_kernel<bf16_t, 8>), grid, threads, 0, s, L);
+        CHIMERA_LAUNCH_CHECK("AdamW");
+    }
+    return CHIMERA_OK;
+}
+
+int adamw_check(int dtype, int bits, const chimera_adamw_hyper* h_hyper, const void* d_hyper) {
+    if (dtype != CHIMERA_F32 && dtype != CHIMERA_BF16) return fail(CHIMERA_EINVAL, "unknown dtype %d", dtype);
+    if (bits != 32 && bits != 8) return fail(CHIMERA_EINVAL, "moments of %d bits (8 or 32)", bits);
+    if (!d_hyper && !h_hyper) return fail(CHIMERA_EINVAL, "hyperparameters are NULL");
+    if ((uintptr_t)d_hyper & 15) return fail(CHIMERA_EINVAL, "device hyperparameters must be 16-byte aligned");
+    return d_hyper ? CHIMERA_OK : check_hyper(*h_hyper);
+}
+
+}  // namespace chimera
+
+using namespace chimera;
+
+#define STEP_TRY(expr) do { int rc__ = (expr); if (rc__) return rc__; } while (0)
+
+extern "C" {
+
+size_t chimera_op_grad_norm_workspace_bytes(int count, const int64_t* h_n) {
+    NormPlan p;
+    return count < 1 || !h_n || !norm_plan(count, h_n, p) ? 0 : (size_t)std::max(p.chunks, 1ll) * sizeof(double);
+}
+
+int chimera_op_grad_norm(int count, const int64_t* h_n, const float* const* h_grad, float max_norm, float* d_out, void* d_workspace, size_t workspace_bytes,
+                         void* hip_stream) {
+    if (count < 1 || !h_n || !h_grad) return fail(CHIMERA_EINVAL, "no tensors");
+    if (!d_out || !d_workspace) return fail(CHIMERA_EINVAL, "NULL operand");
+    if (!(max_norm > 0)) return fail(CHIMERA_EINVAL, "max_norm must be positive");
+    if (((uintptr_t)d_workspace & 7) || ((uintptr_t)d_out & 3)) return fail(CHIMERA_EINVAL, "workspace must be 8-byte aligned, the result 4-byte aligned");
+    NormPlan p;
+    if (!norm_plan(count, h_n, p)) return fail(CHIMERA_EINVAL, "a tensor's size is negative, or the tensors are too large");
+    for (int i = 0; i < count; ++i)
+        if (h_n[i] && (!h_grad[i] || ((uintptr_t)h_grad[i] & 3))) return fail(CHIMERA_EINVAL, "gradient %d is NULL or not aligned to floats", i);
+    const size_t need = (size_t)std::max(p.chunks, 1ll) * sizeof(double);
+    if (workspace_bytes < need) return fail(CHIMERA_ENOMEM, "workspace holds %zu bytes, need %zu", workspace_bytes, need);
+    hipStream_t s = (hipStream_t)hip_stream;
+    NormLaunch L{};
+    L.chunk = p.chunk;
+    long long done = 0;
+    for (int i = 0; i < count;) {
+        std::fill(std::begin(L.first), std::end(L.first), INT_MAX);
+        long long chunks = 0;
+        int used = 0;
+        for (; i < count && used < NORM_TENSORS; ++i) {
+            if (!h_n[i]) continue;
+            L.g[used] = h_grad[i]; L.n[used] = h_n[i]; L.first[used++] = (int)chunks;
+            chunks += (h_n[i] + p.chunk - 1) / p.chunk;
+        }
+        if (!used) continue;
+        L.partial = (double*)d_workspace + done;
+        hipLaunchKernelGGL(grad_square_kernel, dim3((unsigned)chunks), dim3(STEP_THREADS), 0, s, L);
+        CHIMERA_LAUNCH_CHECK("gradient norm");
+        done += chunks;
+    }
+    hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(1024), 0, s, (const double*)d_workspace, (int)done, max_norm, d_out);
+    CHIMERA_LAUNCH_CHECK("gradient norm");
+    return CHIMERA_OK;
+}
+
+int chimera_op_adamw(int dtype, int state_bits, int count, const int64_t* h_n, void* const* h_param, float* const* h_master, const float* const* h_grad,
+                     void* const* h_m, void* const* h_v, float* const* h_scale, const float* h_decay, const chimera_adamw_hyper* h_hyper, void* d_hyper,
+                     const float* d_grad_scale, void* hip_stream) {
+    STEP_TRY(adamw_check(dtype, state_bits, h_hyper, d_hyper));
+    if (count < 1 || !h_n || !h_param || !h_grad || !h_m || !h_v) return fail(CHIMERA_EINVAL, "no tensors");
+    if (dtype == CHIMERA_BF16 && !h_master) return fail(CHIMERA_EINVAL, "bf16 weights need float master weights");
+    if (state_bits == 8 && !h_scale) return fail(CHIMERA_EINVAL, "8-bit moments need scales");
+    const size_t e = dtype == CHIMERA_F32 ? 4 : 2;
+    try {
+        std::vector<AdamwTensor> t((size_t)count);
+        std::vector<std::pair<uintptr_t, uintptr_t>> spans;
+        spans.reserve((size_t)count);
+        for (int i = 0; i < count; ++i) {
+            if (h_n[i] < 0 || h_n[i] > 1ll << 34) return fail(CHIMERA_EINVAL, "tensor %d of %lld values", i, (long long)h_n[i]);
+            t[i] = {h_param[i], h_m[i], h_v[i], dtype == CHIMERA_BF16 ? h_master[i] : nullptr, state_bits == 8 ? h_scale[i] : nullptr, h_grad[i], h_n[i],
+                    h_decay ? h_decay[i] : 0.f};
+            if (!h_n[i]) continue;
+            const AdamwTensor& q = t[i];
+            if (!q.p || !q.m || !q.v || !q.g || (dtype == CHIMERA_BF16 && !q.master) || (state_bits == 8 && !q.scale)) return fail(CHIMERA_EINVAL, "NULL operand in tensor %d", i);
+            if (((uintptr_t)q.p & (e - 1)) || (((uintptr_t)q.master | (uintptr_t)q.g | (uintptr_t)q.scale) & 3) ||
+                (state_bits == 32 && (((uintptr_t)q.m | (uintptr_t)q.v) & 3)))
+                return fail(CHIMERA_EINVAL, "tensor %d is not aligned to its elements", i);
+            if (!(q.decay >= 0) || !std::isfinite(q.decay)) return fail(CHIMERA_EINVAL, "weight decay of tensor %d must be finite and not negative", i);
+            spans.push_back({(uintptr_t)q.p, (uintptr_t)q.p + (size_t)h_n[i] * e});
+        }
+        std::sort(spans.begin(), spans.end());
+        for (size_t i = 1; i < spans.size(); ++i)
+            if (spans[i].first < spans[i - 1].second) return fail(CHIMERA_EINVAL, "weights of two tensors overlap");
+        return adamw_step(dtype, state_bits, count, t.data(), h_hyper, d_hyper, d_grad_scale, hip_stream);
+    } catch (const std::bad_alloc&) {
+        return fail(CHIMERA_ENOMEM, "out of host memory");
+    }
+}
+
+}  // extern "C"

@@ -518,6 +518,12 @@ HeadLayout head_layout(int dtype, int M, int H, int V) {
 }
 
 }  // namespace
+
+int loss_sum(const float* loss_rows, int n, float* loss, void* stream) {
+    hipLaunchKernelGGL(loss_sum_kernel, dim3(1), dim3(EDGE_THREADS), 0, (hipStream_t)stream, loss_rows, n, loss);
+    CHIMERA_LAUNCH_CHECK("loss sum");
+    return CHIMERA_OK;
+}
 }  // namespace chimera
 
 using namespace chimera;
@@ -594,9 +600,7 @@ int chimera_op_softmax_xent(int dtype, int rows, int vocab, void* d_logits, cons
 #undef XENT_ROW
     }
     CHIMERA_LAUNCH_CHECK("softmax cross-entropy");
-    hipLaunchKernelGGL(loss_sum_kernel, dim3(1), dim3(EDGE_THREADS), 0, s, d_loss_rows, rows, d_loss);
-    CHIMERA_LAUNCH_CHECK("loss sum");
-    return CHIMERA_OK;
+    return loss_sum(d_loss_rows, rows, d_loss, hip_stream);
 }
 
 size_t chimera_head_workspace_bytes(int dtype, int tokens, int hidden, int vocab) {

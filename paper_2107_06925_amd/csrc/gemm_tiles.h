@@ -16,6 +16,7 @@ namespace {
 typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int BK = 64;
 constexpr int GROUP_M = 8;       // tile rows per raster group
@@ -268,11 +269,13 @@ template <typename F> __device__ __forceinline__ void with_epilogue(int epi, int
 // with 8, in two instructions, each had every other 16 bytes of the lines, and C, where it passes the caches by, was written in parts of
 // lines.  8 columns -> 4: blocks of 1344, 1792 and 2560 at 2048 tokens 95.6 -> 94.5, 172.6 -> 163.2 and 363 -> 355 us; six blocks of 1600
 // and 2048, forward and backward, at 448 tokens 1501 -> 1466 and 2099 -> 1879, at 632 1689 -> 1667 and 2457 -> 2357.
-template <bool ONCE, int TM, int TN, typename Acc>
-__device__ __forceinline__ void accumulate(const Acc& acc, float* slab, int row_base, int col_base, int m, int n, float* __restrict__ C, int epi_flag, int lane) {
+// PART: C is a part of the columns of a wider matrix, of any number n (rows of C are readable up to a multiple of 4), and the sums count 2^-shift.
+template <bool ONCE, bool PART, int TM, int TN, typename Acc>
+__device__ __forceinline__ void accumulate(const Acc& acc, float* slab, int row_base, int col_base, int m, int n, int ldc, int shift, float* __restrict__ C,
+                                           int epi_flag, int lane) {
     constexpr int CPR = EpiSlab<TN>::WN / 4, RPP = 64 / CPR, NP = 32 / RPP;       // lanes per row, rows at once, passes per band of 32 rows
     constexpr int DEPTH = TM < 2 ? TM : 2;                                         // bands whose old values are asked for ahead
-    const int pr = lane / CPR, piece = lane % CPR, gcol = col_base + piece * 4, lcol = min(gcol, n - 4);
+    const int pr = lane / CPR, piece = lane % CPR, gcol = col_base + piece * 4, lcol = min(gcol, (PART ? (n + 3) & ~3 : n) - 4);
     const bool reads = !(epi_flag & ACCUM_OVERWRITE);
     f32x4 old[DEPTH][NP];
     auto request = [&](int a, auto slot_c) {
@@ -280,7 +283,7 @@ __device__ __forceinline__ void accumulate(const Acc& acc, float* slab, int row_
 #pragma unroll
         for (int j = 0; j < NP; ++j) {
             // pieces outside the matrix are requested from its last row / last piece (never used)
-            const f32x4* from = reinterpret_cast<const f32x4*>(C + (size_t)min(row_base + a * 32 + j * RPP + pr, m - 1) * n + lcol);
+            const f32x4* from = reinterpret_cast<const f32x4*>(C + (size_t)min(row_base + a * 32 + j * RPP + pr, m - 1) * ldc + lcol);
             if constexpr (ONCE) old[SLOT][j] = __builtin_nontemporal_load(from);
             else old[SLOT][j] = *from;
         }
@@ -298,9 +301,19 @@ __device__ __forceinline__ void accumulate(const Acc& acc, float* slab, int row_
         for (int j = 0; j < NP; ++j) {
             const int lr = j * RPP + pr, grow = row_base + a * 32 + lr;
             f32x4 v = *reinterpret_cast<const f32x4*>(EpiSlab<TN>::at(slab, lr, piece));
+            if constexpr (PART)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = ldexpf(v[e], -shift);
             if (reads) v += old[SLOT][j];
             if (grow >= m || gcol >= n) continue;
-            f32x4* to = reinterpret_cast<f32x4*>(C + (size_t)grow * n + gcol);
+            f32x4* to = reinterpret_cast<f32x4*>(C + (size_t)grow * ldc + gcol);
+            if constexpr (PART)
+                if (gcol + 4 > n) {
+#pragma unroll
+                    for (int e = 0; e < 3; ++e)
+                        if (gcol + e < n) C[(size_t)grow * ldc + gcol + e] = v[e];
+                    continue;
+                }
             if constexpr (ONCE) __builtin_nontemporal_store(v, to);
             else *to = v;
         }
@@ -318,8 +331,8 @@ __device__ __forceinline__ void epilogue(const Acc& acc, float* slab, int row_ba
                                          int n, const bf16_t* __restrict__ bias, const bf16_t* __restrict__ R,
                                          void* __restrict__ c, bf16_t* __restrict__ C2, int epi_flag, int lane) {
     if constexpr (EPI == EPI_ACCUM_F32) {
-        if (epi_flag & ACCUM_ONCE) accumulate<true, TM, TN>(acc, slab, row_base, col_base, m, n, (float*)c, epi_flag, lane);
-        else accumulate<false, TM, TN>(acc, slab, row_base, col_base, m, n, (float*)c, epi_flag, lane);
+        if (epi_flag & ACCUM_ONCE) accumulate<true, false, TM, TN>(acc, slab, row_base, col_base, m, n, n, 0, (float*)c, epi_flag, lane);
+        else accumulate<false, false, TM, TN>(acc, slab, row_base, col_base, m, n, n, 0, (float*)c, epi_flag, lane);
         return;
     }
     constexpr int WN = EpiSlab<TN>::WN;
@@ -746,12 +759,16 @@ template <int PER_CU> __device__ __forceinline__ int dealt(int id, int tiles) {
 __device__ __forceinline__ void lds_dma16_s(const void* sbase, unsigned voff, unsigned lds_base) {
     asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(sbase), "{m0}"(lds_base) : "memory");
 }
-template <int BM, int BN, int WGM, int WGN, int WGK, bool A_KC, bool B_KC, int ONLY_EPI>
+// A tile's own way to end (ONLY_EPI = EPI_OWN), in place of the epilogues above: begin() ahead of the k loop, end() with the accumulators
+// once every wavefront has left it.
+constexpr int EPI_OWN = 6;
+struct NoEnd {};
+template <int BM, int BN, int WGM, int WGN, int WGK, bool A_KC, bool B_KC, int ONLY_EPI, bool F16 = false, typename End = NoEnd>
 __device__ __forceinline__ void gemm_ring_tile(
     char* lds, const bf16_t* __restrict__ A, const bf16_t* __restrict__ B, const bf16_t* __restrict__ bias,
     const bf16_t* __restrict__ R, void* __restrict__ C, bf16_t* __restrict__ C2, int m, int n, int k, int lda,
     int ldb, int epi, int epi_flag, int res_types, int tiles_m, int tiles_n, int group_m, int block_id,
-    float* __restrict__ bsum = nullptr, bool xcd_remap = true, int col0 = 0, const Ahead& ahead = {nullptr, 0}, int band = 0) {
+    float* __restrict__ bsum = nullptr, bool xcd_remap = true, int col0 = 0, const Ahead& ahead = {nullptr, 0}, int band = 0, End own_end = {}) {
     using Lds = RingLds<BM, BN, WGM, WGN, WGK>;
     constexpr int NT = WGM * WGN * WGK * 64, NS = Lds::STAGES;
     constexpr int WM = BM / WGM, WN = BN / WGN, TM = WM / 16, TN = WN / 16, HM = TM / 2;      // 16x16 tiles per wavefront
@@ -776,6 +793,7 @@ __device__ __forceinline__ void gemm_ring_tile(
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wk = wave / (WGM * WGN), wmn = wave % (WGM * WGN);
     const int wm0 = (wmn / WGN) * WM, wn0 = (wmn % WGN) * WN;
+    if constexpr (ONLY_EPI == EPI_OWN) own_end.begin(i0, tid);
 
     // Piece `slot` of a stage: its k inside the stage, and its byte offset from the tile's corner
     // (rows beyond the matrix repeat its last ones: their results are not stored).
@@ -885,7 +903,8 @@ __device__ __forceinline__ void gemm_ring_tile(
         constexpr bool sums = decltype(sums_c)::value;
         static_for<HM * TN>([&](auto i_c) {
             constexpr int i = decltype(i_c)::value, a = half * HM + i / TN, b = i % TN;
-            acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[set][b], fa[a], acc[a][b], 0, 0, 0);
+            if constexpr (F16) acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, fb[set][b]), __builtin_bit_cast(f16x8, fa[a]), acc[a][b], 0, 0, 0);
+            else acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[set][b], fa[a], acc[a][b], 0, 0, 0);
             if constexpr (sums && a == 0) cs[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, fb[set][b], cs[b], 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
             between(i_c);
@@ -1046,9 +1065,13 @@ __device__ __forceinline__ void gemm_ring_tile(
     float* slab = reinterpret_cast<float*>(lds) + (size_t)wave * EpiSlab<TN / 2>::FLOATS;
     auto finish = [&](const auto& out, auto rows_c, int rb0) {
         constexpr int TO = decltype(rows_c)::value;              // 32-row bands of this wavefront
-        auto run = [&]<int E, bool RF, bool CF>() { epilogue<E, RF, CF, TO, TN / 2>(out, slab, rb0, cb0, m, n, bias, R, C, C2, epi_flag, lane); };
-        if constexpr (ONLY_EPI == EPI_ACCUM_F32) run.template operator()<EPI_ACCUM_F32, false, false>();
-        else with_epilogue(epi, res_types, run);
+        if constexpr (ONLY_EPI == EPI_OWN) {
+            own_end.template end<TO, TN / 2>(out, lds, i0, rb0, cb0, tile_n, wave, lane);
+        } else {
+            auto run = [&]<int E, bool RF, bool CF>() { epilogue<E, RF, CF, TO, TN / 2>(out, slab, rb0, cb0, m, n, bias, R, C, C2, epi_flag, lane); };
+            if constexpr (ONLY_EPI == EPI_ACCUM_F32) run.template operator()<EPI_ACCUM_F32, false, false>();
+            else with_epilogue(epi, res_types, run);
+        }
     };
     __syncthreads();                           // the buffers become the wavefronts' slabs
     if constexpr (WGK == 1) {

@@ -118,6 +118,12 @@ int layernorm_bwd_reduce(int dtype, int rows, int cols, int count, const float* 
 size_t colsum_scratch_floats(int rows, int cols);
 int colsum(int dtype, int rows, int cols, const void* x, float* out, float* scratch, void* stream);
 int fill_zero_f32(float* p, size_t n, void* stream);
+int loss_sum(const float* loss_rows, int n, float* loss, void* stream);      // loss[0] += their sum, in a fixed order
+
+// AdamW over tensors whose arguments have been checked (chimera_op_adamw); hyperparameters: see adamw_check
+struct AdamwTensor { void *p, *m, *v; float *master, *scale; const float* g; int64_t n; float decay; };
+int adamw_check(int dtype, int bits, const chimera_adamw_hyper* h_hyper, const void* d_hyper);
+int adamw_step(int dtype, int bits, int count, const AdamwTensor* t, const chimera_adamw_hyper* h_hyper, void* d_hyper, const float* d_factor, void* stream);
 
 struct AttnArgs {
     int batch, seq, heads, head_dim, causal;

@@ -717,6 +717,40 @@ std::pair<ReplayPlan*, bool> find_plan(std::list<ReplayPlan>& plans, std::vector
     }
     return {&plans.front(), known};
 }
+
+// Layout of a stage's step state: master weights (bf16), then the moments of all parameters in the weights' order; in 8 bits every tensor begins
+// at a block of 256 and the scales follow.
+struct StepState { size_t master, m, v, scale, total; };
+constexpr size_t MOMENTS = 256;
+constexpr int STAGE_TENSORS = 12;
+std::array<std::pair<size_t, bool>, STAGE_TENSORS> tensors_of(const chimera_stage* st) {      // elements of a block's tensors in order, and which decay
+    const size_t H = st->H;
+    return {{{H, false}, {H, false}, {3 * H * H, true}, {3 * H, false}, {H * H, true}, {H, false}, {H, false}, {H, false}, {4 * H * H, true}, {4 * H, false}, {4 * H * H, true}, {H, false}}};
+}
+StepState step_state(const chimera_stage* st, int bits) {
+    const size_t params = st->layer_params * st->L;
+    size_t blocks = 0, b = 0;
+    for (const auto& [n, decays] : tensors_of(st)) blocks += (n + MOMENTS - 1) / MOMENTS * st->L;
+    auto take = [&](size_t bytes) { size_t r = b; b += align_up(bytes); return r; };
+    StepState s{};
+    s.master = take(st->dtype == CHIMERA_BF16 ? params * 4 : 0);
+    s.m = take(bits == 32 ? params * 4 : blocks * MOMENTS);
+    s.v = take(bits == 32 ? params * 4 : blocks * MOMENTS);
+    s.scale = take(bits == 32 ? 0 : blocks * 8);
+    s.total = b;
+    return s;
+}
+int check_step(const chimera_stage* st, const void* d_weights, const void* d_state, int bits) {
+    if (!st) return fail(CHIMERA_EINVAL, "stage is NULL");
+    if (!st->bound) return fail(CHIMERA_ESTATE, "stage is not bound");
+    if (bits != 32 && bits != 8) return fail(CHIMERA_EINVAL, "moments of %d bits (8 or 32)", bits);
+    if (!d_weights || !d_state) return fail(CHIMERA_EINVAL, "a device buffer is NULL");
+    if (((uintptr_t)d_weights | (uintptr_t)d_state) & 255) return fail(CHIMERA_EINVAL, "device buffers must be 256-byte aligned");
+    return CHIMERA_OK;
+}
+__global__ __launch_bounds__(256) void widen_kernel(const __bf16* __restrict__ from, float* __restrict__ to, size_t n) {
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) to[i] = (float)from[i];
+}
 }  // namespace
 
 // ----------------------------------------------------------------------- ABI
@@ -901,6 +935,50 @@ int chimera_stage_read_grads(chimera_stage* st, float* h_dst, size_t bytes) {
     if (e == hipSuccess) e = hipStreamSynchronize(st->stream);
     if (e != hipSuccess) return fail(CHIMERA_EDEVICE, "gradient readback: %s", hipGetErrorString(e));
     return CHIMERA_OK;
+}
+
+size_t chimera_stage_adamw_state_bytes(const chimera_stage* st, int state_bits) {
+    return st && (state_bits == 32 || state_bits == 8) ? step_state(st, state_bits).total : 0;
+}
+
+int chimera_stage_adamw_init(chimera_stage* st, const void* d_weights, void* d_state, int state_bits) {
+    TRY(check_step(st, d_weights, d_state, state_bits));
+    const StepState s = step_state(st, state_bits);
+    const size_t params = st->layer_params * st->L;
+    if (st->dtype == CHIMERA_BF16) {
+        hipLaunchKernelGGL(widen_kernel, dim3(2048), dim3(256), 0, st->stream, (const __bf16*)d_weights, (float*)((char*)d_state + s.master), params);
+        if (hipError_t e = hipGetLastError(); e != hipSuccess) return fail(CHIMERA_EDEVICE, "AdamW: %s", hipGetErrorString(e));
+    }
+    return fill_zero_f32((float*)((char*)d_state + s.m), (s.total - s.m) / 4, st->stream);
+}
+
+int chimera_stage_adamw_step(chimera_stage* st, void* d_weights, void* d_state, int state_bits, float decay, const chimera_adamw_hyper* h_hyper,
+                             void* d_hyper, const float* d_grad_scale) {
+    TRY(check_step(st, d_weights, d_state, state_bits));
+    TRY(adamw_check(st->dtype, state_bits, h_hyper, d_hyper));
+    if (!(decay >= 0 && decay <= 3e38f)) return fail(CHIMERA_EINVAL, "weight decay must be finite and not negative");
+    if (!st->in_flight.empty()) return fail(CHIMERA_ESTATE, "micro-batches are in flight");
+    TRY(flush_pending_zero(st));
+    const StepState s = step_state(st, state_bits);
+    char* state = (char*)d_state;
+    try {
+        std::vector<AdamwTensor> t;
+        t.reserve((size_t)st->L * STAGE_TENSORS);
+        size_t at = 0, block = 0;
+        const size_t width = state_bits == 32 ? 4 : 1;
+        for (int l = 0; l < st->L; ++l)
+            for (const auto& [n, decays] : tensors_of(st)) {
+                const size_t moment = (state_bits == 32 ? at : block * MOMENTS) * width;
+                t.push_back({(char*)d_weights + at * st->esz, state + s.m + moment, state + s.v + moment,
+                             st->dtype == CHIMERA_BF16 ? (float*)(state + s.master) + at : nullptr, state_bits == 8 ? (float*)(state + s.scale) + block * 2 : nullptr,
+                             st->grads + at, (int64_t)n, decays ? decay : 0.f});
+                at += n;
+                block += (n + MOMENTS - 1) / MOMENTS;
+            }
+        return adamw_step(st->dtype, state_bits, (int)t.size(), t.data(), h_hyper, d_hyper, d_grad_scale, st->stream);
+    } catch (const std::bad_alloc&) {
+        return fail(CHIMERA_ENOMEM, "out of host memory");
+    }
 }
 
 int chimera_worker_bind_pipes(chimera_stage* const* h_stages, int count) {

@@ -1,0 +1,606 @@
+"""GPU parity of the loss without logits, the gradient norm and AdamW against plain 64-bit arithmetic (torch float64).
+
+Tolerances are per element and count roundings.  A sum of K products in floats, in any order, is off by at most K 2^-24 of the sum of the products'
+magnitudes (float operands, held as three bf16 numbers, leave out 2^-24 of each product more); the hardware's exp2 by 2^-22 relative, its argument,
+rounded, by 2^-23 |x| more; a result in bf16 by 2^-8, half a step."""
+import math
+
+import pytest
+
+from paper_2107_06925_amd import binding as b
+
+pytestmark = pytest.mark.gpu
+
+E24, E23, E22 = 2.0 ** -24, 2.0 ** -23, 2.0 ** -22
+
+
+def _torch():
+    import torch
+    return torch
+
+
+def _dtype(dtype):
+    torch = _torch()
+    return torch.float32 if dtype == b.F32 else torch.bfloat16
+
+
+def _case(dtype, tokens, hidden, vocab, ldw=None, ldh=None, ignore=0.2, seed=0, peak=2.0, poison=True):
+    """h, w, targets on views whose rows lie further apart than they are long; NaN wherever the operators must not look."""
+    torch = _torch()
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    ldw, ldh = ldw or (vocab + 7) // 8 * 8, ldh or hidden
+    t = _dtype(dtype)
+    w = torch.full((hidden, ldw), float("nan") if poison else 0.0, device="cuda", dtype=t)
+    w[:, :vocab] = (torch.randn((hidden, vocab), device="cuda", generator=gen) * (peak / math.sqrt(hidden))).to(t)
+    h = torch.full((tokens, ldh), float("nan") if poison else 0.0, device="cuda", dtype=t)
+    h[:, :hidden] = torch.randn((tokens, hidden), device="cuda", generator=gen).to(t)
+    targets = torch.randint(0, vocab, (tokens,), device="cuda", generator=gen, dtype=torch.int32)
+    drop = torch.rand(tokens, device="cuda", generator=gen) < ignore
+    if ignore and tokens > 2:
+        drop[tokens // 2] = True
+    targets[drop] = torch.tensor([-1, -100, vocab, 2 ** 31 - 1, -2 ** 31], device="cuda", dtype=torch.int64).to(torch.int32)[torch.arange(int(drop.sum())).cuda() % 5]
+    return h[:, :hidden], w[:, :vocab], targets
+
+
+def _logits(h, w, dtype):
+    """z in 64 bits and how far a float z may be from it."""
+    z = h.double() @ w.double()
+    k = h.shape[1]
+    off = (k + 8 + (16 if dtype == b.F32 else 0)) * E24 * (h.double().abs() @ w.double().abs())
+    return z, off
+
+
+def _forward(h, w, targets, scale, loss0=0.5, workspace=None):
+    torch = _torch()
+    tokens = h.shape[0]
+    rows, lse = torch.full((tokens,), float("nan"), device="cuda"), torch.full((tokens,), float("nan"), device="cuda")
+    loss = torch.full((1,), loss0, device="cuda")
+    b.chimera_op_linear_xent_fwd(h, w, targets, scale, rows, lse, loss, workspace=workspace)
+    return rows, lse, loss
+
+
+def _check_forward(dtype, h, w, targets, scale, rows, lse, loss, loss0=0.5):
+    torch = _torch()
+    z, off = _logits(h, w, dtype)
+    want = torch.logsumexp(z, 1)
+    # a shift of all logits by `off`, and sums of exponentials off by (V + 64) 2^-24 + 2^-22 + what the arguments lose (x 2^-23 weighted with e^-x: below 2^-23)
+    lse_off = off.amax(1) + (w.shape[1] * E24 if w.shape[1] < 4096 else 4096 * E24) + 4 * E22 + want.abs() * E23
+    assert ((lse.double() - want).abs() <= lse_off).all(), float(((lse.double() - want).abs() / lse_off).max())
+    valid = (targets >= 0) & (targets < w.shape[1])
+    at = z.gather(1, targets.clamp(0, w.shape[1] - 1).long()[:, None])[:, 0]
+    per = torch.where(valid, scale * (want - at), torch.zeros_like(at))
+    per_off = torch.where(valid, abs(scale) * (lse_off + off.amax(1) + 2 * E24 * (want.abs() + at.abs())), torch.zeros_like(at))
+    assert ((rows.double() - per).abs() <= per_off).all()
+    total = float(rows.double().sum()) + loss0
+    assert abs(float(loss) - total) <= (rows.numel() + 8) * E24 * (float(rows.double().abs().sum()) + abs(loss0))
+
+
+# tiles of 256x256 need 144 of them (1024 x 9300), more 128x128 tiles than CUs 2200 tokens x 2000; both ends of a tile, one token, one word
+FWD = [(1, 8, 1, 8, 8), (1, 64, 7, 16, 64), (2, 8, 8, 8, 16), (24, 256, 1000, 1000, 256), (33, 72, 257, 264, 80), (130, 136, 513, 576, 136), (128, 64, 384, 384, 64),
+       (1, 1600, 50257, 50304, 1600), (1024, 64, 9300, 9304, 64), (1000, 192, 9473, 9480, 200), (2200, 128, 2001, 2008, 128)]
+
+
+@pytest.mark.parametrize("dtype", [b.F32, b.BF16])
+@pytest.mark.parametrize("tokens,hidden,vocab,ldw,ldh", FWD)
+def test_linear_xent_fwd(dtype, tokens, hidden, vocab, ldw, ldh):
+    print("linear xent fwd", dtype, tokens, hidden, vocab, ldw, ldh, flush=True)
+    h, w, targets = _case(dtype, tokens, hidden, vocab, ldw, ldh, seed=tokens + vocab)
+    rows, lse, loss = _forward(h, w, targets, 0.25)
+    _check_forward(dtype, h, w, targets, 0.25, rows, lse, loss)
+
+
+@pytest.mark.parametrize("dtype", [b.F32, b.BF16])
+def test_linear_xent_fwd_extreme_logits(dtype):
+    # one word holds all of the probability; all logits equal; logits of +-80 000; every token ignored
+    torch = _torch()
+    h, w, targets = _case(dtype, 40, 64, 3001, ignore=0.0, seed=5)
+    h[:10] *= 40
+    h[10:20] = 0
+    h[20:30] *= 20000
+    targets[30:] = -1
+    rows, lse, loss = _forward(h, w, targets, 1.0)
+    _check_forward(dtype, h, w, targets, 1.0, rows, lse, loss)
+    assert (lse[10:20] - math.log(3001)).abs().max() <= 1e-5
+    targets.fill_(-1)
+    rows, _, loss = _forward(h, w, targets, 1.0)
+    assert torch.equal(rows, torch.zeros_like(rows)) and float(loss) == 0.5
+
+
+def _backward(dtype, h, w, targets, lse, scale, dloss=None, overwrite=False, piece=0, want=("dh", "dw"), lddw=None, lddh=None, seed=9, workspace=None):
+    torch = _torch()
+    (tokens, hidden), vocab = h.shape, w.shape[1]
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    dh = torch.full((tokens, lddh or hidden), 7.0, device="cuda", dtype=_dtype(dtype))
+    dw0 = torch.randn((hidden, lddw or (vocab + 7) // 8 * 8), device="cuda", generator=gen) * 1e-3
+    dw = dw0.clone()
+    if overwrite:
+        dw[:, :vocab] = float("nan")
+    b.chimera_op_linear_xent_bwd(h, w, targets, lse, scale, dh[:, :hidden] if "dh" in want else None, dw[:, :vocab] if "dw" in want else None, dloss=dloss,
+                                 overwrite=overwrite, piece=piece, workspace=workspace)
+    assert torch.equal(dw[:, vocab:], dw0[:, vocab:]), "columns behind the vocabulary are left as they are"
+    assert (dh[:, hidden:] == 7.0).all()
+    return dh[:, :hidden], dw[:, :vocab], dw0[:, :vocab]
+
+
+def _check_backward(dtype, h, w, targets, lse, scale, dloss, dh, dw, dw0):
+    torch = _torch()
+    tokens, vocab = h.shape[0], w.shape[1]
+    valid = (targets >= 0) & (targets < vocab)
+    h = torch.where(valid[:, None], h, torch.zeros_like(h))                # (a token that does not count may hold anything)
+    lse = torch.where(valid, lse, torch.zeros_like(lse))
+    z, off = _logits(h, w, dtype)
+    x = z - lse.double()[:, None]
+    p = x.exp()
+    # p: z is off by `off`, z - lse and its product with log2 e are rounded, exp2; one rounding of p - 1, one of its product with coef
+    p_off = p * (off + 3 * E24 * (x.abs() + z.abs()) + E22) + E23 * (p + 1)
+    coef = scale * (valid.double() if dloss is None else torch.where(valid, dloss.double(), torch.zeros_like(dloss).double()))
+    dz = p.clone()
+    rows = torch.arange(tokens, device="cuda")
+    dz[rows, targets.clamp(0, vocab - 1).long()] -= 1
+    dz *= coef[:, None]
+    dz_off = coef.abs()[:, None] * p_off + 2 * E24 * dz.abs()
+    hd, wd = h.double(), w.double()
+    if dh is not None:
+        want = dz @ wd.t()
+        mag = dz.abs() @ wd.abs().t()
+        rounding = 2.0 ** -8 if dtype == b.BF16 else 3 * E24
+        tol = dz_off @ wd.abs().t() + (rounding + (vocab + 64 + 80) * E24) * mag + (2.0 ** -8 if dtype == b.BF16 else E24) * want.abs() + 1e-38
+        assert ((dh.double() - want).abs() <= tol).all(), float(((dh.double() - want).abs() / tol).max())
+        assert (dh[~valid] == 0).all()
+    if dw is not None:
+        want = hd.t() @ dz
+        mag = hd.abs().t() @ dz.abs()
+        # dz in two fp16 numbers: 2^-22 of it, and 2^-25 2^-14 of the largest there is (below fp16's smallest numbers)
+        top = float((coef.abs() * hd.abs().amax(1)).max())
+        tol = hd.abs().t() @ dz_off + (E22 + (2 * tokens + 80) * E24) * mag + tokens * 2.0 ** -36 * top + E24 * (want + dw0.double()).abs() + 1e-38
+        got = dw.double() - dw0.double()
+        assert ((got - want).abs() <= tol + E24 * dw0.double().abs()).all(), float(((got - want).abs() / tol).max())
+
+
+# (tokens, hidden, vocab, ldw, piece): one piece and several, the last a few columns or ending inside a group of 8; tiles of 256 for dz
+# (1024 x 9300), dh (4100 x 2304: more 256x256 tiles than 128x128 ones pay for) and dW (1000 x 9473)
+BWD = [(1, 8, 1, 8, 0), (1, 64, 7, 16, 0), (2, 8, 8, 8, 0), (3, 16, 9, 24, 0), (24, 256, 1000, 1000, 0), (33, 72, 257, 264, 256), (130, 136, 1027, 1088, 256),
+       (260, 264, 771, 776, 512), (60, 512, 8000, 8000, 0), (1024, 64, 9300, 9304, 0), (40, 1000, 9473, 9480, 4864), (2200, 128, 2001, 2008, 0),
+       (4100, 2304, 1031, 1032, 512)]
+
+
+@pytest.mark.parametrize("dtype", [b.F32, b.BF16])
+@pytest.mark.parametrize("tokens,hidden,vocab,ldw,piece", BWD)
+def test_linear_xent_bwd(dtype, tokens, hidden, vocab, ldw, piece):
+    torch = _torch()
+    print("linear xent bwd", dtype, tokens, hidden, vocab, ldw, piece, flush=True)
+    h, w, targets = _case(dtype, tokens, hidden, vocab, ldw, hidden + 8, seed=tokens + vocab)
+    lse = torch.logsumexp(h.double() @ w.double(), 1).float()
+    valid = (targets >= 0) & (targets < vocab)
+    h[~valid] = float("nan")
+    lse[~valid] = float("nan")
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    dloss = torch.randn(tokens, device="cuda", generator=gen) * torch.exp(3 * torch.randn(tokens, device="cuda", generator=gen))
+    for weights, overwrite in ((None, True), (dloss, False)):
+        dh, dw, dw0 = _backward(dtype, h, w, targets, lse, 0.01, weights, overwrite, piece, lddw=ldw + 8, lddh=hidden + 16)
+        _check_backward(dtype, h, w, targets, lse, 0.01, weights, dh, dw, torch.zeros_like(dw0) if overwrite else dw0)
+
+
+@pytest.mark.parametrize("dtype", [b.F32, b.BF16])
+def test_linear_xent_bwd_one_gradient_alone_and_bit_for_bit(dtype):
+    torch = _torch()
+    h, w, targets = _case(dtype, 150, 136, 1027, seed=2)
+    _, lse, _ = _forward(h, w, targets, 1.0)
+    both = _backward(dtype, h, w, targets, lse, 0.1, piece=512)
+    again = _backward(dtype, h, w, targets, lse, 0.1, piece=512)
+    assert torch.equal(both[0], again[0]) and torch.equal(both[1], again[1])
+    dh, dw, dw0 = _backward(dtype, h, w, targets, lse, 0.1, piece=512, want=("dh",))
+    assert torch.equal(dh, both[0]) and torch.equal(dw, dw0)
+    dh, dw, _ = _backward(dtype, h, w, targets, lse, 0.1, piece=512, want=("dw",))
+    assert torch.equal(dw, both[1]) and (dh == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype", [b.F32, b.BF16])
+def test_linear_xent_bwd_ranges(dtype):
+    # rows of h and weights of very different size: fp16 holds 2^-24 .. 65504, the operands here span 2^-100 .. 2^40
+    torch = _torch()
+    h, w, targets = _case(dtype, 64, 64, 500, ignore=0.0, seed=11)
+    for i, e in enumerate((-100, -60, -30, -20, -10, 0, 10, 16)):
+        h[i * 8:i * 8 + 8] *= 2.0 ** e
+    w *= 2.0 ** -14                                                         # logits of at most a few
+    lse = torch.logsumexp(h.double() @ w.double(), 1).float()
+    for dloss in (None, torch.exp2(torch.linspace(-60, 40, 64, device="cuda")), torch.zeros(64, device="cuda")):
+        dh, dw, dw0 = _backward(dtype, h, w, targets, lse, 2.0 ** -10, dloss, overwrite=True)
+        _check_backward(dtype, h, w, targets, lse, 2.0 ** -10, dloss, dh, dw, torch.zeros_like(dw0))
+    targets.fill_(500)                                                      # nothing counts
+    dh, dw, _ = _backward(dtype, h, w, targets, lse, 1.0, None, overwrite=True)
+    assert (dh == 0).all() and (dw == 0).all()
+    dh, dw, dw0 = _backward(dtype, h, w, targets, lse, 1.0, None)
+    assert torch.equal(dw, dw0)
+
+
+def test_linear_xent_gradient_against_differences():
+    # the gradients the backward leaves are those of the loss the forward leaves (float, central differences along random directions)
+    torch = _torch()
+    h, w, targets = _case(b.F32, 30, 40, 203, seed=4, poison=False)
+    h, w = h.contiguous(), w
+    _, lse, _ = _forward(h, w, targets, 0.1)
+    dh, dw, _ = _backward(b.F32, h, w, targets, lse, 0.1, overwrite=True)
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    for k in range(4):
+        u, v = torch.randn(h.shape, device="cuda", generator=gen), torch.randn(w.shape, device="cuda", generator=gen)
+        u, v = u / u.norm(), v / v.norm()
+        step = 2.0 ** -4
+        f = []
+        for s in (step, -step):
+            wide = torch.zeros((40, 208), device="cuda")
+            wide[:, :203] = w + s * v
+            f.append(float(_forward(h + s * u, wide[:, :203], targets, 0.1)[0].double().sum()))
+        slope = float((dh.double() * u).sum() + (dw.double() * v).sum())
+        assert abs((f[0] - f[1]) / (2 * step) - slope) <= 2e-3 * max(1.0, abs(slope))      # step^2/6 of the third derivative, 2^-24 of a loss of 50 / step
+
+
+def test_linear_xent_captured_and_on_another_stream():
+    torch = _torch()
+    h, w, targets = _case(b.BF16, 200, 128, 3001, seed=6)
+    rows, lse, loss = _forward(h, w, targets, 0.1)
+    want = _backward(b.BF16, h, w, targets, lse, 0.1, piece=1024, overwrite=True)
+    side = torch.cuda.Stream()
+    ws_f = torch.empty(b.lib().chimera_op_linear_xent_fwd_workspace_bytes(b.BF16, 200, 128, 3001), dtype=torch.uint8, device="cuda")
+    ws_b = torch.empty(b.lib().chimera_op_linear_xent_bwd_workspace_bytes(b.BF16, 200, 128, 3001, 1024), dtype=torch.uint8, device="cuda")
+    rows2, lse2, loss2 = torch.zeros(200, device="cuda"), torch.zeros(200, device="cuda"), torch.zeros(1, device="cuda")
+    dh2, dw2 = torch.zeros((200, 128), device="cuda", dtype=torch.bfloat16), torch.zeros((128, 3008), device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+
+    def both():
+        b.chimera_op_linear_xent_fwd(h, w, targets, 0.1, rows2, lse2, loss2, workspace=ws_f)
+        b.chimera_op_linear_xent_bwd(h, w, targets, lse2, 0.1, dh2, dw2[:, :3001], overwrite=True, piece=1024, workspace=ws_b)
+    with torch.cuda.stream(side):
+        both()
+        side.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            both()
+    for _ in range(3):
+        for t in (rows2, lse2, loss2, dh2, dw2):
+            t.fill_(-3.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(rows2, rows) and torch.equal(lse2, lse) and torch.equal(dh2, want[0]) and torch.equal(dw2[:, :3001], want[1])
+        assert abs(float(loss2) + 3.0 - (float(loss) - 0.5)) <= 1e-5
+
+
+@pytest.mark.parametrize("dtype", [b.F32, b.BF16])
+@pytest.mark.parametrize("tokens,hidden,vocab,ldw,piece", [(96, 64, 504, 504, 256), (130, 256, 1001, 1016, 0)])
+def test_head_loss_pieces_against_head_loss(dtype, tokens, hidden, vocab, ldw, piece):
+    torch = _torch()
+    print("head pieces", dtype, tokens, hidden, vocab, flush=True)
+    t = _dtype(dtype)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    rnd = lambda *s: torch.randn(s, device="cuda", generator=gen)  # noqa: E731
+    y, g, be = rnd(tokens, hidden).to(t), (1 + 0.1 * rnd(hidden)).to(t), (0.1 * rnd(hidden)).to(t)
+    w = torch.zeros((hidden, ldw), device="cuda", dtype=t)
+    w[:, :vocab] = (0.2 * rnd(hidden, vocab)).to(t)
+    targets = torch.randint(0, vocab, (tokens,), device="cuda", generator=gen, dtype=torch.int32)
+
+    def outputs(ld):
+        return [torch.zeros((tokens, hidden), device="cuda", dtype=t), torch.full((hidden,), 0.5, device="cuda"), torch.full((hidden,), -0.5, device="cuda"),
+                torch.full((hidden, ld), 0.25, device="cuda"), torch.full((1,), 2.0, device="cuda")]
+    got = outputs(ldw)
+    b.chimera_head_loss_pieces(y, targets, g, be, w[:, :vocab], 1.0 / tokens, *got, piece=piece)
+    # 64 bits, through autograd
+    p = [x.double().requires_grad_() for x in (y, g, be, w[:, :vocab])]
+    h = torch.nn.functional.layer_norm(p[0], (hidden,), p[1], p[2], 1e-5)
+    loss = torch.nn.functional.cross_entropy(h @ p[3], targets.long())
+    loss.backward()
+    tol = 2e-2 if dtype == b.BF16 else 1e-4                                   # the head's bars: h is rounded to the type between the kernels
+    want = [p[0].grad, p[1].grad + 0.5, p[2].grad - 0.5, p[3].grad + 0.25]
+    for name, a, q in zip(("dy", "dg", "db", "dw"), [got[0], got[1], got[2], got[3][:, :vocab]], want):
+        base = {"dy": 0.0, "dg": 0.5, "db": -0.5, "dw": 0.25}[name]
+        err = float((a.double() - q).abs().max() / (q - base).abs().max())
+        assert err <= tol, (name, err)
+    assert (got[3][:, vocab:] == 0.25).all()
+    assert abs(float(got[4]) - 2.0 - float(loss)) <= tol * float(loss)
+    if vocab % 8 == 0:                                                        # and the head that keeps its logits agrees
+        kept = outputs(vocab)
+        b.chimera_head_loss(y, targets, g, be, w, 1.0 / tokens, *kept)
+        for a, q in zip(got, kept):
+            assert float((a.double() - q.double()).abs().max()) <= 2 * tol * max(1e-3, float(q.double().abs().max()))
+    # tokens that do not count: as if they were not there
+    targets[::3] = -1
+    few = outputs(ldw)
+    b.chimera_head_loss_pieces(y, targets, g, be, w[:, :vocab], 1.0 / tokens, *few, piece=piece)
+    assert (few[0][::3].float() == 0).all()
+
+
+# ---------------------------------------------------------------- gradient norm
+@pytest.mark.parametrize("sizes", [[1], [3], [4095, 1, 0, 4097], [100003] * 5, [7] * 150, [5_000_001, 20_000_003], [70_000_000]])
+def test_grad_norm(sizes):
+    torch = _torch()
+    print("grad norm", len(sizes), sum(sizes), flush=True)
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    grads = [torch.randn(n + 1, device="cuda", generator=gen)[1:] * 1e-3 for n in sizes]       # 4-byte aligned only
+    out = torch.empty(2, device="cuda")
+    want = math.sqrt(sum(float(g.double().square().sum()) for g in grads))
+    for max_norm in (want * 0.5, want * 2, 1e-20):
+        b.chimera_op_grad_norm(grads, max_norm, out)
+        norm, factor = (float(x) for x in out)
+        assert abs(norm - want) <= 2 * E24 * want                                 # one rounding: the sum is in double
+        assert abs(factor - min(1.0, max_norm / want)) <= 3 * E24 * factor
+    b.chimera_op_grad_norm(grads, want * 2, out)
+    assert float(out[1]) == 1.0
+
+
+def test_grad_norm_ranges():
+    torch = _torch()
+    out = torch.empty(2, device="cuda")
+    for values, norm, factor in (([0.0, 0.0], 0.0, 1.0), ([3e30, 4e30], 5e30, 2e-31), ([3e-30, -4e-30], 5e-30, 1.0), ([3.4e38, 1.0], 3.4e38, 1 / 3.4e38)):
+        b.chimera_op_grad_norm([torch.tensor(values, device="cuda")], 1.0, out)
+        assert abs(float(out[0]) - norm) <= 4 * E24 * norm and abs(float(out[1]) - factor) <= 4 * E24 * factor + 2.0 ** -149
+    for bad in (float("inf"), float("nan"), -float("inf")):
+        b.chimera_op_grad_norm([torch.tensor([1.0, bad, 2.0], device="cuda")], 1.0, out)
+        assert not math.isfinite(float(out[0])) and math.isnan(float(out[1]))
+    b.chimera_op_grad_norm([torch.full((2000,), 3e38, device="cuda")], 1.0, out)          # the norm itself overflows
+    assert math.isinf(float(out[0])) and math.isnan(float(out[1]))
+
+
+# ------------------------------------------------------------------------ AdamW
+def _tensors(dtype, sizes, bits, seed=0, shift=0):
+    """Weights, gradients and moments of tensors that lie in one buffer, `shift` elements from an aligned place."""
+    torch = _torch()
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    total = sum(sizes) + shift
+    cut = lambda x: [p for p in x[shift:].split(sizes)]  # noqa: E731
+    size = torch.exp(torch.randn(total, device="cuda", generator=gen))
+    master, grad = torch.randn(total, device="cuda", generator=gen) * 0.02, torch.randn(total, device="cuda", generator=gen) * size * 1e-3
+    s = dict(grads=cut(grad), params=cut(master.to(_dtype(dtype))), masters=cut(master) if dtype == b.BF16 else None, scales=None)
+    if dtype == b.F32:
+        s["params"] = cut(master)
+    if bits == 32:
+        s["ms"], s["vs"] = cut(torch.randn(total, device="cuda", generator=gen) * size * 3e-4), cut((torch.randn(total, device="cuda", generator=gen) * size * 1e-3) ** 2)
+    else:
+        s["ms"], s["vs"] = (cut(torch.randint(0, 127, (total,), device="cuda", generator=gen, dtype=torch.uint8).view(torch.float8_e4m3fn)) for _ in range(2))
+        s["scales"] = [torch.rand(2 * ((n + 255) // 256), device="cuda", generator=gen) * 1e-5 for n in sizes]
+    return s
+
+
+def _moments(s, i):
+    """m and v of tensor i in 64 bits."""
+    torch = _torch()
+    if s["scales"] is None:
+        return s["ms"][i].double(), s["vs"][i].double()
+    n = s["ms"][i].numel()
+    scale = s["scales"][i].double().view(-1, 2).repeat_interleave(256, 0)[:n]
+    return s["ms"][i].to(torch.float64) * scale[:, 0], (s["vs"][i].to(torch.float64) * scale[:, 1]) ** 2
+
+
+def _clone(s):
+    return {k: None if x is None else [t.clone() for t in x] for k, x in s.items()}
+
+
+H = dict(beta1=0.9, beta2=0.95, eps=1e-8)
+SIZES = [[1], [255, 1, 257], [4096, 4095, 0, 4097, 3], [64] * 120, [300_001, 12], [2_000_003]]
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("dtype", [b.F32, b.BF16])
+@pytest.mark.parametrize("sizes", SIZES, ids=lambda s: "%dx%d" % (len(s), max(s)))
+@pytest.mark.parametrize("shift", [0, 3])
+def test_adamw(dtype, bits, sizes, shift):
+    torch = _torch()
+    print("adamw", dtype, bits, len(sizes), shift, flush=True)
+    s = _tensors(dtype, sizes, bits, shift=shift)
+    old = _clone(s)
+    decay = [0.1 * (i % 3) for i in range(len(sizes))]
+    factor = torch.tensor([0.4], device="cuda")
+    b.AdamW(decay=decay, **H, **s).step(lr=2e-3, step=5, seed=77, grad_scale=factor)
+    for i, n in enumerate(sizes):
+        g = old["grads"][i].double() * float(factor)
+        m0, v0 = _moments(old, i)
+        m, v = 0.9 * m0 + (1 - 0.9) * g, 0.95 * v0 + (1 - 0.95) * g * g
+        p0 = (old["masters"] or old["params"])[i].double()
+        update = 2e-3 / (1 - 0.9 ** 5) * m / (v.sqrt() / math.sqrt(1 - 0.95 ** 5) + 1e-8)
+        p = p0 * (1 - 2e-3 * decay[i]) - update
+        new = (s["masters"] or s["params"])[i].double()
+        # m: three roundings of terms that may cancel; v, its root, the quotient: some ten of 2^-24
+        m_off = 4 * E24 * (0.9 * m0.abs() + 0.1 * g.abs())
+        rel = 2e-3 / (1 - 0.9 ** 5) / (v.sqrt() / math.sqrt(1 - 0.95 ** 5) + 1e-8)
+        off = rel * m_off + 12 * E24 * update.abs() + 3 * E24 * p0.abs() + E24 * p.abs()
+        assert ((new - p).abs() <= off).all(), float(((new - p).abs() / off).max())
+        if dtype == b.BF16:
+            assert torch.equal(s["params"][i], s["masters"][i].to(torch.bfloat16))
+        assert torch.equal(s["grads"][i], old["grads"][i])
+        if bits == 32:
+            assert ((s["ms"][i].double() - m).abs() <= m_off).all()
+            assert ((s["vs"][i].double() - v).abs() <= 6 * E24 * v).all()
+            continue
+        got_m, got_v = _moments(s, i)
+        pad = (n + 255) // 256 * 256 - n
+        blocks = lambda x: torch.nn.functional.pad(x, (0, pad)).view(-1, 256)  # noqa: E731
+        top = torch.stack((blocks(m.abs()).amax(1), blocks(v.sqrt()).amax(1)), 1) if n else torch.zeros((0, 2), device="cuda").double()
+        top_off = 8 * E24 * top
+        if n:
+            top_off[:, 0] += blocks(m_off).amax(1)
+        assert ((s["scales"][i].double().view(-1, 2) - top / 448).abs() <= top_off / 448 + 1e-33).all()
+        for got, want, big, off in ((got_m, m, top[:, 0], m_off), (got_v.sqrt(), v.sqrt(), top[:, 1], 8 * E24 * v.sqrt())):
+            # rounded to one of the two codes beside it: a step of e4m3 is 2^-3 of the power of two below, at least 2^-9 of 448ths
+            unit = big.repeat_interleave(256)[:n] / 448
+            step = unit * torch.exp2(torch.floor(torch.log2((want.abs() / unit).clamp(min=2.0 ** -6))) - 3)
+            assert ((got - want).abs() <= step * (1 + 1e-5) + off + 8 * E24 * want.abs()).all()
+        assert ((got_v > 0) == (v > 0)).all()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_is_a_function_of_its_arguments(bits):
+    torch = _torch()
+    runs = []
+    for seed, step in ((1, 3), (1, 3), (2, 3), (1, 4)):
+        s = _tensors(b.BF16, [5000, 333], bits)
+        b.AdamW(**H, **s).step(lr=1e-3, step=step, seed=seed)
+        runs.append(s)
+    same = lambda x, y: all(torch.equal(a.view(torch.uint8), c.view(torch.uint8)) for a, c in zip(x["ms"] + x["vs"], y["ms"] + y["vs"]))  # noqa: E731
+    assert same(runs[0], runs[1]) and torch.equal(runs[0]["masters"][0], runs[1]["masters"][0])
+    if bits == 8:
+        assert not same(runs[0], runs[2]) and not same(runs[0], runs[3])
+    # tensors that are stepped together round as tensors of one call whose blocks are counted on: the second one alone starts at block 0
+    s = _tensors(b.BF16, [5120, 333], bits)
+    t = _clone(s)
+    b.AdamW(**H, **s).step(lr=1e-3, step=3, seed=1)
+    flat = {k: None if x is None else [torch.cat(x)] for k, x in t.items()}                   # 5120 = 20 blocks: the same numbers
+    b.AdamW(**H, **flat).step(lr=1e-3, step=3, seed=1)
+    assert torch.equal(flat["masters"][0], torch.cat(s["masters"])) and torch.equal(flat["ms"][0].view(torch.uint8), torch.cat(s["ms"]).view(torch.uint8))
+
+
+def test_adamw_eight_bit_rounding_is_unbiased():
+    # v decays by 0.999 a step while gradients are zero: rounding to nearest would never move it.  After 1000 steps sqrt(v) is
+    # 0.6063 of what it was on average; a value takes random steps of 6 to 12 %, its standard deviation is below 0.4, the mean of 65536 below 0.0016
+    torch = _torch()
+    n = 65536
+    p, g = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+    m = torch.zeros(n, device="cuda", dtype=torch.uint8).view(torch.float8_e4m3fn)
+    v = torch.full((n,), 64.0, device="cuda").to(torch.float8_e4m3fn)
+    scale = torch.ones(2 * n // 256, device="cuda")
+    scale[0::2] = 0
+    v[::256], g[::256] = 448.0, 448.0                         # the block's largest stays, and its scale with it
+    opt = b.AdamW([p], [g], [m], [v], scales=[scale], beta1=0.9, beta2=0.999)
+    for step in range(1, 1001):
+        opt.step(lr=0.0, step=step, seed=5)
+    r = v.float() * scale.view(-1, 2)[:, 1].repeat_interleave(256)
+    keep = torch.ones(n, dtype=torch.bool, device="cuda")
+    keep[::256] = False
+    assert abs(float(r[keep].mean()) / 64.0 - 0.999 ** 500) <= 0.008
+    assert abs(float(scale[1]) - 1) <= 1e-3
+    # one step's bits: the mean of many values that lie between two codes, and both moments rounded independently
+    g = torch.full((n,), 1.0, device="cuda")
+    g[::256] = 3.3
+    m.view(torch.uint8).zero_(), v.view(torch.uint8).zero_(), scale.zero_()
+    opt = b.AdamW([p], [g], [m], [v], scales=[scale], beta1=0.0, beta2=0.5)
+    opt.step(lr=0.0, step=1, seed=9)
+    x, y = m.float()[keep] / (448 / 3.3), v.float()[keep] / (448 / 3.3)
+    assert abs(float(x.mean()) - 1) <= 5 * 0.06 / math.sqrt(n) and abs(float(y.mean()) - 1) <= 5 * 0.06 / math.sqrt(n)
+    a, c = (x > x.mean()).float(), (y > y.mean()).float()
+    assert abs(float(((a - a.mean()) * (c - c.mean())).mean())) <= 5 * 0.25 / math.sqrt(n)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_left_out_and_poisoned(bits):
+    torch = _torch()
+    s = _tensors(b.BF16, [1000, 300], bits)
+    old = _clone(s)
+    for bad in (float("nan"), float("inf"), -float("inf")):
+        b.AdamW(**H, **s).step(lr=1e-3, step=2, grad_scale=torch.tensor([bad], device="cuda"))
+        for k in s:
+            for x, y in zip(s[k] or [], old[k] or []):
+                assert torch.equal(x.view(torch.uint8), y.view(torch.uint8)), k
+    # a gradient that is not a number stays in its value (in 8 bits an infinite one in its block)
+    s["grads"][0][7] = float("nan")
+    b.AdamW(**H, **s).step(lr=1e-3, step=2)
+    assert torch.isnan(s["masters"][0][7]) and torch.isfinite(s["masters"][0][8:]).all() and torch.isfinite(s["masters"][1]).all()
+    m, v = _moments(s, 0)
+    assert torch.isnan(m[7]) and torch.isnan(v[7]) and torch.isfinite(m[8:]).all() and torch.isfinite(v[8:]).all()
+    # tiny and huge gradients
+    s = _tensors(b.F32, [512], bits)
+    s["grads"][0][:256] = 1e-40
+    s["grads"][0][256:] = 1e15
+    if bits == 8:
+        s["ms"][0].view(torch.uint8).zero_(), s["vs"][0].view(torch.uint8).zero_(), s["scales"][0].zero_()
+    else:
+        s["ms"][0].zero_(), s["vs"][0].zero_()
+    b.AdamW(**H, **s).step(lr=1e-3, step=1)
+    assert torch.isfinite(s["params"][0]).all()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_recorded_steps_follow_device_hyperparameters(bits):
+    torch = _torch()
+    import ctypes as C
+    import numpy as np
+    want, got = _tensors(b.BF16, [3000, 77], bits), _tensors(b.BF16, [3000, 77], bits)
+    opt = b.AdamW(**H, **got)
+    hyper = torch.zeros(b.ADAMW_HYPER_BYTES, dtype=torch.uint8, device="cuda")
+
+    def tell(lr, step, seed):
+        h = b.AdamWHyper(lr, 0.9, 0.95, 1e-8, step, seed)
+        raw = np.frombuffer(bytes(C.string_at(C.addressof(h), C.sizeof(h))), dtype=np.uint8).copy()
+        hyper[:raw.size].copy_(torch.from_numpy(raw))
+    start = _clone(got)
+    tell(1e-3, 1, 4)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        opt.step(lr=0, step=0, d_hyper=hyper)
+        side.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            opt.step(lr=0, step=0, d_hyper=hyper)
+    for k in got:
+        for x, y in zip(got[k] or [], start[k] or []):
+            x.copy_(y)
+    ref = b.AdamW(**H, **want)
+    for step in range(1, 5):
+        ref.step(lr=1e-3 / step, step=step, seed=step * 10)
+        tell(1e-3 / step, step, step * 10)
+        graph.replay()
+        torch.cuda.synchronize()
+        for k in got:
+            for x, y in zip(got[k] or [], want[k] or []):
+                assert torch.equal(x.view(torch.uint8), y.view(torch.uint8)), (step, k)
+
+
+# ----------------------------------------------------------- together, in a stage
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("dtype", [b.F32, b.BF16])
+def test_stage_steps(dtype, bits):
+    """Forward, loss in pieces, backward, norm, step, three times over: every step's weights against 64 bits from the gradients the library left."""
+    torch = _torch()
+    from paper_2107_06925_amd import synth
+    from gpu_util import make_stage
+    print("stage steps", dtype, bits, flush=True)
+    L, hidden, seq, mb, vocab = 2, 72, 24, 3, 1003
+    tokens = seq * mb
+    st, _ = make_stage(L, hidden, 4, seq, mb, dtype, 0)
+    t = _dtype(dtype)
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    rnd = lambda *s: torch.randn(s, device="cuda", generator=gen)  # noqa: E731
+    x, targets = rnd(tokens, hidden).to(t), torch.randint(-1, vocab, (tokens,), device="cuda", generator=gen, dtype=torch.int32)
+    g, be = torch.ones(hidden, device="cuda", dtype=t), torch.zeros(hidden, device="cuda", dtype=t)
+    w = torch.zeros((hidden, 1008), device="cuda", dtype=t)
+    w[:, :vocab] = (0.1 * rnd(hidden, vocab)).to(t)
+    dy = torch.empty((tokens, hidden), device="cuda", dtype=t)
+    y, _ = st.set_io(0, x, dy)
+    wm = w.float().clone()
+    dg, db, dw = torch.zeros(hidden, device="cuda"), torch.zeros(hidden, device="cuda"), torch.zeros((hidden, 1008), device="cuda")
+    moments = dict(ms=[torch.zeros_like(dw)], vs=[torch.zeros_like(dw)], scales=None)
+    head = b.AdamW([w if dtype == b.BF16 else wm], [dw], masters=[wm] if dtype == b.BF16 else None, **moments, decay=[0.01])
+    st.adamw_init(bits)
+    norm, loss = torch.empty(2, device="cuda"), torch.zeros(1, device="cuda")
+    params = st.grads.numel()
+    sizes = [int(math.prod(s)) for _ in range(L) for s in synth.param_shapes(hidden).values()]
+    matrix = torch.cat([torch.full((n,), float(len(s) == 2)) for (n, s) in zip(sizes, list(synth.param_shapes(hidden).values()) * L)]).double().cuda()
+    m = v = torch.zeros(params, device="cuda", dtype=torch.float64)
+    p = st.weights.double().clone()
+    for step in range(1, 4):
+        st.zero_grads()
+        st.fwd(0)
+        for a in (dg, db, dw, loss):
+            a.zero_()
+        b.chimera_head_loss_pieces(y, targets, g, be, (w if dtype == b.BF16 else wm.to(t))[:, :vocab], 1.0 / tokens, dy, dg, db, dw, loss, piece=256)
+        with pytest.raises(b.ChimeraError) as e:
+            st.adamw_step(1e-3, step)                          # a micro-batch is in flight
+        assert e.value.code == b.ESTATE
+        st.bwd(0)
+        b.chimera_op_grad_norm([st.grads, dw], 0.05, norm)
+        st.adamw_step(3e-3, step, decay=0.1, seed=3, grad_scale=norm[1:])
+        head.step(3e-3, step, grad_scale=norm[1:])
+        assert math.isfinite(float(loss)) and 0 < float(norm[1]) <= 1
+        grad = st.grads.double() * float(norm[1])
+        want = math.sqrt(float(st.grads.double().square().sum() + dw.double().square().sum()))
+        assert abs(float(norm[0]) - want) <= 2 * E24 * want
+        m, v = 0.9 * m + 0.1 * grad, 0.95 * v + 0.05 * grad * grad
+        update = 3e-3 / (1 - 0.9 ** step) * m / ((v / (1 - 0.95 ** step)).sqrt() + 1e-8)
+        p = p * (1 - 3e-3 * 0.1 * matrix) - update
+        got = st.weights.double()
+        if bits == 32:
+            off = 1e-4 * update.abs().amax() * step + 1e-6 * p.abs() + (2.0 ** -8 * p.abs() if dtype == b.BF16 else 0)
+            assert ((got - p).abs() <= off).all()
+        else:
+            # m and sqrt(v) to 12.5 % each a step at the worst: a quarter of an update, once a moment has been rounded (after the first step), on
+            # top of what the smallest codes of a block lose; seen over all weights
+            err = float((got - p).norm() / (3e-3 * math.sqrt(params)))
+            assert err <= (0.01 if step == 1 else 0.3 * step) + (2.0 ** -9 * float(p.norm()) / (3e-3 * math.sqrt(params)) if dtype == b.BF16 else 0), err
+        p = st.weights.double().clone() if dtype == b.F32 else p

@@ -1,0 +1,146 @@
+"""What the loss without logits, the gradient norm and AdamW refuse, and the sizes they ask for: all decided on the host, before any launch."""
+import ctypes as C
+
+import pytest
+
+from paper_2107_06925_amd import binding as b
+
+P = 0x10000                                     # an aligned address that no call below follows
+U64 = 1 << 62
+
+
+
+def fwd(dtype=b.BF16, tokens=4, hidden=64, vocab=100, h=P, ldh=64, w=P, ldw=104, targets=P, rows=P, lse=P, loss=P, ws=P, size=U64):
+    return b.lib().chimera_op_linear_xent_fwd(dtype, tokens, hidden, vocab, h, ldh, w, ldw, targets, 1.0, rows, lse, loss, ws, size, None)
+
+
+def bwd(dtype=b.BF16, tokens=4, hidden=64, vocab=100, h=P, ldh=64, w=P, ldw=104, targets=P, lse=P, dloss=None, dh=P, lddh=64, dw=P, lddw=104,
+        piece=0, ws=P, size=U64):
+    return b.lib().chimera_op_linear_xent_bwd(dtype, tokens, hidden, vocab, h, ldh, w, ldw, targets, lse, 1.0, dloss, dh, lddh, dw, lddw, 0, piece, ws, size, None)
+
+
+BAD_SIZES = [dict(dtype=2), dict(tokens=0), dict(tokens=-3), dict(tokens=(1 << 22) + 1), dict(hidden=0), dict(hidden=60), dict(hidden=(1 << 16) + 8, ldh=(1 << 16) + 8),
+             dict(vocab=0), dict(vocab=105), dict(vocab=(1 << 22) + 8, ldw=(1 << 22) + 8), dict(ldh=56), dict(ldh=68), dict(ldw=108), dict(ldw=1 << 23),
+             dict(h=None), dict(w=None), dict(targets=None), dict(lse=None), dict(ws=None), dict(h=P + 8), dict(w=P + 2), dict(ws=P + 16)]
+
+
+@pytest.mark.parametrize("bad", BAD_SIZES + [dict(rows=None)], ids=str)
+def test_linear_xent_fwd_refuses(bad):
+    assert fwd(**bad) == b.EINVAL, b.last_error()
+    assert b.last_error()
+
+
+@pytest.mark.parametrize("bad", BAD_SIZES + [dict(dh=None, dw=None), dict(piece=-1), dict(lddh=56), dict(lddh=68), dict(lddw=96), dict(lddw=106),
+                                             dict(dh=P + 4), dict(dw=P + 4)], ids=str)
+def test_linear_xent_bwd_refuses(bad):
+    assert bwd(**bad) == b.EINVAL, b.last_error()
+    assert b.last_error()
+
+
+@pytest.mark.parametrize("dtype", [b.F32, b.BF16])
+@pytest.mark.parametrize("tokens,hidden,vocab,piece", [(1, 8, 1, 0), (5, 64, 1001, 256), (4096, 1600, 50257, 0), (1 << 20, 2048, 65536, 0)])
+def test_linear_xent_workspaces(dtype, tokens, hidden, vocab, piece):
+    l = b.lib()
+    f, g = l.chimera_op_linear_xent_fwd_workspace_bytes(dtype, tokens, hidden, vocab), l.chimera_op_linear_xent_bwd_workspace_bytes(dtype, tokens, hidden, vocab, piece)
+    assert f > 0 and g > 0
+    ld = (vocab + 7) // 8 * 8
+    sizes = dict(dtype=dtype, tokens=tokens, hidden=hidden, vocab=vocab, ldh=hidden, ldw=ld)
+    assert fwd(**sizes, size=f - 1) == b.ENOMEM
+    assert bwd(**sizes, lddh=hidden, lddw=ld, piece=piece, size=g - 1) == b.ENOMEM
+    if tokens >= 4096:                         # no logits: half of them at the very most, and the rows that the weight gradient takes
+        e = 4 if dtype == b.F32 else 2
+        assert f < tokens * vocab * e // 2
+        assert l.chimera_head_pieces_workspace_bytes(dtype, tokens, hidden, vocab, 256) < tokens * vocab * e
+
+
+def test_linear_xent_workspace_of_refused_sizes_is_zero():
+    l = b.lib()
+    for args in ((2, 4, 64, 100), (b.BF16, 0, 64, 100), (b.BF16, 4, 60, 100), (b.BF16, 4, 64, 0), (b.BF16, 4, 64, (1 << 22) + 1)):
+        assert l.chimera_op_linear_xent_fwd_workspace_bytes(*args) == 0
+        assert l.chimera_op_linear_xent_bwd_workspace_bytes(*args, 0) == 0
+        assert l.chimera_head_pieces_workspace_bytes(*args, 0) == 0
+    assert l.chimera_op_linear_xent_bwd_workspace_bytes(b.BF16, 4, 64, 100, -1) == 0
+
+
+def test_head_loss_pieces_refuses():
+    def call(**o):
+        a = dict(dtype=b.BF16, tokens=4, hidden=64, vocab=100, y=P, t=P, g=P, be=P, w=P, ldw=104, dy=P, dg=P, db=P, dw=P, loss=P, piece=0, ws=P, size=U64)
+        a.update(o)
+        return b.lib().chimera_head_loss_pieces(a["dtype"], a["tokens"], a["hidden"], a["vocab"], a["y"], a["t"], a["g"], a["be"], a["w"], a["ldw"], 1.0, a["dy"],
+                                                a["dg"], a["db"], a["dw"], a["loss"], a["piece"], a["ws"], a["size"], None)
+    for bad in (dict(dtype=5), dict(tokens=0), dict(hidden=12), dict(ldw=100), dict(ldw=96), dict(y=None), dict(t=None), dict(loss=None), dict(dw=None),
+                dict(piece=-1), dict(ws=P + 1), dict(dy=P + 8)):
+        assert call(**bad) == b.EINVAL, bad
+    need = b.lib().chimera_head_pieces_workspace_bytes(b.BF16, 4, 64, 100, 0)
+    assert call(size=need - 1) == b.ENOMEM
+
+
+def norm(n=(8, 0, 5), grads=(P, None, P), max_norm=1.0, out=P, ws=P, size=U64, count=None):
+    c = len(n) if count is None else count
+    return b.lib().chimera_op_grad_norm(c, (C.c_int64 * len(n))(*n), (C.c_void_p * len(grads))(*grads), max_norm, out, ws, size, None)
+
+
+@pytest.mark.parametrize("bad", [dict(count=0), dict(count=-1), dict(n=(8, -1, 5)), dict(n=(8, 1 << 60, 5), grads=(P, P, P)), dict(grads=(P, None, None)),
+                                 dict(grads=(P, None, P + 2)), dict(max_norm=0.0), dict(max_norm=-1.0), dict(max_norm=float("nan")), dict(out=None),
+                                 dict(ws=None), dict(ws=P + 4)], ids=str)
+def test_grad_norm_refuses(bad):
+    assert norm(**bad) == b.EINVAL
+    assert b.last_error()
+
+
+def test_grad_norm_workspace():
+    n = (C.c_int64 * 2)(10 ** 8, 3)
+    need = b.lib().chimera_op_grad_norm_workspace_bytes(2, n)
+    assert 0 < need < 10 ** 6
+    assert norm(n=(10 ** 8, 3), grads=(P, P), size=need - 1) == b.ENOMEM
+    assert b.lib().chimera_op_grad_norm_workspace_bytes(0, n) == 0
+
+
+def adamw(dtype=b.BF16, bits=32, n=(16, 0, 9), param=(P, None, 2 * P), master=(P, None, P), grad=(P, None, P), m=(P, None, P), v=(P, None, P),
+          scale=None, decay=None, hyper=(1e-3, 0.9, 0.95, 1e-8, 1, 0), device=None, count=None):
+    arr = lambda x: None if x is None else (C.c_void_p * len(x))(*x)  # noqa: E731
+    h = None if hyper is None else C.byref(b.AdamWHyper(*hyper))
+    return b.lib().chimera_op_adamw(dtype, bits, len(n) if count is None else count, (C.c_int64 * len(n))(*n), arr(param), arr(master), arr(grad), arr(m), arr(v),
+                                    arr(scale), None if decay is None else (C.c_float * len(decay))(*decay), h, device, None, None)
+
+
+NAN, INF = float("nan"), float("inf")
+
+
+@pytest.mark.parametrize("bad", [dict(dtype=3), dict(bits=16), dict(bits=0), dict(count=0), dict(count=-5), dict(n=(16, 0, -9)), dict(n=(16, 0, 1 << 40)),
+                                 dict(param=None), dict(master=None), dict(grad=None), dict(m=None), dict(v=None), dict(bits=8), dict(param=(P, None, None)),
+                                 dict(master=(P, None, None)), dict(grad=(None, None, P)), dict(bits=8, scale=(P, None, None)), dict(param=(P, None, P)),
+                                 dict(param=(P, None, P + 30)), dict(param=(P + 1, None, 2 * P)), dict(grad=(P + 2, None, P)), dict(m=(P + 1, None, P)),
+                                 dict(decay=(0.0, 0.0, -0.1)), dict(decay=(NAN, 0.0, 0.1)), dict(decay=(0.1, 0.0, INF)), dict(hyper=None), dict(device=P + 8),
+                                 dict(hyper=(-1e-3, 0.9, 0.95, 1e-8, 1, 0)), dict(hyper=(NAN, 0.9, 0.95, 1e-8, 1, 0)), dict(hyper=(1e-3, 1.0, 0.95, 1e-8, 1, 0)),
+                                 dict(hyper=(1e-3, 0.9, -0.1, 1e-8, 1, 0)), dict(hyper=(1e-3, 0.9, 0.95, 0.0, 1, 0)), dict(hyper=(1e-3, 0.9, 0.95, 1e-8, 0, 0))],
+                         ids=str)
+def test_adamw_refuses(bad):
+    assert adamw(**bad) == b.EINVAL
+    assert b.last_error()
+
+
+def test_stage_step_refuses_and_its_state_sizes():
+    l = b.lib()
+    for dtype, e in ((b.F32, 0), (b.BF16, 4)):
+        st = l.chimera_stage_create(2, 64, 4, 16, 2, dtype)
+        params = 2 * (12 * 64 * 64 + 13 * 64)
+        assert l.chimera_stage_adamw_state_bytes(st, 32) >= params * (8 + e)
+        assert params * (2 + e) <= l.chimera_stage_adamw_state_bytes(st, 8) < l.chimera_stage_adamw_state_bytes(st, 32)
+        assert l.chimera_stage_adamw_state_bytes(st, 16) == 0 and l.chimera_stage_adamw_state_bytes(None, 32) == 0
+        h = b.AdamWHyper(1e-3, 0.9, 0.95, 1e-8, 1, 0)
+        assert l.chimera_stage_adamw_init(st, P, P, 32) == b.ESTATE                 # not bound
+        assert l.chimera_stage_adamw_step(st, P, P, 32, 0.0, C.byref(h), None, None) == b.ESTATE
+        assert l.chimera_stage_adamw_step(None, P, P, 32, 0.0, C.byref(h), None, None) == b.EINVAL
+        l.chimera_stage_destroy(st)
+
+
+def test_adamw_handle_checks_its_lists():
+    torch = pytest.importorskip("torch")
+    t = lambda n, d=torch.float32: torch.zeros(n, dtype=d)  # noqa: E731
+    for bad in (dict(grads=[t(4)]), dict(grads=[t(4), t(4)]), dict(decay=[0.1]), dict(scales=[t(2)]), dict(scales=[t(2), t(1)]),
+                dict(grads=[t(4), t((9, 2))[:, 0]]), dict(masters=[t(4), t(8)])):
+        args = dict(params=[t(4), t(9)], grads=[t(4), t(9)], ms=[t(4), t(9)], vs=[t(4), t(9)])
+        args.update(bad)
+        with pytest.raises(ValueError):
+            b.AdamW(**args)
