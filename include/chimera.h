@@ -512,7 +512,7 @@ int chimera_head_loss(int dtype, int tokens, int hidden, int vocab, const void* 
 /* The vocabulary projection and its cross-entropy without the logits: nothing of size [tokens, vocab] is kept or
  * written.  h [tokens, hidden] with rows ldh apart, W [hidden, vocab] with rows ldw apart (ldw >= vocab; the columns between may hold anything), both
  * in the given dtype; z = h W.  vocab is any number; hidden and the leading dimensions are multiples of 8, leading dimensions below 2^23, tokens up
- * to 2^22, hidden to 2^16, vocab to 2^22; tensors 16-byte, the workspace 256-byte aligned.  A target outside [0, vocab) marks a token that does
+ * to 2^22, hidden to 2^15, vocab to 2^22, tokens * vocab to 2^38; tensors 16-byte, the workspace 256-byte aligned.  A target outside [0, vocab) marks a token that does
  * not count (padding): its loss is 0 and it takes no part in any gradient, whatever its hidden state holds.
  *
  * Forward (evaluation, scoring, or the first half of training):
@@ -521,7 +521,7 @@ int chimera_head_loss(int dtype, int tokens, int hidden, int vocab, const void* 
  *   d_dh [tokens, hidden] (dtype, rows lddh apart) = dz W^T,  d_dw [hidden, vocab] (float, rows lddw apart, columns from vocab on left as they are)
  *   += h^T dz, or = with overwrite != 0.  Either may be NULL, not both.  z is formed again, `piece` columns of the vocabulary at a time (rounded up to
  *   a multiple of 256; 0: the library's choice); the workspace grows with it.
- * bf16: dh is formed from dz rounded to bf16 (2^-8 a term), dW from dz in 22 bits, so that it is as exact as a sum of floats; the products' sums are float.
+ * bf16: dh is formed from dz in 11 bits, dW from dz in 22, so that it is as exact as a sum of floats; the products' sums are float.
  * All sums have a fixed order.  ENOMEM if the workspace is too small (a function of the same sizes; 0 for sizes that the calls refuse). */
 size_t chimera_op_linear_xent_fwd_workspace_bytes(int dtype, int tokens, int hidden, int vocab);
 int chimera_op_linear_xent_fwd(int dtype, int tokens, int hidden, int vocab, const void* d_h, int ldh, const void* d_w, int ldw,

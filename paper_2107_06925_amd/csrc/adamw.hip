@@ -183,7 +183,7 @@ __global__ __launch_bounds__(STEP_THREADS) void adamw_kernel(StepLaunch L) {
                 if (e < have) { tm = fmaxf(tm, fabsf(m[e])); tv = fmaxf(tv, r[e]); }
             tm = wave_max(tm);
             tv = wave_max(tv);
-            const float im = tm > CODE_LEAST ? __fdiv_rn(CODE_TOP, tm) : 0.f, iv = tv > CODE_LEAST ? __fdiv_rn(CODE_TOP, tv) : 0.f;
+            const float im = tm > CODE_LEAST ? __fdiv_rn(1.0f, tm) * CODE_TOP : 0.f, iv = tv > CODE_LEAST ? __fdiv_rn(1.0f, tv) * CODE_TOP : 0.f;
             unsigned qm = 0, qv = 0;
             const unsigned long long number = (unsigned long long)(t.block0 * MOMENT_BLOCK + i);
 #pragma unroll
@@ -195,8 +195,8 @@ __global__ __launch_bounds__(STEP_THREADS) void adamw_kernel(StepLaunch L) {
             put_codes(t.m, qm);
             put_codes(t.v, qv);
             if (lane == 0) {
-                t.scale[i0 / MOMENT_BLOCK * 2] = tm > CODE_LEAST ? __fdiv_rn(tm, CODE_TOP) : 0.f;
-                t.scale[i0 / MOMENT_BLOCK * 2 + 1] = tv > CODE_LEAST ? __fdiv_rn(tv, CODE_TOP) : 0.f;
+                t.scale[i0 / MOMENT_BLOCK * 2] = tm > CODE_LEAST ? tm * (1.0f / CODE_TOP) : 0.f;
+                t.scale[i0 / MOMENT_BLOCK * 2 + 1] = tv > CODE_LEAST ? tv * (1.0f / CODE_TOP) : 0.f;
             }
         }
     }

@@ -760,10 +760,11 @@ __device__ __forceinline__ void lds_dma16_s(const void* sbase, unsigned voff, un
     asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(sbase), "{m0}"(lds_base) : "memory");
 }
 // A tile's own way to end (ONLY_EPI = EPI_OWN), in place of the epilogues above: begin() ahead of the k loop, end() with the accumulators
-// once every wavefront has left it.
+// once every wavefront has left it.  F16: operands of fp16 in place of bf16.  PAIRED (index-contiguous operands): the contraction takes every row of A twice, with
+// the row of B and with the one own_end.pair elements behind it, 32 rows of A a step.
 constexpr int EPI_OWN = 6;
 struct NoEnd {};
-template <int BM, int BN, int WGM, int WGN, int WGK, bool A_KC, bool B_KC, int ONLY_EPI, bool F16 = false, typename End = NoEnd>
+template <int BM, int BN, int WGM, int WGN, int WGK, bool A_KC, bool B_KC, int ONLY_EPI, bool F16 = false, bool PAIRED = false, typename End = NoEnd>
 __device__ __forceinline__ void gemm_ring_tile(
     char* lds, const bf16_t* __restrict__ A, const bf16_t* __restrict__ B, const bf16_t* __restrict__ bias,
     const bf16_t* __restrict__ R, void* __restrict__ C, bf16_t* __restrict__ C2, int m, int n, int k, int lda,
@@ -820,11 +821,17 @@ __device__ __forceinline__ void gemm_ring_tile(
 #pragma unroll
     for (int it = 0; it < OB; ++it) vb[it] = piece(ldb, j0, n, std::integral_constant<int, BN>{}, B_KC, it * NT + tid, kb);
 #pragma unroll
-    for (int it = 0; it < PA; ++it) sa[it] = (const char*)(A + (A_KC ? (size_t)i0 * lda : (size_t)i0 + (size_t)it * KIA * lda));
+    for (int it = 0; it < PA; ++it) sa[it] = (const char*)(A + (A_KC ? (size_t)i0 * lda : (size_t)i0 + (size_t)(PAIRED ? it * KIA & 31 : it * KIA) * lda));
 #pragma unroll
-    for (int it = 0; it < PB; ++it) sb[it] = (const char*)(B + (B_KC ? (size_t)j0 * ldb : (size_t)j0 + (size_t)it * KIB * ldb));
+    for (int it = 0; it < PB; ++it) {
+        sb[it] = (const char*)(B + (B_KC ? (size_t)j0 * ldb : (size_t)j0 + (size_t)(PAIRED ? it * KIB & 31 : it * KIB) * ldb));
+        if constexpr (PAIRED)
+            if (it * KIB >= 32) sb[it] += (size_t)own_end.pair * 2;
+    }
     static_assert(KIA % 16 == 0 && KIB % 16 == 0, "requests of one lane share a swizzle");
-    const size_t step_a = (A_KC ? (size_t)RK : (size_t)RK * lda) * 2, step_b = (B_KC ? (size_t)RK : (size_t)RK * ldb) * 2;
+    static_assert(!PAIRED || (!A_KC && !B_KC && KIA <= 32 && KIB <= 32), "a request lies within 32 rows");
+    constexpr int ROWS = PAIRED ? RK / 2 : RK;
+    const size_t step_a = (A_KC ? (size_t)RK : (size_t)ROWS * lda) * 2, step_b = (B_KC ? (size_t)RK : (size_t)ROWS * ldb) * 2;
     const unsigned lds0 = lds_address(lds), dma0 = lds0 + wave * 1024;
 
     // Operand reads: lane l holds k 8(l/16)..+7 of row (column) l%16 of a 16-row tile.

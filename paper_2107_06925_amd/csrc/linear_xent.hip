@@ -5,12 +5,14 @@
 //
 // bf16.  The forward's product ends in the statistics of its tile instead of in z: a (maximum, sum) pair per row and tile,
 // which a second kernel combines.  The backward forms z again, a piece of the vocabulary at a time, and ends in dz of
-// that piece; two products take it from there, and the next piece takes its place.
-// dz goes into dW as two fp16 numbers, because dW is a float sum: one bf16 dz would leave it 2e-3 off, two 3e-6, two of fp16
-// (11 bits each) 1e-7.  fp16 holds h, a bf16 number, exactly only within its range, so every row of h is scaled by a power of two,
-// 2^up_t, that puts its largest number into [2^14, 2^15), where fp16 loses nothing above 2^-28 of it; dz_t takes 2^(shift - up_t), with the
-// largest `shift` that keeps all of dz below 2^15, and dW's epilogue takes 2^-shift off again.
-// dh is rounded to bf16 itself, and takes dz as one bf16 number.
+// that piece; two products take it from there.  One launch per piece holds both, and z of the next piece, so that no product's last round leaves
+// the chip idle.
+// dz is kept as two fp16 numbers, hi + lo.  dW takes both, because it is a float sum: one bf16 dz would leave it 2e-3 off, two 3e-6, two of fp16
+// (11 bits each) 1e-7.  dh is rounded to bf16 itself, and takes hi: a bf16 dz would add as much error as that rounding.  fp16's range is met by powers of two:
+//   dz_t times 2^lift_t: the row's coef comes to lie in [2^13, 2^14);
+//   W's rows within a piece times 2^raise_i: the row's largest number in [2^14, 2^15), where fp16 holds a bf16 number exactly down to 2^-28 of it;
+//   h_t times 2^(shift - lift_t), for dW, which sums over tokens: one shift for all, the largest that keeps all rows below 2^15.
+// The products' epilogues take the powers off again.
 //
 // float.  The framework's float products on pieces of z that are in memory, row kernels between them.
 #include "gemm_tiles.h"
@@ -121,89 +123,123 @@ __global__ __launch_bounds__(256) void xent_join_kernel(const float2* __restrict
     loss_rows[row] = counts(targets[row], vocab) ? scale * (l - at_target[row]) : 0.f;
 }
 
-// ---- backward: the rows of h that the weight gradient takes, tokens that do not count (and the padding behind the last one) as zeros: their dz is
-// zero, but h may hold anything.  bf16: fp16 numbers times 2^up, written twice, once for either half of dz, and the largest
-// shift that this row allows (INT_MAX: any).  One wavefront per row.
-template <typename T, typename U>
-__global__ __launch_bounds__(ROW_THREADS) void xent_rows_kernel(const T* __restrict__ h, int ldh, const int* __restrict__ targets, const float* __restrict__ dloss,
-                                                                float scale, int m, int mp, int cols, int vocab, U* __restrict__ out, int* __restrict__ up,
-                                                                int* __restrict__ room) {
-    constexpr int V = Elem<T>::VEC;
-    const int t = blockIdx.x * (ROW_THREADS / WAVE) + threadIdx.x / WAVE, lane = threadIdx.x % WAVE;
-    if (t >= mp) return;
-    const float coef = t < m && counts(targets[t], vocab) ? (dloss ? scale * dloss[t] : scale) : 0.f;
-    const T* src = h + (size_t)min(t, m - 1) * ldh;
-    int lift = 0;
-    if constexpr (sizeof(U) == 2) {
-        float top = 0.f;
-        if (coef != 0.f)
-            for (int c = lane; c < cols / V; c += WAVE) {
-                float x[V];
-                load_vec<T>(src + c * V, x);
-#pragma unroll
-                for (int e = 0; e < V; ++e) top = fmaxf(top, fabsf(x[e]));
-            }
-        top = wave_max(top);
-        lift = top > 0.f ? 15 - __builtin_amdgcn_frexp_expf(top) : 0;       // top = f 2^exp, f in [1/2, 1)
-        // |dz| <= |coef| = f 2^exp, and one bit to spare
-        if (lane == 0 && t < m) { up[t] = lift; room[t] = top > 0.f && coef != 0.f ? lift + 14 - __builtin_amdgcn_frexp_expf(coef) : INT_MAX; }
-    }
-    for (int c = lane; c < cols / V; c += WAVE) {
-        float x[V];
-        load_vec<T>(src + c * V, x);
-        U* to = out + (size_t)t * cols + c * V;
-        if constexpr (sizeof(U) == 2) {
-            f16x8 y;
-#pragma unroll
-            for (int e = 0; e < V; ++e) y[e] = coef != 0.f ? (_Float16)ldexpf(x[e], lift) : (_Float16)0.f;
-            *reinterpret_cast<f16x8*>(to) = y;
-            *reinterpret_cast<f16x8*>(to + (size_t)mp * cols) = y;
-        } else {
-#pragma unroll
-            for (int e = 0; e < V; ++e) x[e] = coef != 0.f ? x[e] : 0.f;
-            store_vec<U>(to, x);
-        }
-    }
+// ---- backward
+// A token's coef, and the power of two that brings it to [2^13, 2^14) (0 where it is zero)
+__device__ __forceinline__ float coef_of(const int* targets, const float* dloss, float scale, int t, int m, int vocab) {
+    return t < m && counts(targets[min(t, m - 1)], vocab) ? (dloss ? scale * dloss[min(t, m - 1)] : scale) : 0.f;
 }
-// The largest shift that every row allows.
-__global__ __launch_bounds__(1024) void xent_shift_kernel(const int* __restrict__ room, int m, int* __restrict__ shift) {
-    __shared__ int part[16];
-    int v = INT_MAX;
-    for (int t = threadIdx.x; t < m; t += 1024) v = min(v, room[t]);
+__device__ __forceinline__ int lift_of(float coef) { return coef != 0.f ? 14 - __builtin_amdgcn_frexp_expf(coef) : 0; }      // coef = f 2^exp, f in [1/2, 1)
+
+// The largest shift that each token allows: h_t 2^(shift - lift_t) stays below 2^15.  INT_MAX: any.  One wavefront per token.
+__global__ __launch_bounds__(ROW_THREADS) void xent_room_kernel(const bf16_t* __restrict__ h, int ldh, const int* __restrict__ targets, const float* __restrict__ dloss,
+                                                                float scale, int m, int cols, int vocab, int* __restrict__ room) {
+    const int t = blockIdx.x * (ROW_THREADS / WAVE) + threadIdx.x / WAVE, lane = threadIdx.x % WAVE;
+    if (t >= m) return;
+    const float coef = coef_of(targets, dloss, scale, t, m, vocab);
+    float top = 0.f;
+    if (coef != 0.f)
+        for (int c = lane; c < cols / 8; c += WAVE) {
+            float x[8];
+            load_vec<bf16_t>(h + (size_t)t * ldh + c * 8, x);
 #pragma unroll
-    for (int o = 32; o; o >>= 1) v = min(v, __shfl_xor(v, o, WAVE));
-    if (threadIdx.x % WAVE == 0) part[threadIdx.x / WAVE] = v;
-    __syncthreads();
-    if (threadIdx.x) return;
-    for (int i = 1; i < 16; ++i) v = min(v, part[i]);
-    *shift = v == INT_MAX ? 0 : v;
+            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[e]));
+        }
+    top = wave_max(top);
+    if (lane == 0) room[t] = top > 0.f ? 15 - __builtin_amdgcn_frexp_expf(top) + lift_of(coef) : INT_MAX;
 }
 
-// ---- what the backward's tiles of z end in: dz of the piece, as one bf16 number for dh and as two of fp16 for dW
-struct RowInfo { float lse, coef, scaled; int at; };        // at: the target's column in the piece
-template <int BM, int SLABS> struct GradEnd {
-    const float* lse;
+// What the launches of a pass work on
+struct Piece {
+    int v0, cols, ld;                // first column of the vocabulary, columns, columns rounded up to 8
+    _Float16* dz;                    // [mp][2][ld]: hi and lo of a token
+    _Float16* w;                     // [hidden, ldp] W's rows, times 2^raise
+    int* raise;                      // [hidden]
+};
+struct Pass {
+    const bf16_t *h, *w;
     const int* targets;
-    const float* dloss;
-    const int *up, *shift;
+    const float *lse, *dloss;
     float scale;
-    int m, mp, vocab, v0, cols, ld;                         // tokens (padded to mp); the piece's first column, its columns, the rows of dz
-    bf16_t* dz;                                             // [mp, ld]
-    _Float16* parts;                                        // [2 mp, ld]
+    int m, mp, hidden, vocab, ldh, ldw, ldp;
+    int *room, *shift;
+    _Float16* rows;                  // [mp, hidden]: h_t 2^(shift - lift_t)
+    int rows_per_wg;
+    Piece now, next;                 // the products' piece, and the one that dz is formed of
+    // dW: columns of `now`
+    float* dw;
+    int lddw, dw_flags;
+    // dh: float slabs [split][m, hidden]
+    float* slabs;
+    int k_per, dh_flags;
+    // workgroups of each kind, in this order, and the rasters of their tiles
+    int first[5];                    // dW, dh, dz, W's rows, h's rows
+    struct Raster { int tiles_m, tiles_n, group_m, band; } dw_r, dh_r, dz_r;
+};
+
+// dW (+)= h^T dz, 2^shift taken off
+struct ColumnsEnd {
+    float* c;
+    const int* shift;
+    int m, n, ldc, flags, pair;
+    __device__ __forceinline__ void begin(int, int) {}
+    template <int TO, int TN2, typename Acc>
+    __device__ __forceinline__ void end(const Acc& out, char* lds, int, int rb0, int cb0, int, int wave, int lane) const {
+        float* slab = reinterpret_cast<float*>(lds) + (size_t)wave * EpiSlab<TN2>::FLOATS;
+        accumulate<false, true, TO, TN2>(out, slab, rb0, cb0, m, n, ldc, *shift, c, flags, lane);
+    }
+};
+// a split of dh, of the columns' 2^raise alone: the tokens' 2^lift goes when the slabs are added
+struct SlabEnd {
+    float* c;
+    const int* raise;
+    int m, n, flags;
+    __device__ __forceinline__ void begin(int, int) {}
+    template <int TO, int TN2, typename Acc>
+    __device__ __forceinline__ void end(const Acc& out, char* lds, int, int rb0, int cb0, int, int wave, int lane) const {
+        constexpr int CPR = EpiSlab<TN2>::WN / 4, RPP = 64 / CPR, NP = 32 / RPP;
+        float* slab = reinterpret_cast<float*>(lds) + (size_t)wave * EpiSlab<TN2>::FLOATS;
+        const int pr = lane / CPR, piece = lane % CPR, gcol = cb0 + piece * 4, lcol = min(gcol, n - 4);
+        const bool reads = !(flags & ACCUM_OVERWRITE);
+        const int4 r = *reinterpret_cast<const int4*>(raise + lcol);
+        static_for<TO>([&](auto a_c) {
+            constexpr int a = decltype(a_c)::value;
+            f32x4 old[NP];
+            if (reads)
+#pragma unroll
+                for (int j = 0; j < NP; ++j)
+                    old[j] = *reinterpret_cast<const f32x4*>(c + (size_t)min(rb0 + a * 32 + j * RPP + pr, m - 1) * n + lcol);
+            out.template put<a>(slab, lane);
+            __builtin_amdgcn_s_waitcnt(0xc07f);                   // lgkmcnt(0): the slab is written (wavefront-private)
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int j = 0; j < NP; ++j) {
+                const int lr = j * RPP + pr, row = rb0 + a * 32 + lr;
+                f32x4 v = *reinterpret_cast<const f32x4*>(EpiSlab<TN2>::at(slab, lr, piece));
+                v = f32x4{ldexpf(v[0], -r.x), ldexpf(v[1], -r.y), ldexpf(v[2], -r.z), ldexpf(v[3], -r.w)};
+                if (reads) v += old[j];
+                if (row < m && gcol < n) *reinterpret_cast<f32x4*>(c + (size_t)row * n + gcol) = v;
+            }
+            __builtin_amdgcn_wave_barrier();                      // all lanes have read the slab before it is rewritten
+        });
+    }
+};
+// dz of a piece
+struct RowInfo { float lse, scaled; int at, on; };          // coef 2^lift, the target's column in the piece, whether coef is not zero
+template <int BM> struct GradEnd {
+    const Pass* p;
     RowInfo mine;
     __device__ __forceinline__ void begin(int i0, int tid) {
         // (no branches: the compiler keeps the tile's operand addresses in scalar registers only outside of divergent code)
-        const int t = min(i0 + tid, m - 1), target = targets[t];
-        const bool on = i0 + tid < m && counts(target, vocab);
-        const float coef = on ? (dloss ? scale * dloss[t] : scale) : 0.f;
-        mine = {lse[t], coef, ldexpf(coef, *shift - up[t]), on ? target - v0 : -1};
+        const int t = min(i0 + tid, p->m - 1);
+        const float coef = coef_of(p->targets, p->dloss, p->scale, i0 + tid, p->m, p->vocab);
+        mine = {p->lse[t], ldexpf(coef, lift_of(coef)), p->targets[t] - p->next.v0, coef != 0.f};
     }
     template <int TO, int TN2, typename Acc>
     __device__ __forceinline__ void end(const Acc& out, char* lds, int i0, int rb0, int cb0, int, int wave, int lane) const {
         constexpr int CPR = EpiSlab<TN2>::WN / 8, RPP = 64 / CPR, NP = 32 / RPP;
-        RowInfo* tab = reinterpret_cast<RowInfo*>(lds + SLABS * EpiSlab<TN2>::FLOATS * sizeof(float));
+        RowInfo* tab = reinterpret_cast<RowInfo*>(lds + 8 * EpiSlab<TN2>::FLOATS * sizeof(float));
         float* slab = reinterpret_cast<float*>(lds) + (size_t)wave * EpiSlab<TN2>::FLOATS;
-        const int tid = threadIdx.x;
+        const int tid = threadIdx.x, cols = p->next.cols, ld = p->next.ld, mp = p->mp;
         if (tid < BM) tab[tid] = mine;
         __syncthreads();
         const int pr = lane / CPR, pc = lane % CPR * 8, col = cb0 + pc;
@@ -224,114 +260,162 @@ template <int BM, int SLABS> struct GradEnd {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     float d = __builtin_amdgcn_exp2f((v[e] - r.lse) * LOG2E) - (col + e == r.at ? 1.0f : 0.0f);
-                    if (r.coef == 0.f || col + e >= cols) d = 0.f;
-                    v[e] = r.coef * d;
-                    const float x = r.scaled * d;
-                    hi[e] = (_Float16)x;
-                    lo[e] = (_Float16)(x - (float)hi[e]);
+                    d = !r.on || col + e >= cols ? 0.f : r.scaled * d;
+                    hi[e] = (_Float16)d;
+                    lo[e] = (_Float16)(d - (float)hi[e]);
                 }
-                const size_t at = (size_t)row * ld + col;
-                store_vec<bf16_t>(dz + at, v);
-                *reinterpret_cast<f16x8*>(parts + at) = hi;
-                *reinterpret_cast<f16x8*>(parts + (size_t)mp * ld + at) = lo;
+                _Float16* to = p->next.dz + (size_t)row * 2 * ld + col;
+                *reinterpret_cast<f16x8*>(to) = hi;
+                *reinterpret_cast<f16x8*>(to + ld) = lo;
             }
             __builtin_amdgcn_wave_barrier();                      // all lanes have read the slab before it is rewritten
         });
     }
 };
 
-template <int BM, int BN, int WGM, int WGN, int WGK>
-__global__ __launch_bounds__(WGM* WGN * WGK * 64, 2) void xent_dz_kernel(
-    const bf16_t* __restrict__ h, const bf16_t* __restrict__ w, int k, int ldh, int ldw, int tiles_m, int tiles_n, int group_m, int band,
-    GradEnd<BM, WGM * WGN * WGK> end) {
-    __shared__ __attribute__((aligned(1024))) char lds[RingLds<BM, BN, WGM, WGN, WGK>::BYTES];
-    static_assert(sizeof lds >= WGM * WGN * WGK * EpiSlab<BN / WGN / 32>::FLOATS * sizeof(float) + BM * sizeof(RowInfo), "room for the slabs and the rows");
-    gemm_ring_tile<BM, BN, WGM, WGN, WGK, true, false, EPI_OWN>(lds, h, w + end.v0, nullptr, nullptr, nullptr, nullptr, end.m, end.ld, k, ldh, ldw, EPI_OWN, 0, 0,
-                                                                tiles_m, tiles_n, group_m, (int)blockIdx.x, nullptr, true, 0, Ahead{nullptr, 0}, band, end);
+// Rows of W within the next piece as fp16 numbers times 2^raise; columns behind the vocabulary as zeros, whatever they hold.
+__device__ __forceinline__ void raise_row(const Pass& p, int i, char* lds) {
+    const bf16_t* src = p.w + (size_t)i * p.ldw + p.next.v0;
+    _Float16* to = p.next.w + (size_t)i * p.ldp;
+    float* part = reinterpret_cast<float*>(lds);
+    float top = 0.f;
+    for (int c = threadIdx.x * 8; c < p.next.ld; c += 512 * 8) {
+        float x[8];
+        load_vec<bf16_t>(src + c, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = fmaxf(top, c + e < p.next.cols ? fabsf(x[e]) : 0.f);
+    }
+    top = wave_max(top);
+    if (threadIdx.x % WAVE == 0) part[threadIdx.x / WAVE] = top;
+    __syncthreads();
+    top = wave_max(part[threadIdx.x % 8]);
+    __syncthreads();                                              // (the next row's)
+    const int up = top > 0.f ? 15 - __builtin_amdgcn_frexp_expf(top) : 0;
+    if (threadIdx.x == 0) p.next.raise[i] = up;
+    for (int c = threadIdx.x * 8; c < p.next.ld; c += 512 * 8) {
+        float x[8];
+        load_vec<bf16_t>(src + c, x);
+        f16x8 y;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = c + e < p.next.cols ? (_Float16)ldexpf(x[e], up) : (_Float16)0.f;
+        *reinterpret_cast<f16x8*>(to + c) = y;
+    }
+}
+// Rows of h times 2^(shift - lift); tokens that do not count, and the padding behind the last one, as zeros: their dz is zero, but h may hold anything.
+constexpr int W_ROWS_PER_WG = 4;
+__device__ __forceinline__ void shift_rows(const Pass& p, int t0, char* lds, bool tells) {
+    int* part = reinterpret_cast<int*>(lds);
+    int least = INT_MAX;
+    for (int t = threadIdx.x; t < p.m; t += 512) least = min(least, p.room[t]);
+#pragma unroll
+    for (int o = 32; o; o >>= 1) least = min(least, __shfl_xor(least, o, WAVE));
+    if (threadIdx.x % WAVE == 0) part[threadIdx.x / WAVE] = least;
+    __syncthreads();
+    for (int i = 0; i < 8; ++i) least = min(least, part[i]);
+    const int shift = least == INT_MAX ? 0 : least;
+    if (tells && threadIdx.x == 0) *p.shift = shift;
+    for (int t = t0 + threadIdx.x / WAVE; t < min(t0 + p.rows_per_wg, p.mp); t += 8) {
+        const float coef = coef_of(p.targets, p.dloss, p.scale, t, p.m, p.vocab);
+        const int up = shift - lift_of(coef);
+        for (int c = threadIdx.x % WAVE * 8; c < p.hidden; c += WAVE * 8) {
+            float x[8];
+            load_vec<bf16_t>(p.h + (size_t)min(t, p.m - 1) * p.ldh + c, x);
+            f16x8 y;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = coef != 0.f ? (_Float16)ldexpf(x[e], up) : (_Float16)0.f;
+            *reinterpret_cast<f16x8*>(p.rows + (size_t)t * p.hidden + c) = y;
+        }
+    }
 }
 
-// ---- dh: float slabs [split][m, n] (+)= dz W^T over the splits of a piece's columns
-template <int BM, int BN, int WGM, int WGN, int WGK>
-__global__ __launch_bounds__(WGM* WGN * WGK * 64, 2) void xent_dh_kernel(
-    const bf16_t* __restrict__ dz, const bf16_t* __restrict__ w, float* __restrict__ slabs, int m, int n, int k, int ldz, int ldw, int tiles_m, int tiles_n,
-    int group_m, int splits, int k_per, int flags) {
-    const int tiles = tiles_m * tiles_n, total = tiles * splits;
-    const int xcd = (int)blockIdx.x & 7, local = (int)blockIdx.x >> 3;
-    const int pid = xcd * (total >> 3) + min(xcd, total & 7) + local;
-    const int split = __builtin_amdgcn_readfirstlane(pid / tiles), k0 = split * k_per;
-    __shared__ __attribute__((aligned(1024))) char lds[RingLds<BM, BN, WGM, WGN, WGK>::BYTES];
-    gemm_ring_tile<BM, BN, WGM, WGN, WGK, true, true, EPI_ACCUM_F32>(lds, dz + k0, w + k0, nullptr, nullptr, slabs + (size_t)split * m * n, nullptr, m, n,
-                                                                     min(k_per, k - k0), ldz, ldw, EPI_ACCUM_F32, flags, 0, tiles_m, tiles_n, group_m,
-                                                                     pid - split * tiles, nullptr, false);
+// One launch: dW and dh of a piece, dz and the rows of W of the next, and, in a pass's first, the rows of h.  Tiles of DW x DW for dW, of TOK x TOK for
+// the products over tokens.
+template <int DW, int TOK>
+__global__ __launch_bounds__(512, 2) void xent_pass_kernel(Pass p) {
+    constexpr int BYTES = RingLds<256, 256, 2, 4, 1>::BYTES;
+    static_assert(RingLds<128, 128, 2, 2, 2>::BYTES <= BYTES, "the larger of the two");
+    static_assert(BYTES >= 8 * EpiSlab<2>::FLOATS * sizeof(float) + 256 * sizeof(RowInfo), "room for the slabs and the rows");
+    __shared__ __attribute__((aligned(1024))) char lds[BYTES];
+    const int id = blockIdx.x;
+#define XENT_TILE(T, AKC, BKC, F16, PAIRED, A, B, M, N, K, LDA, LDB, R, ID, BAND, XCD, END)                                                                          \
+    do {                                                                                                                                                       \
+        if constexpr (T == 256)                                                                                                                                \
+            gemm_ring_tile<256, 256, 2, 4, 1, AKC, BKC, EPI_OWN, F16, PAIRED>(lds, A, B, nullptr, nullptr, nullptr, nullptr, M, N, K, LDA, LDB, EPI_OWN, 0, 0,  \
+                                                                              R.tiles_m, R.tiles_n, R.group_m, ID, nullptr, XCD, 0, Ahead{nullptr, 0}, BAND, END); \
+        else                                                                                                                                                   \
+            gemm_ring_tile<128, 128, 2, 2, 2, AKC, BKC, EPI_OWN, F16, PAIRED>(lds, A, B, nullptr, nullptr, nullptr, nullptr, M, N, K, LDA, LDB, EPI_OWN, 0, 0,  \
+                                                                              R.tiles_m, R.tiles_n, R.group_m, ID, nullptr, XCD, 0, Ahead{nullptr, 0}, BAND, END); \
+    } while (0)
+    if (id < p.first[1]) {
+        const ColumnsEnd end{p.dw + p.now.v0, p.shift, p.hidden, p.now.cols, p.lddw, p.dw_flags, p.now.ld};
+        XENT_TILE(DW, false, false, true, true, (const bf16_t*)p.rows, (const bf16_t*)p.now.dz, p.hidden, p.now.ld, 2 * p.mp, p.hidden, 2 * p.now.ld, p.dw_r, id,
+                  p.dw_r.band, true, end);
+    } else if (id < p.first[2]) {
+        const int at = id - p.first[1], tiles = p.dh_r.tiles_m * p.dh_r.tiles_n, total = p.first[2] - p.first[1];
+        const int xcd = at & 7, local = at >> 3, pid = xcd * (total >> 3) + min(xcd, total & 7) + local;
+        const int split = __builtin_amdgcn_readfirstlane(pid / tiles), k0 = split * p.k_per;
+        const SlabEnd end{p.slabs + (size_t)split * p.m * p.hidden, p.now.raise, p.m, p.hidden, p.dh_flags};
+        XENT_TILE(TOK, true, true, true, false, (const bf16_t*)p.now.dz + k0, (const bf16_t*)p.now.w + k0, p.m, p.hidden, min(p.k_per, p.now.ld - k0), 2 * p.now.ld,
+                  p.ldp, p.dh_r, pid - split * tiles, 0, false, end);
+    } else if (id < p.first[3]) {
+        XENT_TILE(TOK, true, false, false, false, p.h, p.w + p.next.v0, p.m, p.next.ld, p.hidden, p.ldh, p.ldw, p.dz_r, id - p.first[2], p.dz_r.band, true,
+                  (GradEnd<TOK>{&p, {}}));
+    } else if (id < p.first[4]) {
+        for (int i = (id - p.first[3]) * W_ROWS_PER_WG; i < min((id - p.first[3] + 1) * W_ROWS_PER_WG, p.hidden); ++i) raise_row(p, i, lds);
+    } else {
+        shift_rows(p, (id - p.first[4]) * p.rows_per_wg, lds, id == p.first[4]);
+    }
+#undef XENT_TILE
 }
 
-// dh = the slabs' sum, and the product of the last vocabulary columns, fewer than 8, that no slab holds: what lies beside them in
-// W's rows does not count and need not be a number.  A thread owns 4 columns, a workgroup ROWS tokens.
-constexpr int DH_ROWS = 8;
+// dh = the slabs' sum, the tokens' 2^lift taken off (bf16); float: with the product of the last vocabulary columns, fewer than 8, that no slab holds
+// (what lies beside them in W's rows does not count and need not be a number).  A thread owns 4 columns of a token.
 template <typename T>
 __global__ __launch_bounds__(ROW_THREADS) void xent_dh_sum_kernel(const float* __restrict__ slabs, int splits, const T* __restrict__ dz, int ldz,
-                                                                  const T* __restrict__ w, int ldw, int tail, int m, int n, T* __restrict__ dh, int lddh) {
-    const int c = (blockIdx.y * ROW_THREADS + threadIdx.x) * 4;
-    if (c >= n) return;
-    float wt[4][8];
+                                                                  const T* __restrict__ w, int ldw, int tail, const int* __restrict__ targets,
+                                                                  const float* __restrict__ dloss, float scale, int vocab, int m, int n, T* __restrict__ dh, int lddh) {
+    for (size_t at = (size_t)blockIdx.x * ROW_THREADS + threadIdx.x; at < (size_t)m * (n / 4); at += (size_t)gridDim.x * ROW_THREADS) {
+        const int t = (int)(at / (n / 4)), c = (int)(at % (n / 4)) * 4;
+        const float* from = slabs + (size_t)t * n + c;
+        const size_t stride = (size_t)m * n;
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+        int s = 0;
+        for (; s + 4 <= splits; s += 4) {
+            f32x4 u[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 4; ++i) u[i] = *reinterpret_cast<const f32x4*>(from + (s + i) * stride);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) wt[i][j] = 0.f;
-    if (tail) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            load_elems<T, 8>(w + (size_t)(c + i) * ldw, wt[i]);
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (j >= tail) wt[i][j] = 0.f;
+            for (int i = 0; i < 4; ++i) v += u[i];
         }
-    }
-    for (int t = blockIdx.x * DH_ROWS; t < min((int)(blockIdx.x + 1) * DH_ROWS, m); ++t) {
-        float v[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int s = 0; s < splits; ++s) {
-            float u[4];
-            load_vec<float>(slabs + ((size_t)s * m + t) * n + c, u);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] += u[i];
-        }
-        if (tail) {
-            float d[8];
-            load_elems<T, 8>(dz + (size_t)t * ldz, d);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[i] += d[j] * wt[i][j];
-        }
+        for (; s < splits; ++s) v += *reinterpret_cast<const f32x4*>(from + s * stride);
         T* to = dh + (size_t)t * lddh + c;
         if constexpr (sizeof(T) == 4) {
-            store_vec<float>(to, v);
+            for (int j = 0; j < tail; ++j) {
+                const float d = dz[(size_t)t * ldz + j];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] += d * w[(size_t)(c + i) * ldw + j];
+            }
+            *reinterpret_cast<f32x4*>(to) = v;
         } else {
-            typedef bf16_t bf16x4_t __attribute__((ext_vector_type(4)));
-            *reinterpret_cast<bf16x4_t*>(to) = bf16x4_t{(bf16_t)v[0], (bf16_t)v[1], (bf16_t)v[2], (bf16_t)v[3]};
+            const int lift = lift_of(coef_of(targets, dloss, scale, t, m, vocab));
+            *reinterpret_cast<bf16x4*>(to) = bf16x4{(bf16_t)ldexpf(v[0], -lift), (bf16_t)ldexpf(v[1], -lift), (bf16_t)ldexpf(v[2], -lift), (bf16_t)ldexpf(v[3], -lift)};
         }
     }
 }
 
-// ---- dW: a piece's columns (+)= h^T dz, 2^shift taken off
-struct ColumnsEnd {
-    float* c;
-    const int* shift;
-    int m, n, ldc, flags;
-    __device__ __forceinline__ void begin(int, int) {}
-    template <int TO, int TN2, typename Acc>
-    __device__ __forceinline__ void end(const Acc& out, char* lds, int, int rb0, int cb0, int, int wave, int lane) const {
-        float* slab = reinterpret_cast<float*>(lds) + (size_t)wave * EpiSlab<TN2>::FLOATS;
-        accumulate<false, true, TO, TN2>(out, slab, rb0, cb0, m, n, ldc, *shift, c, flags, lane);
+// float: the rows of h that the weight gradient takes, tokens that do not count as zeros
+__global__ __launch_bounds__(ROW_THREADS) void xent_rows_f32_kernel(const float* __restrict__ h, int ldh, const int* __restrict__ targets, const float* __restrict__ dloss,
+                                                                    float scale, int m, int cols, int vocab, float* __restrict__ out) {
+    const int t = blockIdx.x * (ROW_THREADS / WAVE) + threadIdx.x / WAVE, lane = threadIdx.x % WAVE;
+    if (t >= m) return;
+    const bool on = coef_of(targets, dloss, scale, t, m, vocab) != 0.f;
+    for (int c = lane * 4; c < cols; c += WAVE * 4) {
+        float x[4];
+        load_vec<float>(h + (size_t)t * ldh + c, x);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = on ? x[e] : 0.f;
+        store_vec<float>(out + (size_t)t * cols + c, x);
     }
-};
-template <int BM, int BN, int WGM, int WGN, int WGK>
-__global__ __launch_bounds__(WGM* WGN * WGK * 64, 2) void xent_dw_kernel(const _Float16* __restrict__ h, const _Float16* __restrict__ parts, int k, int ldz,
-                                                                         int tiles_m, int tiles_n, int group_m, int band, ColumnsEnd end) {
-    __shared__ __attribute__((aligned(1024))) char lds[RingLds<BM, BN, WGM, WGN, WGK>::BYTES];
-    gemm_ring_tile<BM, BN, WGM, WGN, WGK, false, false, EPI_OWN, true>(lds, (const bf16_t*)h, (const bf16_t*)parts, nullptr, nullptr, nullptr, nullptr, end.m, ldz, k,
-                                                                       end.m, ldz, EPI_OWN, 0, 0, tiles_m, tiles_n, group_m, (int)blockIdx.x, nullptr, true, 0,
-                                                                       Ahead{nullptr, 0}, band, end);
 }
 
 // ---- float: a piece of z is in memory, [m, ld], of which `cols` columns from v0 on count
@@ -402,47 +486,37 @@ __global__ __launch_bounds__(ROW_THREADS) void xent_columns_kernel(const float* 
 size_t aligned(size_t b) { return (b + 255) / 256 * 256; }
 int round_up(int v, int a) { return (v + a - 1) / a * a; }
 long tiles_of(int m, int n, int tile) { return (long)((m + tile - 1) / tile) * ((n + tile - 1) / tile); }
-double rounds(long tiles) { return (double)((tiles + NUM_CUS - 1) / NUM_CUS); }
 
 // 256x256 tiles where they fill most of the chip, else 128x128 (as for the stages' products).
 int z_tile(int m, int n) { return tiles_of(m, n, 256) >= 144 ? 256 : 128; }
 
-// Columns of the vocabulary per piece where the caller leaves it open: dz of a piece takes at most this.
-constexpr size_t PIECE_BYTES = (size_t)512 << 20;
-constexpr int PIECE_STEP = 256;
-// Time of a round of tiles per step of 64 of the contraction, us (one tile per CU; see split_plan in gemm_mfma.hip)
-constexpr double STEP256 = 1.4, STEP128 = 0.5, SLAB = 8 / 4.5e6, LAUNCH = 10;
-double product_cost(int m, int n, long k) {
-    const double steps = (double)((k + 63) / 64);
-    return z_tile(m, n) == 256 ? rounds(tiles_of(m, n, 256)) * steps * STEP256 : rounds(tiles_of(m, n, 128)) * steps * STEP128;
-}
-struct SplitOf { int tile, splits, k_per; double cost; };
-// How the contraction of dh over a piece is cut: slabs are read and written once for every piece.
-SplitOf split_of(int m, int n, int k) {
-    const long steps = (k + 63) / 64;
-    SplitOf best{256, 1, round_up(k, 64), 1e300};
-    for (int tile : {256, 128})
-        for (int s = 1; s <= 64 && (s == 1 || steps / s >= 4); ++s) {
-            const long per = (steps + s - 1) / s;
-            if ((steps + per - 1) / per != s) continue;
-            const double cost = rounds(tiles_of(m, n, tile) * s) * per * (tile == 256 ? STEP256 : STEP128) + SLAB * s * m * n;
-            if (cost < best.cost) best = {tile, s, (int)per * 64, cost};
-        }
-    return best;
-}
+// Columns of the vocabulary per piece where the caller leaves it open: 8192, more where their buffers stay small, fewer where they get large.
+constexpr size_t PIECE_BYTES_MIN = (size_t)128 << 20, PIECE_BYTES_MAX = (size_t)512 << 20;
+constexpr int PIECE_STEP = 256, PIECE_USUAL = 8192;
 int default_piece(int dtype, int m, int hidden, int vocab) {
-    const int all = round_up(vocab, PIECE_STEP), mp = round_up(m, TOKEN_PAD);
-    const size_t column = dtype == CHIMERA_F32 ? ((size_t)m + hidden) * 4 : (size_t)mp * 6;
-    const int most = std::max<int>(PIECE_STEP, (int)std::min<size_t>(all, PIECE_BYTES / column / PIECE_STEP * PIECE_STEP));
-    if (most >= all) return all;
-    int best = most;
-    double least = 1e300;
-    for (int p = most; p >= PIECE_STEP && p >= most / 2; p -= PIECE_STEP) {
-        const int n = (vocab + p - 1) / p;
-        const double cost = n * (product_cost(m, p, hidden) + product_cost(hidden, p, 2l * mp) + split_of(m, hidden, p).cost + 3 * LAUNCH);
-        if (cost < least) { least = cost; best = p; }
-    }
-    return best;
+    const int all = round_up(vocab, PIECE_STEP);
+    const size_t column = dtype == CHIMERA_F32 ? ((size_t)m + hidden) * 4 : (size_t)round_up(m, TOKEN_PAD) * 8 + (size_t)hidden * 4;
+    const size_t usual = std::max(PIECE_BYTES_MIN / column, std::min<size_t>(PIECE_USUAL, PIECE_BYTES_MAX / column));
+    const int most = (int)std::min<size_t>(all, std::max<size_t>(usual / PIECE_STEP * PIECE_STEP, PIECE_STEP));
+    return round_up((vocab + (vocab + most - 1) / most - 1) / ((vocab + most - 1) / most), PIECE_STEP);        // equal pieces
+}
+// The launches' tiles, and the splits of dh's contraction.  256x256 tiles where the products of a piece fill the chip with them; rows of 128 for
+// up to 128 tokens.  dh's tiles are cut along the vocabulary so that none is longer than dW's, or than a piece's work shared by all CUs.
+struct PassPlan { int dw_tile, tok_tile, splits, k_per; };
+PassPlan plan_of(int mp, int hidden, int ld) {
+    PassPlan p{};
+    const long all256 = tiles_of(hidden, ld, 256) + tiles_of(mp, ld, 256);
+    p.dw_tile = tiles_of(hidden, ld, 256) >= 128 || all256 >= 320 ? 256 : 128;
+    p.tok_tile = p.dw_tile == 256 && mp > 128 ? 256 : 128;
+    auto work = [](int tile, long tiles, long steps) { return tiles * steps * (tile == 256 ? 1.0 : 0.35); };        // in steps of a 256x256 tile
+    const long dw_steps = mp / 32, dh_steps = (ld + 63) / 64, z_steps = (hidden + 63) / 64;
+    const double each = (work(p.dw_tile, tiles_of(hidden, ld, p.dw_tile), dw_steps) + work(p.tok_tile, tiles_of(mp, hidden, p.tok_tile), dh_steps) +
+                         work(p.tok_tile, tiles_of(mp, ld, p.tok_tile), z_steps)) / NUM_CUS;
+    const long most = std::max<long>(8, (long)(each / 3 * (p.tok_tile == 256 ? 1.0 : 1 / 0.35)));
+    const long splits = std::min<long>((dh_steps + most - 1) / most, 64), per = (dh_steps + splits - 1) / splits;
+    p.splits = (int)((dh_steps + per - 1) / per);
+    p.k_per = (int)per * 64;
+    return p;
 }
 
 struct FwdLayout { int tile, parts; size_t stats, at_target, z, total; int piece; };
@@ -459,28 +533,37 @@ FwdLayout fwd_layout(int dtype, int m, int hidden, int vocab) {
     l.total = b;
     return l;
 }
-struct BwdLayout { int piece, ld, mp; SplitOf split; size_t rows, up, room, shift, dz, parts, slabs, columns, total; };
+struct BwdLayout { int piece, ld, mp, ldp, buffers; PassPlan plan; size_t room, shift, rows, dz[2], w[2], raise[2], slabs, columns, total; };
 BwdLayout bwd_layout(int dtype, int m, int hidden, int vocab, int piece) {
     BwdLayout l{};
     size_t b = 0;
     auto take = [&](size_t bytes) { size_t r = b; b += aligned(bytes); return r; };
-    const bool f32 = dtype == CHIMERA_F32;
-    l.piece = piece ? round_up(piece, PIECE_STEP) : default_piece(dtype, m, hidden, vocab);
+    l.piece = piece ? round_up(std::min(piece, 1 << 22), PIECE_STEP) : default_piece(dtype, m, hidden, vocab);
     l.ld = std::min(l.piece, round_up(vocab, 8));
-    l.mp = f32 ? m : round_up(m, TOKEN_PAD);
-    l.split = f32 ? SplitOf{0, 1, l.ld, 0} : split_of(m, hidden, l.ld);
-    l.rows = take((size_t)l.mp * hidden * 4);                       // float rows, or fp16 rows twice
-    l.up = take((size_t)m * 4);
-    l.room = take((size_t)m * 4);
-    l.shift = take(4);
-    l.dz = take((size_t)l.mp * l.ld * (f32 ? 4 : 2));
-    l.parts = take(f32 ? 0 : (size_t)l.mp * l.ld * 4);
-    l.slabs = take((size_t)l.split.splits * m * hidden * 4);
-    l.columns = take(f32 ? (size_t)hidden * l.ld * 4 : 0);
+    if (dtype == CHIMERA_F32) {
+        l.mp = m;
+        l.rows = take((size_t)m * hidden * 4);
+        l.dz[0] = take((size_t)m * l.ld * 4);
+        l.slabs = take((size_t)m * hidden * 4);
+        l.columns = take((size_t)hidden * l.ld * 4);
+    } else {
+        l.mp = round_up(m, TOKEN_PAD);
+        l.plan = plan_of(l.mp, hidden, l.ld);
+        l.ldp = round_up(l.ld, 64) + 64;              // rows of W a power of two apart would meet in few memory channels
+        l.buffers = l.piece < vocab ? 2 : 1;
+        l.room = take((size_t)m * 4);
+        l.shift = take(4);
+        l.rows = take((size_t)l.mp * hidden * 2);
+        for (int i = 0; i < l.buffers; ++i) {
+            l.dz[i] = take((size_t)l.mp * l.ld * 4);
+            l.w[i] = take((size_t)hidden * l.ldp * 2);
+            l.raise[i] = take((size_t)hidden * 4);
+        }
+        l.slabs = take((size_t)l.plan.splits * m * hidden * 4);
+    }
     l.total = b;
     return l;
 }
-
 struct HeadLayout { size_t h, mean, rstd, loss_rows, lse, dh, scratch, ops, total; };
 HeadLayout head_layout(int dtype, int m, int hidden, int vocab, int piece) {
     const size_t e = dtype == CHIMERA_F32 ? 4 : 2;
@@ -504,7 +587,8 @@ HeadLayout head_layout(int dtype, int m, int hidden, int vocab, int piece) {
 int check_xent(int dtype, int tokens, int hidden, int vocab, int ldh, int ldw) {
     if (dtype != CHIMERA_F32 && dtype != CHIMERA_BF16) return fail(CHIMERA_EINVAL, "unknown dtype %d", dtype);
     if (tokens < 1 || hidden < 1 || vocab < 1) return fail(CHIMERA_EINVAL, "sizes must be positive");
-    if (tokens > 1 << 22 || hidden > 1 << 16 || vocab > 1 << 22) return fail(CHIMERA_EINVAL, "more than 2^22 tokens, 2^16 hidden or 2^22 vocabulary columns");
+    if (tokens > 1 << 22 || hidden > 1 << 15 || vocab > 1 << 22 || (long)tokens * vocab > 1l << 38)
+        return fail(CHIMERA_EINVAL, "more than 2^22 tokens, 2^15 hidden or 2^22 vocabulary columns, or 2^38 logits");
     if (hidden % 8) return fail(CHIMERA_EINVAL, "hidden=%d must be a multiple of 8", hidden);
     if (ldh % 8 || ldw % 8) return fail(CHIMERA_EINVAL, "leading dimensions ldh=%d, ldw=%d must be multiples of 8", ldh, ldw);
     if (ldh < hidden || ldw < vocab) return fail(CHIMERA_EINVAL, "leading dimension too small");
@@ -529,6 +613,16 @@ template <typename F> int with_tile(int m, int n, F&& f) {
     return f.template operator()<128, 2, 2, 1>();
 }
 
+template <typename T>
+int launch_dh_sum(const float* slabs, int splits, const T* dz, int ldz, const T* w, int ldw, int tail, const int* targets, const float* dloss, float scale, int vocab,
+                  int m, int n, T* dh, int lddh, hipStream_t s) {
+    const size_t threads = (size_t)m * (n / 4);
+    hipLaunchKernelGGL(xent_dh_sum_kernel<T>, dim3((unsigned)std::min<size_t>((threads + ROW_THREADS - 1) / ROW_THREADS, 1 << 20)), dim3(ROW_THREADS), 0, s, slabs, splits, dz, ldz, w, ldw, tail,
+                       targets, dloss, scale, vocab, m, n, dh, lddh);
+    CHIMERA_LAUNCH_CHECK("linear cross-entropy");
+    return CHIMERA_OK;
+}
+
 int xent_fwd_f32(int m, int hidden, int vocab, const float* h, int ldh, const float* w, int ldw, const int* targets, const FwdLayout& l, char* ws, void* stream) {
     for (int v0 = 0, p = 0; v0 < vocab; v0 += l.piece, ++p) {
         const int cols = std::min(l.piece, vocab - v0), ld = round_up(cols, 8);
@@ -545,10 +639,9 @@ int xent_fwd_f32(int m, int hidden, int vocab, const float* h, int ldh, const fl
 int xent_bwd_f32(int m, int hidden, int vocab, const float* h, int ldh, const float* w, int ldw, const int* targets, const float* lse, float scale,
                  const float* dloss, float* dh, int lddh, float* dw, int lddw, int overwrite, const BwdLayout& l, char* ws, void* stream) {
     hipStream_t s = (hipStream_t)stream;
-    float *rows = (float*)(ws + l.rows), *z = (float*)(ws + l.dz), *slab = (float*)(ws + l.slabs), *columns = (float*)(ws + l.columns);
+    float *rows = (float*)(ws + l.rows), *z = (float*)(ws + l.dz[0]), *slab = (float*)(ws + l.slabs), *columns = (float*)(ws + l.columns);
     if (dw) {
-        hipLaunchKernelGGL((xent_rows_kernel<float, float>), dim3((m + 3) / 4), dim3(ROW_THREADS), 0, s, h, ldh, targets, dloss, scale, m, m, hidden, vocab, rows,
-                           nullptr, nullptr);
+        hipLaunchKernelGGL(xent_rows_f32_kernel, dim3((m + 3) / 4), dim3(ROW_THREADS), 0, s, h, ldh, targets, dloss, scale, m, hidden, vocab, rows);
         CHIMERA_LAUNCH_CHECK("linear cross-entropy");
     }
     int slabs = 0;
@@ -575,9 +668,7 @@ int xent_bwd_f32(int m, int hidden, int vocab, const float* h, int ldh, const fl
             CHIMERA_LAUNCH_CHECK("linear cross-entropy");
         }
         if (dh && v0 + l.piece >= vocab) {
-            hipLaunchKernelGGL(xent_dh_sum_kernel<float>, dim3((m + DH_ROWS - 1) / DH_ROWS, (hidden / 4 + ROW_THREADS - 1) / ROW_THREADS), dim3(ROW_THREADS), 0, s,
-                               slab, slabs, z + whole, ld, w + v0 + whole, ldw, cols - whole, m, hidden, dh, lddh);
-            CHIMERA_LAUNCH_CHECK("linear cross-entropy");
+            XENT_TRY(launch_dh_sum(slab, slabs, z + whole, ld, w + v0 + whole, ldw, cols - whole, targets, dloss, scale, vocab, m, hidden, dh, lddh, s));
         }
     }
     return CHIMERA_OK;
@@ -586,53 +677,58 @@ int xent_bwd_f32(int m, int hidden, int vocab, const float* h, int ldh, const fl
 int xent_bwd_bf16(int m, int hidden, int vocab, const bf16_t* h, int ldh, const bf16_t* w, int ldw, const int* targets, const float* lse, float scale,
                   const float* dloss, bf16_t* dh, int lddh, float* dw, int lddw, int overwrite, const BwdLayout& l, char* ws, void* stream) {
     hipStream_t s = (hipStream_t)stream;
-    _Float16 *rows = (_Float16*)(ws + l.rows), *parts = (_Float16*)(ws + l.parts);
-    int *up = (int*)(ws + l.up), *room = (int*)(ws + l.room), *shift = (int*)(ws + l.shift);
-    bf16_t* dz = (bf16_t*)(ws + l.dz);
-    float* slabs = (float*)(ws + l.slabs);
-    hipLaunchKernelGGL((xent_rows_kernel<bf16_t, _Float16>), dim3((l.mp + 3) / 4), dim3(ROW_THREADS), 0, s, h, ldh, targets, dloss, scale, m, l.mp, hidden, vocab,
-                       rows, up, room);
-    CHIMERA_LAUNCH_CHECK("linear cross-entropy");
-    hipLaunchKernelGGL(xent_shift_kernel, dim3(1), dim3(1024), 0, s, room, m, shift);
-    CHIMERA_LAUNCH_CHECK("linear cross-entropy");
-    int splits = 0;
-    for (int v0 = 0; v0 < vocab; v0 += l.piece) {
-        const int cols = std::min(l.piece, vocab - v0), ld = round_up(cols, 8), whole = cols & ~7;
-        XENT_TRY(with_tile(m, ld, [&]<int BM, int WGM, int WGN, int WGK>() {
-            return with_raster<BM, WGM, WGN, WGK>(l.mp, ld, hidden, [&](int tm, int tn, int gm, int band) {
-                const GradEnd<BM, WGM * WGN * WGK> end{lse, targets, dloss, up, shift, scale, m, l.mp, vocab, v0, cols, ld, dz, parts, {}};
-                hipLaunchKernelGGL((xent_dz_kernel<BM, BM, WGM, WGN, WGK>), dim3(tm * tn), dim3(WGM * WGN * WGK * 64), 0, s, h, w, hidden, ldh, ldw, tm, tn, gm,
-                                   band, end);
-            });
-        }));
-        if (dh && whole) {
-            // the last piece is cut where the others are: a split that it does not reach adds nothing
-            const int t = l.split.tile, tm = (m + t - 1) / t, tn = (hidden + t - 1) / t, now = (whole + l.split.k_per - 1) / l.split.k_per;
-            const int gm = raster_group(tm, tn, std::min(tm * tn, (tm * tn * now + 7) / 8), t, t);
-            const dim3 grid(tm * tn * now), block(512);
-            const int flags = splits ? 0 : ACCUM_OVERWRITE;
-#define XENT_DH(...) hipLaunchKernelGGL((xent_dh_kernel<__VA_ARGS__>), grid, block, 0, s, dz, w + v0, slabs, m, hidden, whole, ld, ldw, tm, tn, gm, now, l.split.k_per, flags)
-            if (t == 256) XENT_DH(256, 256, 2, 4, 1);
-            else XENT_DH(128, 128, 2, 2, 2);
-#undef XENT_DH
-            CHIMERA_LAUNCH_CHECK("linear cross-entropy");
-            if (!splits) splits = now;
-        }
-        if (dw)
-            XENT_TRY(with_tile(hidden, ld, [&]<int BM, int WGM, int WGN, int WGK>() {
-                return with_raster<BM, WGM, WGN, WGK>(hidden, ld, 2 * l.mp, [&](int tm, int tn, int gm, int band) {
-                    const ColumnsEnd end{dw + v0, shift, hidden, cols, lddw, overwrite ? ACCUM_OVERWRITE : 0};
-                    hipLaunchKernelGGL((xent_dw_kernel<BM, BM, WGM, WGN, WGK>), dim3(tm * tn), dim3(WGM * WGN * WGK * 64), 0, s, rows, parts, 2 * l.mp, ld, tm, tn,
-                                       gm, band, end);
-                });
-            }));
-        if (dh && v0 + l.piece >= vocab) {
-            hipLaunchKernelGGL(xent_dh_sum_kernel<bf16_t>, dim3((m + DH_ROWS - 1) / DH_ROWS, (hidden / 4 + ROW_THREADS - 1) / ROW_THREADS), dim3(ROW_THREADS), 0, s,
-                               slabs, splits, dz + whole, ld, w + v0 + whole, ldw, cols - whole, m, hidden, dh, lddh);
-            CHIMERA_LAUNCH_CHECK("linear cross-entropy");
-        }
+    Pass p{};
+    p.h = h; p.w = w; p.targets = targets; p.lse = lse; p.dloss = dloss; p.scale = scale;
+    p.m = m; p.mp = l.mp; p.hidden = hidden; p.vocab = vocab; p.ldh = ldh; p.ldw = ldw; p.ldp = l.ldp;
+    p.room = (int*)(ws + l.room); p.shift = (int*)(ws + l.shift); p.rows = (_Float16*)(ws + l.rows);
+    p.rows_per_wg = std::max(32, l.mp / 1024);               // every workgroup looks for the shift by itself
+    p.dw = dw; p.lddw = lddw; p.dw_flags = overwrite ? ACCUM_OVERWRITE : 0;
+    p.slabs = (float*)(ws + l.slabs); p.k_per = l.plan.k_per;
+    if (dw) {
+        hipLaunchKernelGGL(xent_room_kernel, dim3((m + 3) / 4), dim3(ROW_THREADS), 0, s, h, ldh, targets, dloss, scale, m, hidden, vocab, p.room);
+        CHIMERA_LAUNCH_CHECK("linear cross-entropy");
     }
-    return CHIMERA_OK;
+    auto raster = [](int tile, int rows, int cols, int k, bool bands) {
+        Pass::Raster r{(rows + tile - 1) / tile, (cols + tile - 1) / tile, 1, 0};
+        if (bands) r.band = raster_band(r.tiles_m, r.tiles_n, NUM_CUS, (size_t)cols * k * 2);
+        r.group_m = raster_group(r.tiles_m, r.band ? r.band : r.tiles_n, std::min((r.tiles_m * r.tiles_n + 7) / 8, PER_XCD), tile, tile);
+        return r;
+    };
+    const int pieces = (vocab + l.piece - 1) / l.piece;
+    int splits = 0;
+    for (int i = 0; i <= pieces; ++i) {
+        p.now = p.next;
+        int count[5] = {};
+        if (i > 0) {
+            if (dw) {
+                p.dw_r = raster(l.plan.dw_tile, hidden, p.now.ld, 2 * l.mp, true);
+                count[0] = p.dw_r.tiles_m * p.dw_r.tiles_n;
+            }
+            if (dh) {
+                // the last piece is cut where the others are: a split that it does not reach adds nothing
+                const int now = (p.now.ld + l.plan.k_per - 1) / l.plan.k_per;
+                p.dh_r = raster(l.plan.tok_tile, m, hidden, 0, false);
+                count[1] = p.dh_r.tiles_m * p.dh_r.tiles_n * now;
+                p.dh_flags = i == 1 ? ACCUM_OVERWRITE : 0;
+                if (i == 1) splits = now;
+            }
+        }
+        if (i < pieces) {
+            const int v0 = i * l.piece, cols = std::min(l.piece, vocab - v0), at = i & (l.buffers - 1);
+            p.next = {v0, cols, round_up(cols, 8), (_Float16*)(ws + l.dz[at]), (_Float16*)(ws + l.w[at]), (int*)(ws + l.raise[at])};
+            p.dz_r = raster(l.plan.tok_tile, l.mp, p.next.ld, hidden, true);
+            count[2] = p.dz_r.tiles_m * p.dz_r.tiles_n;
+            if (dh) count[3] = (hidden + W_ROWS_PER_WG - 1) / W_ROWS_PER_WG;
+            if (dw && i == 0) count[4] = (l.mp + p.rows_per_wg - 1) / p.rows_per_wg;
+        }
+        int total = 0;
+        for (int k = 0; k < 5; ++k) { p.first[k] = total; total += count[k]; }
+        if (l.plan.dw_tile == 256 && l.plan.tok_tile == 256) hipLaunchKernelGGL((xent_pass_kernel<256, 256>), dim3(total), dim3(512), 0, s, p);
+        else if (l.plan.dw_tile == 256) hipLaunchKernelGGL((xent_pass_kernel<256, 128>), dim3(total), dim3(512), 0, s, p);
+        else hipLaunchKernelGGL((xent_pass_kernel<128, 128>), dim3(total), dim3(512), 0, s, p);
+        CHIMERA_LAUNCH_CHECK("linear cross-entropy");
+    }
+    return dh ? launch_dh_sum<bf16_t>(p.slabs, splits, nullptr, 0, nullptr, 0, 0, targets, dloss, scale, vocab, m, hidden, dh, lddh, s) : CHIMERA_OK;
 }
 
 }  // namespace

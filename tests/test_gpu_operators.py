@@ -143,7 +143,7 @@ def _check_backward(dtype, h, w, targets, lse, scale, dloss, dh, dw, dw0):
     if dh is not None:
         want = dz @ wd.t()
         mag = dz.abs() @ wd.abs().t()
-        rounding = 2.0 ** -8 if dtype == b.BF16 else 3 * E24
+        rounding = 2.0 ** -11 if dtype == b.BF16 else 3 * E24          # dz as one fp16 number
         tol = dz_off @ wd.abs().t() + (rounding + (vocab + 64 + 80) * E24) * mag + (2.0 ** -8 if dtype == b.BF16 else E24) * want.abs() + 1e-38
         assert ((dh.double() - want).abs() <= tol).all(), float(((dh.double() - want).abs() / tol).max())
         assert (dh[~valid] == 0).all()

@@ -19,7 +19,7 @@ def bwd(dtype=b.BF16, tokens=4, hidden=64, vocab=100, h=P, ldh=64, w=P, ldw=104,
     return b.lib().chimera_op_linear_xent_bwd(dtype, tokens, hidden, vocab, h, ldh, w, ldw, targets, lse, 1.0, dloss, dh, lddh, dw, lddw, 0, piece, ws, size, None)
 
 
-BAD_SIZES = [dict(dtype=2), dict(tokens=0), dict(tokens=-3), dict(tokens=(1 << 22) + 1), dict(hidden=0), dict(hidden=60), dict(hidden=(1 << 16) + 8, ldh=(1 << 16) + 8),
+BAD_SIZES = [dict(dtype=2), dict(tokens=0), dict(tokens=-3), dict(tokens=(1 << 22) + 1), dict(hidden=0), dict(hidden=60), dict(hidden=(1 << 15) + 8, ldh=(1 << 15) + 8), dict(tokens=1 << 22, vocab=65537, ldw=65544),
              dict(vocab=0), dict(vocab=105), dict(vocab=(1 << 22) + 8, ldw=(1 << 22) + 8), dict(ldh=56), dict(ldh=68), dict(ldw=108), dict(ldw=1 << 23),
              dict(h=None), dict(w=None), dict(targets=None), dict(lse=None), dict(ws=None), dict(h=P + 8), dict(w=P + 2), dict(ws=P + 16)]
 
