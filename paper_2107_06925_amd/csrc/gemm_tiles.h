@@ -760,11 +760,11 @@ __device__ __forceinline__ void lds_dma16_s(const void* sbase, unsigned voff, un
     asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(sbase), "{m0}"(lds_base) : "memory");
 }
 // A tile's own way to end (ONLY_EPI = EPI_OWN), in place of the epilogues above: begin() ahead of the k loop, end() with the accumulators
-// once every wavefront has left it.  F16: operands of fp16 in place of bf16.  PAIRED (index-contiguous operands): the contraction takes every row of A twice, with
-// the row of B and with the one own_end.pair elements behind it, 32 rows of A a step.
+// once every wavefront has left it.  F16: operands of fp16 in place of bf16.  PAIRED (A k-contiguous, B index-contiguous): the contraction takes every k of A
+// twice, with the row of B and with the one own_end.pair elements behind it, 32 k of A a step.
 constexpr int EPI_OWN = 6;
 struct NoEnd {};
-template <int BM, int BN, int WGM, int WGN, int WGK, bool A_KC, bool B_KC, int ONLY_EPI, bool F16 = false, bool PAIRED = false, typename End = NoEnd>
+template <int BM, int BN, int WGM, int WGN, int WGK, bool A_KC, bool B_KC, int ONLY_EPI, bool F16 = false, bool PAIRED = false, bool TOUCH = false, typename End = NoEnd>
 __device__ __forceinline__ void gemm_ring_tile(
     char* lds, const bf16_t* __restrict__ A, const bf16_t* __restrict__ B, const bf16_t* __restrict__ bias,
     const bf16_t* __restrict__ R, void* __restrict__ C, bf16_t* __restrict__ C2, int m, int n, int k, int lda,
@@ -803,7 +803,7 @@ __device__ __forceinline__ void gemm_ring_tile(
         if (kc) {
             const int row = slot >> 3;
             kk = ((slot & 7) ^ rswz(row)) * 8;
-            return (unsigned)((min(row0 + row, nrows - 1) - row0) * ld + kk) * 2u;
+            return (unsigned)((min(row0 + row, nrows - 1) - row0) * ld + (PAIRED ? kk & 31 : kk)) * 2u;
         }
         kk = slot / (rows / 8);
         const int pc = slot % (rows / 8), ic = (((pc >> 1) ^ rkswz(kk)) << 1) | (pc & 1);
@@ -821,7 +821,7 @@ __device__ __forceinline__ void gemm_ring_tile(
 #pragma unroll
     for (int it = 0; it < OB; ++it) vb[it] = piece(ldb, j0, n, std::integral_constant<int, BN>{}, B_KC, it * NT + tid, kb);
 #pragma unroll
-    for (int it = 0; it < PA; ++it) sa[it] = (const char*)(A + (A_KC ? (size_t)i0 * lda : (size_t)i0 + (size_t)(PAIRED ? it * KIA & 31 : it * KIA) * lda));
+    for (int it = 0; it < PA; ++it) sa[it] = (const char*)(A + (A_KC ? (size_t)i0 * lda : (size_t)i0 + (size_t)it * KIA * lda));
 #pragma unroll
     for (int it = 0; it < PB; ++it) {
         sb[it] = (const char*)(B + (B_KC ? (size_t)j0 * ldb : (size_t)j0 + (size_t)(PAIRED ? it * KIB & 31 : it * KIB) * ldb));
@@ -829,12 +829,46 @@ __device__ __forceinline__ void gemm_ring_tile(
             if (it * KIB >= 32) sb[it] += (size_t)own_end.pair * 2;
     }
     static_assert(KIA % 16 == 0 && KIB % 16 == 0, "requests of one lane share a swizzle");
-    static_assert(!PAIRED || (!A_KC && !B_KC && KIA <= 32 && KIB <= 32), "a request lies within 32 rows");
+    static_assert(!PAIRED || (A_KC && !B_KC && KIB <= 32), "a request of B lies within 32 rows");
     constexpr int ROWS = PAIRED ? RK / 2 : RK;
-    const size_t step_a = (A_KC ? (size_t)RK : (size_t)ROWS * lda) * 2, step_b = (B_KC ? (size_t)RK : (size_t)ROWS * ldb) * 2;
+    const size_t step_a = (A_KC ? (size_t)ROWS : (size_t)RK * lda) * 2, step_b = (B_KC ? (size_t)RK : (size_t)ROWS * ldb) * 2;
     const unsigned lds0 = lds_address(lds), dma0 = lds0 + wave * 1024;
 
     // Operand reads: lane l holds k 8(l/16)..+7 of row (column) l%16 of a 16-row tile.
+    // TOUCH: a wavefront touches sixteen lines of 128 bytes of the stage three steps ahead, so that its requests find them in L2.  Tiles of a raster share
+    // operand panels, and each touches a quarter of either panel's lines.
+    static_assert(!TOUCH || (WGK == 1 && BM == 256 && BN == 256 && A_KC), "256 lines of either operand a stage");
+    const char* line = nullptr;
+    size_t line_step = 0;
+    unsigned strip = 0;
+    int left = (k + RK - 1) / RK - 3;
+    if constexpr (TOUCH) {
+        __shared__ __attribute__((aligned(16))) char lines[AHEAD_STRIP];
+        strip = lds_address(lines);
+        const int q = (wave * 16 + (lane >> 2)) & 63, whole = 2 - (k % RK ? 1 : 0);        // of stage 2
+        if (wave < 4) {
+            const int row = min(i0 + q * 4 + (tile_n & 3), m - 1);
+            line = (const char*)(A + (size_t)row * lda) + whole * step_a;
+            line_step = step_a;
+        } else {
+            const int at = q * 4 + (tile_m & 3);
+            if constexpr (B_KC) line = (const char*)(B + (size_t)min(j0 + at, n - 1) * ldb);
+            else {
+                const int kk = at >> 2;
+                line = (const char*)(B + (size_t)(PAIRED ? kk & 31 : kk) * ldb + min(j0 + (at & 3) * 64, n - 8));
+                if constexpr (PAIRED) line += kk >= 32 ? (size_t)own_end.pair * 2 : 0;
+            }
+            line += whole * step_b;
+            line_step = step_b;
+        }
+    }
+    auto touch = [&] {
+        if constexpr (TOUCH) {
+            asm volatile("global_load_lds_dword %0, off" ::"v"(line), "{m0}"(strip) : "memory");
+            line += left > 0 ? line_step : 0;                  // (the last stage's lines more than once)
+            --left;
+        }
+    };
     typedef bf16x8 __attribute__((address_space(3))) * lds_v8;
     typedef bf16x4 __attribute__((address_space(3))) * lds_v4;
     // half h (32 k) of buffer q: the offset field of an LDS instruction reaches over one buffer (64 KiB)
@@ -964,8 +998,10 @@ __device__ __forceinline__ void gemm_ring_tile(
             constexpr int ROOM_B = HM * TN - TN - HM, ROOM_A = HM * TN - HM;
             constexpr int D3 = CS / 2 < ROOM_B ? CS / 2 : ROOM_B, D0 = CS - D3;       // a step's requests in their first and second phase
             if (!rest) static_for<CS>([&](auto i) { request(i, CHIMERA_C(0)); });
-            if (KT > 1) { static_for<CS>([&](auto i) { if constexpr (decltype(i)::value < D3) request(i, CHIMERA_C(1)); }); arrived(CHIMERA_C(D3)); }
-            else arrived(CHIMERA_C(0));
+            if (KT > 1) { static_for<CS>([&](auto i) { if constexpr (decltype(i)::value < D3) request(i, CHIMERA_C(1)); });
+                if (TOUCH && KT > 2) { touch(); arrived(CHIMERA_C(D3 + 1)); }
+                else arrived(CHIMERA_C(D3));
+            } else arrived(CHIMERA_C(0));
             meet();
             static_for<TN>([&](auto b) { read_b(b, CHIMERA_C(0), CHIMERA_C(0)); });
             static_for<HM>([&](auto a) { read_a(a, CHIMERA_C(0), CHIMERA_C(0)); });
@@ -987,12 +1023,14 @@ __device__ __forceinline__ void gemm_ring_tile(
                     constexpr int i = decltype(i_c)::value;
                     if constexpr (i < TN) read_b(i_c, CHIMERA_C(1), q_c);
                     else if constexpr (i < TN + HM) read_a(CHIMERA_C(i - TN), CHIMERA_C(1), q_c);
+                    else if constexpr (TOUCH && always && i == TN + HM) touch();
                 });
                 phase(CHIMERA_C(0), CHIMERA_C(1), sums_c, [&](auto i_c) {
                     constexpr int i = decltype(i_c)::value;
                     if constexpr (i < HM) read_a(CHIMERA_C(HM + i), CHIMERA_C(1), q_c);
                 });
-                arrived(CHIMERA_C(0));
+                if constexpr (TOUCH && always) arrived(CHIMERA_C(1));          // the youngest is the touch
+                else arrived(CHIMERA_C(0));
                 meet();
                 phase(CHIMERA_C(1), CHIMERA_C(1), sums_c, [&](auto i_c) {
                     constexpr int i = decltype(i_c)::value;

@@ -162,8 +162,7 @@ struct Pass {
     float scale;
     int m, mp, hidden, vocab, ldh, ldw, ldp;
     int *room, *shift;
-    _Float16* rows;                  // [mp, hidden]: h_t 2^(shift - lift_t)
-    int rows_per_wg;
+    _Float16* rows;                  // [hidden, mp]: h_t 2^(shift - lift_t), transposed
     Piece now, next;                 // the products' piece, and the one that dz is formed of
     // dW: columns of `now`
     float* dw;
@@ -172,7 +171,7 @@ struct Pass {
     float* slabs;
     int k_per, dh_flags;
     // workgroups of each kind, in this order, and the rasters of their tiles
-    int first[5];                    // dW, dh, dz, W's rows, h's rows
+    int first[5];                    // dW, dh, dz, W's rows, h^T
     struct Raster { int tiles_m, tiles_n, group_m, band; } dw_r, dh_r, dz_r;
 };
 
@@ -223,8 +222,9 @@ struct SlabEnd {
         });
     }
 };
-// dz of a piece
-struct RowInfo { float lse, scaled; int at, on; };          // coef 2^lift, the target's column in the piece, whether coef is not zero
+// dz of a piece.  Its vector instructions are what bounds it (a tile's 65536 exponentials and conversions, with the matrix pipes idle), so a band of 32 rows
+// looks for targets only where it holds one.
+struct RowInfo { float lse, scaled; int at; };              // coef 2^lift (0: the token does not count), the target's column in the piece
 template <int BM> struct GradEnd {
     const Pass* p;
     RowInfo mine;
@@ -232,7 +232,7 @@ template <int BM> struct GradEnd {
         // (no branches: the compiler keeps the tile's operand addresses in scalar registers only outside of divergent code)
         const int t = min(i0 + tid, p->m - 1);
         const float coef = coef_of(p->targets, p->dloss, p->scale, i0 + tid, p->m, p->vocab);
-        mine = {p->lse[t], ldexpf(coef, lift_of(coef)), p->targets[t] - p->next.v0, coef != 0.f};
+        mine = {p->lse[t], ldexpf(coef, lift_of(coef)), coef != 0.f ? p->targets[t] - p->next.v0 : -1};
     }
     template <int TO, int TN2, typename Acc>
     __device__ __forceinline__ void end(const Acc& out, char* lds, int i0, int rb0, int cb0, int, int wave, int lane) const {
@@ -243,31 +243,49 @@ template <int BM> struct GradEnd {
         if (tid < BM) tab[tid] = mine;
         __syncthreads();
         const int pr = lane / CPR, pc = lane % CPR * 8, col = cb0 + pc;
+        _Float16* const first = p->next.dz + (size_t)(rb0 + pr) * 2 * ld + col;
         static_for<TO>([&](auto a_c) {
             constexpr int a = decltype(a_c)::value;
             out.template put<a>(slab, lane);
+            const bool usual = cb0 + EpiSlab<TN2>::WN <= cols && !__any((unsigned)(tab[rb0 - i0 + a * 32 + (lane & 31)].at - cb0) < (unsigned)EpiSlab<TN2>::WN);
             __builtin_amdgcn_s_waitcnt(0xc07f);                   // lgkmcnt(0): the slab is written (wavefront-private)
             __builtin_amdgcn_wave_barrier();
+            auto rows = [&](auto usual_c) {
 #pragma unroll
-            for (int j = 0; j < NP; ++j) {
-                const int lr = a * 32 + j * RPP + pr, row = rb0 + lr;
-                const RowInfo r = tab[rb0 - i0 + lr];
-                float v[8];
-                load_vec<float>(EpiSlab<TN2>::at(slab, j * RPP + pr, pc / 4), v);
-                load_vec<float>(EpiSlab<TN2>::at(slab, j * RPP + pr, pc / 4 + 1), v + 4);
-                if (row >= mp || col >= ld) continue;
-                f16x8 hi, lo;
+                for (int j = 0; j < NP; ++j) {
+                    const int lr = a * 32 + j * RPP + pr, row = rb0 + lr;
+                    const RowInfo r = tab[rb0 - i0 + lr];
+                    float v[8];
+                    load_vec<float>(EpiSlab<TN2>::at(slab, j * RPP + pr, pc / 4), v);
+                    load_vec<float>(EpiSlab<TN2>::at(slab, j * RPP + pr, pc / 4 + 1), v + 4);
+                    typedef float f32x2 __attribute__((ext_vector_type(2)));
+                    typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+                    f16x2 hi[4], lo[4];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    float d = __builtin_amdgcn_exp2f((v[e] - r.lse) * LOG2E) - (col + e == r.at ? 1.0f : 0.0f);
-                    d = !r.on || col + e >= cols ? 0.f : r.scaled * d;
-                    hi[e] = (_Float16)d;
-                    lo[e] = (_Float16)(d - (float)hi[e]);
+                    for (int e = 0; e < 8; e += 2) {
+                        f32x2 d;
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) {
+                            // (the smaller of 126 and what is no number is 126: a token that does not count has zeros)
+                            float x = __builtin_amdgcn_exp2f(fminf((v[e + q] - r.lse) * LOG2E, 126.0f));
+                            if constexpr (!decltype(usual_c)::value) {
+                                x -= col + e + q == r.at ? 1.0f : 0.0f;
+                                if (col + e + q >= cols) x = 0.f;
+                            }
+                            d[q] = r.scaled * x;
+                        }
+                        hi[e / 2] = __builtin_convertvector(d, f16x2);
+                        const f32x2 rest = d - __builtin_convertvector(hi[e / 2], f32x2);
+                        lo[e / 2] = __builtin_convertvector(rest, f16x2);
+                    }
+                    if (row >= mp || col >= ld) continue;
+                    _Float16* to = first + (size_t)(a * 32 + j * RPP) * (2 * ld);
+                    *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(hi);
+                    *reinterpret_cast<uint4*>(to + ld) = *reinterpret_cast<const uint4*>(lo);
                 }
-                _Float16* to = p->next.dz + (size_t)row * 2 * ld + col;
-                *reinterpret_cast<f16x8*>(to) = hi;
-                *reinterpret_cast<f16x8*>(to + ld) = lo;
-            }
+            };
+            if (usual) rows(std::true_type{});
+            else rows(std::false_type{});
             __builtin_amdgcn_wave_barrier();                      // all lanes have read the slab before it is rewritten
         });
     }
@@ -301,10 +319,14 @@ __device__ __forceinline__ void raise_row(const Pass& p, int i, char* lds) {
         *reinterpret_cast<f16x8*>(to + c) = y;
     }
 }
-// Rows of h times 2^(shift - lift); tokens that do not count, and the padding behind the last one, as zeros: their dz is zero, but h may hold anything.
-constexpr int W_ROWS_PER_WG = 4;
-__device__ __forceinline__ void shift_rows(const Pass& p, int t0, char* lds, bool tells) {
+// h^T times 2^(shift - lift); tokens that do not count, and the padding behind the last one, as zeros: their dz is zero, but h may hold anything.
+// Transposed, because the matrix instructions take runs of the contraction's index: both operands of dW through the transposing LDS reads, which
+// deliver 64 bytes a clock, make its step 3072 clocks of LDS to 2048 of matrix instructions (measured: 3080; dW at 8192 x 2048 x 8192 442 us).
+constexpr int W_ROWS_PER_WG = 4, TURN_TOKENS = 64, TURN_COLS = 256, TURN_WGS = 1024;
+__device__ __forceinline__ void turn_rows(const Pass& p, int id, int wgs, char* lds) {
     int* part = reinterpret_cast<int*>(lds);
+    constexpr int LD = TURN_TOKENS + 8;
+    _Float16* tile = reinterpret_cast<_Float16*>(lds + 64);        // [64 columns][LD]
     int least = INT_MAX;
     for (int t = threadIdx.x; t < p.m; t += 512) least = min(least, p.room[t]);
 #pragma unroll
@@ -313,22 +335,29 @@ __device__ __forceinline__ void shift_rows(const Pass& p, int t0, char* lds, boo
     __syncthreads();
     for (int i = 0; i < 8; ++i) least = min(least, part[i]);
     const int shift = least == INT_MAX ? 0 : least;
-    if (tells && threadIdx.x == 0) *p.shift = shift;
-    for (int t = t0 + threadIdx.x / WAVE; t < min(t0 + p.rows_per_wg, p.mp); t += 8) {
-        const float coef = coef_of(p.targets, p.dloss, p.scale, t, p.m, p.vocab);
+    if (id == 0 && threadIdx.x == 0) *p.shift = shift;
+    const int groups = (p.hidden + TURN_COLS - 1) / TURN_COLS, units = (p.mp + TURN_TOKENS - 1) / TURN_TOKENS * groups;
+    const int a = threadIdx.x >> 3, b = threadIdx.x & 7;          // token and 8 columns on the way in, column and 8 tokens on the way out
+    for (int u = id; u < units; u += wgs) {
+        const int t0 = u / groups * TURN_TOKENS, g0 = u % groups * TURN_COLS;
+        const float coef = coef_of(p.targets, p.dloss, p.scale, t0 + a, p.m, p.vocab);
         const int up = shift - lift_of(coef);
-        for (int c = threadIdx.x % WAVE * 8; c < p.hidden; c += WAVE * 8) {
-            float x[8];
-            load_vec<bf16_t>(p.h + (size_t)min(t, p.m - 1) * p.ldh + c, x);
-            f16x8 y;
+        for (int c0 = g0; c0 < min(g0 + TURN_COLS, p.hidden); c0 += 64) {
+            if (c0 + b * 8 < p.hidden) {
+                float x[8];
+                load_vec<bf16_t>(p.h + (size_t)min(t0 + a, p.m - 1) * p.ldh + c0 + b * 8, x);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = coef != 0.f ? (_Float16)ldexpf(x[e], up) : (_Float16)0.f;
-            *reinterpret_cast<f16x8*>(p.rows + (size_t)t * p.hidden + c) = y;
+                for (int e = 0; e < 8; ++e) tile[(b * 8 + e) * LD + a] = coef != 0.f ? (_Float16)ldexpf(x[e], up) : (_Float16)0.f;
+            }
+            __syncthreads();
+            if (c0 + a < p.hidden && t0 + b * 8 < p.mp)
+                *reinterpret_cast<f16x8*>(p.rows + (size_t)(c0 + a) * p.mp + t0 + b * 8) = *reinterpret_cast<const f16x8*>(tile + a * LD + b * 8);
+            __syncthreads();
         }
     }
 }
 
-// One launch: dW and dh of a piece, dz and the rows of W of the next, and, in a pass's first, the rows of h.  Tiles of DW x DW for dW, of TOK x TOK for
+// One launch: dW and dh of a piece, dz and the rows of W of the next, and, in a pass's first, h^T.  Tiles of DW x DW for dW, of TOK x TOK for
 // the products over tokens.
 template <int DW, int TOK>
 __global__ __launch_bounds__(512, 2) void xent_pass_kernel(Pass p) {
@@ -340,7 +369,7 @@ __global__ __launch_bounds__(512, 2) void xent_pass_kernel(Pass p) {
 #define XENT_TILE(T, AKC, BKC, F16, PAIRED, A, B, M, N, K, LDA, LDB, R, ID, BAND, XCD, END)                                                                          \
     do {                                                                                                                                                       \
         if constexpr (T == 256)                                                                                                                                \
-            gemm_ring_tile<256, 256, 2, 4, 1, AKC, BKC, EPI_OWN, F16, PAIRED>(lds, A, B, nullptr, nullptr, nullptr, nullptr, M, N, K, LDA, LDB, EPI_OWN, 0, 0,  \
+            gemm_ring_tile<256, 256, 2, 4, 1, AKC, BKC, EPI_OWN, F16, PAIRED, true>(lds, A, B, nullptr, nullptr, nullptr, nullptr, M, N, K, LDA, LDB, EPI_OWN, 0, 0,  \
                                                                               R.tiles_m, R.tiles_n, R.group_m, ID, nullptr, XCD, 0, Ahead{nullptr, 0}, BAND, END); \
         else                                                                                                                                                   \
             gemm_ring_tile<128, 128, 2, 2, 2, AKC, BKC, EPI_OWN, F16, PAIRED>(lds, A, B, nullptr, nullptr, nullptr, nullptr, M, N, K, LDA, LDB, EPI_OWN, 0, 0,  \
@@ -348,7 +377,7 @@ __global__ __launch_bounds__(512, 2) void xent_pass_kernel(Pass p) {
     } while (0)
     if (id < p.first[1]) {
         const ColumnsEnd end{p.dw + p.now.v0, p.shift, p.hidden, p.now.cols, p.lddw, p.dw_flags, p.now.ld};
-        XENT_TILE(DW, false, false, true, true, (const bf16_t*)p.rows, (const bf16_t*)p.now.dz, p.hidden, p.now.ld, 2 * p.mp, p.hidden, 2 * p.now.ld, p.dw_r, id,
+        XENT_TILE(DW, true, false, true, true, (const bf16_t*)p.rows, (const bf16_t*)p.now.dz, p.hidden, p.now.ld, 2 * p.mp, p.mp, 2 * p.now.ld, p.dw_r, id,
                   p.dw_r.band, true, end);
     } else if (id < p.first[2]) {
         const int at = id - p.first[1], tiles = p.dh_r.tiles_m * p.dh_r.tiles_n, total = p.first[2] - p.first[1];
@@ -363,7 +392,7 @@ __global__ __launch_bounds__(512, 2) void xent_pass_kernel(Pass p) {
     } else if (id < p.first[4]) {
         for (int i = (id - p.first[3]) * W_ROWS_PER_WG; i < min((id - p.first[3] + 1) * W_ROWS_PER_WG, p.hidden); ++i) raise_row(p, i, lds);
     } else {
-        shift_rows(p, (id - p.first[4]) * p.rows_per_wg, lds, id == p.first[4]);
+        turn_rows(p, id - p.first[4], (int)gridDim.x - p.first[4], lds);
     }
 #undef XENT_TILE
 }
@@ -549,7 +578,7 @@ BwdLayout bwd_layout(int dtype, int m, int hidden, int vocab, int piece) {
     } else {
         l.mp = round_up(m, TOKEN_PAD);
         l.plan = plan_of(l.mp, hidden, l.ld);
-        l.ldp = round_up(l.ld, 64) + 64;              // rows of W a power of two apart would meet in few memory channels
+        l.ldp = l.ld;
         l.buffers = l.piece < vocab ? 2 : 1;
         l.room = take((size_t)m * 4);
         l.shift = take(4);
@@ -681,7 +710,6 @@ int xent_bwd_bf16(int m, int hidden, int vocab, const bf16_t* h, int ldh, const 
     p.h = h; p.w = w; p.targets = targets; p.lse = lse; p.dloss = dloss; p.scale = scale;
     p.m = m; p.mp = l.mp; p.hidden = hidden; p.vocab = vocab; p.ldh = ldh; p.ldw = ldw; p.ldp = l.ldp;
     p.room = (int*)(ws + l.room); p.shift = (int*)(ws + l.shift); p.rows = (_Float16*)(ws + l.rows);
-    p.rows_per_wg = std::max(32, l.mp / 1024);               // every workgroup looks for the shift by itself
     p.dw = dw; p.lddw = lddw; p.dw_flags = overwrite ? ACCUM_OVERWRITE : 0;
     p.slabs = (float*)(ws + l.slabs); p.k_per = l.plan.k_per;
     if (dw) {
@@ -719,7 +747,7 @@ int xent_bwd_bf16(int m, int hidden, int vocab, const bf16_t* h, int ldh, const 
             p.dz_r = raster(l.plan.tok_tile, l.mp, p.next.ld, hidden, true);
             count[2] = p.dz_r.tiles_m * p.dz_r.tiles_n;
             if (dh) count[3] = (hidden + W_ROWS_PER_WG - 1) / W_ROWS_PER_WG;
-            if (dw && i == 0) count[4] = (l.mp + p.rows_per_wg - 1) / p.rows_per_wg;
+            if (dw && i == 0) count[4] = (int)std::min<long>((long)((l.mp + TURN_TOKENS - 1) / TURN_TOKENS) * ((hidden + TURN_COLS - 1) / TURN_COLS), TURN_WGS);
         }
         int total = 0;
         for (int k = 0; k < 5; ++k) { p.first[k] = total; total += count[k]; }
