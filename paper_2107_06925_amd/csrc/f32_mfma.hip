@@ -866,6 +866,31 @@ int gemm_f32(const GemmArgs& g, void* stream) {
     return g.b_kc ? launch_epi<true, true>(L, form, s) : launch_epi<true, false>(L, form, s);
 }
 
+int gemm_f32_splits(int m, int n, int k) {
+    const long t64 = (long)((m + 63) / 64) * ((n + 63) / 64);
+    int s = 1;
+    while (s < MAX_PRODUCTS && t64 * s < NUM_CUS && k / (s + 1) >= 512) ++s;
+    return s;
+}
+int gemm_f32_split(const GemmArgs& g, int splits, size_t slab, void* stream) {
+    if (!g.a_kc || !g.b_kc || !gemm_f32_supports(g) || (g.epilogue != EPI_NONE && g.epilogue != EPI_ACCUM_F32) || splits < 1 || splits > MAX_PRODUCTS)
+        return fail(CHIMERA_EINVAL, "float split product: k-contiguous operands and a plain or added result");
+    if (splits == 1) return gemm_f32(g, stream);
+    F32Launch L{};
+    L.count = splits; L.epi = g.epilogue;
+    GemmArgs part[MAX_PRODUCTS];
+    const int per = (g.k / splits + 7) / 8 * 8;
+    for (int i = 0; i < splits; ++i) {
+        part[i] = g;
+        part[i].a = (const float*)g.a + (size_t)i * per; part[i].b = (const float*)g.b + (size_t)i * per;
+        part[i].c = (float*)g.c + i * slab;
+        part[i].k = std::min(per, g.k - i * per);
+        if (part[i].k < 4) return fail(CHIMERA_EINVAL, "float split product: k=%d is too short for %d parts", g.k, splits);
+        L.p[i] = product_of(part[i]);
+    }
+    return launch_epi<true, true>(L, choose_form(splits, part), (hipStream_t)stream);
+}
+
 bool gemm_f32_group_supports(int count, const GemmArgs* g) {
     if (count < 1 || count > MAX_PRODUCTS) return false;
     for (int i = 0; i < count; ++i)

@@ -46,7 +46,7 @@ __device__ __forceinline__ float2 join(float2 a, float2 b) {
 // a wavefront's 64 columns are 16 numbers and a fold over four lanes; the wavefronts of a tile row join theirs in LDS.
 template <int BM, int BN> struct StatsEnd {
     const int* targets;
-    float2* stats;               // [tile column][token]
+    float2* stats;               // [tile column][token], from this launch's first on
     float* at_target;            // [token]
     int m, vocab;
     __device__ __forceinline__ void begin(int, int) {}
@@ -95,32 +95,73 @@ template <int BM, int BN> struct StatsEnd {
     }
 };
 
-template <int BM, int BN, int WGM, int WGN, int WGK>
-__global__ __launch_bounds__(WGM* WGN * WGK * 64, 2) void xent_stats_kernel(
-    const bf16_t* __restrict__ h, const bf16_t* __restrict__ w, const int* __restrict__ targets, float2* __restrict__ stats,
-    float* __restrict__ at_target, int m, int vocab, int k, int ldh, int ldw, int tiles_m, int tiles_n, int group_m, int band) {
-    __shared__ __attribute__((aligned(1024))) char lds[RingLds<BM, BN, WGM, WGN, WGK>::BYTES];
-    gemm_ring_tile<BM, BN, WGM, WGN, WGK, true, false, EPI_OWN>(lds, h, w, nullptr, nullptr, nullptr, nullptr, m, (vocab + 7) & ~7, k, ldh, ldw, EPI_OWN, 0, 0,
-                                                                tiles_m, tiles_n, group_m, (int)blockIdx.x, nullptr, true, 0, Ahead{nullptr, 0}, band,
-                                                                StatsEnd<BM, BN>{targets, stats, at_target, m, vocab});
+// Columns [0, wide) on 256x256 tiles, a whole number of rounds of them, and what is left on 128x128 tiles, begun first: a last round of a few large tiles
+// costs as much as a full one.
+struct StatsPass {
+    const bf16_t *h, *w;
+    const int* targets;
+    float2* stats;
+    float* at_target;
+    int m, vocab, k, ldh, ldw, wide;
+    int small;                   // workgroups of 128x128 tiles
+    struct Raster { int tiles_m, tiles_n, group_m, band; } r256, r128;
+};
+__global__ __launch_bounds__(512, 2) void xent_stats_kernel(StatsPass p) {
+    __shared__ __attribute__((aligned(1024))) char lds[RingLds<256, 256, 2, 4, 1>::BYTES];
+    static_assert(sizeof lds >= RingLds<128, 128, 2, 2, 2>::BYTES, "the larger of the two");
+    const int n = (p.vocab + 7) & ~7, id = blockIdx.x;
+    if (id < p.small)
+        gemm_ring_tile<128, 128, 2, 2, 2, true, false, EPI_OWN>(lds, p.h, p.w, nullptr, nullptr, nullptr, nullptr, p.m, n, p.k, p.ldh, p.ldw, EPI_OWN, 0, 0, p.r128.tiles_m,
+                                                                p.r128.tiles_n, p.r128.group_m, id, nullptr, true, p.wide, Ahead{nullptr, 0}, p.r128.band,
+                                                                StatsEnd<128, 128>{p.targets, p.stats + (size_t)(p.wide / 256) * p.m, p.at_target, p.m, p.vocab});
+    else
+        gemm_ring_tile<256, 256, 2, 4, 1, true, false, EPI_OWN, false, false, true>(lds, p.h, p.w, nullptr, nullptr, nullptr, nullptr, p.m, n, p.k, p.ldh, p.ldw, EPI_OWN, 0,
+                                                                                    0, p.r256.tiles_m, p.r256.tiles_n, p.r256.group_m, id - p.small, nullptr, true, 0,
+                                                                                    Ahead{nullptr, 0}, p.r256.band,
+                                                                                    StatsEnd<256, 256>{p.targets, p.stats, p.at_target, p.m, p.vocab});
 }
 
-// The pairs of a row, joined: 16 rows a workgroup, 16 lanes each, which take every sixteenth pair and join theirs in order.
-__global__ __launch_bounds__(256) void xent_join_kernel(const float2* __restrict__ stats, const float* __restrict__ at_target, const int* __restrict__ targets,
-                                                        int m, int vocab, int parts, float scale, float* __restrict__ loss_rows, float* __restrict__ lse) {
-    __shared__ float2 tab[16][16];
-    const int r = threadIdx.x & 15, q = threadIdx.x >> 4, row = blockIdx.x * 16 + r;
-    float2 s = make_float2(LOWEST, 0.f);
-    if (row < m)
-        for (int p = q; p < parts; p += 16) s = join(s, stats[(size_t)p * m + row]);
-    tab[q][r] = s;
-    __syncthreads();
-    if (q || row >= m) return;
+// The pairs of a row, joined by 16 lanes, which take every sixteenth pair and join theirs in order; then the loss.  Up to JOIN_ALONE tokens one
+// workgroup of 64 rows at a time does it all, beyond, workgroups of 16 rows leave the sum to a launch of its own (fixed order either way).
+constexpr int JOIN_ALONE = 256;
+template <int ROWS>
+__global__ __launch_bounds__(16 * ROWS) void xent_join_kernel(const float2* __restrict__ stats, const float* __restrict__ at_target, const int* __restrict__ targets,
+                                                              int m, int vocab, int parts, float scale, float* __restrict__ loss_rows, float* __restrict__ lse,
+                                                              float* __restrict__ loss) {
+    __shared__ float2 tab[16][ROWS];
+    const int r = threadIdx.x % ROWS, q = threadIdx.x / ROWS;
+    float sum = 0.f;
+    for (int r0 = blockIdx.x * ROWS; r0 < m; r0 += gridDim.x * ROWS) {
+        const int row = r0 + r;
+        float2 s = make_float2(LOWEST, 0.f);
+        if (row < m) {
+            int p = q;
+            for (; p + 48 < parts; p += 64) {
+                float2 u[4];
 #pragma unroll
-    for (int i = 1; i < 16; ++i) s = join(s, tab[i][r]);
-    const float l = s.x + logf(s.y);
-    lse[row] = l;
-    loss_rows[row] = counts(targets[row], vocab) ? scale * (l - at_target[row]) : 0.f;
+                for (int i = 0; i < 4; ++i) u[i] = stats[(size_t)(p + 16 * i) * m + row];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s = join(s, u[i]);
+            }
+            for (; p < parts; p += 16) s = join(s, stats[(size_t)p * m + row]);
+        }
+        tab[q][r] = s;
+        __syncthreads();
+        if (!q && row < m) {
+#pragma unroll
+            for (int i = 1; i < 16; ++i) s = join(s, tab[i][r]);
+            const float l = s.x + logf(s.y), own = counts(targets[row], vocab) ? scale * (l - at_target[row]) : 0.f;
+            lse[row] = l;
+            loss_rows[row] = own;
+            sum += own;
+        }
+        __syncthreads();
+    }
+    if constexpr (ROWS == WAVE) {                // (the first wavefront holds the rows' sums)
+        if (!loss || q) return;
+        sum = wave_sum(sum);
+        if (threadIdx.x == 0) loss[0] += sum;
+    }
 }
 
 // ---- backward
@@ -227,12 +268,14 @@ struct SlabEnd {
 struct RowInfo { float lse, scaled; int at; };              // coef 2^lift (0: the token does not count), the target's column in the piece
 template <int BM> struct GradEnd {
     const Pass* p;
-    RowInfo mine;
-    __device__ __forceinline__ void begin(int i0, int tid) {
-        // (no branches: the compiler keeps the tile's operand addresses in scalar registers only outside of divergent code)
+    float lse, weight;
+    int target;
+    __device__ __forceinline__ void begin(int i0, int tid) {                     // requests only: their values are looked at behind the k loop
         const int t = min(i0 + tid, p->m - 1);
-        const float coef = coef_of(p->targets, p->dloss, p->scale, i0 + tid, p->m, p->vocab);
-        mine = {p->lse[t], ldexpf(coef, lift_of(coef)), coef != 0.f ? p->targets[t] - p->next.v0 : -1};
+        lse = p->lse[t];
+        target = p->targets[t];
+        weight = 1.0f;
+        if (p->dloss) weight = p->dloss[t];
     }
     template <int TO, int TN2, typename Acc>
     __device__ __forceinline__ void end(const Acc& out, char* lds, int i0, int rb0, int cb0, int, int wave, int lane) const {
@@ -240,7 +283,10 @@ template <int BM> struct GradEnd {
         RowInfo* tab = reinterpret_cast<RowInfo*>(lds + 8 * EpiSlab<TN2>::FLOATS * sizeof(float));
         float* slab = reinterpret_cast<float*>(lds) + (size_t)wave * EpiSlab<TN2>::FLOATS;
         const int tid = threadIdx.x, cols = p->next.cols, ld = p->next.ld, mp = p->mp;
-        if (tid < BM) tab[tid] = mine;
+        if (tid < BM) {
+            const float coef = i0 + tid < p->m && counts(target, p->vocab) ? p->scale * weight : 0.f;
+            tab[tid] = {lse, ldexpf(coef, lift_of(coef)), coef != 0.f ? target - p->next.v0 : -1};
+        }
         __syncthreads();
         const int pr = lane / CPR, pc = lane % CPR * 8, col = cb0 + pc;
         _Float16* const first = p->next.dz + (size_t)(rb0 + pr) * 2 * ld + col;
@@ -388,7 +434,7 @@ __global__ __launch_bounds__(512, 2) void xent_pass_kernel(Pass p) {
                   p.ldp, p.dh_r, pid - split * tiles, 0, false, end);
     } else if (id < p.first[3]) {
         XENT_TILE(TOK, true, false, false, false, p.h, p.w + p.next.v0, p.m, p.next.ld, p.hidden, p.ldh, p.ldw, p.dz_r, id - p.first[2], p.dz_r.band, true,
-                  (GradEnd<TOK>{&p, {}}));
+                  (GradEnd<TOK>{&p, 0.f, 0.f, 0}));
     } else if (id < p.first[4]) {
         for (int i = (id - p.first[3]) * W_ROWS_PER_WG; i < min((id - p.first[3] + 1) * W_ROWS_PER_WG, p.hidden); ++i) raise_row(p, i, lds);
     } else {
@@ -516,8 +562,15 @@ size_t aligned(size_t b) { return (b + 255) / 256 * 256; }
 int round_up(int v, int a) { return (v + a - 1) / a * a; }
 long tiles_of(int m, int n, int tile) { return (long)((m + tile - 1) / tile) * ((n + tile - 1) / tile); }
 
-// 256x256 tiles where they fill most of the chip, else 128x128 (as for the stages' products).
-int z_tile(int m, int n) { return tiles_of(m, n, 256) >= 144 ? 256 : 128; }
+// Columns of the forward's product on 256x256 tiles: whole rounds of them, and the rest too where it fills most of one (the rest on 128x128 tiles takes
+// 0.38 of a round's time for up to 64 of the large).  A small product has none.
+int wide_columns(int m, int n) {
+    const int tm = (m + 255) / 256, tn = (n + 255) / 256;
+    const long tiles = (long)tm * tn, over = tiles % NUM_CUS;
+    if (tiles < 144) return 0;
+    if (over >= 144 || over == 0) return tn * 256;
+    return (int)((tiles - over) / tm) * 256;
+}
 
 // Columns of the vocabulary per piece where the caller leaves it open: 8192, more where their buffers stay small, fewer where they get large.
 constexpr size_t PIECE_BYTES_MIN = (size_t)128 << 20, PIECE_BYTES_MAX = (size_t)512 << 20;
@@ -548,21 +601,21 @@ PassPlan plan_of(int mp, int hidden, int ld) {
     return p;
 }
 
-struct FwdLayout { int tile, parts; size_t stats, at_target, z, total; int piece; };
+struct FwdLayout { int wide, parts; size_t stats, at_target, z, total; int piece; };
 FwdLayout fwd_layout(int dtype, int m, int hidden, int vocab) {
     FwdLayout l{};
     size_t b = 0;
     auto take = [&](size_t bytes) { size_t r = b; b += aligned(bytes); return r; };
-    l.tile = z_tile(m, vocab);
+    l.wide = wide_columns(m, vocab);
     l.piece = default_piece(dtype, m, hidden, vocab);
-    l.parts = dtype == CHIMERA_F32 ? (vocab + l.piece - 1) / l.piece : (vocab + l.tile - 1) / l.tile;
+    l.parts = dtype == CHIMERA_F32 ? (vocab + l.piece - 1) / l.piece : l.wide / 256 + std::max(0, vocab - l.wide + 127) / 128;
     l.stats = take((size_t)l.parts * m * sizeof(float2));
     l.at_target = take((size_t)m * 4);
     l.z = take(dtype == CHIMERA_F32 ? (size_t)m * std::min(l.piece, round_up(vocab, 8)) * 4 : 0);
     l.total = b;
     return l;
 }
-struct BwdLayout { int piece, ld, mp, ldp, buffers; PassPlan plan; size_t room, shift, rows, dz[2], w[2], raise[2], slabs, columns, total; };
+struct BwdLayout { int piece, ld, mp, ldp, buffers, f32_splits; PassPlan plan; size_t room, shift, rows, dz[2], w[2], raise[2], slabs, columns, total; };
 BwdLayout bwd_layout(int dtype, int m, int hidden, int vocab, int piece) {
     BwdLayout l{};
     size_t b = 0;
@@ -573,7 +626,8 @@ BwdLayout bwd_layout(int dtype, int m, int hidden, int vocab, int piece) {
         l.mp = m;
         l.rows = take((size_t)m * hidden * 4);
         l.dz[0] = take((size_t)m * l.ld * 4);
-        l.slabs = take((size_t)m * hidden * 4);
+        l.f32_splits = gemm_f32_splits(m, hidden, l.ld & ~7);
+        l.slabs = take((size_t)l.f32_splits * m * hidden * 4);
         l.columns = take((size_t)hidden * l.ld * 4);
     } else {
         l.mp = round_up(m, TOKEN_PAD);
@@ -625,21 +679,21 @@ int check_xent(int dtype, int tokens, int hidden, int vocab, int ldh, int ldw) {
     return CHIMERA_OK;
 }
 
-template <int BM, int WGM, int WGN, int WGK, typename F>
-int with_raster(int m, int n, int k, F&& launch) {
-    const int tm = (m + BM - 1) / BM, tn = (n + BM - 1) / BM;
-    constexpr int PER_CU = RingLds<BM, BM, WGM, WGN, WGK>::PER_CU;
-    const int band = raster_band(tm, tn, NUM_CUS * PER_CU, (size_t)n * k * 2);
-    const int gm = raster_group(tm, band ? band : tn, std::min((tm * tn + 7) / 8, PER_XCD * PER_CU), BM, BM);
-    launch(tm, tn, gm, band);
+template <typename R> R raster_of(int tile, int rows, int cols, int k, bool bands = true) {
+    R r{(rows + tile - 1) / tile, (cols + tile - 1) / tile, 1, 0};
+    if (bands) r.band = raster_band(r.tiles_m, r.tiles_n, NUM_CUS, (size_t)cols * k * 2);
+    r.group_m = raster_group(r.tiles_m, r.band ? r.band : r.tiles_n, std::min((r.tiles_m * r.tiles_n + 7) / 8, PER_XCD), tile, tile);
+    return r;
+}
+
+int xent_fwd_bf16(int m, int hidden, int vocab, const bf16_t* h, int ldh, const bf16_t* w, int ldw, const int* targets, const FwdLayout& l, char* ws, hipStream_t s) {
+    StatsPass p{h, w, targets, (float2*)(ws + l.stats), (float*)(ws + l.at_target), m, vocab, hidden, ldh, ldw, l.wide, 0, {}, {}};
+    int large = 0;
+    if (l.wide) { p.r256 = raster_of<StatsPass::Raster>(256, m, std::min(l.wide, vocab), hidden); large = p.r256.tiles_m * p.r256.tiles_n; }
+    if (l.wide < vocab) { p.r128 = raster_of<StatsPass::Raster>(128, m, vocab - l.wide, hidden); p.small = p.r128.tiles_m * p.r128.tiles_n; }
+    hipLaunchKernelGGL(xent_stats_kernel, dim3(p.small + large), dim3(512), 0, s, p);
     CHIMERA_LAUNCH_CHECK("linear cross-entropy");
     return CHIMERA_OK;
-}
-// The launches of a product m x n on one of the three forms of tiles: f.operator()<BM, WGM, WGN, WGK>()
-template <typename F> int with_tile(int m, int n, F&& f) {
-    if (z_tile(m, n) == 256) return f.template operator()<256, 2, 4, 1>();
-    if (tiles_of(m, n, 128) <= NUM_CUS) return f.template operator()<128, 2, 2, 2>();
-    return f.template operator()<128, 2, 2, 1>();
 }
 
 template <typename T>
@@ -685,8 +739,10 @@ int xent_bwd_f32(int m, int hidden, int vocab, const float* h, int ldh, const fl
             GemmArgs d{};
             d.m = m; d.n = hidden; d.k = whole; d.a = z; d.lda = ld; d.a_kc = 1; d.b = w + v0; d.ldb = ldw; d.b_kc = 1; d.c = slab;
             d.epilogue = slabs ? EPI_ACCUM_F32 : EPI_NONE;
-            XENT_TRY(gemm_f32(d, stream));
-            slabs = 1;
+            // (a last piece that is too short to be cut goes into the first slab)
+            const int now = slabs && whole / l.f32_splits < 64 ? 1 : l.f32_splits;
+            XENT_TRY(gemm_f32_split(d, now, (size_t)m * hidden, stream));
+            if (!slabs) slabs = now;
         }
         if (dw) {
             GemmArgs q{};
@@ -716,12 +772,6 @@ int xent_bwd_bf16(int m, int hidden, int vocab, const bf16_t* h, int ldh, const 
         hipLaunchKernelGGL(xent_room_kernel, dim3((m + 3) / 4), dim3(ROW_THREADS), 0, s, h, ldh, targets, dloss, scale, m, hidden, vocab, p.room);
         CHIMERA_LAUNCH_CHECK("linear cross-entropy");
     }
-    auto raster = [](int tile, int rows, int cols, int k, bool bands) {
-        Pass::Raster r{(rows + tile - 1) / tile, (cols + tile - 1) / tile, 1, 0};
-        if (bands) r.band = raster_band(r.tiles_m, r.tiles_n, NUM_CUS, (size_t)cols * k * 2);
-        r.group_m = raster_group(r.tiles_m, r.band ? r.band : r.tiles_n, std::min((r.tiles_m * r.tiles_n + 7) / 8, PER_XCD), tile, tile);
-        return r;
-    };
     const int pieces = (vocab + l.piece - 1) / l.piece;
     int splits = 0;
     for (int i = 0; i <= pieces; ++i) {
@@ -729,13 +779,13 @@ int xent_bwd_bf16(int m, int hidden, int vocab, const bf16_t* h, int ldh, const 
         int count[5] = {};
         if (i > 0) {
             if (dw) {
-                p.dw_r = raster(l.plan.dw_tile, hidden, p.now.ld, 2 * l.mp, true);
+                p.dw_r = raster_of<Pass::Raster>(l.plan.dw_tile, hidden, p.now.ld, 2 * l.mp);
                 count[0] = p.dw_r.tiles_m * p.dw_r.tiles_n;
             }
             if (dh) {
                 // the last piece is cut where the others are: a split that it does not reach adds nothing
                 const int now = (p.now.ld + l.plan.k_per - 1) / l.plan.k_per;
-                p.dh_r = raster(l.plan.tok_tile, m, hidden, 0, false);
+                p.dh_r = raster_of<Pass::Raster>(l.plan.tok_tile, m, hidden, 0, false);
                 count[1] = p.dh_r.tiles_m * p.dh_r.tiles_n * now;
                 p.dh_flags = i == 1 ? ACCUM_OVERWRITE : 0;
                 if (i == 1) splits = now;
@@ -744,7 +794,7 @@ int xent_bwd_bf16(int m, int hidden, int vocab, const bf16_t* h, int ldh, const 
         if (i < pieces) {
             const int v0 = i * l.piece, cols = std::min(l.piece, vocab - v0), at = i & (l.buffers - 1);
             p.next = {v0, cols, round_up(cols, 8), (_Float16*)(ws + l.dz[at]), (_Float16*)(ws + l.w[at]), (int*)(ws + l.raise[at])};
-            p.dz_r = raster(l.plan.tok_tile, l.mp, p.next.ld, hidden, true);
+            p.dz_r = raster_of<Pass::Raster>(l.plan.tok_tile, l.mp, p.next.ld, hidden);
             count[2] = p.dz_r.tiles_m * p.dz_r.tiles_n;
             if (dh) count[3] = (hidden + W_ROWS_PER_WG - 1) / W_ROWS_PER_WG;
             if (dw && i == 0) count[4] = (int)std::min<long>((long)((l.mp + TURN_TOKENS - 1) / TURN_TOKENS) * ((hidden + TURN_COLS - 1) / TURN_COLS), TURN_WGS);
@@ -789,13 +839,14 @@ int chimera_op_linear_xent_fwd(int dtype, int tokens, int hidden, int vocab, con
     if (dtype == CHIMERA_F32)
         XENT_TRY(xent_fwd_f32(tokens, hidden, vocab, (const float*)d_h, ldh, (const float*)d_w, ldw, d_targets, l, ws, hip_stream));
     else
-        XENT_TRY(with_tile(tokens, vocab, [&]<int BM, int WGM, int WGN, int WGK>() {
-            return with_raster<BM, WGM, WGN, WGK>(tokens, vocab, hidden, [&](int tm, int tn, int gm, int band) {
-                hipLaunchKernelGGL((xent_stats_kernel<BM, BM, WGM, WGN, WGK>), dim3(tm * tn), dim3(WGM * WGN * WGK * 64), 0, s, (const bf16_t*)d_h,
-                                   (const bf16_t*)d_w, d_targets, stats, at_target, tokens, vocab, hidden, ldh, ldw, tm, tn, gm, band);
-            });
-        }));
-    hipLaunchKernelGGL(xent_join_kernel, dim3((tokens + 15) / 16), dim3(256), 0, s, stats, at_target, d_targets, tokens, vocab, l.parts, scale, d_loss_rows, d_lse);
+        XENT_TRY(xent_fwd_bf16(tokens, hidden, vocab, (const bf16_t*)d_h, ldh, (const bf16_t*)d_w, ldw, d_targets, l, ws, s));
+    if (tokens <= JOIN_ALONE) {
+        hipLaunchKernelGGL(xent_join_kernel<WAVE>, dim3(1), dim3(16 * WAVE), 0, s, stats, at_target, d_targets, tokens, vocab, l.parts, scale, d_loss_rows, d_lse, d_loss);
+        CHIMERA_LAUNCH_CHECK("linear cross-entropy");
+        return CHIMERA_OK;
+    }
+    hipLaunchKernelGGL(xent_join_kernel<16>, dim3((tokens + 15) / 16), dim3(256), 0, s, stats, at_target, d_targets, tokens, vocab, l.parts, scale, d_loss_rows, d_lse,
+                       nullptr);
     CHIMERA_LAUNCH_CHECK("linear cross-entropy");
     return d_loss ? loss_sum(d_loss_rows, tokens, d_loss, hip_stream) : CHIMERA_OK;
 }
