@@ -97,7 +97,7 @@ _SIGNATURES = {
     "chimera_op_linear_xent_bwd": (_i, [_i] * 4 + [_p, _i, _p, _i, _p, _p, C.c_float, _p, _p, _i, _p, _i, _i, _i, _p, _sz, _p]),
     "chimera_head_pieces_workspace_bytes": (_sz, [_i] * 5),
     "chimera_head_loss_pieces": (_i, [_i] * 4 + [_p] * 5 + [_i, C.c_float] + [_p] * 5 + [_i, _p, _sz, _p]),
-    "chimera_op_grad_norm_workspace_bytes": (_sz, [_i, _p]),
+    "chimera_op_grad_norm_workspace_bytes": (_sz, [_i]),
     "chimera_op_grad_norm": (_i, [_i, _p, _p, C.c_float, _p, _p, _sz, _p]),
     "chimera_op_adamw": (_i, [_i, _i, _i] + [_p] * 11),
     "chimera_stage_adamw_state_bytes": (_sz, [_p, _i]),
@@ -591,7 +591,7 @@ def chimera_op_grad_norm(grads, max_norm, out, workspace=None):
     import torch
     n = _counts(grads)
     if workspace is None:
-        workspace = torch.empty(lib().chimera_op_grad_norm_workspace_bytes(len(grads), n), dtype=torch.uint8, device=out.device)
+        workspace = torch.empty(lib().chimera_op_grad_norm_workspace_bytes(len(grads)), dtype=torch.uint8, device=out.device)
     check(lib().chimera_op_grad_norm(len(grads), n, _pointers(grads), max_norm, _ptr(out), _ptr(workspace), workspace.numel(), _stream(out)))
     return workspace
 

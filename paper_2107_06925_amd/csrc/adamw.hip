@@ -20,7 +20,7 @@
 namespace chimera {
 namespace {
 
-constexpr int STEP_THREADS = 256, STEP_CHUNK = 4096, MOMENT_BLOCK = 256;
+constexpr int STEP_THREADS = 256, MOMENT_BLOCK = 256;
 static_assert(MOMENT_BLOCK == 4 * WAVE, "a wavefront holds one block of moments, four values a lane");
 constexpr float CODE_TOP = 448.0f, CODE_LEAST = 1e-30f;      // largest e4m3 number; blocks whose largest value is below this hold zeros
 
@@ -58,6 +58,7 @@ struct StepLaunch {
     StepTensor t[STEP_TENSORS];
     int first[STEP_TENSORS];     // a tensor's first chunk (INT_MAX behind the last tensor)
     Scalars s;
+    int chunk;                   // values per workgroup
     const DeviceHyper* device;   // null: s
     const float* factor;
 };
@@ -100,7 +101,7 @@ __global__ __launch_bounds__(STEP_THREADS) void adamw_kernel(StepLaunch L) {
     const Scalars s = L.device ? L.device->derived : L.s;
     const int k = tensor_of(L.first, (int)blockIdx.x);
     const StepTensor& t = L.t[k];
-    const long long n = t.n, begin = (long long)((int)blockIdx.x - L.first[k]) * STEP_CHUNK, end = min(begin + STEP_CHUNK, n);
+    const long long n = t.n, begin = (long long)((int)blockIdx.x - L.first[k]) * L.chunk, end = min(begin + L.chunk, n);
     const float keep = 1.0f - t.decay * s.lr;
     T* __restrict__ const param = (T*)t.p;
     float* __restrict__ const weight = sizeof(T) == 4 ? (float*)t.p : t.master;
@@ -257,19 +258,17 @@ __global__ __launch_bounds__(1024) void grad_norm_kernel(const double* __restric
     out[1] = !(norm <= 3.4028235e38) ? __builtin_nanf("") : norm > max_norm ? (float)(max_norm / norm) : 1.0f;
 }
 
-// Values per workgroup: some eight workgroups a CU, pieces of 4096 to 65536.
-struct NormPlan { long long chunk, chunks; };
-bool norm_plan(int count, const int64_t* h_n, NormPlan& p) {
+// Values per workgroup: eight workgroups a CU, pieces of at least 4096
+constexpr long long NORM_CHUNKS = 2048;
+bool norm_chunk(int count, const int64_t* h_n, long long& chunk) {
     long long total = 0;
     for (int i = 0; i < count; ++i) {
-        if (h_n[i] < 0 || h_n[i] > 1ll << 40) return false;
-        total += h_n[i];
+        if (h_n[i] < 0 || h_n[i] > 1ll << 40 || (total += h_n[i]) > 1ll << 40) return false;
     }
-    p.chunk = std::clamp((total / 2048 + 4095) / 4096 * 4096, 4096ll, 65536ll);
-    p.chunks = 0;
-    for (int i = 0; i < count; ++i) p.chunks += (h_n[i] + p.chunk - 1) / p.chunk;
-    return p.chunks < 1 << 22;
+    chunk = std::max((total / NORM_CHUNKS + 1023) / 1024 * 1024, 4096ll);
+    return true;
 }
+size_t norm_bytes(int count) { return ((size_t)NORM_CHUNKS + count) * sizeof(double); }
 
 int check_hyper(const chimera_adamw_hyper& h) {
     if (!(h.lr >= 0) || !std::isfinite(h.lr)) return fail(CHIMERA_EINVAL, "lr must be finite and not negative");
@@ -292,16 +291,20 @@ int adamw_step(int dtype, int bits, int count, const AdamwTensor* t, const chime
     } else {
         L.s = scalars_of(*h_hyper);
     }
-    long long block = 0;
+    // A workgroup that goes round takes a trip to memory each time; small steps are as long as one of them
+    long long total = 0, block = 0;
+    for (int i = 0; i < count; ++i) total += t[i].n;
+    L.chunk = total <= 4 << 20 ? 1024 : 4096;
+    auto chunks_of = [&](int i) { return (t[i].n + L.chunk - 1) / L.chunk; };
     for (int i = 0; i < count;) {
         std::fill(std::begin(L.first), std::end(L.first), INT_MAX);
         long long chunks = 0;
         int used = 0;
-        for (; i < count && used < STEP_TENSORS && chunks + (t[i].n + STEP_CHUNK - 1) / STEP_CHUNK < 1 << 23; ++i) {
+        for (; i < count && used < STEP_TENSORS && chunks + chunks_of(i) < 1 << 23; ++i) {
             if (!t[i].n) continue;
             L.t[used] = {t[i].p, t[i].m, t[i].v, t[i].master, t[i].scale, t[i].g, (long long)t[i].n, block, t[i].decay};
             L.first[used++] = (int)chunks;
-            chunks += (t[i].n + STEP_CHUNK - 1) / STEP_CHUNK;
+            chunks += chunks_of(i);
             block += (t[i].n + MOMENT_BLOCK - 1) / MOMENT_BLOCK;
         }
         if (!used) continue;
@@ -331,10 +334,7 @@ using namespace chimera;
 
 extern "C" {
 
-size_t chimera_op_grad_norm_workspace_bytes(int count, const int64_t* h_n) {
-    NormPlan p;
-    return count < 1 || !h_n || !norm_plan(count, h_n, p) ? 0 : (size_t)std::max(p.chunks, 1ll) * sizeof(double);
-}
+size_t chimera_op_grad_norm_workspace_bytes(int count) { return count < 1 ? 0 : norm_bytes(count); }
 
 int chimera_op_grad_norm(int count, const int64_t* h_n, const float* const* h_grad, float max_norm, float* d_out, void* d_workspace, size_t workspace_bytes,
                          void* hip_stream) {
@@ -342,15 +342,14 @@ int chimera_op_grad_norm(int count, const int64_t* h_n, const float* const* h_gr
     if (!d_out || !d_workspace) return fail(CHIMERA_EINVAL, "NULL operand");
     if (!(max_norm > 0)) return fail(CHIMERA_EINVAL, "max_norm must be positive");
     if (((uintptr_t)d_workspace & 7) || ((uintptr_t)d_out & 3)) return fail(CHIMERA_EINVAL, "workspace must be 8-byte aligned, the result 4-byte aligned");
-    NormPlan p;
-    if (!norm_plan(count, h_n, p)) return fail(CHIMERA_EINVAL, "a tensor's size is negative, or the tensors are too large");
+    long long chunk;
+    if (!norm_chunk(count, h_n, chunk)) return fail(CHIMERA_EINVAL, "a tensor's size is negative, or the tensors are too large");
     for (int i = 0; i < count; ++i)
         if (h_n[i] && (!h_grad[i] || ((uintptr_t)h_grad[i] & 3))) return fail(CHIMERA_EINVAL, "gradient %d is NULL or not aligned to floats", i);
-    const size_t need = (size_t)std::max(p.chunks, 1ll) * sizeof(double);
-    if (workspace_bytes < need) return fail(CHIMERA_ENOMEM, "workspace holds %zu bytes, need %zu", workspace_bytes, need);
+    if (workspace_bytes < norm_bytes(count)) return fail(CHIMERA_ENOMEM, "workspace holds %zu bytes, need %zu", workspace_bytes, norm_bytes(count));
     hipStream_t s = (hipStream_t)hip_stream;
     NormLaunch L{};
-    L.chunk = p.chunk;
+    L.chunk = chunk;
     long long done = 0;
     for (int i = 0; i < count;) {
         std::fill(std::begin(L.first), std::end(L.first), INT_MAX);
@@ -359,7 +358,7 @@ int chimera_op_grad_norm(int count, const int64_t* h_n, const float* const* h_gr
         for (; i < count && used < NORM_TENSORS; ++i) {
             if (!h_n[i]) continue;
             L.g[used] = h_grad[i]; L.n[used] = h_n[i]; L.first[used++] = (int)chunks;
-            chunks += (h_n[i] + p.chunk - 1) / p.chunk;
+            chunks += (h_n[i] + chunk - 1) / chunk;
         }
         if (!used) continue;
         L.partial = (double*)d_workspace + done;

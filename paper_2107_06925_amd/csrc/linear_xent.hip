@@ -567,7 +567,7 @@ long tiles_of(int m, int n, int tile) { return (long)((m + tile - 1) / tile) * (
 int wide_columns(int m, int n) {
     const int tm = (m + 255) / 256, tn = (n + 255) / 256;
     const long tiles = (long)tm * tn, over = tiles % NUM_CUS;
-    if (tiles < 144) return 0;
+    if (tiles < 144 || m <= 128) return 0;                   // (few tokens: a step of a large tile is 2048 clocks of matrix instructions whatever its rows hold)
     if (over >= 144 || over == 0) return tn * 256;
     return (int)((tiles - over) / tm) * 256;
 }
