@@ -558,7 +558,7 @@ int chimera_op_grad_norm(int count, const int64_t* h_n, const float* const* h_gr
  * sqrt(v) as multiples of a float scale for each 256 elements of a tensor; h_scale to the pairs (m's, sqrt(v)'s), ceil(n / 256) of them.  Zeros are the
  * state before the first step in either width.  Codes are rounded up or down at random, with the right mean, by a hash of seed, step and the
  * element's number in the call (tensors counted in whole blocks of 256): the same call on the same state gives the same bits.
- * Tensors are aligned to their elements.  d_hyper (may be NULL): device memory of CHIMERA_ADAMW_HYPER_BYTES bytes, 16-byte aligned, that begins with a
+ * Tensors are aligned to their elements.  lr >= 0, beta1 and beta2 in [0, 1), eps in [2^-126, 1], decay >= 0, step >= 1.  d_hyper (may be NULL): device memory of CHIMERA_ADAMW_HYPER_BYTES bytes, 16-byte aligned, that begins with a
  * chimera_adamw_hyper to be used in place of h_hyper, so that a recorded call can be replayed for further steps; its values are the caller's to
  * check, the bytes behind the struct the call's, and calls that overlap need one each. */
 typedef struct {

@@ -72,8 +72,10 @@ template <int N> __device__ __forceinline__ int tensor_of(const int (&first)[N],
     return __builtin_amdgcn_readfirstlane(__popcll(__ballot(at)) - 1);
 }
 
-__device__ __forceinline__ unsigned random_bits(unsigned long long i, unsigned key) {
-    unsigned x = (unsigned)i * 0x9E3779B1u + (unsigned)(i >> 32) * 0x6A09E667u + key;
+// of value i: mixed(start(i, key)), and i + 1 starts RANDOM_STEP later
+constexpr unsigned RANDOM_STEP = 0x9E3779B1u;
+__device__ __forceinline__ unsigned random_start(unsigned long long i, unsigned key) { return (unsigned)i * RANDOM_STEP + (unsigned)(i >> 32) * 0x6A09E667u + key; }
+__device__ __forceinline__ unsigned mixed(unsigned x) {
     x = (x ^ (x >> 15)) * 0x6A09E667u;
     x = (x ^ (x >> 13)) * 0xBB67AE85u;
     return x ^ (x >> 16);
@@ -92,7 +94,8 @@ __device__ __forceinline__ float decode(unsigned code, float scale) {
     return ((code & 0x7f) == 0x7f ? __builtin_nanf("") : code & 0x80 ? -v : v) * scale;
 }
 
-// Every operation is rounded by itself (no contraction), so that a step of the same numbers is the same everywhere, the choice of codes included.
+// Every operation on the moments is rounded by itself (no contraction), so that the choice of codes is a function of the numbers; the update's quotient takes the
+// hardware's reciprocal (1 ulp), half of a correctly rounded division's instructions: they are what the 8-bit step is short of beside memory.
 template <typename T, int BITS>
 __global__ __launch_bounds__(STEP_THREADS) void adamw_kernel(StepLaunch L) {
 #pragma clang fp contract(off)
@@ -164,7 +167,7 @@ __global__ __launch_bounds__(STEP_THREADS) void adamw_kernel(StepLaunch L) {
             m[e] = m[e] * s.b1 + x * s.w1;
             v[e] = v[e] * s.b2 + (x * x) * s.w2;
             r[e] = __fsqrt_rn(v[e]);
-            w[e] = w[e] * keep - __fdiv_rn(m[e] * s.rate, r[e] * s.root + s.eps);
+            w[e] = w[e] * keep - (m[e] * s.rate) * __builtin_amdgcn_rcpf(r[e] * s.root + s.eps);
         }
         put(weight, w);
         if constexpr (sizeof(T) == 2) {
@@ -186,10 +189,10 @@ __global__ __launch_bounds__(STEP_THREADS) void adamw_kernel(StepLaunch L) {
             tv = wave_max(tv);
             const float im = tm > CODE_LEAST ? __fdiv_rn(1.0f, tm) * CODE_TOP : 0.f, iv = tv > CODE_LEAST ? __fdiv_rn(1.0f, tv) * CODE_TOP : 0.f;
             unsigned qm = 0, qv = 0;
-            const unsigned long long number = (unsigned long long)(t.block0 * MOMENT_BLOCK + i);
+            const unsigned start = random_start((unsigned long long)(t.block0 * MOMENT_BLOCK + i), s.key);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const unsigned bits = random_bits(number + e, s.key);
+                const unsigned bits = mixed(start + e * RANDOM_STEP);
                 qm |= encode(m[e], im, bits & 0xffff, false) << (8 * e);
                 qv |= encode(r[e], iv, bits >> 16, iv > 0.f) << (8 * e);
             }
@@ -273,7 +276,7 @@ size_t norm_bytes(int count) { return ((size_t)NORM_CHUNKS + count) * sizeof(dou
 int check_hyper(const chimera_adamw_hyper& h) {
     if (!(h.lr >= 0) || !std::isfinite(h.lr)) return fail(CHIMERA_EINVAL, "lr must be finite and not negative");
     if (!(h.beta1 >= 0 && h.beta1 < 1) || !(h.beta2 >= 0 && h.beta2 < 1)) return fail(CHIMERA_EINVAL, "beta1 and beta2 must lie in [0, 1)");
-    if (!(h.eps > 0) || !std::isfinite(h.eps)) return fail(CHIMERA_EINVAL, "eps must be finite and positive");
+    if (!(h.eps >= 0x1p-126) || !(h.eps <= 1)) return fail(CHIMERA_EINVAL, "eps must lie in [2^-126, 1]");
     if (h.step < 1) return fail(CHIMERA_EINVAL, "step=%lld: the first step is 1", (long long)h.step);
     return CHIMERA_OK;
 }

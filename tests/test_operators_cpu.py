@@ -112,7 +112,7 @@ NAN, INF = float("nan"), float("inf")
                                  dict(param=(P, None, P + 30)), dict(param=(P + 1, None, 2 * P)), dict(grad=(P + 2, None, P)), dict(m=(P + 1, None, P)),
                                  dict(decay=(0.0, 0.0, -0.1)), dict(decay=(NAN, 0.0, 0.1)), dict(decay=(0.1, 0.0, INF)), dict(hyper=None), dict(device=P + 8),
                                  dict(hyper=(-1e-3, 0.9, 0.95, 1e-8, 1, 0)), dict(hyper=(NAN, 0.9, 0.95, 1e-8, 1, 0)), dict(hyper=(1e-3, 1.0, 0.95, 1e-8, 1, 0)),
-                                 dict(hyper=(1e-3, 0.9, -0.1, 1e-8, 1, 0)), dict(hyper=(1e-3, 0.9, 0.95, 0.0, 1, 0)), dict(hyper=(1e-3, 0.9, 0.95, 1e-8, 0, 0))],
+                                 dict(hyper=(1e-3, 0.9, -0.1, 1e-8, 1, 0)), dict(hyper=(1e-3, 0.9, 0.95, 0.0, 1, 0)), dict(hyper=(1e-3, 0.9, 0.95, 1e-40, 1, 0)), dict(hyper=(1e-3, 0.9, 0.95, 2.0, 1, 0)), dict(hyper=(1e-3, 0.9, 0.95, 1e-8, 0, 0))],
                          ids=str)
 def test_adamw_refuses(bad):
     assert adamw(**bad) == b.EINVAL
