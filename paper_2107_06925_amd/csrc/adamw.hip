@@ -96,7 +96,8 @@ __device__ __forceinline__ float decode(unsigned code, float scale) {
 
 // Every operation on the moments is rounded by itself (no contraction), so that the choice of codes is a function of the numbers; the update's quotient takes the
 // hardware's reciprocal (1 ulp), half of a correctly rounded division's instructions: they are what the 8-bit step is short of beside memory.
-template <typename T, int BITS>
+// ONCE: what a step touches is more than the memory-side cache holds, and passes it by.
+template <typename T, int BITS, bool ONCE>
 __global__ __launch_bounds__(STEP_THREADS) void adamw_kernel(StepLaunch L) {
 #pragma clang fp contract(off)
     const float factor = L.factor ? *L.factor : 1.0f;
@@ -115,15 +116,19 @@ __global__ __launch_bounds__(STEP_THREADS) void adamw_kernel(StepLaunch L) {
         const int have = (int)max(0ll, min(4ll, n - i));     // of this lane's four values
         f4_t g = {0.f, 0.f, 0.f, 0.f}, w = g, m = g, v = g, r;
         auto get = [&](const float* from, f4_t& to) {
-            if (have == 4) to = *reinterpret_cast<const f4_u*>(from + i);
-            else
+            if (have == 4) {
+                if constexpr (ONCE) to = __builtin_nontemporal_load(reinterpret_cast<const f4_u*>(from + i));
+                else to = *reinterpret_cast<const f4_u*>(from + i);
+            } else
 #pragma unroll
                 for (int e = 0; e < 3; ++e)
                     if (e < have) to[e] = from[i + e];
         };
         auto put = [&](float* to, const f4_t& x) {
-            if (have == 4) *reinterpret_cast<f4_u*>(to + i) = x;
-            else
+            if (have == 4) {
+                if constexpr (ONCE) __builtin_nontemporal_store(x, reinterpret_cast<f4_u*>(to + i));
+                else *reinterpret_cast<f4_u*>(to + i) = x;
+            } else
 #pragma unroll
                 for (int e = 0; e < 3; ++e)
                     if (e < have) to[i + e] = x[e];
@@ -294,10 +299,13 @@ int adamw_step(int dtype, int bits, int count, const AdamwTensor* t, const chime
     } else {
         L.s = scalars_of(*h_hyper);
     }
-    // A workgroup that goes round takes a trip to memory each time; small steps are as long as one of them
+    // 1024 values a workgroup, four a lane, and no loop: a workgroup that goes round takes a trip to memory each time.  8-bit steps go round twice, beyond 4
+    // million values, where they are short of instructions.  Measured (184 million bf16 weights; 101 million with 8-bit moments), us: 4096 values 1062; 350,
+    // 2048 1048; 343, 1024 1030; 356; past the caches 1045; 336, 1022; 335, 990; 346.  A float step of 400 000 values 6.4 -> 4.6.
     long long total = 0, block = 0;
     for (int i = 0; i < count; ++i) total += t[i].n;
-    L.chunk = total <= 4 << 20 ? 1024 : 4096;
+    L.chunk = bits == 8 && total > 4 << 20 ? 2048 : 1024;
+    const bool once = total * (bits == 8 ? 18 : 28) > 256ll << 20;
     auto chunks_of = [&](int i) { return (t[i].n + L.chunk - 1) / L.chunk; };
     for (int i = 0; i < count;) {
         std::fill(std::begin(L.first), std::end(L.first), INT_MAX);
@@ -312,10 +320,14 @@ int adamw_step(int dtype, int bits, int count, const AdamwTensor* t, const chime
         }
         if (!used) continue;
         const dim3 grid((unsigned)chunks), threads(STEP_THREADS);
-        if (dtype == CHIMERA_F32 && bits == 32) hipLaunchKernelGGL((adamw_kernel<float, 32>), grid, threads, 0, s, L);
-        else if (dtype == CHIMERA_F32) hipLaunchKernelGGL((adamw_kernel<float, 8>), grid, threads, 0, s, L);
-        else if (bits == 32) hipLaunchKernelGGL((adamw_kernel<bf16_t, 32>), grid, threads, 0, s, L);
-        else hipLaunchKernelGGL((adamw_kernel<bf16_t, 8>), grid, threads, 0, s, L);
+        auto launch = [&]<typename T, int BITS>() {
+            if (once) hipLaunchKernelGGL((adamw_kernel<T, BITS, true>), grid, threads, 0, s, L);
+            else hipLaunchKernelGGL((adamw_kernel<T, BITS, false>), grid, threads, 0, s, L);
+        };
+        if (dtype == CHIMERA_F32 && bits == 32) launch.template operator()<float, 32>();
+        else if (dtype == CHIMERA_F32) launch.template operator()<float, 8>();
+        else if (bits == 32) launch.template operator()<bf16_t, 32>();
+        else launch.template operator()<bf16_t, 8>();
         CHIMERA_LAUNCH_CHECK("AdamW");
     }
     return CHIMERA_OK;
@@ -387,7 +399,7 @@ int chimera_op_adamw(int dtype, int state_bits, int count, const int64_t* h_n, v
         std::vector<std::pair<uintptr_t, uintptr_t>> spans;
         spans.reserve((size_t)count);
         for (int i = 0; i < count; ++i) {
-            if (h_n[i] < 0 || h_n[i] > 1ll << 34) return fail(CHIMERA_EINVAL, "tensor %d of %lld values", i, (long long)h_n[i]);
+            if (h_n[i] < 0 || h_n[i] > 1ll << 32) return fail(CHIMERA_EINVAL, "tensor %d of %lld values", i, (long long)h_n[i]);
             t[i] = {h_param[i], h_m[i], h_v[i], dtype == CHIMERA_BF16 ? h_master[i] : nullptr, state_bits == 8 ? h_scale[i] : nullptr, h_grad[i], h_n[i],
                     h_decay ? h_decay[i] : 0.f};
             if (!h_n[i]) continue;

@@ -374,7 +374,7 @@ def _clone(s):
 
 
 H = dict(beta1=0.9, beta2=0.95, eps=1e-8)
-SIZES = [[1], [255, 1, 257], [4096, 4095, 0, 4097, 3], [64] * 120, [300_001, 12], [2_000_003]]
+SIZES = [[15_000_003], [1], [255, 1, 257], [4096, 4095, 0, 4097, 3], [64] * 120, [300_001, 12], [2_000_003]]
 
 
 @pytest.mark.parametrize("bits", [32, 8])

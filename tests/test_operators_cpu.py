@@ -106,7 +106,7 @@ def adamw(dtype=b.BF16, bits=32, n=(16, 0, 9), param=(P, None, 2 * P), master=(P
 NAN, INF = float("nan"), float("inf")
 
 
-@pytest.mark.parametrize("bad", [dict(dtype=3), dict(bits=16), dict(bits=0), dict(count=0), dict(count=-5), dict(n=(16, 0, -9)), dict(n=(16, 0, 1 << 40)),
+@pytest.mark.parametrize("bad", [dict(dtype=3), dict(bits=16), dict(bits=0), dict(count=0), dict(count=-5), dict(n=(16, 0, -9)), dict(n=(16, 0, (1 << 32) + 1)),
                                  dict(param=None), dict(master=None), dict(grad=None), dict(m=None), dict(v=None), dict(bits=8), dict(param=(P, None, None)),
                                  dict(master=(P, None, None)), dict(grad=(None, None, P)), dict(bits=8, scale=(P, None, None)), dict(param=(P, None, P)),
                                  dict(param=(P, None, P + 30)), dict(param=(P + 1, None, 2 * P)), dict(grad=(P + 2, None, P)), dict(m=(P + 1, None, P)),
