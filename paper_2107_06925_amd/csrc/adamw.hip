@@ -171,7 +171,7 @@ __global__ __launch_bounds__(STEP_THREADS) void adamw_kernel(StepLaunch L) {
             const float x = g[e] * factor;
             m[e] = m[e] * s.b1 + x * s.w1;
             v[e] = v[e] * s.b2 + (x * x) * s.w2;
-            r[e] = __fsqrt_rn(v[e]);
+            r[e] = sqrtf(v[e]);                               // correctly rounded
             w[e] = w[e] * keep - (m[e] * s.rate) * __builtin_amdgcn_rcpf(r[e] * s.root + s.eps);
         }
         put(weight, w);
