@@ -30,7 +30,7 @@ constexpr int NUM_CUS = 256;
 struct F32Product {
     const float* a; const float* b; const float* bias; const float* r; float* c; float* c2;
     float* bsum;                         // optional: bsum[j] += sum_k B(k, j)
-    int m, n, k, lda, ldb, tiles_m, tiles_n, first;
+    int m, n, k, lda, ldb, ldc, tiles_m, tiles_n, first;      // ldc: of C and R
 };
 constexpr int MAX_PRODUCTS = 4;
 struct F32Launch { F32Product p[MAX_PRODUCTS]; int count, total, epi, flag; };     // flag: GeLU form, or overwrite of an accumulate
@@ -62,7 +62,7 @@ template <int EPI> __device__ __forceinline__ void finish_one(const F32Product& 
 // N consecutive results of one row (columns col..col+N-1, inside the matrix)
 template <int EPI, int N>
 __device__ __forceinline__ void finish(const F32Product& p, int flag, int row, int col, const float* acc) {
-    const size_t idx = (size_t)row * p.n + col;
+    const size_t idx = (size_t)row * p.ldc + col;
     float v[N], w[N];
 #pragma unroll
     for (int e = 0; e < N; ++e) {
@@ -84,7 +84,7 @@ __device__ __forceinline__ void finish(const F32Product& p, int flag, int row, i
 struct F32Ahead {
     f32x4 bias, r;
     template <int EPI> __device__ __forceinline__ void request(const F32Product& p, int flag, int row, int col) {
-        const size_t idx = (size_t)row * p.n + col;
+        const size_t idx = (size_t)row * p.ldc + col;
         // n is a multiple of 4, but C, R and the bias need not be aligned to 16 bytes
         typedef f32x4 __attribute__((aligned(4))) f32x4_u;
         if constexpr (EPI == EPI_BIAS || EPI == EPI_BIAS_GELU || EPI == EPI_BIAS_RESIDUAL) bias = *reinterpret_cast<const f32x4_u*>(p.bias + col);
@@ -92,7 +92,7 @@ struct F32Ahead {
         if constexpr (EPI == EPI_ACCUM_F32) { r = f32x4{0.f, 0.f, 0.f, 0.f}; if (!flag) r = *reinterpret_cast<const f32x4_u*>(p.c + idx); }
     }
     template <int EPI> __device__ __forceinline__ void finish(const F32Product& p, int flag, int row, int col, const f32x4& acc) const {
-        const size_t idx = (size_t)row * p.n + col;
+        const size_t idx = (size_t)row * p.ldc + col;
         float v[4], w[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -278,7 +278,7 @@ __global__ __launch_bounds__(8 * WAVE, 4) void gemm_f32_tile_kernel(F32Launch L)
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             other[r] = 0.f;
-            if (READS && !(EPI == EPI_ACCUM_F32 && L.flag)) other[r] = (EPI == EPI_ACCUM_F32 ? p.c : p.r)[(size_t)min(row_of(r), m - 1) * n + c];
+            if (READS && !(EPI == EPI_ACCUM_F32 && L.flag)) other[r] = (EPI == EPI_ACCUM_F32 ? p.c : p.r)[(size_t)min(row_of(r), m - 1) * p.ldc + c];
         }
     };
     auto steps = [&](auto kc_c, auto sums_c, const float* __restrict__ from, int ld, int row0, int rows) {
@@ -430,7 +430,7 @@ __global__ __launch_bounds__(8 * WAVE, 4) void gemm_f32_tile_kernel(F32Launch L)
     if (col >= n) return;
 #pragma unroll
     for (int r = 0; r < R; ++r)
-        if (row_of(r) < m) finish_one<EPI>(p, L.flag, (size_t)row_of(r) * n + col, out[r], bias, other[r]);
+        if (row_of(r) < m) finish_one<EPI>(p, L.flag, (size_t)row_of(r) * p.ldc + col, out[r], bias, other[r]);
 }
 
 // Larger outputs: 128x128, 4 wavefronts of 64x64, two workgroups on a CU, each thread stages a chunk of either operand: half of the vector
@@ -837,7 +837,7 @@ F32Product product_of(const GemmArgs& g) {
     F32Product p{};
     p.a = (const float*)g.a; p.b = (const float*)g.b; p.bias = (const float*)g.bias; p.r = (const float*)g.r;
     p.c = (float*)g.c; p.c2 = (float*)g.c2;
-    p.m = g.m; p.n = g.n; p.k = g.k; p.lda = g.lda; p.ldb = g.ldb;
+    p.m = g.m; p.n = g.n; p.k = g.k; p.lda = g.lda; p.ldb = g.ldb; p.ldc = g.ldc ? g.ldc : g.n;
     return p;
 }
 

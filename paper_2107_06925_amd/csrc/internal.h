@@ -58,6 +58,7 @@ struct GemmArgs {
     const void* r;                      // [m,n], stage dtype (float if r_f32)
     int r_f32, c_f32;                   // EPI_BIAS_RESIDUAL on bf16 only: R is / C becomes float
     void* c;                            // [m,n]
+    int ldc;                            // its leading dimension (0: n); float products only, and n is a multiple of 4
     void* c2;                           // [m,n]
     int epilogue;
     int gelu_erf;

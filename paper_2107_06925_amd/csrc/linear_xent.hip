@@ -541,21 +541,14 @@ __global__ __launch_bounds__(ROW_THREADS) void xent_dz_f32_kernel(float* __restr
         store_vec<float>(row + c, v);
     }
 }
-// columns of a wider matrix: to (+)= from [rows, ld], `cols` of them
-__global__ __launch_bounds__(ROW_THREADS) void xent_columns_kernel(const float* __restrict__ from, int ld, int cols, float* __restrict__ to, int ldto, int overwrite) {
-    const int c = (blockIdx.x * ROW_THREADS + threadIdx.x) * 4;
-    if (c >= cols) return;
-    float v[4], o[4] = {0.f, 0.f, 0.f, 0.f};
-    load_vec<float>(from + (size_t)blockIdx.y * ld + c, v);
-    float* dst = to + (size_t)blockIdx.y * ldto + c;
-    if (!overwrite) load_vec<float>(dst, o);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] += o[e];
-    if (c + 4 <= cols) store_vec<float>(dst, v);
-    else
-#pragma unroll
-        for (int e = 0; e < 3; ++e)
-            if (c + e < cols) dst[e] = v[e];
+// up to three columns of a wider matrix: to (+)= from [rows, 4]
+__global__ __launch_bounds__(ROW_THREADS) void xent_columns_kernel(const float* __restrict__ from, int rows, int cols, float* __restrict__ to, int ldto, int overwrite) {
+    const int i = blockIdx.x * ROW_THREADS + threadIdx.x;
+    if (i >= rows) return;
+    for (int c = 0; c < cols; ++c) {
+        float* dst = to + (size_t)i * ldto + c;
+        *dst = overwrite ? from[(size_t)i * 4 + c] : *dst + from[(size_t)i * 4 + c];
+    }
 }
 
 size_t aligned(size_t b) { return (b + 255) / 256 * 256; }
@@ -577,7 +570,7 @@ constexpr size_t PIECE_BYTES_MIN = (size_t)128 << 20, PIECE_BYTES_MAX = (size_t)
 constexpr int PIECE_STEP = 256, PIECE_USUAL = 8192;
 int default_piece(int dtype, int m, int hidden, int vocab) {
     const int all = round_up(vocab, PIECE_STEP);
-    const size_t column = dtype == CHIMERA_F32 ? ((size_t)m + hidden) * 4 : (size_t)round_up(m, TOKEN_PAD) * 8 + (size_t)hidden * 4;
+    const size_t column = dtype == CHIMERA_F32 ? (size_t)m * 4 : (size_t)round_up(m, TOKEN_PAD) * 8 + (size_t)hidden * 4;
     const size_t usual = std::max(PIECE_BYTES_MIN / column, std::min<size_t>(PIECE_USUAL, PIECE_BYTES_MAX / column));
     const int most = (int)std::min<size_t>(all, std::max<size_t>(usual / PIECE_STEP * PIECE_STEP, PIECE_STEP));
     return round_up((vocab + (vocab + most - 1) / most - 1) / ((vocab + most - 1) / most), PIECE_STEP);        // equal pieces
@@ -628,7 +621,7 @@ BwdLayout bwd_layout(int dtype, int m, int hidden, int vocab, int piece) {
         l.dz[0] = take((size_t)m * l.ld * 4);
         l.f32_splits = gemm_f32_splits(m, hidden, l.ld & ~7);
         l.slabs = take((size_t)l.f32_splits * m * hidden * 4);
-        l.columns = take((size_t)hidden * l.ld * 4);
+        l.columns = take((size_t)hidden * 16);
     } else {
         l.mp = round_up(m, TOKEN_PAD);
         l.plan = plan_of(l.mp, hidden, l.ld);
@@ -745,11 +738,18 @@ int xent_bwd_f32(int m, int hidden, int vocab, const float* h, int ldh, const fl
             if (!slabs) slabs = now;
         }
         if (dw) {
+            // whole groups of four columns where they belong, up to three more by way of a matrix of their own
+            const int fours = cols & ~3;
             GemmArgs q{};
-            q.m = hidden; q.n = ld; q.k = m; q.a = rows; q.lda = hidden; q.a_kc = 0; q.b = z; q.ldb = ld; q.b_kc = 0; q.c = columns; q.epilogue = EPI_ACCUM_F32;
-            XENT_TRY(gemm_f32_group(1, &q, nullptr, 1, stream));
-            hipLaunchKernelGGL(xent_columns_kernel, dim3((cols + ROW_THREADS * 4 - 1) / (ROW_THREADS * 4), hidden), dim3(ROW_THREADS), 0, s, columns, ld, cols,
-                               dw + v0, lddw, overwrite);
+            q.m = hidden; q.n = fours; q.k = m; q.a = rows; q.lda = hidden; q.a_kc = 0; q.b = z; q.ldb = ld; q.b_kc = 0; q.c = dw + v0; q.ldc = lddw;
+            q.epilogue = EPI_ACCUM_F32;
+            if (fours) XENT_TRY(gemm_f32_group(1, &q, nullptr, overwrite, stream));
+            if (fours < cols) {
+                q.n = 4; q.b = z + fours; q.c = columns; q.ldc = 4;
+                XENT_TRY(gemm_f32_group(1, &q, nullptr, 1, stream));
+                hipLaunchKernelGGL(xent_columns_kernel, dim3((hidden + ROW_THREADS - 1) / ROW_THREADS), dim3(ROW_THREADS), 0, s, columns, hidden, cols - fours,
+                                   dw + v0 + fours, lddw, overwrite);
+            }
             CHIMERA_LAUNCH_CHECK("linear cross-entropy");
         }
         if (dh && v0 + l.piece >= vocab) {
