@@ -337,38 +337,50 @@ template <int BM> struct GradEnd {
     }
 };
 
-// Rows of W within the next piece as fp16 numbers times 2^raise; columns behind the vocabulary as zeros, whatever they hold.
-__device__ __forceinline__ void raise_row(const Pass& p, int i, char* lds) {
+// A row of W within the next piece as fp16 numbers times 2^raise; columns behind the vocabulary as zeros, whatever they hold.  One wavefront: looked over
+// once, and once more, out of the cache, to be written.
+__device__ __forceinline__ void raise_row(const Pass& p, int i) {
+    const int lane = threadIdx.x % WAVE, ld = p.next.ld, cols = p.next.cols;
     const bf16_t* src = p.w + (size_t)i * p.ldw + p.next.v0;
     _Float16* to = p.next.w + (size_t)i * p.ldp;
-    float* part = reinterpret_cast<float*>(lds);
+    constexpr int FLY = 8, STRIDE = WAVE * 8;
     float top = 0.f;
-    for (int c = threadIdx.x * 8; c < p.next.ld; c += 512 * 8) {
+    auto look = [&](int c, const uint4& q) {
         float x[8];
-        load_vec<bf16_t>(src + c, x);
+        load_vec<bf16_t>(reinterpret_cast<const bf16_t*>(&q), x);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) top = fmaxf(top, c + e < p.next.cols ? fabsf(x[e]) : 0.f);
+        for (int e = 0; e < 8; ++e) top = fmaxf(top, c + e < cols ? fabsf(x[e]) : 0.f);
+    };
+    for (int c0 = lane * 8; c0 < ld; c0 += FLY * STRIDE) {
+        uint4 q[FLY];
+#pragma unroll
+        for (int u = 0; u < FLY; ++u) q[u] = *reinterpret_cast<const uint4*>(src + min(c0 + u * STRIDE, ld - 8));      // (what is behind the row counts once more)
+#pragma unroll
+        for (int u = 0; u < FLY; ++u) look(min(c0 + u * STRIDE, ld - 8), q[u]);
     }
     top = wave_max(top);
-    if (threadIdx.x % WAVE == 0) part[threadIdx.x / WAVE] = top;
-    __syncthreads();
-    top = wave_max(part[threadIdx.x % 8]);
-    __syncthreads();                                              // (the next row's)
     const int up = top > 0.f ? 15 - __builtin_amdgcn_frexp_expf(top) : 0;
-    if (threadIdx.x == 0) p.next.raise[i] = up;
-    for (int c = threadIdx.x * 8; c < p.next.ld; c += 512 * 8) {
-        float x[8];
-        load_vec<bf16_t>(src + c, x);
-        f16x8 y;
+    if (lane == 0) p.next.raise[i] = up;
+    for (int c0 = lane * 8; c0 < ld; c0 += FLY * STRIDE) {
+        uint4 q[FLY];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = c + e < p.next.cols ? (_Float16)ldexpf(x[e], up) : (_Float16)0.f;
-        *reinterpret_cast<f16x8*>(to + c) = y;
+        for (int u = 0; u < FLY; ++u) q[u] = *reinterpret_cast<const uint4*>(src + min(c0 + u * STRIDE, ld - 8));
+#pragma unroll
+        for (int u = 0; u < FLY; ++u) {
+            const int c = c0 + u * STRIDE;
+            float x[8];
+            load_vec<bf16_t>(reinterpret_cast<const bf16_t*>(&q[u]), x);
+            f16x8 y;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = c + e < cols ? (_Float16)ldexpf(x[e], up) : (_Float16)0.f;
+            if (c < ld) *reinterpret_cast<f16x8*>(to + c) = y;
+        }
     }
 }
 // h^T times 2^(shift - lift); tokens that do not count, and the padding behind the last one, as zeros: their dz is zero, but h may hold anything.
 // Transposed, because the matrix instructions take runs of the contraction's index: both operands of dW through the transposing LDS reads, which
 // deliver 64 bytes a clock, make its step 3072 clocks of LDS to 2048 of matrix instructions (measured: 3080; dW at 8192 x 2048 x 8192 442 us).
-constexpr int W_ROWS_PER_WG = 4, TURN_TOKENS = 64, TURN_COLS = 256, TURN_WGS = 1024;
+constexpr int W_ROWS_PER_WG = 8, TURN_TOKENS = 64, TURN_COLS = 256, TURN_WGS = 1024;
 __device__ __forceinline__ void turn_rows(const Pass& p, int id, int wgs, char* lds) {
     int* part = reinterpret_cast<int*>(lds);
     constexpr int LD = TURN_TOKENS + 8;
@@ -436,7 +448,8 @@ __global__ __launch_bounds__(512, 2) void xent_pass_kernel(Pass p) {
         XENT_TILE(TOK, true, false, false, false, p.h, p.w + p.next.v0, p.m, p.next.ld, p.hidden, p.ldh, p.ldw, p.dz_r, id - p.first[2], p.dz_r.band, true,
                   (GradEnd<TOK>{&p, 0.f, 0.f, 0}));
     } else if (id < p.first[4]) {
-        for (int i = (id - p.first[3]) * W_ROWS_PER_WG; i < min((id - p.first[3] + 1) * W_ROWS_PER_WG, p.hidden); ++i) raise_row(p, i, lds);
+        const int i = (id - p.first[3]) * W_ROWS_PER_WG + threadIdx.x / WAVE;
+        if (i < p.hidden) raise_row(p, i);
     } else {
         turn_rows(p, id - p.first[4], (int)gridDim.x - p.first[4], lds);
     }
@@ -576,7 +589,9 @@ int default_piece(int dtype, int m, int hidden, int vocab) {
     return round_up((vocab + (vocab + most - 1) / most - 1) / ((vocab + most - 1) / most), PIECE_STEP);        // equal pieces
 }
 // The launches' tiles, and the splits of dh's contraction.  256x256 tiles where the products of a piece fill the chip with them; rows of 128 for
-// up to 128 tokens.  dh's tiles are cut along the vocabulary so that none is longer than dW's, or than a piece's work shared by all CUs.
+// up to 128 tokens.  dh's tiles are cut along the vocabulary
+// to half of what a CU has to do in all, or 32 steps, whichever is more (a third and a quarter: 1380 -> 1400 us at 2048 x 1600 x 50256, 360 -> 388 at 512 x 1024,
+// every part is read and written once a piece).
 struct PassPlan { int dw_tile, tok_tile, splits, k_per; };
 PassPlan plan_of(int mp, int hidden, int ld) {
     PassPlan p{};
@@ -587,7 +602,8 @@ PassPlan plan_of(int mp, int hidden, int ld) {
     const long dw_steps = mp / 32, dh_steps = (ld + 63) / 64, z_steps = (hidden + 63) / 64;
     const double each = (work(p.dw_tile, tiles_of(hidden, ld, p.dw_tile), dw_steps) + work(p.tok_tile, tiles_of(mp, hidden, p.tok_tile), dh_steps) +
                          work(p.tok_tile, tiles_of(mp, ld, p.tok_tile), z_steps)) / NUM_CUS;
-    const long most = std::max<long>(8, (long)(each / 3 * (p.tok_tile == 256 ? 1.0 : 1 / 0.35)));
+    const double share = p.tok_tile == 256 ? each : each / 0.35;
+    const long most = std::max<long>(8, (long)(share < 32 ? share : std::max(32.0, share / 2)));
     const long splits = std::min<long>((dh_steps + most - 1) / most, 64), per = (dh_steps + splits - 1) / splits;
     p.splits = (int)((dh_steps + per - 1) / per);
     p.k_per = (int)per * 64;
