@@ -522,7 +522,7 @@ int chimera_head_loss(int dtype, int tokens, int hidden, int vocab, const void* 
  *   += h^T dz, or = with overwrite != 0.  Either may be NULL, not both.  z is formed again, `piece` columns of the vocabulary at a time (rounded up to
  *   a multiple of 256; 0: the library's choice); the workspace grows with it.
  * bf16: dh is formed from dz in 11 bits, dW from dz in 22, so that it is as exact as a sum of floats; the products' sums are float.
- * All sums have a fixed order.  ENOMEM if the workspace is too small (a function of the same sizes; 0 for sizes that the calls refuse). */
+ * All sums have a fixed order.  Calls that overlap in time need workspaces of their own.  ENOMEM if the workspace is too small (a function of the same sizes; 0 for sizes that the calls refuse). */
 size_t chimera_op_linear_xent_fwd_workspace_bytes(int dtype, int tokens, int hidden, int vocab);
 int chimera_op_linear_xent_fwd(int dtype, int tokens, int hidden, int vocab, const void* d_h, int ldh, const void* d_w, int ldw,
                                const int32_t* d_targets, float scale, float* d_loss_rows, float* d_lse, float* d_loss,
@@ -552,7 +552,8 @@ int chimera_op_grad_norm(int count, const int64_t* h_n, const float* const* h_gr
  *   p = p (1 - lr decay) - lr / (1 - beta1^step) m / (sqrt(v) / sqrt(1 - beta2^step) + eps),
  * factor = d_grad_scale[0] (NULL: 1); where that is not finite the call changes nothing, so a step behind a gradient norm that overflowed is left out.
  * h_param: the weights in `dtype`.  CHIMERA_BF16: h_master holds them in float as well; the step updates those and rounds.  h_grad: float.
- * h_decay: one float per tensor (NULL: none decays).  Weights of two tensors must not overlap (EINVAL).
+ * h_decay: one float per tensor (NULL: none decays).  Weights, master weights or moments of two tensors must not
+ * overlap (EINVAL).
  * state_bits 32: h_m, h_v point to floats, the moments above; h_scale is not used.
  * state_bits 8: h_m and h_v point to one byte per element, e4m3 numbers (4 exponent bits, bias 7, 3 of mantissa, no infinities) that hold m and
  * sqrt(v) as multiples of a float scale for each 256 elements of a tensor; h_scale to the pairs (m's, sqrt(v)'s), ceil(n / 256) of them.  Zeros are the

@@ -533,6 +533,19 @@ def chimera_head_loss(y, targets, lnf_g, lnf_b, w_head, scale, dy, dlnf_g, dlnf_
     return ws
 
 
+def _rows(t, dtype, what):
+    """Rows of a matrix whose rows are contiguous: how far they are apart."""
+    if t.dim() != 2 or t.dtype != dtype or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("%s: a matrix of %s with contiguous rows expected" % (what, dtype))
+    return t.stride(0) if t.shape[0] > 1 else (t.shape[1] + 7) // 8 * 8
+
+
+def _vector(t, dtype, n, what):
+    if t is not None and (t.dtype != dtype or t.numel() != n or not t.is_contiguous()):
+        raise ValueError("%s: %d contiguous values of %s expected" % (what, n, dtype))
+    return _ptr(t)
+
+
 def chimera_op_linear_xent_fwd(h, w, targets, scale, loss_rows, lse, loss=None, workspace=None):
     """h [tokens, hidden], w [hidden, vocab] (rows may lie further apart than they are long), targets int32; fills loss_rows and lse
     (float, [tokens]) and adds to loss.  Allocates the workspace (a torch uint8 tensor) unless one is given, and returns it."""
@@ -540,8 +553,10 @@ def chimera_op_linear_xent_fwd(h, w, targets, scale, loss_rows, lse, loss=None, 
     (tokens, hidden), vocab = h.shape, w.shape[1]
     if workspace is None:
         workspace = torch.empty(lib().chimera_op_linear_xent_fwd_workspace_bytes(_dt(h), tokens, hidden, vocab), dtype=torch.uint8, device=h.device)
-    check(lib().chimera_op_linear_xent_fwd(_dt(h), tokens, hidden, vocab, _ptr(h), h.stride(0), _ptr(w), w.stride(0), _ptr(targets), scale,
-                                           _ptr(loss_rows), _ptr(lse), _ptr(loss), _ptr(workspace), workspace.numel(), _stream(h)))
+    f = torch.float32
+    check(lib().chimera_op_linear_xent_fwd(_dt(h), tokens, hidden, vocab, _ptr(h), _rows(h, h.dtype, "h"), _ptr(w), _rows(w, h.dtype, "w"),
+                                           _vector(targets, torch.int32, tokens, "targets"), scale, _vector(loss_rows, f, tokens, "loss_rows"),
+                                           _vector(lse, f, tokens, "lse"), _vector(loss, f, 1, "loss"), _ptr(workspace), workspace.numel(), _stream(h)))
     return workspace
 
 
@@ -551,9 +566,13 @@ def chimera_op_linear_xent_bwd(h, w, targets, lse, scale, dh=None, dw=None, dlos
     (tokens, hidden), vocab = h.shape, w.shape[1]
     if workspace is None:
         workspace = torch.empty(lib().chimera_op_linear_xent_bwd_workspace_bytes(_dt(h), tokens, hidden, vocab, piece), dtype=torch.uint8, device=h.device)
-    check(lib().chimera_op_linear_xent_bwd(_dt(h), tokens, hidden, vocab, _ptr(h), h.stride(0), _ptr(w), w.stride(0), _ptr(targets), _ptr(lse),
-                                           scale, _ptr(dloss), _ptr(dh), 0 if dh is None else dh.stride(0), _ptr(dw),
-                                           0 if dw is None else dw.stride(0), int(overwrite), piece, _ptr(workspace), workspace.numel(), _stream(h)))
+    f = torch.float32
+    if (dh is not None and dh.shape != h.shape) or (dw is not None and dw.shape != w.shape):
+        raise ValueError("dh and dw have the shapes of h and w")
+    check(lib().chimera_op_linear_xent_bwd(_dt(h), tokens, hidden, vocab, _ptr(h), _rows(h, h.dtype, "h"), _ptr(w), _rows(w, h.dtype, "w"),
+                                           _vector(targets, torch.int32, tokens, "targets"), _vector(lse, f, tokens, "lse"), scale,
+                                           _vector(dloss, f, tokens, "dloss"), _ptr(dh), 0 if dh is None else _rows(dh, h.dtype, "dh"), _ptr(dw),
+                                           0 if dw is None else _rows(dw, f, "dw"), int(overwrite), piece, _ptr(workspace), workspace.numel(), _stream(h)))
     return workspace
 
 
@@ -561,11 +580,13 @@ def chimera_head_loss_pieces(y, targets, lnf_g, lnf_b, w_head, scale, dy, dlnf_g
     """w_head [hidden, vocab]; dw_head has the same row stride.  Allocates the workspace unless one is given, and returns it."""
     import torch
     tokens, hidden, vocab = y.shape[0], y.shape[1], w_head.shape[1]
-    assert dw_head.stride(0) == w_head.stride(0)
+    ldw = _rows(w_head, y.dtype, "w_head")
+    if _rows(dw_head, torch.float32, "dw_head") != ldw or dw_head.shape[0] != hidden or dw_head.shape[1] < vocab:
+        raise ValueError("dw_head has the rows of w_head, as far apart")
     if workspace is None:
         workspace = torch.empty(lib().chimera_head_pieces_workspace_bytes(_dt(y), tokens, hidden, vocab, piece), dtype=torch.uint8, device=y.device)
-    check(lib().chimera_head_loss_pieces(_dt(y), tokens, hidden, vocab, _ptr(y), _ptr(targets), _ptr(lnf_g), _ptr(lnf_b), _ptr(w_head),
-                                         w_head.stride(0), scale, _ptr(dy), _ptr(dlnf_g), _ptr(dlnf_b), _ptr(dw_head), _ptr(loss), piece,
+    check(lib().chimera_head_loss_pieces(_dt(y), tokens, hidden, vocab, _ptr(y), _vector(targets, torch.int32, tokens, "targets"), _ptr(lnf_g), _ptr(lnf_b),
+                                         _ptr(w_head), ldw, scale, _ptr(dy), _ptr(dlnf_g), _ptr(dlnf_b), _ptr(dw_head), _ptr(loss), piece,
                                          _ptr(workspace), workspace.numel(), _stream(y)))
     return workspace
 
@@ -589,6 +610,8 @@ def _counts(tensors):
 def chimera_op_grad_norm(grads, max_norm, out, workspace=None):
     """grads: float tensors (contiguous); out: float [2], the norm and the factor that brings it down to max_norm."""
     import torch
+    if any(g.dtype != torch.float32 or not g.is_contiguous() for g in grads) or out.dtype != torch.float32 or out.numel() != 2:
+        raise ValueError("contiguous float32 gradients and two float32 results expected")
     n = _counts(grads)
     if workspace is None:
         workspace = torch.empty(lib().chimera_op_grad_norm_workspace_bytes(len(grads)), dtype=torch.uint8, device=out.device)
@@ -603,6 +626,13 @@ class AdamW:
     float8_e4m3fn (or uint8) and scales float32, a pair for each 256 elements of a tensor.  decay: a number per tensor, or None."""
 
     def __init__(self, params, grads, ms, vs, masters=None, scales=None, decay=None, beta1=0.9, beta2=0.95, eps=1e-8):
+        import torch
+        if not params or any(p.dtype != params[0].dtype for p in params) or params[0].dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError("params: float32 or bfloat16 tensors of one type")
+        if any(t.dtype != torch.float32 for x in (grads, masters, scales) if x is not None for t in x):
+            raise ValueError("grads, masters and scales: float32")
+        if any(t.dtype not in ((torch.float32,) if scales is None else (torch.uint8, torch.float8_e4m3fn)) for t in list(ms) + list(vs)):
+            raise ValueError("moments: float32, or float8_e4m3fn (uint8) with scales")
         lists = [params, grads, ms, vs] + [x for x in (masters, scales, decay) if x is not None]
         if any(len(x) != len(params) for x in lists):
             raise ValueError("one entry per tensor expected")

@@ -396,8 +396,8 @@ int chimera_op_adamw(int dtype, int state_bits, int count, const int64_t* h_n, v
     const size_t e = dtype == CHIMERA_F32 ? 4 : 2;
     try {
         std::vector<AdamwTensor> t((size_t)count);
-        std::vector<std::pair<uintptr_t, uintptr_t>> spans;
-        spans.reserve((size_t)count);
+        std::vector<std::pair<uintptr_t, uintptr_t>> spans[4];                // of what is written: weights, master weights, moments
+        for (auto& v : spans) v.reserve((size_t)count);
         for (int i = 0; i < count; ++i) {
             if (h_n[i] < 0 || h_n[i] > 1ll << 32) return fail(CHIMERA_EINVAL, "tensor %d of %lld values", i, (long long)h_n[i]);
             t[i] = {h_param[i], h_m[i], h_v[i], dtype == CHIMERA_BF16 ? h_master[i] : nullptr, state_bits == 8 ? h_scale[i] : nullptr, h_grad[i], h_n[i],
@@ -409,11 +409,17 @@ int chimera_op_adamw(int dtype, int state_bits, int count, const int64_t* h_n, v
                 (state_bits == 32 && (((uintptr_t)q.m | (uintptr_t)q.v) & 3)))
                 return fail(CHIMERA_EINVAL, "tensor %d is not aligned to its elements", i);
             if (!(q.decay >= 0) || !std::isfinite(q.decay)) return fail(CHIMERA_EINVAL, "weight decay of tensor %d must be finite and not negative", i);
-            spans.push_back({(uintptr_t)q.p, (uintptr_t)q.p + (size_t)h_n[i] * e});
+            const size_t moment = (size_t)h_n[i] * (state_bits == 32 ? 4 : 1);
+            spans[0].push_back({(uintptr_t)q.p, (uintptr_t)q.p + (size_t)h_n[i] * e});
+            if (q.master) spans[1].push_back({(uintptr_t)q.master, (uintptr_t)q.master + (size_t)h_n[i] * 4});
+            spans[2].push_back({(uintptr_t)q.m, (uintptr_t)q.m + moment});
+            spans[3].push_back({(uintptr_t)q.v, (uintptr_t)q.v + moment});
         }
-        std::sort(spans.begin(), spans.end());
-        for (size_t i = 1; i < spans.size(); ++i)
-            if (spans[i].first < spans[i - 1].second) return fail(CHIMERA_EINVAL, "weights of two tensors overlap");
+        for (auto& v : spans) {
+            if (!std::is_sorted(v.begin(), v.end())) std::sort(v.begin(), v.end());
+            for (size_t i = 1; i < v.size(); ++i)
+                if (v[i].first < v[i - 1].second) return fail(CHIMERA_EINVAL, "weights or moments of two tensors overlap");
+        }
         return adamw_step(dtype, state_bits, count, t.data(), h_hyper, d_hyper, d_grad_scale, hip_stream);
     } catch (const std::bad_alloc&) {
         return fail(CHIMERA_ENOMEM, "out of host memory");

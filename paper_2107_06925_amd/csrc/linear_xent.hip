@@ -17,6 +17,7 @@
 // float.  The framework's float products on pieces of z that are in memory, row kernels between them.
 #include "gemm_tiles.h"
 
+#include <array>
 #include <climits>
 
 namespace chimera {
@@ -211,8 +212,8 @@ struct Pass {
     // dh: float slabs [split][m, hidden]
     float* slabs;
     int k_per, dh_flags;
-    // workgroups of each kind, in this order, and the rasters of their tiles
-    int first[5];                    // dW, dh, dz, W's rows, h^T
+    int w_rows;                      // rows of W a workgroup
+    int first[5], count[5];          // workgroups of each kind: dW, dh, dz, W's rows, h^T; and the rasters of their tiles
     struct Raster { int tiles_m, tiles_n, group_m, band; } dw_r, dh_r, dz_r;
 };
 
@@ -337,13 +338,16 @@ template <int BM> struct GradEnd {
     }
 };
 
-// A row of W within the next piece as fp16 numbers times 2^raise; columns behind the vocabulary as zeros, whatever they hold.  One wavefront: looked over
-// once, and once more, out of the cache, to be written.
-__device__ __forceinline__ void raise_row(const Pass& p, int i) {
-    const int lane = threadIdx.x % WAVE, ld = p.next.ld, cols = p.next.cols;
+// A row of W within the next piece as fp16 numbers times 2^raise; columns behind the vocabulary as zeros, whatever they hold.  Looked over
+// once, and once more, out of the cache, to be written.  A workgroup takes w_rows of them, 8 / w_rows wavefronts each.
+__device__ __forceinline__ void raise_rows(const Pass& p, int id, char* lds) {
+    const int waves = 8 / p.w_rows, wave = threadIdx.x / WAVE, at = wave % waves * WAVE + threadIdx.x % WAVE, ld = p.next.ld, cols = p.next.cols;
+    const int own = id * p.w_rows + wave / waves, i = min(own, p.hidden - 1);
     const bf16_t* src = p.w + (size_t)i * p.ldw + p.next.v0;
     _Float16* to = p.next.w + (size_t)i * p.ldp;
-    constexpr int FLY = 8, STRIDE = WAVE * 8;
+    float* part = reinterpret_cast<float*>(lds);
+    constexpr int FLY = 8;
+    const int STRIDE = waves * WAVE * 8;
     float top = 0.f;
     auto look = [&](int c, const uint4& q) {
         float x[8];
@@ -351,7 +355,7 @@ __device__ __forceinline__ void raise_row(const Pass& p, int i) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) top = fmaxf(top, c + e < cols ? fabsf(x[e]) : 0.f);
     };
-    for (int c0 = lane * 8; c0 < ld; c0 += FLY * STRIDE) {
+    for (int c0 = at * 8; c0 < ld; c0 += FLY * STRIDE) {
         uint4 q[FLY];
 #pragma unroll
         for (int u = 0; u < FLY; ++u) q[u] = *reinterpret_cast<const uint4*>(src + min(c0 + u * STRIDE, ld - 8));      // (what is behind the row counts once more)
@@ -359,9 +363,13 @@ __device__ __forceinline__ void raise_row(const Pass& p, int i) {
         for (int u = 0; u < FLY; ++u) look(min(c0 + u * STRIDE, ld - 8), q[u]);
     }
     top = wave_max(top);
+    if (threadIdx.x % WAVE == 0) part[wave] = top;
+    __syncthreads();
+    for (int k = 0; k < waves; ++k) top = fmaxf(top, part[wave / waves * waves + k]);
+    if (own >= p.hidden) return;
     const int up = top > 0.f ? 15 - __builtin_amdgcn_frexp_expf(top) : 0;
-    if (lane == 0) p.next.raise[i] = up;
-    for (int c0 = lane * 8; c0 < ld; c0 += FLY * STRIDE) {
+    if (at == 0) p.next.raise[i] = up;
+    for (int c0 = at * 8; c0 < ld; c0 += FLY * STRIDE) {
         uint4 q[FLY];
 #pragma unroll
         for (int u = 0; u < FLY; ++u) q[u] = *reinterpret_cast<const uint4*>(src + min(c0 + u * STRIDE, ld - 8));
@@ -380,7 +388,7 @@ __device__ __forceinline__ void raise_row(const Pass& p, int i) {
 // h^T times 2^(shift - lift); tokens that do not count, and the padding behind the last one, as zeros: their dz is zero, but h may hold anything.
 // Transposed, because the matrix instructions take runs of the contraction's index: both operands of dW through the transposing LDS reads, which
 // deliver 64 bytes a clock, make its step 3072 clocks of LDS to 2048 of matrix instructions (measured: 3080; dW at 8192 x 2048 x 8192 442 us).
-constexpr int W_ROWS_PER_WG = 8, TURN_TOKENS = 64, TURN_COLS = 256, TURN_WGS = 1024;
+constexpr int TURN_TOKENS = 64, TURN_COLS = 256, TURN_WGS = 1024;
 __device__ __forceinline__ void turn_rows(const Pass& p, int id, int wgs, char* lds) {
     int* part = reinterpret_cast<int*>(lds);
     constexpr int LD = TURN_TOKENS + 8;
@@ -423,7 +431,7 @@ __global__ __launch_bounds__(512, 2) void xent_pass_kernel(Pass p) {
     static_assert(RingLds<128, 128, 2, 2, 2>::BYTES <= BYTES, "the larger of the two");
     static_assert(BYTES >= 8 * EpiSlab<2>::FLOATS * sizeof(float) + 256 * sizeof(RowInfo), "room for the slabs and the rows");
     __shared__ __attribute__((aligned(1024))) char lds[BYTES];
-    const int id = blockIdx.x;
+    const int block = blockIdx.x;
 #define XENT_TILE(T, AKC, BKC, F16, PAIRED, A, B, M, N, K, LDA, LDB, R, ID, BAND, XCD, END)                                                                          \
     do {                                                                                                                                                       \
         if constexpr (T == 256)                                                                                                                                \
@@ -433,25 +441,26 @@ __global__ __launch_bounds__(512, 2) void xent_pass_kernel(Pass p) {
             gemm_ring_tile<128, 128, 2, 2, 2, AKC, BKC, EPI_OWN, F16, PAIRED>(lds, A, B, nullptr, nullptr, nullptr, nullptr, M, N, K, LDA, LDB, EPI_OWN, 0, 0,  \
                                                                               R.tiles_m, R.tiles_n, R.group_m, ID, nullptr, XCD, 0, Ahead{nullptr, 0}, BAND, END); \
     } while (0)
-    if (id < p.first[1]) {
+    auto kind = [&](int k) { return (unsigned)(block - p.first[k]) < (unsigned)p.count[k]; };
+    if (kind(0)) {
+        const int id = block - p.first[0];
         const ColumnsEnd end{p.dw + p.now.v0, p.shift, p.hidden, p.now.cols, p.lddw, p.dw_flags, p.now.ld};
         XENT_TILE(DW, true, false, true, true, (const bf16_t*)p.rows, (const bf16_t*)p.now.dz, p.hidden, p.now.ld, 2 * p.mp, p.mp, 2 * p.now.ld, p.dw_r, id,
                   p.dw_r.band, true, end);
-    } else if (id < p.first[2]) {
-        const int at = id - p.first[1], tiles = p.dh_r.tiles_m * p.dh_r.tiles_n, total = p.first[2] - p.first[1];
+    } else if (kind(1)) {
+        const int at = block - p.first[1], tiles = p.dh_r.tiles_m * p.dh_r.tiles_n, total = p.count[1];
         const int xcd = at & 7, local = at >> 3, pid = xcd * (total >> 3) + min(xcd, total & 7) + local;
         const int split = __builtin_amdgcn_readfirstlane(pid / tiles), k0 = split * p.k_per;
         const SlabEnd end{p.slabs + (size_t)split * p.m * p.hidden, p.now.raise, p.m, p.hidden, p.dh_flags};
         XENT_TILE(TOK, true, true, true, false, (const bf16_t*)p.now.dz + k0, (const bf16_t*)p.now.w + k0, p.m, p.hidden, min(p.k_per, p.now.ld - k0), 2 * p.now.ld,
                   p.ldp, p.dh_r, pid - split * tiles, 0, false, end);
-    } else if (id < p.first[3]) {
-        XENT_TILE(TOK, true, false, false, false, p.h, p.w + p.next.v0, p.m, p.next.ld, p.hidden, p.ldh, p.ldw, p.dz_r, id - p.first[2], p.dz_r.band, true,
+    } else if (kind(2)) {
+        XENT_TILE(TOK, true, false, false, false, p.h, p.w + p.next.v0, p.m, p.next.ld, p.hidden, p.ldh, p.ldw, p.dz_r, block - p.first[2], p.dz_r.band, true,
                   (GradEnd<TOK>{&p, 0.f, 0.f, 0}));
-    } else if (id < p.first[4]) {
-        const int i = (id - p.first[3]) * W_ROWS_PER_WG + threadIdx.x / WAVE;
-        if (i < p.hidden) raise_row(p, i);
+    } else if (kind(3)) {
+        raise_rows(p, block - p.first[3], lds);
     } else {
-        turn_rows(p, id - p.first[4], (int)gridDim.x - p.first[4], lds);
+        turn_rows(p, block - p.first[4], p.count[4], lds);
     }
 #undef XENT_TILE
 }
@@ -784,6 +793,8 @@ int xent_bwd_bf16(int m, int hidden, int vocab, const bf16_t* h, int ldh, const 
     p.room = (int*)(ws + l.room); p.shift = (int*)(ws + l.shift); p.rows = (_Float16*)(ws + l.rows);
     p.dw = dw; p.lddw = lddw; p.dw_flags = overwrite ? ACCUM_OVERWRITE : 0;
     p.slabs = (float*)(ws + l.slabs); p.k_per = l.plan.k_per;
+    p.w_rows = 8;                                          // fewer where that leaves few workgroups
+    while (p.w_rows > 1 && hidden / p.w_rows < 128) p.w_rows /= 2;
     if (dw) {
         hipLaunchKernelGGL(xent_room_kernel, dim3((m + 3) / 4), dim3(ROW_THREADS), 0, s, h, ldh, targets, dloss, scale, m, hidden, vocab, p.room);
         CHIMERA_LAUNCH_CHECK("linear cross-entropy");
@@ -792,7 +803,8 @@ int xent_bwd_bf16(int m, int hidden, int vocab, const bf16_t* h, int ldh, const 
     int splits = 0;
     for (int i = 0; i <= pieces; ++i) {
         p.now = p.next;
-        int count[5] = {};
+        int (&count)[5] = p.count;
+        std::fill(std::begin(count), std::end(count), 0);
         if (i > 0) {
             if (dw) {
                 p.dw_r = raster_of<Pass::Raster>(l.plan.dw_tile, hidden, p.now.ld, 2 * l.mp);
@@ -812,11 +824,14 @@ int xent_bwd_bf16(int m, int hidden, int vocab, const bf16_t* h, int ldh, const 
             p.next = {v0, cols, round_up(cols, 8), (_Float16*)(ws + l.dz[at]), (_Float16*)(ws + l.w[at]), (int*)(ws + l.raise[at])};
             p.dz_r = raster_of<Pass::Raster>(l.plan.tok_tile, l.mp, p.next.ld, hidden);
             count[2] = p.dz_r.tiles_m * p.dz_r.tiles_n;
-            if (dh) count[3] = (hidden + W_ROWS_PER_WG - 1) / W_ROWS_PER_WG;
+            if (dh) count[3] = (hidden + p.w_rows - 1) / p.w_rows;
             if (dw && i == 0) count[4] = (int)std::min<long>((long)((l.mp + TURN_TOKENS - 1) / TURN_TOKENS) * ((hidden + TURN_COLS - 1) / TURN_COLS), TURN_WGS);
         }
+        // The longest first.  Where dz has few tiles these are the rows, which wait for memory (1 x 128 x 44312 64 -> 39 us; but 8192 x 2048 x 32768, 1024 tiles,
+        // 3555 -> 3585).
+        const bool rows_first = i == 0 && count[2] <= 2 * NUM_CUS;
         int total = 0;
-        for (int k = 0; k < 5; ++k) { p.first[k] = total; total += count[k]; }
+        for (int k : rows_first ? std::array{4, 3, 2, 1, 0} : std::array{0, 1, 2, 3, 4}) { p.first[k] = total; total += count[k]; }
         if (l.plan.dw_tile == 256 && l.plan.tok_tile == 256) hipLaunchKernelGGL((xent_pass_kernel<256, 256>), dim3(total), dim3(512), 0, s, p);
         else if (l.plan.dw_tile == 256) hipLaunchKernelGGL((xent_pass_kernel<256, 128>), dim3(total), dim3(512), 0, s, p);
         else hipLaunchKernelGGL((xent_pass_kernel<128, 128>), dim3(total), dim3(512), 0, s, p);

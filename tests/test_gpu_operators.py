@@ -161,7 +161,7 @@ def _check_backward(dtype, h, w, targets, lse, scale, dloss, dh, dw, dw0):
 # (1024 x 9300), dh (4100 x 2304: more 256x256 tiles than 128x128 ones pay for) and dW (1000 x 9473)
 BWD = [(1, 8, 1, 8, 0), (1, 64, 7, 16, 0), (2, 8, 8, 8, 0), (3, 16, 9, 24, 0), (24, 256, 1000, 1000, 0), (33, 72, 257, 264, 256), (130, 136, 1027, 1088, 256),
        (260, 264, 771, 776, 512), (60, 512, 8000, 8000, 0), (1024, 64, 9300, 9304, 0), (40, 1000, 9473, 9480, 4864), (2200, 128, 2001, 2008, 0),
-       (4100, 2304, 1031, 1032, 512)]
+       (4100, 2304, 1031, 1032, 512), (3000, 256, 30001, 30008, 0)]
 
 
 @pytest.mark.parametrize("dtype", [b.F32, b.BF16])
@@ -263,6 +263,27 @@ def test_linear_xent_captured_and_on_another_stream():
         torch.cuda.synchronize()
         assert torch.equal(rows2, rows) and torch.equal(lse2, lse) and torch.equal(dh2, want[0]) and torch.equal(dw2[:, :3001], want[1])
         assert abs(float(loss2) + 3.0 - (float(loss) - 0.5)) <= 1e-5
+
+
+def test_linear_xent_two_calls_at_once():
+    torch = _torch()
+    cases = [_case(b.BF16, 700, 256, 5003, seed=s) for s in (1, 2)]
+    alone, streams = [], [torch.cuda.Stream(), torch.cuda.Stream()]
+    for h, w, targets in cases:
+        rows, lse, _ = _forward(h, w, targets, 0.1)
+        alone.append((rows, lse) + _backward(b.BF16, h, w, targets, lse, 0.1, piece=2048, overwrite=True)[:2])
+    torch.cuda.synchronize()
+    got = [None, None]
+    for _ in range(3):
+        for i, (h, w, targets) in enumerate(cases):
+            with torch.cuda.stream(streams[i]):
+                rows, lse, _ = _forward(h, w, targets, 0.1)
+                dh, dw = torch.empty_like(h, memory_format=torch.contiguous_format), torch.empty((256, 5008), device="cuda")
+                ws = b.chimera_op_linear_xent_bwd(h, w, targets, lse, 0.1, dh, dw[:, :5003], overwrite=True, piece=2048)
+                got[i] = (rows, lse, dh, dw[:, :5003], ws)
+        torch.cuda.synchronize()
+        for i in range(2):
+            assert all(torch.equal(x, y) for x, y in zip(got[i], alone[i]))
 
 
 @pytest.mark.parametrize("dtype", [b.F32, b.BF16])

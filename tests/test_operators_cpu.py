@@ -95,7 +95,7 @@ def test_grad_norm_workspace():
     assert b.lib().chimera_op_grad_norm_workspace_bytes(0) == 0 and b.lib().chimera_op_grad_norm_workspace_bytes(-1) == 0
 
 
-def adamw(dtype=b.BF16, bits=32, n=(16, 0, 9), param=(P, None, 2 * P), master=(P, None, P), grad=(P, None, P), m=(P, None, P), v=(P, None, P),
+def adamw(dtype=b.BF16, bits=32, n=(16, 0, 9), param=(P, None, 2 * P), master=(P, None, 2 * P), grad=(P, None, P), m=(P, None, 2 * P), v=(2 * P, None, P),
           scale=None, decay=None, hyper=(1e-3, 0.9, 0.95, 1e-8, 1, 0), device=None, count=None):
     arr = lambda x: None if x is None else (C.c_void_p * len(x))(*x)  # noqa: E731
     h = None if hyper is None else C.byref(b.AdamWHyper(*hyper))
@@ -109,7 +109,7 @@ NAN, INF = float("nan"), float("inf")
 @pytest.mark.parametrize("bad", [dict(dtype=3), dict(bits=16), dict(bits=0), dict(count=0), dict(count=-5), dict(n=(16, 0, -9)), dict(n=(16, 0, (1 << 32) + 1)),
                                  dict(param=None), dict(master=None), dict(grad=None), dict(m=None), dict(v=None), dict(bits=8), dict(param=(P, None, None)),
                                  dict(master=(P, None, None)), dict(grad=(None, None, P)), dict(bits=8, scale=(P, None, None)), dict(param=(P, None, P)),
-                                 dict(param=(P, None, P + 30)), dict(param=(P + 1, None, 2 * P)), dict(grad=(P + 2, None, P)), dict(m=(P + 1, None, P)),
+                                 dict(param=(P, None, P + 30)), dict(master=(P, None, P + 60)), dict(m=(2 * P, None, 2 * P + 32)), dict(v=(P + 32, None, P)), dict(param=(P + 1, None, 2 * P)), dict(grad=(P + 2, None, P)), dict(m=(P + 1, None, P)),
                                  dict(decay=(0.0, 0.0, -0.1)), dict(decay=(NAN, 0.0, 0.1)), dict(decay=(0.1, 0.0, INF)), dict(hyper=None), dict(device=P + 8),
                                  dict(hyper=(-1e-3, 0.9, 0.95, 1e-8, 1, 0)), dict(hyper=(NAN, 0.9, 0.95, 1e-8, 1, 0)), dict(hyper=(1e-3, 1.0, 0.95, 1e-8, 1, 0)),
                                  dict(hyper=(1e-3, 0.9, -0.1, 1e-8, 1, 0)), dict(hyper=(1e-3, 0.9, 0.95, 0.0, 1, 0)), dict(hyper=(1e-3, 0.9, 0.95, 1e-40, 1, 0)), dict(hyper=(1e-3, 0.9, 0.95, 2.0, 1, 0)), dict(hyper=(1e-3, 0.9, 0.95, 1e-8, 0, 0))],
@@ -138,8 +138,28 @@ def test_adamw_handle_checks_its_lists():
     torch = pytest.importorskip("torch")
     t = lambda n, d=torch.float32: torch.zeros(n, dtype=d)  # noqa: E731
     for bad in (dict(grads=[t(4)]), dict(grads=[t(4), t(4)]), dict(decay=[0.1]), dict(scales=[t(2)]), dict(scales=[t(2), t(1)]),
-                dict(grads=[t(4), t((9, 2))[:, 0]]), dict(masters=[t(4), t(8)])):
+                dict(grads=[t(4), t((9, 2))[:, 0]]), dict(masters=[t(4), t(8)]),
+                dict(params=[t(4), t(9, torch.float16)]), dict(grads=[t(4), t(9, torch.bfloat16)]), dict(ms=[t(4), t(9, torch.uint8)]),
+                dict(scales=[t(2), t(2)]), dict(params=[])):
         args = dict(params=[t(4), t(9)], grads=[t(4), t(9)], ms=[t(4), t(9)], vs=[t(4), t(9)])
         args.update(bad)
         with pytest.raises(ValueError):
             b.AdamW(**args)
+
+
+def test_binding_checks_matrices_and_vectors():
+    torch = pytest.importorskip("torch")
+    z = lambda *s, d=torch.float32: torch.zeros(s, dtype=d)  # noqa: E731
+    i32 = torch.int32
+    good = dict(h=z(3, 16), w=z(16, 24), targets=z(3, d=i32), scale=1.0, loss_rows=z(3), lse=z(3), loss=z(1), workspace=z(8, d=torch.uint8))
+    for bad in (dict(h=z(16, 3).t()), dict(w=z(16, 24, d=torch.bfloat16)), dict(w=z(24, 16).t()), dict(targets=z(3, d=torch.int64)), dict(targets=z(4, d=i32)),
+                dict(loss_rows=z(6)[::2]), dict(lse=z(3, d=torch.float64)), dict(loss=z(2))):
+        with pytest.raises(ValueError):
+            b.chimera_op_linear_xent_fwd(**dict(good, **bad))
+    good = dict(h=z(3, 16), w=z(16, 24), targets=z(3, d=i32), lse=z(3), scale=1.0, dh=z(3, 16), dw=z(16, 24), workspace=z(8, d=torch.uint8))
+    for bad in (dict(dh=z(3, 8)), dict(dw=z(16, 16)), dict(dw=z(16, 24, d=torch.bfloat16)), dict(dloss=z(2)), dict(dh=z(16, 3).t())):
+        with pytest.raises(ValueError):
+            b.chimera_op_linear_xent_bwd(**dict(good, **bad))
+    for grads, out in (([z(4, d=torch.bfloat16)], z(2)), ([z(4, 2)[:, 0]], z(2)), ([z(4)], z(3))):
+        with pytest.raises(ValueError):
+            b.chimera_op_grad_norm(grads, 1.0, out, workspace=z(8, d=torch.uint8))
