@@ -760,8 +760,9 @@ __device__ __forceinline__ void lds_dma16_s(const void* sbase, unsigned voff, un
     asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(sbase), "{m0}"(lds_base) : "memory");
 }
 // A tile's own way to end (ONLY_EPI = EPI_OWN), in place of the epilogues above: begin() ahead of the k loop, end() with the accumulators
-// once every wavefront has left it.  F16: operands of fp16 in place of bf16.  PAIRED (A k-contiguous, B index-contiguous): the contraction takes every k of A
-// twice, with the row of B and with the one own_end.pair elements behind it, 32 k of A a step.
+// once every wavefront has left it.  F16: operands of fp16 in place of bf16.  PAIRED (A k-contiguous, B index-contiguous, k a multiple of RK): the contraction
+// takes every k of A twice, with the row of B and with the one own_end.pair elements behind it, 32 k of A a step.  The tiles of eight wavefronts over an
+// undivided contraction request and read these 32 k once (ALONE): a row of LDS holds those of rows r and BM / 2 + r.
 constexpr int EPI_OWN = 6;
 struct NoEnd {};
 template <int BM, int BN, int WGM, int WGN, int WGK, bool A_KC, bool B_KC, int ONLY_EPI, bool F16 = false, bool PAIRED = false, bool TOUCH = false, typename End = NoEnd>
@@ -773,7 +774,8 @@ __device__ __forceinline__ void gemm_ring_tile(
     using Lds = RingLds<BM, BN, WGM, WGN, WGK>;
     constexpr int NT = WGM * WGN * WGK * 64, NS = Lds::STAGES;
     constexpr int WM = BM / WGM, WN = BN / WGN, TM = WM / 16, TN = WN / 16, HM = TM / 2;      // 16x16 tiles per wavefront
-    constexpr int CA = BM * (RK / 8) / NT, CB = BN * (RK / 8) / NT, CS = CA + CB;     // 16-byte pieces per thread and stage
+    constexpr bool ALONE = PAIRED && WGK == 1;
+    constexpr int CA = BM * (RK / 8) / NT / (ALONE ? 2 : 1), CB = BN * (RK / 8) / NT, CS = CA + CB;     // 16-byte pieces per thread and stage
     constexpr unsigned STAGE = Lds::STAGE, ABYTES = BM * RK * 2;
 
     const int nblk = tiles_m * tiles_n;
@@ -803,7 +805,7 @@ __device__ __forceinline__ void gemm_ring_tile(
         if (kc) {
             const int row = slot >> 3;
             kk = ((slot & 7) ^ rswz(row)) * 8;
-            return (unsigned)((min(row0 + row, nrows - 1) - row0) * ld + (PAIRED ? kk & 31 : kk)) * 2u;
+            return (unsigned)((min(row0 + row + (ALONE ? (kk >> 5) * (BM / 2) : 0), nrows - 1) - row0) * ld + (PAIRED ? kk & 31 : kk)) * 2u;
         }
         kk = slot / (rows / 8);
         const int pc = slot % (rows / 8), ic = (((pc >> 1) ^ rkswz(kk)) << 1) | (pc & 1);
@@ -830,6 +832,7 @@ __device__ __forceinline__ void gemm_ring_tile(
     }
     static_assert(KIA % 16 == 0 && KIB % 16 == 0, "requests of one lane share a swizzle");
     static_assert(!PAIRED || (A_KC && !B_KC && KIB <= 32), "a request of B lies within 32 rows");
+    static_assert(!ALONE || WGM == 2, "a half of the rows each");
     constexpr int ROWS = PAIRED ? RK / 2 : RK;
     const size_t step_a = (A_KC ? (size_t)ROWS : (size_t)RK * lda) * 2, step_b = (B_KC ? (size_t)RK : (size_t)ROWS * ldb) * 2;
     const unsigned lds0 = lds_address(lds), dma0 = lds0 + wave * 1024;
@@ -883,7 +886,7 @@ __device__ __forceinline__ void gemm_ring_tile(
         return lds0 + (unsigned)(kk * rows * 2 + ((row0 >> 4) ^ rkswz(kk)) * 32 + (l16 & 3) * 8);
     };
 #pragma unroll
-    for (int a = 0; a < NPA; ++a) pa[a] = read_base(std::integral_constant<int, BM>{}, A_KC, wm0, WGK == 2 ? wk : a);
+    for (int a = 0; a < NPA; ++a) pa[a] = read_base(std::integral_constant<int, BM>{}, A_KC, ALONE ? 0 : wm0, ALONE ? wm0 / (BM / 2) : WGK == 2 ? wk : a);
 #pragma unroll
     for (int b = 0; b < NPB; ++b) pb[b] = read_base(std::integral_constant<int, BN>{}, B_KC, wn0, WGK == 2 ? wk : b) + ABYTES;
     auto read_tr = [&](unsigned p, int rows) {                 // rows k and k + 4 share a swizzle
@@ -1022,12 +1025,12 @@ __device__ __forceinline__ void gemm_ring_tile(
                 phase(CHIMERA_C(1), CHIMERA_C(0), sums_c, [&](auto i_c) {
                     constexpr int i = decltype(i_c)::value;
                     if constexpr (i < TN) read_b(i_c, CHIMERA_C(1), q_c);
-                    else if constexpr (i < TN + HM) read_a(CHIMERA_C(i - TN), CHIMERA_C(1), q_c);
+                    else if constexpr (i < TN + HM) { if constexpr (!ALONE) read_a(CHIMERA_C(i - TN), CHIMERA_C(1), q_c); }
                     else if constexpr (TOUCH && always && i == TN + HM) touch();
                 });
                 phase(CHIMERA_C(0), CHIMERA_C(1), sums_c, [&](auto i_c) {
                     constexpr int i = decltype(i_c)::value;
-                    if constexpr (i < HM) read_a(CHIMERA_C(HM + i), CHIMERA_C(1), q_c);
+                    if constexpr (i < HM && !ALONE) read_a(CHIMERA_C(HM + i), CHIMERA_C(1), q_c);
                 });
                 if constexpr (TOUCH && always) arrived(CHIMERA_C(1));          // the youngest is the touch
                 else arrived(CHIMERA_C(0));
