@@ -99,7 +99,7 @@ _SIGNATURES = {
     "chimera_head_loss_pieces": (_i, [_i] * 4 + [_p] * 5 + [_i, C.c_float] + [_p] * 5 + [_i, _p, _sz, _p]),
     "chimera_op_grad_norm_workspace_bytes": (_sz, [_i]),
     "chimera_op_grad_norm": (_i, [_i, _p, _p, C.c_float, _p, _p, _sz, _p]),
-    "chimera_op_adamw": (_i, [_i, _i, _i] + [_p] * 11),
+    "chimera_op_adamw": (_i, [_i, _i, _i] + [_p] * 12),
     "chimera_stage_adamw_state_bytes": (_sz, [_p, _i]),
     "chimera_stage_adamw_init": (_i, [_p, _p, _p, _i]),
     "chimera_stage_adamw_step": (_i, [_p, _p, _p, _i, C.c_float, _p, _p, _p]),
@@ -543,7 +543,19 @@ def _rows(t, dtype, what):
 def _vector(t, dtype, n, what):
     if t is not None and (t.dtype != dtype or t.numel() != n or not t.is_contiguous()):
         raise ValueError("%s: %d contiguous values of %s expected" % (what, n, dtype))
-    return _ptr(t)
+    return None if t is None else t.data_ptr()
+
+
+def _stream_of(*tensors):
+    """The current stream of the current GPU, which has to hold all of the tensors (None: not given)."""
+    import torch
+    at = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != at:
+            at = -1
+    if at < 0 or at != torch.cuda.current_device():
+        raise ValueError("tensors on the current GPU expected")
+    return torch._C._cuda_getCurrentRawStream(at)       # (as current_stream().cuda_stream, without the 2 us of the object between)
 
 
 def chimera_op_linear_xent_fwd(h, w, targets, scale, loss_rows, lse, loss=None, workspace=None):
@@ -554,9 +566,10 @@ def chimera_op_linear_xent_fwd(h, w, targets, scale, loss_rows, lse, loss=None, 
     if workspace is None:
         workspace = torch.empty(lib().chimera_op_linear_xent_fwd_workspace_bytes(_dt(h), tokens, hidden, vocab), dtype=torch.uint8, device=h.device)
     f = torch.float32
-    check(lib().chimera_op_linear_xent_fwd(_dt(h), tokens, hidden, vocab, _ptr(h), _rows(h, h.dtype, "h"), _ptr(w), _rows(w, h.dtype, "w"),
+    check(lib().chimera_op_linear_xent_fwd(_dt(h), tokens, hidden, vocab, h.data_ptr(), _rows(h, h.dtype, "h"), w.data_ptr(), _rows(w, h.dtype, "w"),
                                            _vector(targets, torch.int32, tokens, "targets"), scale, _vector(loss_rows, f, tokens, "loss_rows"),
-                                           _vector(lse, f, tokens, "lse"), _vector(loss, f, 1, "loss"), _ptr(workspace), workspace.numel(), _stream(h)))
+                                           _vector(lse, f, tokens, "lse"), _vector(loss, f, 1, "loss"), workspace.data_ptr(), workspace.numel(),
+                                           _stream_of(h, w, targets, loss_rows, lse, loss, workspace)))
     return workspace
 
 
@@ -569,10 +582,11 @@ def chimera_op_linear_xent_bwd(h, w, targets, lse, scale, dh=None, dw=None, dlos
     f = torch.float32
     if (dh is not None and dh.shape != h.shape) or (dw is not None and dw.shape != w.shape):
         raise ValueError("dh and dw have the shapes of h and w")
-    check(lib().chimera_op_linear_xent_bwd(_dt(h), tokens, hidden, vocab, _ptr(h), _rows(h, h.dtype, "h"), _ptr(w), _rows(w, h.dtype, "w"),
+    check(lib().chimera_op_linear_xent_bwd(_dt(h), tokens, hidden, vocab, h.data_ptr(), _rows(h, h.dtype, "h"), w.data_ptr(), _rows(w, h.dtype, "w"),
                                            _vector(targets, torch.int32, tokens, "targets"), _vector(lse, f, tokens, "lse"), scale,
-                                           _vector(dloss, f, tokens, "dloss"), _ptr(dh), 0 if dh is None else _rows(dh, h.dtype, "dh"), _ptr(dw),
-                                           0 if dw is None else _rows(dw, f, "dw"), int(overwrite), piece, _ptr(workspace), workspace.numel(), _stream(h)))
+                                           _vector(dloss, f, tokens, "dloss"), None if dh is None else dh.data_ptr(),
+                                           0 if dh is None else _rows(dh, h.dtype, "dh"), None if dw is None else dw.data_ptr(), 0 if dw is None else _rows(dw, f, "dw"), int(overwrite), piece, workspace.data_ptr(), workspace.numel(),
+                                           _stream_of(h, w, targets, lse, dh, dw, dloss, workspace)))
     return workspace
 
 
@@ -583,11 +597,16 @@ def chimera_head_loss_pieces(y, targets, lnf_g, lnf_b, w_head, scale, dy, dlnf_g
     ldw = _rows(w_head, y.dtype, "w_head")
     if _rows(dw_head, torch.float32, "dw_head") != ldw or dw_head.shape[0] != hidden or dw_head.shape[1] < vocab:
         raise ValueError("dw_head has the rows of w_head, as far apart")
+    if dy.shape != y.shape or dy.dtype != y.dtype or not (y.is_contiguous() and dy.is_contiguous()):
+        raise ValueError("y and dy: contiguous, of one shape and type")
+    f = torch.float32
     if workspace is None:
         workspace = torch.empty(lib().chimera_head_pieces_workspace_bytes(_dt(y), tokens, hidden, vocab, piece), dtype=torch.uint8, device=y.device)
-    check(lib().chimera_head_loss_pieces(_dt(y), tokens, hidden, vocab, _ptr(y), _vector(targets, torch.int32, tokens, "targets"), _ptr(lnf_g), _ptr(lnf_b),
-                                         _ptr(w_head), ldw, scale, _ptr(dy), _ptr(dlnf_g), _ptr(dlnf_b), _ptr(dw_head), _ptr(loss), piece,
-                                         _ptr(workspace), workspace.numel(), _stream(y)))
+    check(lib().chimera_head_loss_pieces(_dt(y), tokens, hidden, vocab, y.data_ptr(), _vector(targets, torch.int32, tokens, "targets"),
+                                         _vector(lnf_g, y.dtype, hidden, "lnf_g"), _vector(lnf_b, y.dtype, hidden, "lnf_b"), w_head.data_ptr(), ldw, scale, dy.data_ptr(),
+                                         _vector(dlnf_g, f, hidden, "dlnf_g"), _vector(dlnf_b, f, hidden, "dlnf_b"), dw_head.data_ptr(), _vector(loss, f, 1, "loss"), piece,
+                                         workspace.data_ptr(), workspace.numel(),
+                                         _stream_of(y, targets, lnf_g, lnf_b, w_head, dy, dlnf_g, dlnf_b, dw_head, loss, workspace)))
     return workspace
 
 
@@ -615,12 +634,12 @@ def chimera_op_grad_norm(grads, max_norm, out, workspace=None):
     n = _counts(grads)
     if workspace is None:
         workspace = torch.empty(lib().chimera_op_grad_norm_workspace_bytes(len(grads)), dtype=torch.uint8, device=out.device)
-    check(lib().chimera_op_grad_norm(len(grads), n, _pointers(grads), max_norm, _ptr(out), _ptr(workspace), workspace.numel(), _stream(out)))
+    check(lib().chimera_op_grad_norm(len(grads), n, _pointers(grads), max_norm, out.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_of(out, workspace, *grads)))
     return workspace
 
 
 class AdamW:
-    """The argument arrays of chimera_op_adamw for a list of tensors, kept from step to step.
+    """The argument arrays of chimera_op_adamw for a list of tensors of the current GPU, kept from step to step.
 
     params: float32, or bfloat16 with float32 `masters`; grads: float32.  32-bit moments: ms, vs float32 and scales None; 8-bit: ms, vs
     float8_e4m3fn (or uint8) and scales float32, a pair for each 256 elements of a tensor.  decay: a number per tensor, or None."""
@@ -645,6 +664,7 @@ class AdamW:
         if scales is not None and any(a.numel() != 2 * ((p.numel() + 255) // 256) for a, p in zip(scales, params)):
             raise ValueError("scales: a pair for each 256 elements")
         self.tensors = lists                               # the library borrows them
+        _stream_of(*(t for x in (params, grads, ms, vs, masters or [], scales or []) for t in x))
         self.dtype, self.bits, self.count = _dt(params[0]), 32 if scales is None else 8, len(params)
         self.n, self.param, self.grad, self.m, self.v = _counts(params), _pointers(params), _pointers(grads), _pointers(ms), _pointers(vs)
         self.master, self.scale = _pointers(masters), _pointers(scales)
@@ -653,7 +673,9 @@ class AdamW:
 
     def step(self, lr, step, seed=0, grad_scale=None, d_hyper=None):
         """grad_scale: device float or None; d_hyper: device copy of an AdamWHyper in ADAMW_HYPER_BYTES bytes, used in place of lr, step and seed."""
+        import torch
         h = self.hyper
         h.lr, h.step, h.seed = lr, step, seed
         check(lib().chimera_op_adamw(self.dtype, self.bits, self.count, self.n, self.param, self.master, self.grad, self.m, self.v, self.scale,
-                                     self.decay, C.byref(h), _ptr(d_hyper), _ptr(grad_scale), _stream(self.tensors[0][0])))
+                                     self.decay, C.byref(h), _ptr(d_hyper), _vector(grad_scale, torch.float32, 1, "grad_scale"),
+                                     _stream_of(self.tensors[0][0], grad_scale, d_hyper)))

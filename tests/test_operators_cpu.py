@@ -163,3 +163,40 @@ def test_binding_checks_matrices_and_vectors():
     for grads, out in (([z(4, d=torch.bfloat16)], z(2)), ([z(4, 2)[:, 0]], z(2)), ([z(4)], z(3))):
         with pytest.raises(ValueError):
             b.chimera_op_grad_norm(grads, 1.0, out, workspace=z(8, d=torch.uint8))
+
+
+def test_binding_refuses_tensors_that_are_not_on_the_current_gpu():
+    torch = pytest.importorskip("torch")
+    z = lambda *s, d=torch.float32: torch.zeros(s, dtype=d)  # noqa: E731
+    i32, ws = torch.int32, z(8, d=torch.uint8)
+    t = dict(params=[z(4), z(9)], grads=[z(4), z(9)], ms=[z(4), z(9)], vs=[z(4), z(9)])
+    for call in (lambda: b.chimera_op_linear_xent_fwd(z(3, 16), z(16, 24), z(3, d=i32), 1.0, z(3), z(3), workspace=ws),
+                 lambda: b.chimera_op_linear_xent_bwd(z(3, 16), z(16, 24), z(3, d=i32), z(3), 1.0, dw=z(16, 24), workspace=ws),
+                 lambda: b.chimera_head_loss_pieces(z(3, 16), z(3, d=i32), z(16), z(16), z(16, 24), 1.0, z(3, 16), z(16), z(16), z(16, 24), z(1), workspace=ws),
+                 lambda: b.chimera_op_grad_norm([z(4)], 1.0, z(2), workspace=ws), lambda: b.AdamW(**t)):
+        with pytest.raises(ValueError, match="current GPU"):
+            call()
+
+
+def test_head_in_pieces_checks_its_tensors():
+    torch = pytest.importorskip("torch")
+    z = lambda *s, d=torch.float32: torch.zeros(s, dtype=d)  # noqa: E731
+    good = dict(y=z(3, 16), targets=z(3, d=torch.int32), lnf_g=z(16), lnf_b=z(16), w_head=z(16, 24), scale=1.0, dy=z(3, 16), dlnf_g=z(16), dlnf_b=z(16),
+                dw_head=z(16, 24), loss=z(1), workspace=z(8, d=torch.uint8))
+    for bad, what in ((dict(y=z(16, 3).t()), "contiguous"), (dict(dy=z(3, 32)[:, :16]), "contiguous"), (dict(dy=z(3, 8)), "one shape"), (dict(lnf_g=z(8)), "lnf_g"),
+                      (dict(lnf_b=z(16, d=torch.bfloat16)), "lnf_b"), (dict(dlnf_g=z(32)[::2]), "dlnf_g"), (dict(dlnf_b=z(16, d=torch.float64)), "dlnf_b"),
+                      (dict(loss=z(2)), "loss"), (dict(targets=z(3, d=torch.int64)), "targets"), (dict(dw_head=z(16, 32)), "w_head")):
+        with pytest.raises(ValueError, match=what):
+            b.chimera_head_loss_pieces(**dict(good, **bad))
+
+
+def test_every_argument_has_a_type():
+    """Arguments behind the declared ones travel as 32-bit numbers, pointers cut in half among them."""
+    import os
+    import re
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "chimera.h")).read()
+    text = re.sub(r"/\*.*?\*/", "", text, flags=re.S)
+    declared = {name: 0 if args.strip() in ("", "void") else args.count(",") + 1 for name, args in re.findall(r"\b(chimera_\w+)\s*\(([^()]*)\)\s*;", text)}
+    assert "chimera_op_adamw" in declared
+    for name, (_, args) in b._SIGNATURES.items():
+        assert declared.get(name) == len(args), name
