@@ -77,10 +77,10 @@ int gemm_reference(int dtype, const GemmArgs& g, void* stream);
 bool gemm_f32_supports(const GemmArgs& g);
 int gemm_f32(const GemmArgs& g, void* stream);
 bool gemm_f32_group_supports(int count, const GemmArgs* g);
-// C = A B^T or C += A B^T (both k-contiguous) with the contraction cut into `splits` parts, each with a C of its own, `slab` floats after the last;
-// gemm_f32_splits: parts that fill the chip, each at least 512 long
-int gemm_f32_splits(int m, int n, int k);
-int gemm_f32_split(const GemmArgs& g, int splits, size_t slab, void* stream);
+// C = A B^T or C += A B^T (both k-contiguous) with the contraction cut into parts of `part` (a multiple of 8), each with a C of its own, `slab` floats
+// after the last; gemm_f32_part: parts that fill the chip
+int gemm_f32_part(int m, int n, int k);
+int gemm_f32_parts(const GemmArgs& g, int part, size_t slab, void* stream);
 int gemm_f32_group(int count, const GemmArgs* g, float* const* bsum, int overwrite, void* stream);
 int gemm_mfma_bf16(const GemmArgs& g, void* stream);
 bool gemm_mfma_supports(const GemmArgs& g);

@@ -19,6 +19,7 @@
 
 #include <array>
 #include <climits>
+#include <cmath>
 
 namespace chimera {
 namespace {
@@ -26,7 +27,7 @@ namespace {
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LOWEST = -3.0e38f;              // stands for the maximum of nothing: differences from it stay finite
 constexpr int TOKEN_PAD = 32;                   // the weight gradient's contraction, two rows a token, is walked in steps of 64
-constexpr int ROW_THREADS = 256;
+constexpr int ROW_THREADS = 256, ROW_FLY = 4;   // float rows: loads in flight a thread
 
 // f over the four lanes that hold a row of a 16x16 tile (l, l ^ 16, l ^ 32, l ^ 48)
 template <typename F> __device__ __forceinline__ float fold_row(float v, F f) {
@@ -196,6 +197,7 @@ struct Piece {
     _Float16* dz;                    // [mp][2][ld]: hi and lo of a token
     _Float16* w;                     // [hidden, ldp] W's rows, times 2^raise
     int* raise;                      // [hidden]
+    float* dw;                       // [parts][hidden, ld], where dW's contraction is cut
 };
 struct Pass {
     const bf16_t *h, *w;
@@ -206,14 +208,15 @@ struct Pass {
     int *room, *shift;
     _Float16* rows;                  // [hidden, mp]: h_t 2^(shift - lift_t), transposed
     Piece now, next;                 // the products' piece, and the one that dz is formed of
+    Piece past;                      // whose parts of dW are added
     // dW: columns of `now`
     float* dw;
-    int lddw, dw_flags;
+    int lddw, dw_flags, dw_per, dw_splits;       // tokens a part
     // dh: float slabs [split][m, hidden]
     float* slabs;
     int k_per, dh_flags;
     int w_rows;                      // rows of W a workgroup
-    int first[5], count[5];          // workgroups of each kind: dW, dh, dz, W's rows, h^T; and the rasters of their tiles
+    int first[6], count[6];          // workgroups of each kind: dW, dh, dz, W's rows, h^T, sums of dW; and the rasters of their tiles
     struct Raster { int tiles_m, tiles_n, group_m, band; } dw_r, dh_r, dz_r;
 };
 
@@ -264,8 +267,8 @@ struct SlabEnd {
         });
     }
 };
-// dz of a piece.  Its vector instructions are what bounds it (a tile's 65536 exponentials and conversions, with the matrix pipes idle), so a band of 32 rows
-// looks for targets only where it holds one.
+// dz of a piece.  Behind a tile's k loop come 256 KB of stores, 65536 exponentials and conversions, with the matrix pipes idle: of a round of 256 tiles at hidden
+// 2048, 61 us, some 20 (the stores 6, the exponentials 3).  A band of 32 rows looks for targets only where it holds one.
 struct RowInfo { float lse, scaled; int at; };              // coef 2^lift (0: the token does not count), the target's column in the piece
 template <int BM> struct GradEnd {
     const Pass* p;
@@ -293,6 +296,7 @@ template <int BM> struct GradEnd {
         _Float16* const first = p->next.dz + (size_t)(rb0 + pr) * 2 * ld + col;
         static_for<TO>([&](auto a_c) {
             constexpr int a = decltype(a_c)::value;
+            if (rb0 + a * 32 >= mp) return;                       // (mp is a multiple of 32)
             out.template put<a>(slab, lane);
             const bool usual = cb0 + EpiSlab<TN2>::WN <= cols && !__any((unsigned)(tab[rb0 - i0 + a * 32 + (lane & 31)].at - cb0) < (unsigned)EpiSlab<TN2>::WN);
             __builtin_amdgcn_s_waitcnt(0xc07f);                   // lgkmcnt(0): the slab is written (wavefront-private)
@@ -300,7 +304,7 @@ template <int BM> struct GradEnd {
             auto rows = [&](auto usual_c) {
 #pragma unroll
                 for (int j = 0; j < NP; ++j) {
-                    const int lr = a * 32 + j * RPP + pr, row = rb0 + lr;
+                    const int lr = a * 32 + j * RPP + pr;
                     const RowInfo r = tab[rb0 - i0 + lr];
                     float v[8];
                     load_vec<float>(EpiSlab<TN2>::at(slab, j * RPP + pr, pc / 4), v);
@@ -325,7 +329,8 @@ template <int BM> struct GradEnd {
                         const f32x2 rest = d - __builtin_convertvector(hi[e / 2], f32x2);
                         lo[e / 2] = __builtin_convertvector(rest, f16x2);
                     }
-                    if (row >= mp || col >= ld) continue;
+                    if constexpr (!decltype(usual_c)::value)
+                        if (col >= ld) continue;
                     _Float16* to = first + (size_t)(a * 32 + j * RPP) * (2 * ld);
                     *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(hi);
                     *reinterpret_cast<uint4*>(to + ld) = *reinterpret_cast<const uint4*>(lo);
@@ -386,8 +391,8 @@ __device__ __forceinline__ void raise_rows(const Pass& p, int id, char* lds) {
     }
 }
 // h^T times 2^(shift - lift); tokens that do not count, and the padding behind the last one, as zeros: their dz is zero, but h may hold anything.
-// Transposed, because the matrix instructions take runs of the contraction's index: both operands of dW through the transposing LDS reads, which
-// deliver 64 bytes a clock, make its step 3072 clocks of LDS to 2048 of matrix instructions (measured: 3080; dW at 8192 x 2048 x 8192 442 us).
+// Transposed, so that dW's A is contiguous along the contraction: a tile then asks for its 32 tokens of a step once for both parts of dz (dW of 8192 x 2048 x 65536
+// 6867 -> 6822 us in all, 6813 -> 6714 with half of the requests), and its lines can be touched ahead (a step of dW 3080 -> 2457 clocks).
 constexpr int TURN_TOKENS = 64, TURN_COLS = 256, TURN_WGS = 1024;
 __device__ __forceinline__ void turn_rows(const Pass& p, int id, int wgs, char* lds) {
     int* part = reinterpret_cast<int*>(lds);
@@ -423,6 +428,27 @@ __device__ __forceinline__ void turn_rows(const Pass& p, int id, int wgs, char* 
     }
 }
 
+// dW (+)= the parts of a piece
+constexpr int SUM_WGS = 512;
+__device__ __forceinline__ void sum_columns(const Pass& p, int id, int wgs) {
+    const int fours = p.past.ld / 4;
+    const size_t stride = (size_t)p.hidden * p.past.ld, units = (size_t)p.hidden * fours;
+    for (size_t u = (size_t)id * 512 + threadIdx.x; u < units; u += (size_t)wgs * 512) {
+        const int i = (int)(u / fours), c = (int)(u % fours) * 4;
+        const float* from = p.past.dw + (size_t)i * p.past.ld + c;
+        float* to = p.dw + (size_t)i * p.lddw + p.past.v0 + c;
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+        const bool whole = c + 4 <= p.past.cols;
+        if (whole && !(p.dw_flags & ACCUM_OVERWRITE)) v = *reinterpret_cast<const f32x4*>(to);
+        for (int k = 0; k < p.dw_splits; ++k) v += *reinterpret_cast<const f32x4*>(from + k * stride);
+        if (whole) *reinterpret_cast<f32x4*>(to) = v;
+        else
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+                if (c + e < p.past.cols) to[e] = p.dw_flags & ACCUM_OVERWRITE ? v[e] : to[e] + v[e];
+    }
+}
+
 // One launch: dW and dh of a piece, dz and the rows of W of the next, and, in a pass's first, h^T.  Tiles of DW x DW for dW, of TOK x TOK for
 // the products over tokens.
 template <int DW, int TOK>
@@ -443,10 +469,12 @@ __global__ __launch_bounds__(512, 2) void xent_pass_kernel(Pass p) {
     } while (0)
     auto kind = [&](int k) { return (unsigned)(block - p.first[k]) < (unsigned)p.count[k]; };
     if (kind(0)) {
-        const int id = block - p.first[0];
-        const ColumnsEnd end{p.dw + p.now.v0, p.shift, p.hidden, p.now.cols, p.lddw, p.dw_flags, p.now.ld};
-        XENT_TILE(DW, true, false, true, true, (const bf16_t*)p.rows, (const bf16_t*)p.now.dz, p.hidden, p.now.ld, 2 * p.mp, p.mp, 2 * p.now.ld, p.dw_r, id,
-                  p.dw_r.band, true, end);
+        const int tiles = p.dw_r.tiles_m * p.dw_r.tiles_n, at = block - p.first[0], part = __builtin_amdgcn_readfirstlane(at / tiles), t0 = part * p.dw_per;
+        const bool cut = p.dw_splits > 1;
+        const ColumnsEnd end{cut ? p.now.dw + (size_t)part * p.hidden * p.now.ld : p.dw + p.now.v0, p.shift, p.hidden, cut ? p.now.ld : p.now.cols,
+                             cut ? p.now.ld : p.lddw, cut ? ACCUM_OVERWRITE : p.dw_flags, p.now.ld};
+        XENT_TILE(DW, true, false, true, true, (const bf16_t*)p.rows + t0, (const bf16_t*)p.now.dz + (size_t)t0 * 2 * p.now.ld, p.hidden, p.now.ld,
+                  2 * min(p.dw_per, p.mp - t0), p.mp, 2 * p.now.ld, p.dw_r, at - part * tiles, p.dw_r.band, true, end);
     } else if (kind(1)) {
         const int at = block - p.first[1], tiles = p.dh_r.tiles_m * p.dh_r.tiles_n, total = p.count[1];
         const int xcd = at & 7, local = at >> 3, pid = xcd * (total >> 3) + min(xcd, total & 7) + local;
@@ -459,8 +487,10 @@ __global__ __launch_bounds__(512, 2) void xent_pass_kernel(Pass p) {
                   (GradEnd<TOK>{&p, 0.f, 0.f, 0}));
     } else if (kind(3)) {
         raise_rows(p, block - p.first[3], lds);
-    } else {
+    } else if (kind(4)) {
         turn_rows(p, block - p.first[4], p.count[4], lds);
+    } else {
+        sum_columns(p, block - p.first[5], p.count[5]);
     }
 #undef XENT_TILE
 }
@@ -522,18 +552,23 @@ __global__ __launch_bounds__(ROW_THREADS) void xent_stats_f32_kernel(const float
     const int t = blockIdx.x, tid = threadIdx.x;
     const float* row = z + (size_t)t * ld;
     float2 s = make_float2(LOWEST, 0.f);
-    for (int c = tid * 4; c < cols; c += ROW_THREADS * 4) {
-        float v[4];
-        load_vec<float>(row + c, v);
-        float top = LOWEST, sum = 0.f;
+    for (int c0 = tid * 4; c0 < cols; c0 += ROW_FLY * ROW_THREADS * 4) {
+        float v[ROW_FLY][4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if (c + e >= cols) v[e] = -INFINITY;
-            top = fmaxf(top, v[e]);
+        for (int u = 0; u < ROW_FLY; ++u) load_vec<float>(row + min(c0 + u * ROW_THREADS * 4, ld - 4), v[u]);
+#pragma unroll
+        for (int u = 0; u < ROW_FLY; ++u) {
+            const int c = c0 + u * ROW_THREADS * 4;
+            float top = LOWEST, sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (c + e >= cols) v[u][e] = -INFINITY;
+                top = fmaxf(top, v[u][e]);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f((v[u][e] - top) * LOG2E);
+            s = join(s, make_float2(top, sum));
         }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f((v[e] - top) * LOG2E);
-        s = join(s, make_float2(top, sum));
     }
     const float top = wave_max(s.x);
     const float sum = wave_sum(s.y * __builtin_amdgcn_exp2f((s.x - top) * LOG2E));
@@ -552,15 +587,21 @@ __global__ __launch_bounds__(ROW_THREADS) void xent_dz_f32_kernel(float* __restr
     const int t = blockIdx.x, target = targets[t];
     const float coef = counts(target, vocab) ? (dloss ? scale * dloss[t] : scale) : 0.f, l = lse[t];
     float* row = z + (size_t)t * ld;
-    for (int c = threadIdx.x * 4; c < ld; c += ROW_THREADS * 4) {
-        float v[4];
-        load_vec<float>(row + c, v);
+    for (int c0 = threadIdx.x * 4; c0 < ld; c0 += ROW_FLY * ROW_THREADS * 4) {
+        float v[ROW_FLY][4] = {};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float d = __builtin_amdgcn_exp2f((v[e] - l) * LOG2E) - (c + e == target - v0 ? 1.0f : 0.0f);
-            v[e] = coef == 0.f || c + e >= cols ? 0.f : coef * d;
+        for (int u = 0; u < ROW_FLY; ++u)
+            if (c0 + u * ROW_THREADS * 4 < ld) load_vec<float>(row + c0 + u * ROW_THREADS * 4, v[u]);
+#pragma unroll
+        for (int u = 0; u < ROW_FLY; ++u) {
+            const int c = c0 + u * ROW_THREADS * 4;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float d = __builtin_amdgcn_exp2f((v[u][e] - l) * LOG2E) - (c + e == target - v0 ? 1.0f : 0.0f);
+                v[u][e] = coef == 0.f || c + e >= cols ? 0.f : coef * d;
+            }
+            if (c < ld) store_vec<float>(row + c, v[u]);
         }
-        store_vec<float>(row + c, v);
     }
 }
 // up to three columns of a wider matrix: to (+)= from [rows, 4]
@@ -597,25 +638,34 @@ int default_piece(int dtype, int m, int hidden, int vocab) {
     const int most = (int)std::min<size_t>(all, std::max<size_t>(usual / PIECE_STEP * PIECE_STEP, PIECE_STEP));
     return round_up((vocab + (vocab + most - 1) / most - 1) / ((vocab + most - 1) / most), PIECE_STEP);        // equal pieces
 }
-// The launches' tiles, and the splits of dh's contraction.  256x256 tiles where the products of a piece fill the chip with them; rows of 128 for
+// The launches' tiles, and where contractions are cut.  256x256 tiles where the products of a piece fill the chip with them; rows of 128 for
 // up to 128 tokens.  dh's tiles are cut along the vocabulary
 // to half of what a CU has to do in all, or 32 steps, whichever is more (a third and a quarter: 1380 -> 1400 us at 2048 x 1600 x 50256, 360 -> 388 at 512 x 1024,
-// every part is read and written once a piece).
-struct PassPlan { int dw_tile, tok_tile, splits, k_per; };
+// every part is read and written once a piece).  dW's are cut along the tokens, to what a CU has to do in all, where one would outlast that by a fifth, as many
+// tokens on few columns of h do; their parts are added a pass later (8192 x 256 x 50304 3012 -> 1320 us, 1407 in shorter parts, 1537 uncut in 128x128 tiles;
+// 8192 x 768 2994 -> 2540, 2628, 2734; 16384 x 768 10300 -> 5118, 5204, 5593; 4096 x 768 1493 -> 1392, 1489, 1342).
+struct PassPlan { int dw_tile, tok_tile, splits, k_per, dw_splits, dw_per; };
 PassPlan plan_of(int mp, int hidden, int ld) {
     PassPlan p{};
     const long all256 = tiles_of(hidden, ld, 256) + tiles_of(mp, ld, 256);
     p.dw_tile = tiles_of(hidden, ld, 256) >= 128 || all256 >= 320 ? 256 : 128;
     p.tok_tile = p.dw_tile == 256 && mp > 128 ? 256 : 128;
     auto work = [](int tile, long tiles, long steps) { return tiles * steps * (tile == 256 ? 1.0 : 0.35); };        // in steps of a 256x256 tile
-    const long dw_steps = mp / 32, dh_steps = (ld + 63) / 64, z_steps = (hidden + 63) / 64;
-    const double each = (work(p.dw_tile, tiles_of(hidden, ld, p.dw_tile), dw_steps) + work(p.tok_tile, tiles_of(mp, hidden, p.tok_tile), dh_steps) +
+    const long dw_tiles = tiles_of(hidden, ld, p.dw_tile), dw_steps = mp / 32, dh_steps = (ld + 63) / 64, z_steps = (hidden + 63) / 64;
+    const double each = (work(p.dw_tile, dw_tiles, dw_steps) + work(p.tok_tile, tiles_of(mp, hidden, p.tok_tile), dh_steps) +
                          work(p.tok_tile, tiles_of(mp, ld, p.tok_tile), z_steps)) / NUM_CUS;
     const double share = p.tok_tile == 256 ? each : each / 0.35;
     const long most = std::max<long>(8, (long)(share < 32 ? share : std::max(32.0, share / 2)));
     const long splits = std::min<long>((dh_steps + most - 1) / most, 64), per = (dh_steps + splits - 1) / splits;
     p.splits = (int)((dh_steps + per - 1) / per);
     p.k_per = (int)per * 64;
+    const long rounds = (dw_tiles + NUM_CUS - 1) / NUM_CUS;
+    p.dw_per = mp;
+    if (work(p.dw_tile, rounds, dw_steps) > 1.2 * each && dw_steps >= 64) {
+        const long parts = std::min<long>((long)std::ceil(dw_steps / std::max(32.0, each / work(p.dw_tile, 1, 1))), 16);
+        p.dw_per = (int)((dw_steps + parts - 1) / parts) * 32;
+    }
+    p.dw_splits = (mp + p.dw_per - 1) / p.dw_per;
     return p;
 }
 
@@ -633,7 +683,7 @@ FwdLayout fwd_layout(int dtype, int m, int hidden, int vocab) {
     l.total = b;
     return l;
 }
-struct BwdLayout { int piece, ld, mp, ldp, buffers, f32_splits; PassPlan plan; size_t room, shift, rows, dz[2], w[2], raise[2], slabs, columns, total; };
+struct BwdLayout { int piece, ld, mp, ldp, buffers, f32_part; PassPlan plan; size_t room, shift, rows, dz[2], w[2], raise[2], dw[2], slabs, columns, total; };
 BwdLayout bwd_layout(int dtype, int m, int hidden, int vocab, int piece) {
     BwdLayout l{};
     size_t b = 0;
@@ -644,8 +694,9 @@ BwdLayout bwd_layout(int dtype, int m, int hidden, int vocab, int piece) {
         l.mp = m;
         l.rows = take((size_t)m * hidden * 4);
         l.dz[0] = take((size_t)m * l.ld * 4);
-        l.f32_splits = gemm_f32_splits(m, hidden, l.ld & ~7);
-        l.slabs = take((size_t)l.f32_splits * m * hidden * 4);
+        const int whole = std::max(8, std::min(l.ld, vocab) & ~7);
+        l.f32_part = gemm_f32_part(m, hidden, whole);
+        l.slabs = take((size_t)((whole + l.f32_part - 1) / l.f32_part) * m * hidden * 4);
         l.columns = take((size_t)hidden * 16);
     } else {
         l.mp = round_up(m, TOKEN_PAD);
@@ -659,6 +710,7 @@ BwdLayout bwd_layout(int dtype, int m, int hidden, int vocab, int piece) {
             l.dz[i] = take((size_t)l.mp * l.ld * 4);
             l.w[i] = take((size_t)hidden * l.ldp * 2);
             l.raise[i] = take((size_t)hidden * 4);
+            l.dw[i] = take(l.plan.dw_splits > 1 ? (size_t)l.plan.dw_splits * hidden * l.ld * 4 : 0);
         }
         l.slabs = take((size_t)l.plan.splits * m * hidden * 4);
     }
@@ -757,10 +809,8 @@ int xent_bwd_f32(int m, int hidden, int vocab, const float* h, int ldh, const fl
             GemmArgs d{};
             d.m = m; d.n = hidden; d.k = whole; d.a = z; d.lda = ld; d.a_kc = 1; d.b = w + v0; d.ldb = ldw; d.b_kc = 1; d.c = slab;
             d.epilogue = slabs ? EPI_ACCUM_F32 : EPI_NONE;
-            // (a last piece that is too short to be cut goes into the first slab)
-            const int now = slabs && whole / l.f32_splits < 64 ? 1 : l.f32_splits;
-            XENT_TRY(gemm_f32_split(d, now, (size_t)m * hidden, stream));
-            if (!slabs) slabs = now;
+            XENT_TRY(gemm_f32_parts(d, l.f32_part, (size_t)m * hidden, stream));       // (a last piece is cut where the others are, and may have fewer parts)
+            if (!slabs) slabs = (whole + l.f32_part - 1) / l.f32_part;
         }
         if (dw) {
             // whole groups of four columns where they belong, up to three more by way of a matrix of their own
@@ -792,7 +842,7 @@ int xent_bwd_bf16(int m, int hidden, int vocab, const bf16_t* h, int ldh, const 
     p.m = m; p.mp = l.mp; p.hidden = hidden; p.vocab = vocab; p.ldh = ldh; p.ldw = ldw; p.ldp = l.ldp;
     p.room = (int*)(ws + l.room); p.shift = (int*)(ws + l.shift); p.rows = (_Float16*)(ws + l.rows);
     p.dw = dw; p.lddw = lddw; p.dw_flags = overwrite ? ACCUM_OVERWRITE : 0;
-    p.slabs = (float*)(ws + l.slabs); p.k_per = l.plan.k_per;
+    p.slabs = (float*)(ws + l.slabs); p.k_per = l.plan.k_per; p.dw_per = l.plan.dw_per; p.dw_splits = l.plan.dw_splits;
     p.w_rows = 8;                                          // fewer where that leaves few workgroups
     while (p.w_rows > 1 && hidden / p.w_rows < 128) p.w_rows /= 2;
     if (dw) {
@@ -801,14 +851,17 @@ int xent_bwd_bf16(int m, int hidden, int vocab, const bf16_t* h, int ldh, const 
     }
     const int pieces = (vocab + l.piece - 1) / l.piece;
     int splits = 0;
-    for (int i = 0; i <= pieces; ++i) {
+    const bool cut = dw && l.plan.dw_splits > 1;
+    for (int i = 0; i <= pieces + cut; ++i) {
+        p.past = p.now;
         p.now = p.next;
-        int (&count)[5] = p.count;
+        int (&count)[6] = p.count;
         std::fill(std::begin(count), std::end(count), 0);
-        if (i > 0) {
+        if (cut && i > 1) count[5] = (int)std::min<size_t>(((size_t)hidden * p.past.ld / 4 + 511) / 512, SUM_WGS);
+        if (i > 0 && i <= pieces) {
             if (dw) {
                 p.dw_r = raster_of<Pass::Raster>(l.plan.dw_tile, hidden, p.now.ld, 2 * l.mp);
-                count[0] = p.dw_r.tiles_m * p.dw_r.tiles_n;
+                count[0] = p.dw_r.tiles_m * p.dw_r.tiles_n * l.plan.dw_splits;
             }
             if (dh) {
                 // the last piece is cut where the others are: a split that it does not reach adds nothing
@@ -821,7 +874,8 @@ int xent_bwd_bf16(int m, int hidden, int vocab, const bf16_t* h, int ldh, const 
         }
         if (i < pieces) {
             const int v0 = i * l.piece, cols = std::min(l.piece, vocab - v0), at = i & (l.buffers - 1);
-            p.next = {v0, cols, round_up(cols, 8), (_Float16*)(ws + l.dz[at]), (_Float16*)(ws + l.w[at]), (int*)(ws + l.raise[at])};
+            p.next = {v0, cols, round_up(cols, 8), (_Float16*)(ws + l.dz[at]), (_Float16*)(ws + l.w[at]), (int*)(ws + l.raise[at]),
+                      (float*)(ws + l.dw[at])};
             p.dz_r = raster_of<Pass::Raster>(l.plan.tok_tile, l.mp, p.next.ld, hidden);
             count[2] = p.dz_r.tiles_m * p.dz_r.tiles_n;
             if (dh) count[3] = (hidden + p.w_rows - 1) / p.w_rows;
@@ -831,7 +885,7 @@ int xent_bwd_bf16(int m, int hidden, int vocab, const bf16_t* h, int ldh, const 
         // 3555 -> 3585).
         const bool rows_first = i == 0 && count[2] <= 2 * NUM_CUS;
         int total = 0;
-        for (int k : rows_first ? std::array{4, 3, 2, 1, 0} : std::array{0, 1, 2, 3, 4}) { p.first[k] = total; total += count[k]; }
+        for (int k : rows_first ? std::array{4, 3, 2, 1, 0, 5} : std::array{0, 1, 2, 3, 4, 5}) { p.first[k] = total; total += count[k]; }
         if (l.plan.dw_tile == 256 && l.plan.tok_tile == 256) hipLaunchKernelGGL((xent_pass_kernel<256, 256>), dim3(total), dim3(512), 0, s, p);
         else if (l.plan.dw_tile == 256) hipLaunchKernelGGL((xent_pass_kernel<256, 128>), dim3(total), dim3(512), 0, s, p);
         else hipLaunchKernelGGL((xent_pass_kernel<128, 128>), dim3(total), dim3(512), 0, s, p);

@@ -77,7 +77,7 @@ def _check_forward(dtype, h, w, targets, scale, rows, lse, loss, loss0=0.5):
 
 # tiles of 256x256 need 144 of them (1024 x 9300), more 128x128 tiles than CUs 2200 tokens x 2000; both ends of a tile, one token, one word
 FWD = [(1, 8, 1, 8, 8), (1, 64, 7, 16, 64), (2, 8, 8, 8, 16), (24, 256, 1000, 1000, 256), (33, 72, 257, 264, 80), (130, 136, 513, 576, 136), (128, 64, 384, 384, 64),
-       (1, 1600, 50257, 50304, 1600), (1024, 64, 9300, 9304, 64), (1000, 192, 9473, 9480, 200), (2200, 128, 2001, 2008, 128)]
+       (1, 1600, 50257, 50304, 1600), (1024, 64, 9300, 9304, 64), (1000, 192, 9473, 9480, 200), (2200, 128, 2001, 2008, 128), (70, 128, 30011, 30016, 128)]
 
 
 @pytest.mark.parametrize("dtype", [b.F32, b.BF16])
@@ -161,7 +161,8 @@ def _check_backward(dtype, h, w, targets, lse, scale, dloss, dh, dw, dw0):
 # (1024 x 9300), dh (4100 x 2304: more 256x256 tiles than 128x128 ones pay for) and dW (1000 x 9473)
 BWD = [(1, 8, 1, 8, 0), (1, 64, 7, 16, 0), (2, 8, 8, 8, 0), (3, 16, 9, 24, 0), (24, 256, 1000, 1000, 0), (33, 72, 257, 264, 256), (130, 136, 1027, 1088, 256),
        (260, 264, 771, 776, 512), (60, 512, 8000, 8000, 0), (1024, 64, 9300, 9304, 0), (40, 1000, 9473, 9480, 4864), (2200, 128, 2001, 2008, 0),
-       (4100, 2304, 1031, 1032, 512), (3000, 256, 30001, 30008, 0)]
+       (4100, 2304, 1031, 1032, 512), (3000, 256, 30001, 30008, 0), (100, 320, 20011, 20024, 4608),
+       (6100, 72, 1100, 1104, 512), (9000, 136, 2051, 2056, 0)]
 
 
 @pytest.mark.parametrize("dtype", [b.F32, b.BF16])
@@ -625,3 +626,20 @@ def test_stage_steps(dtype, bits):
             err = float((got - p).norm() / (3e-3 * math.sqrt(params)))
             assert err <= (0.01 if step == 1 else 0.3 * step) + (2.0 ** -9 * float(p.norm()) / (3e-3 * math.sqrt(params)) if dtype == b.BF16 else 0), err
         p = st.weights.double().clone() if dtype == b.F32 else p
+
+
+def test_tensors_elsewhere_are_refused():
+    torch = _torch()
+    z = lambda *s, d=torch.float32, at="cuda": torch.zeros(s, dtype=d, device=at)  # noqa: E731
+    i32 = torch.int32
+    good = dict(h=z(3, 16), w=z(16, 24), targets=z(3, d=i32), scale=1.0, loss_rows=z(3), lse=z(3), loss=z(1))
+    for bad in (dict(h=z(3, 16, at="cpu")), dict(w=z(16, 24, at="cpu")), dict(targets=z(3, d=i32, at="cpu")), dict(lse=z(3, at="cpu")), dict(loss=z(1, at="cpu"))):
+        with pytest.raises(ValueError, match="current GPU"):
+            b.chimera_op_linear_xent_fwd(**dict(good, **bad))
+    with pytest.raises(ValueError, match="current GPU"):
+        b.chimera_op_grad_norm([z(4), z(4, at="cpu")], 1.0, z(2))
+    with pytest.raises(ValueError, match="current GPU"):
+        b.AdamW([z(4)], [z(4, at="cpu")], [z(4)], [z(4)])
+    step = b.AdamW([z(4)], [z(4)], [z(4)], [z(4)])
+    with pytest.raises(ValueError, match="current GPU"):
+        step.step(1e-3, 1, grad_scale=z(1, at="cpu"))
