@@ -20,6 +20,7 @@
 #include <array>
 #include <climits>
 #include <cmath>
+#include <cstdlib>
 
 namespace chimera {
 namespace {
@@ -632,13 +633,27 @@ int wide_columns(int m, int n) {
     return (int)((tiles - over) / tm) * 256;
 }
 
-// Columns of the vocabulary per piece where the caller leaves it open: 8192, more where their buffers stay small, fewer where they get large.
-constexpr size_t PIECE_BYTES_MIN = (size_t)128 << 20, PIECE_BYTES_MAX = (size_t)512 << 20;
-constexpr int PIECE_STEP = 256, PIECE_USUAL = 8192;
+// Columns of the vocabulary per piece where the caller leaves it open: 8192, more where their buffers stay small, fewer where they get large, in equal pieces.
+// Beside 8192 a piece whose dW just fills the chip's rounds of 256x256 tiles is taken as it is, unless that leaves a last one of less than a tenth, a pass
+// for little: 8192 x 2048 x 65536 in 8192 6990 -> 6600 us, 4096 x 1600 x 50304 in 9216 2463 -> 2344, 4096 x 2560 in 6400 3445 -> 3375; but 4096 x 2304 in seven of 7168 and
+// 128 columns 3104 -> 3199, 2048 x 1536 x 65536 in six of 10752 and 1024 1591 -> 1616.
+constexpr size_t PIECE_BYTES_MIN = (size_t)128 << 20, PIECE_BYTES_MAX = (size_t)512 << 20, PIECE_BYTES_FILLED = (size_t)768 << 20;
+constexpr int PIECE_STEP = 256, PIECE_USUAL = 8192, PIECE_FILLED_MIN = 6144, PIECE_FILLED_MAX = 10752;
+int filled_piece(int hidden) {
+    const int rows = (hidden + 255) / 256;
+    int best = 0;
+    for (int rounds = 1; NUM_CUS * rounds / rows * 256 <= PIECE_FILLED_MAX; ++rounds) {
+        const int p = NUM_CUS * rounds / rows * 256;
+        if (p >= PIECE_FILLED_MIN && std::abs(p - PIECE_USUAL) <= std::abs(best - PIECE_USUAL)) best = p;
+    }
+    return best;
+}
 int default_piece(int dtype, int m, int hidden, int vocab) {
     const int all = round_up(vocab, PIECE_STEP);
     const size_t column = dtype == CHIMERA_F32 ? (size_t)m * 4 : (size_t)round_up(m, TOKEN_PAD) * 8 + (size_t)hidden * 4;
     const size_t usual = std::max(PIECE_BYTES_MIN / column, std::min<size_t>(PIECE_USUAL, PIECE_BYTES_MAX / column));
+    const int filled = dtype == CHIMERA_BF16 && usual <= PIECE_USUAL ? filled_piece(hidden) : 0;
+    if (filled && filled < vocab && filled * column <= PIECE_BYTES_FILLED && (vocab % filled == 0 || vocab % filled >= filled / 10)) return filled;
     const int most = (int)std::min<size_t>(all, std::max<size_t>(usual / PIECE_STEP * PIECE_STEP, PIECE_STEP));
     return round_up((vocab + (vocab + most - 1) / most - 1) / ((vocab + most - 1) / most), PIECE_STEP);        // equal pieces
 }
