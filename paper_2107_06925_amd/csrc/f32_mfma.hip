@@ -69,6 +69,16 @@ template <bool PARTS> __device__ __forceinline__ decltype(auto) product_of_workg
     else return tile_of(L, tile_m, tile_n);
 }
 
+// What EPI_XENT knows of a row
+template <int EPI> __device__ __forceinline__ XentRow row_of_xent(const F32Product& p, int row) {
+    if constexpr (EPI == EPI_XENT) return reinterpret_cast<const XentRow*>(p.bias)[min(row, p.m - 1)];
+    else return XentRow{};
+}
+__device__ __forceinline__ float xent_gradient(const XentRow& r, float z, int word) {
+    const float d = __builtin_amdgcn_exp2f((z - r.lse) * 1.4426950408889634f) - (word == r.target ? 1.0f : 0.0f);
+    return r.coef == 0.f || word >= r.vocab ? 0.f : r.coef * d;
+}
+
 // One result whose other operands are there: the bias, and the residual, the GeLU's input or what the result is added to
 template <int EPI> __device__ __forceinline__ void finish_one(const F32Product& p, int flag, size_t idx, float v, float bias, float other) {
     if constexpr (EPI == EPI_BIAS || EPI == EPI_BIAS_GELU || EPI == EPI_BIAS_RESIDUAL) v += bias;
@@ -79,7 +89,7 @@ template <int EPI> __device__ __forceinline__ void finish_one(const F32Product& 
 }
 // N consecutive results of one row (columns col..col+N-1, inside the matrix)
 template <int EPI, int N>
-__device__ __forceinline__ void finish(const F32Product& p, int flag, int row, int col, const float* acc) {
+__device__ __forceinline__ void finish(const F32Product& p, int flag, int row, int col, const float* acc, const XentRow& own = {}) {
     const size_t idx = (size_t)row * p.ldc + col;
     float v[N], w[N];
 #pragma unroll
@@ -90,6 +100,7 @@ __device__ __forceinline__ void finish(const F32Product& p, int flag, int row, i
         if constexpr (EPI == EPI_BIAS_GELU) w[e] = gelu_f(v[e], flag);
         if constexpr (EPI == EPI_DGELU) v[e] *= gelu_grad_f(p.r[idx + e], flag);
         if constexpr (EPI == EPI_ACCUM_F32) v[e] += flag ? 0.f : p.c[idx + e];
+        if constexpr (EPI == EPI_XENT) v[e] = xent_gradient(own, v[e], flag + col + e);
     }
 #pragma unroll
     for (int e = 0; e < N; ++e) {
@@ -101,6 +112,7 @@ __device__ __forceinline__ void finish(const F32Product& p, int flag, int row, i
 // The same for four columns whose other operands are asked for before the k loop: a round trip less at the end of a short launch.
 struct F32Ahead {
     f32x4 bias, r;
+    XentRow own;
     template <int EPI> __device__ __forceinline__ void request(const F32Product& p, int flag, int row, int col) {
         const size_t idx = (size_t)row * p.ldc + col;
         // n is a multiple of 4, but C, R and the bias need not be aligned to 16 bytes
@@ -108,6 +120,7 @@ struct F32Ahead {
         if constexpr (EPI == EPI_BIAS || EPI == EPI_BIAS_GELU || EPI == EPI_BIAS_RESIDUAL) bias = *reinterpret_cast<const f32x4_u*>(p.bias + col);
         if constexpr (EPI == EPI_BIAS_RESIDUAL || EPI == EPI_DGELU) r = *reinterpret_cast<const f32x4_u*>(p.r + idx);
         if constexpr (EPI == EPI_ACCUM_F32) { r = f32x4{0.f, 0.f, 0.f, 0.f}; if (!flag) r = *reinterpret_cast<const f32x4_u*>(p.c + idx); }
+        if constexpr (EPI == EPI_XENT) own = row_of_xent<EPI>(p, row);
     }
     template <int EPI> __device__ __forceinline__ void finish(const F32Product& p, int flag, int row, int col, const f32x4& acc) const {
         const size_t idx = (size_t)row * p.ldc + col;
@@ -119,6 +132,7 @@ struct F32Ahead {
             if constexpr (EPI == EPI_BIAS_RESIDUAL || EPI == EPI_ACCUM_F32) v[e] += r[e];
             if constexpr (EPI == EPI_BIAS_GELU) w[e] = gelu_f(v[e], flag);
             if constexpr (EPI == EPI_DGELU) v[e] *= gelu_grad_f(r[e], flag);
+            if constexpr (EPI == EPI_XENT) v[e] = xent_gradient(own, v[e], flag + col + e);
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -290,11 +304,13 @@ __global__ __launch_bounds__(8 * WAVE, 4) void gemm_f32_tile_kernel(F32Launch L)
     // what the epilogue reads is asked for behind the last requests of the loop
     constexpr bool READS = EPI == EPI_BIAS_RESIDUAL || EPI == EPI_DGELU || EPI == EPI_ACCUM_F32;
     float bias = 0.f, other[R];
+    XentRow own[EPI == EPI_XENT ? R : 1];
     auto ask = [&] {
         const int c = min(col, n - 1);
         if constexpr (EPI == EPI_BIAS || EPI == EPI_BIAS_GELU || EPI == EPI_BIAS_RESIDUAL) bias = p.bias[c];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
+            if constexpr (EPI == EPI_XENT) own[r] = row_of_xent<EPI>(p, row_of(r));
             other[r] = 0.f;
             if (READS && !(EPI == EPI_ACCUM_F32 && L.flag)) other[r] = (EPI == EPI_ACCUM_F32 ? p.c : p.r)[(size_t)min(row_of(r), m - 1) * p.ldc + c];
         }
@@ -448,7 +464,8 @@ __global__ __launch_bounds__(8 * WAVE, 4) void gemm_f32_tile_kernel(F32Launch L)
     if (col >= n) return;
 #pragma unroll
     for (int r = 0; r < R; ++r)
-        if (row_of(r) < m) finish_one<EPI>(p, L.flag, (size_t)row_of(r) * p.ldc + col, out[r], bias, other[r]);
+        if (row_of(r) < m)
+            finish_one<EPI>(p, L.flag, (size_t)row_of(r) * p.ldc + col, EPI == EPI_XENT ? xent_gradient(own[r], out[r], L.flag + col) : out[r], bias, other[r]);
 }
 
 // Larger outputs: 128x128, 4 wavefronts of 64x64, two workgroups on a CU, each thread stages a chunk of either operand: half of the vector
@@ -634,6 +651,7 @@ __global__ __launch_bounds__(4 * WAVE, 2) void gemm_f32_wide_kernel(F32Launch L)
 #pragma unroll
     for (int a = 0; a < TM; ++a) {
         const int row = i0 + wm0 + a * 32 + l32;
+        const XentRow own = row_of_xent<EPI>(p, row);
 #pragma unroll
         for (int b = 0; b < TN; ++b)
 #pragma unroll
@@ -642,7 +660,7 @@ __global__ __launch_bounds__(4 * WAVE, 2) void gemm_f32_wide_kernel(F32Launch L)
                 float v[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[e] = acc[a][b][4 * q + e];
-                if (row < m && col < n) finish<EPI, 4>(p, L.flag, row, col, v);      // n is a multiple of 4
+                if (row < m && col < n) finish<EPI, 4>(p, L.flag, row, col, v, own);      // n is a multiple of 4
             }
     }
 }
@@ -704,7 +722,7 @@ __global__ __launch_bounds__(NW* WAVE) void gemm_f32_small_kernel(F32Launch L) {
 #pragma unroll
         for (int w = 1; w < NW; ++w) s += *reinterpret_cast<const f32x4*>(&red[w][rr * 32 + cc]);
         const float v[4] = {s[0], s[1], s[2], s[3]};
-        if (orow < m && ocol < n) finish<EPI, 4>(p, L.flag, orow, ocol, v);       // n is a multiple of 8
+        if (orow < m && ocol < n) finish<EPI, 4>(p, L.flag, orow, ocol, v, row_of_xent<EPI>(p, orow));       // n is a multiple of 8
         if constexpr (EPI == EPI_ACCUM_F32)
             if (col_sums && tid < 32 && tile_n * 32 + tid < n) {
                 float t = red_cs[0][tid];
@@ -847,6 +865,9 @@ int launch_epi(F32Launch& L, Form form, hipStream_t s) {
         case EPI_BIAS_GELU: return launch_form<A_KC, B_KC, EPI_BIAS_GELU>(L, form, s);
         case EPI_BIAS_RESIDUAL: return launch_form<A_KC, B_KC, EPI_BIAS_RESIDUAL>(L, form, s);
         case EPI_DGELU: return launch_form<A_KC, B_KC, EPI_DGELU>(L, form, s);
+        case EPI_XENT:
+            if constexpr (A_KC && !B_KC) return launch_form<A_KC, B_KC, EPI_XENT>(L, form, s);
+            else return fail(CHIMERA_EINVAL, "unknown epilogue %d", L.epi);
         default: return launch_form<A_KC, B_KC, EPI_ACCUM_F32>(L, form, s);
     }
 }
@@ -873,7 +894,7 @@ bool gemm_f32_supports(const GemmArgs& g) {
 
 int gemm_f32(const GemmArgs& g, void* stream) {
     if (!gemm_f32_supports(g)) return fail(CHIMERA_EINVAL, "float matrix-core gemm: unsupported shape or layout");
-    if (g.epilogue < EPI_NONE || g.epilogue > EPI_ACCUM_F32) return fail(CHIMERA_EINVAL, "unknown epilogue %d", g.epilogue);
+    if (g.epilogue != EPI_XENT && (g.epilogue < EPI_NONE || g.epilogue > EPI_ACCUM_F32)) return fail(CHIMERA_EINVAL, "unknown epilogue %d", g.epilogue);
     F32Launch L{};
     L.count = 1; L.epi = g.epilogue; L.flag = g.epilogue == EPI_ACCUM_F32 ? 0 : g.gelu_erf;
     L.p[0] = product_of(g);

@@ -47,8 +47,11 @@ enum Epilogue {
     EPI_BIAS_GELU = 2,      // C = acc + bias[n], C2 = GeLU(C)
     EPI_BIAS_RESIDUAL = 3,  // C = acc + bias[n] + R[m,n]
     EPI_DGELU = 4,          // C = acc * GeLU'(R[m,n])
-    EPI_ACCUM_F32 = 5       // C (float) += acc
+    EPI_ACCUM_F32 = 5,      // C (float) += acc
+    EPI_XENT = 7            // float A B: C = coef[m] (exp(acc - lse[m]) - [word = target[m]]), word = column + gelu_erf below the vocabulary, bias: XentRow[m]
 };
+
+struct XentRow { float lse, coef; int target, vocab; };
 
 struct GemmArgs {
     int m, n, k;

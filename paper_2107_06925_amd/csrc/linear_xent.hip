@@ -534,23 +534,25 @@ __global__ __launch_bounds__(ROW_THREADS) void xent_dh_sum_kernel(const float* _
     }
 }
 
-// float: the rows of h that the weight gradient takes, tokens that do not count as zeros
-__global__ __launch_bounds__(ROW_THREADS) void xent_rows_f32_kernel(const float* __restrict__ h, int ldh, const int* __restrict__ targets, const float* __restrict__ dloss,
-                                                                    float scale, int m, int cols, int vocab, float* __restrict__ out) {
+// float: what a piece's product needs to know of a token, and the rows of h that the weight gradient takes (may be null), tokens that do not count as zeros
+__global__ __launch_bounds__(ROW_THREADS) void xent_rows_f32_kernel(const float* __restrict__ h, int ldh, const int* __restrict__ targets, const float* __restrict__ lse,
+                                                                    const float* __restrict__ dloss, float scale, int m, int cols, int vocab, XentRow* __restrict__ info,
+                                                                    float* __restrict__ out) {
     const int t = blockIdx.x * (ROW_THREADS / WAVE) + threadIdx.x / WAVE, lane = threadIdx.x % WAVE;
     if (t >= m) return;
-    const bool on = coef_of(targets, dloss, scale, t, m, vocab) != 0.f;
+    const float coef = coef_of(targets, dloss, scale, t, m, vocab);
+    if (lane == 0) info[t] = {lse[t], coef, targets[t], vocab};
+    if (!out) return;
     for (int c = lane * 4; c < cols; c += WAVE * 4) {
         float x[4];
         load_vec<float>(h + (size_t)t * ldh + c, x);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = on ? x[e] : 0.f;
+        for (int e = 0; e < 4; ++e) x[e] = coef != 0.f ? x[e] : 0.f;
         store_vec<float>(out + (size_t)t * cols + c, x);
     }
 }
 
-// ---- float: a piece of z is in memory, [m, ld], of which `cols` columns from v0 on count.  What the row kernels move bounds them (632 x 30001: 25 us of 152 MB);
-// the whole backward of 632 x 320 x 30001 takes 326 us, three products of 87 to 110 us at 110 to 140 TFLOP/s among them.
+// ---- float: a piece of z is in memory, [m, ld], of which `cols` columns from v0 on count
 __global__ __launch_bounds__(ROW_THREADS) void xent_stats_f32_kernel(const float* __restrict__ z, int ld, int cols, int v0, int vocab, const int* __restrict__ targets,
                                                                      float2* __restrict__ stats, float* __restrict__ at_target) {
     __shared__ float2 part[ROW_THREADS / WAVE];
@@ -587,36 +589,36 @@ __global__ __launch_bounds__(ROW_THREADS) void xent_stats_f32_kernel(const float
     const int target = targets[t];
     if (counts(target, vocab) && target >= v0 && target < v0 + cols) at_target[t] = row[target - v0];
 }
-__global__ __launch_bounds__(ROW_THREADS) void xent_dz_f32_kernel(float* __restrict__ z, int ld, int cols, int v0, int vocab, const int* __restrict__ targets,
-                                                                  const float* __restrict__ lse, const float* __restrict__ dloss, float scale) {
-    const int t = blockIdx.x, target = targets[t];
-    const float coef = counts(target, vocab) ? (dloss ? scale * dloss[t] : scale) : 0.f, l = lse[t];
-    float* row = z + (size_t)t * ld;
-    for (int c0 = threadIdx.x * 4; c0 < ld; c0 += ROW_FLY * ROW_THREADS * 4) {
-        float v[ROW_FLY][4] = {};
+// dW of up to three columns, which the products' groups of four leave: to (+)= rows^T dz, 32 rows of W a workgroup, 32 threads each, which take every 32nd token
+// and are added in order.  A few dependent trips to memory bound it.
+constexpr int LAST_FLY = 4;
+__global__ __launch_bounds__(1024) void xent_columns_kernel(const float* __restrict__ rows, int hidden, const float* __restrict__ dz, int ldz, int m, int cols,
+                                                            float* __restrict__ to, int ldto, int overwrite) {
+    __shared__ float part[3][32][33];
+    const int i = blockIdx.x * 32 + threadIdx.x % 32, q = threadIdx.x / 32;
+    float sum[3] = {0.f, 0.f, 0.f};
+    for (int t0 = q; t0 < m; t0 += 32 * LAST_FLY) {
+        float x[LAST_FLY], d[LAST_FLY][3];
 #pragma unroll
-        for (int u = 0; u < ROW_FLY; ++u)
-            if (c0 + u * ROW_THREADS * 4 < ld) load_vec<float>(row + c0 + u * ROW_THREADS * 4, v[u]);
+        for (int u = 0; u < LAST_FLY; ++u) {
+            const int t = min(t0 + 32 * u, m - 1);
+            x[u] = rows[(size_t)t * hidden + min(i, hidden - 1)];
 #pragma unroll
-        for (int u = 0; u < ROW_FLY; ++u) {
-            const int c = c0 + u * ROW_THREADS * 4;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float d = __builtin_amdgcn_exp2f((v[u][e] - l) * LOG2E) - (c + e == target - v0 ? 1.0f : 0.0f);
-                v[u][e] = coef == 0.f || c + e >= cols ? 0.f : coef * d;
-            }
-            if (c < ld) store_vec<float>(row + c, v[u]);
+            for (int c = 0; c < 3; ++c) d[u][c] = dz[(size_t)t * ldz + min(c, cols - 1)];
         }
+#pragma unroll
+        for (int u = 0; u < LAST_FLY; ++u)
+#pragma unroll
+            for (int c = 0; c < 3; ++c) sum[c] += t0 + 32 * u < m ? x[u] * d[u][c] : 0.f;
     }
-}
-// up to three columns of a wider matrix: to (+)= from [rows, 4]
-__global__ __launch_bounds__(ROW_THREADS) void xent_columns_kernel(const float* __restrict__ from, int rows, int cols, float* __restrict__ to, int ldto, int overwrite) {
-    const int i = blockIdx.x * ROW_THREADS + threadIdx.x;
-    if (i >= rows) return;
-    for (int c = 0; c < cols; ++c) {
-        float* dst = to + (size_t)i * ldto + c;
-        *dst = overwrite ? from[(size_t)i * 4 + c] : *dst + from[(size_t)i * 4 + c];
-    }
+#pragma unroll
+    for (int c = 0; c < 3; ++c) part[c][q][threadIdx.x % 32] = sum[c];
+    __syncthreads();
+    if (q >= cols || i >= hidden) return;
+    float v = 0.f;
+    for (int k = 0; k < 32; ++k) v += part[q][k][threadIdx.x % 32];
+    float* dst = to + (size_t)i * ldto + q;
+    *dst = overwrite ? v : *dst + v;
 }
 
 size_t aligned(size_t b) { return (b + 255) / 256 * 256; }
@@ -702,7 +704,7 @@ FwdLayout fwd_layout(int dtype, int m, int hidden, int vocab) {
     l.total = b;
     return l;
 }
-struct BwdLayout { int piece, ld, mp, ldp, buffers, f32_part; PassPlan plan; size_t room, shift, rows, dz[2], w[2], raise[2], dw[2], slabs, columns, total; };
+struct BwdLayout { int piece, ld, mp, ldp, buffers, f32_part; PassPlan plan; size_t room, shift, rows, dz[2], w[2], raise[2], dw[2], slabs, total; };
 BwdLayout bwd_layout(int dtype, int m, int hidden, int vocab, int piece) {
     BwdLayout l{};
     size_t b = 0;
@@ -711,12 +713,12 @@ BwdLayout bwd_layout(int dtype, int m, int hidden, int vocab, int piece) {
     l.ld = std::min(l.piece, round_up(vocab, 8));
     if (dtype == CHIMERA_F32) {
         l.mp = m;
+        l.room = take((size_t)m * sizeof(XentRow));
         l.rows = take((size_t)m * hidden * 4);
         l.dz[0] = take((size_t)m * l.ld * 4);
         const int whole = std::max(8, std::min(l.ld, vocab) & ~7);
         l.f32_part = gemm_f32_part(m, hidden, whole);
         l.slabs = take((size_t)((whole + l.f32_part - 1) / l.f32_part) * m * hidden * 4);
-        l.columns = take((size_t)hidden * 16);
     } else {
         l.mp = round_up(m, TOKEN_PAD);
         l.plan = plan_of(l.mp, hidden, l.ld);
@@ -811,19 +813,17 @@ int xent_fwd_f32(int m, int hidden, int vocab, const float* h, int ldh, const fl
 int xent_bwd_f32(int m, int hidden, int vocab, const float* h, int ldh, const float* w, int ldw, const int* targets, const float* lse, float scale,
                  const float* dloss, float* dh, int lddh, float* dw, int lddw, int overwrite, const BwdLayout& l, char* ws, void* stream) {
     hipStream_t s = (hipStream_t)stream;
-    float *rows = (float*)(ws + l.rows), *z = (float*)(ws + l.dz[0]), *slab = (float*)(ws + l.slabs), *columns = (float*)(ws + l.columns);
-    if (dw) {
-        hipLaunchKernelGGL(xent_rows_f32_kernel, dim3((m + 3) / 4), dim3(ROW_THREADS), 0, s, h, ldh, targets, dloss, scale, m, hidden, vocab, rows);
-        CHIMERA_LAUNCH_CHECK("linear cross-entropy");
-    }
+    float *rows = (float*)(ws + l.rows), *z = (float*)(ws + l.dz[0]), *slab = (float*)(ws + l.slabs);
+    XentRow* info = (XentRow*)(ws + l.room);
+    hipLaunchKernelGGL(xent_rows_f32_kernel, dim3((m + 3) / 4), dim3(ROW_THREADS), 0, s, h, ldh, targets, lse, dloss, scale, m, hidden, vocab, info, dw ? rows : nullptr);
+    CHIMERA_LAUNCH_CHECK("linear cross-entropy");
     int slabs = 0;
     for (int v0 = 0; v0 < vocab; v0 += l.piece) {
         const int cols = std::min(l.piece, vocab - v0), ld = round_up(cols, 8), whole = cols & ~7;
         GemmArgs g{};
-        g.m = m; g.n = ld; g.k = hidden; g.a = h; g.lda = ldh; g.a_kc = 1; g.b = w + v0; g.ldb = ldw; g.b_kc = 0; g.c = z; g.epilogue = EPI_NONE;
+        g.m = m; g.n = ld; g.k = hidden; g.a = h; g.lda = ldh; g.a_kc = 1; g.b = w + v0; g.ldb = ldw; g.b_kc = 0; g.c = z;
+        g.epilogue = EPI_XENT; g.bias = info; g.gelu_erf = v0;
         XENT_TRY(gemm_f32(g, stream));
-        hipLaunchKernelGGL(xent_dz_f32_kernel, dim3(m), dim3(ROW_THREADS), 0, s, z, ld, cols, v0, vocab, targets, lse, dloss, scale);
-        CHIMERA_LAUNCH_CHECK("linear cross-entropy");
         if (dh && whole) {
             GemmArgs d{};
             d.m = m; d.n = hidden; d.k = whole; d.a = z; d.lda = ld; d.a_kc = 1; d.b = w + v0; d.ldb = ldw; d.b_kc = 1; d.c = slab;
@@ -832,18 +832,14 @@ int xent_bwd_f32(int m, int hidden, int vocab, const float* h, int ldh, const fl
             if (!slabs) slabs = (whole + l.f32_part - 1) / l.f32_part;
         }
         if (dw) {
-            // whole groups of four columns where they belong, up to three more by way of a matrix of their own
             const int fours = cols & ~3;
             GemmArgs q{};
             q.m = hidden; q.n = fours; q.k = m; q.a = rows; q.lda = hidden; q.a_kc = 0; q.b = z; q.ldb = ld; q.b_kc = 0; q.c = dw + v0; q.ldc = lddw;
             q.epilogue = EPI_ACCUM_F32;
             if (fours) XENT_TRY(gemm_f32_group(1, &q, nullptr, overwrite, stream));
-            if (fours < cols) {
-                q.n = 4; q.b = z + fours; q.c = columns; q.ldc = 4;
-                XENT_TRY(gemm_f32_group(1, &q, nullptr, 1, stream));
-                hipLaunchKernelGGL(xent_columns_kernel, dim3((hidden + ROW_THREADS - 1) / ROW_THREADS), dim3(ROW_THREADS), 0, s, columns, hidden, cols - fours,
-                                   dw + v0 + fours, lddw, overwrite);
-            }
+            if (fours < cols)
+                hipLaunchKernelGGL(xent_columns_kernel, dim3((hidden + 31) / 32), dim3(1024), 0, s, rows, hidden, z + fours, ld, m, cols - fours, dw + v0 + fours, lddw,
+                                   overwrite);
             CHIMERA_LAUNCH_CHECK("linear cross-entropy");
         }
         if (dh && v0 + l.piece >= vocab) {
