@@ -533,7 +533,7 @@ int chimera_op_linear_xent_bwd(int dtype, int tokens, int hidden, int vocab, con
                                float* d_dw, int lddw, int overwrite, int piece, void* d_workspace, size_t workspace_bytes, void* hip_stream);
 /* chimera_head_loss on these two: the same results (tokens whose target lies outside [0, vocab) do not count here; their rows of y
  * still have to be finite) without its [tokens, vocab] workspace, for any vocab.  d_w_head and d_dw_head have rows ldw apart.  It forms z twice and dW from a
- * finer dz, two thirds more work on the matrix cores: bf16 2048 x 1600 x 50304 1.72 ms in 235 MB, chimera_head_loss 1.22 in 344; float 128 x 128 x 50304 0.14 against 0.28. */
+ * finer dz, two thirds more work on the matrix cores: bf16 2048 x 1600 x 50304 1.69 ms in 276 MB, chimera_head_loss 1.22 in 344; float 128 x 128 x 50304 0.14 against 0.28. */
 size_t chimera_head_pieces_workspace_bytes(int dtype, int tokens, int hidden, int vocab, int piece);
 int chimera_head_loss_pieces(int dtype, int tokens, int hidden, int vocab, const void* d_y, const int32_t* d_targets, const void* d_lnf_g,
                              const void* d_lnf_b, const void* d_w_head, int ldw, float scale, void* d_dy, float* d_dlnf_g, float* d_dlnf_b,

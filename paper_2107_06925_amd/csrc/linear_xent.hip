@@ -14,7 +14,7 @@
 //   h_t times 2^(shift - lift_t), for dW, which sums over tokens: one shift for all, the largest that keeps all rows below 2^15.
 // The products' epilogues take the powers off again.
 //
-// float.  The framework's float products on pieces of z that are in memory, row kernels between them.
+// float.  The framework's float products on pieces that are in memory, z's ending in dz in the backward.
 #include "gemm_tiles.h"
 
 #include <array>
@@ -99,7 +99,7 @@ template <int BM, int BN> struct StatsEnd {
 };
 
 // Columns [0, wide) on 256x256 tiles, a whole number of rounds of them, and what is left on 128x128 tiles, begun first: a last round of a few large tiles
-// costs as much as a full one.  Matrix instructions bound it: 2048 x 1600 x 50257 270 us, 1.22 PFLOP/s, a large square product of this library's 1.4 to 1.5.
+// costs as much as a full one.  Matrix instructions bound it: 2048 x 1600 x 50257 266 to 270 us, 1.22 PFLOP/s, a large square product of this library's 1.4 to 1.5.
 struct StatsPass {
     const bf16_t *h, *w;
     const int* targets;
@@ -452,8 +452,8 @@ __device__ __forceinline__ void sum_columns(const Pass& p, int id, int wgs) {
 
 // One launch: dW and dh of a piece, dz and the rows of W of the next, the sums of dW's parts of the one before, and, in the first, h^T.  Tiles of DW x DW for
 // dW, of TOK x TOK for the products over tokens.  Four products (z, dh, dW of either part of dz), a third more
-// than a dz in one part needs: 8192 x 2048 x 65536 6.82 to 6.89 ms, 1.28 PFLOP/s, where the chip's power is what bounds it (a step of dW takes 2457 clocks for 2048 of matrix instructions, at
-// about 1.7 GHz); 2048 x 1600 x 50257 1.34 ms, 0.98: tiles of 25 to 64 steps, each with some 20 us of first loads and stores on a CU that holds no other.
+// than a dz in one part needs: 8192 x 2048 x 65536 6.36 to 6.47 ms, 1.36 to 1.38 PFLOP/s, where the chip's power is what bounds it (a step of dW takes 2457 clocks for 2048 of matrix instructions, at
+// about 1.7 GHz); 2048 x 1600 x 50257 1.29 to 1.31 ms, 1.0: tiles of 25 to 64 steps, each with some 20 us of first loads and stores on a CU that holds no other.
 template <int DW, int TOK>
 __global__ __launch_bounds__(512, 2) void xent_pass_kernel(Pass p) {
     constexpr int BYTES = RingLds<256, 256, 2, 4, 1>::BYTES;
