@@ -639,7 +639,8 @@ def chimera_op_grad_norm(grads, max_norm, out, workspace=None):
 
 
 class AdamW:
-    """The argument arrays of chimera_op_adamw for a list of tensors of the current GPU, kept from step to step.
+    """The argument arrays of chimera_op_adamw for a list of tensors of the current GPU, kept from step to step, and with them the memory that the
+    tensors have now: whoever gives a tensor other memory (a new gradient, p.data = ...) makes a new handle.
 
     params: float32, or bfloat16 with float32 `masters`; grads: float32.  32-bit moments: ms, vs float32 and scales None; 8-bit: ms, vs
     float8_e4m3fn (or uint8) and scales float32, a pair for each 256 elements of a tensor.  decay: a number per tensor, or None."""
@@ -652,6 +653,8 @@ class AdamW:
             raise ValueError("grads, masters and scales: float32")
         if any(t.dtype not in ((torch.float32,) if scales is None else (torch.uint8, torch.float8_e4m3fn)) for t in list(ms) + list(vs)):
             raise ValueError("moments: float32, or float8_e4m3fn (uint8) with scales")
+        # (own lists, of views of their own: what becomes of the caller's lists and tensors does not touch the memory that the addresses name)
+        params, grads, ms, vs, masters, scales = (None if x is None else [t.detach() for t in x] for x in (params, grads, ms, vs, masters, scales))
         lists = [params, grads, ms, vs] + [x for x in (masters, scales, decay) if x is not None]
         if any(len(x) != len(params) for x in lists):
             raise ValueError("one entry per tensor expected")
@@ -663,7 +666,7 @@ class AdamW:
                 raise ValueError("tensors of one entry must have one size")
         if scales is not None and any(a.numel() != 2 * ((p.numel() + 255) // 256) for a, p in zip(scales, params)):
             raise ValueError("scales: a pair for each 256 elements")
-        self.tensors = lists                               # the library borrows them
+        self.tensors = [x for x in (params, grads, ms, vs, masters, scales) if x is not None]      # the library borrows them
         _stream_of(*(t for x in (params, grads, ms, vs, masters or [], scales or []) for t in x))
         self.dtype, self.bits, self.count = _dt(params[0]), 32 if scales is None else 8, len(params)
         self.n, self.param, self.grad, self.m, self.v = _counts(params), _pointers(params), _pointers(grads), _pointers(ms), _pointers(vs)

@@ -200,3 +200,33 @@ def test_every_argument_has_a_type():
     assert "chimera_op_adamw" in declared
     for name, (_, args) in b._SIGNATURES.items():
         assert declared.get(name) == len(args), name
+
+
+def _handle(monkeypatch, sizes=(4, 9), **more):
+    """A handle of CPU tensors whose steps reach no library: the arguments of each are kept in the list that comes with it."""
+    torch = pytest.importorskip("torch")
+    calls = []
+
+    class Library:
+        @staticmethod
+        def chimera_op_adamw(*args):
+            calls.append(args)
+            return b.OK
+    monkeypatch.setattr(b, "_stream_of", lambda *tensors: 0)
+    monkeypatch.setattr(b, "lib", lambda: Library)
+    lists = {k: [torch.zeros(n) for n in sizes] for k in ("params", "grads", "ms", "vs")}
+    return b.AdamW(**lists, **more), lists, calls
+
+
+def test_adamw_handle_keeps_what_its_addresses_name(monkeypatch):
+    torch = pytest.importorskip("torch")
+    handle, lists, _ = _handle(monkeypatch)
+    arrays = (handle.param, handle.grad, handle.m, handle.v)
+    named = [list(x) for x in arrays]
+    assert named == [[t.data_ptr() for t in lists[k]] for k in ("params", "grads", "ms", "vs")]
+    lists["grads"][0] = torch.ones(4)                       # a new gradient in the caller's list
+    lists["params"][1].data = torch.ones(9)                 # a parameter whose memory is replaced
+    lists["ms"].clear()
+    for x in lists.values():
+        x.clear()
+    assert [[t.data_ptr() for t in x] for x in handle.tensors] == named and [list(x) for x in arrays] == named
