@@ -230,3 +230,12 @@ def test_adamw_handle_keeps_what_its_addresses_name(monkeypatch):
     for x in lists.values():
         x.clear()
     assert [[t.data_ptr() for t in x] for x in handle.tensors] == named and [list(x) for x in arrays] == named
+
+
+def test_adamw_steps_share_no_hyperparameters(monkeypatch):
+    """The library reads them while other threads run: a step beside another must not find the other's."""
+    handle, _, calls = _handle(monkeypatch, beta1=0.8, beta2=0.9, eps=1e-6)
+    handle.step(lr=1e-3, step=3, seed=5)
+    handle.step(lr=2e-3, step=4, seed=6)
+    seen = [next(a._obj for a in call if isinstance(getattr(a, "_obj", None), b.AdamWHyper)) for call in calls]
+    assert [(h.lr, h.beta1, h.beta2, h.eps, h.step, h.seed) for h in seen] == [(1e-3, 0.8, 0.9, 1e-6, 3, 5), (2e-3, 0.8, 0.9, 1e-6, 4, 6)]
