@@ -297,10 +297,13 @@ class Stage:
         check(lib().chimera_stage_adamw_init(self.handle, _ptr(self.weights), _ptr(self.adamw_state), state_bits))
 
     def adamw_step(self, lr, step, beta1=0.9, beta2=0.95, eps=1e-8, decay=0.0, seed=0, grad_scale=None, d_hyper=None):
-        """One step from the stage's gradients; grad_scale: device float (what chimera_op_grad_norm leaves in its second place)."""
+        """One step from the stage's gradients; grad_scale: device float (what chimera_op_grad_norm leaves in its second place); d_hyper:
+        ADAMW_HYPER_BYTES bytes on the device, used in place of the hyperparameters."""
         h = AdamWHyper(lr, beta1, beta2, eps, step, seed)
+        if any(t is not None and t.get_device() != self.weights.get_device() for t in (grad_scale, d_hyper)):
+            raise ValueError("grad_scale and d_hyper on the stage's GPU expected")
         check(lib().chimera_stage_adamw_step(self.handle, _ptr(self.weights), _ptr(self.adamw_state), self.adamw_bits, decay, C.byref(h),
-                                             _ptr(d_hyper), _ptr(grad_scale)))
+                                             _device_hyper(d_hyper), _vector(grad_scale, self.torch.float32, 1, "grad_scale")))
 
     def close(self):
         if self.handle:
@@ -618,6 +621,13 @@ class AdamWHyper(C.Structure):
 ADAMW_HYPER_BYTES = 128
 
 
+def _device_hyper(t):
+    """The library writes up to the last of these bytes."""
+    if t is not None and (t.numel() * t.element_size() < ADAMW_HYPER_BYTES or not t.is_contiguous()):
+        raise ValueError("d_hyper: %d contiguous bytes expected" % ADAMW_HYPER_BYTES)
+    return None if t is None else t.data_ptr()
+
+
 def _pointers(tensors):
     return None if tensors is None else (C.c_void_p * len(tensors))(*[t.data_ptr() for t in tensors])
 
@@ -679,5 +689,5 @@ class AdamW:
         import torch
         h = AdamWHyper(lr, self.beta1, self.beta2, self.eps, step, seed)      # the call's own: threads may step at the same time
         check(lib().chimera_op_adamw(self.dtype, self.bits, self.count, self.n, self.param, self.master, self.grad, self.m, self.v, self.scale,
-                                     self.decay, C.byref(h), _ptr(d_hyper), _vector(grad_scale, torch.float32, 1, "grad_scale"),
+                                     self.decay, C.byref(h), _device_hyper(d_hyper), _vector(grad_scale, torch.float32, 1, "grad_scale"),
                                      _stream_of(self.tensors[0][0], grad_scale, d_hyper)))

@@ -239,3 +239,42 @@ def test_adamw_steps_share_no_hyperparameters(monkeypatch):
     handle.step(lr=2e-3, step=4, seed=6)
     seen = [next(a._obj for a in call if isinstance(getattr(a, "_obj", None), b.AdamWHyper)) for call in calls]
     assert [(h.lr, h.beta1, h.beta2, h.eps, h.step, h.seed) for h in seen] == [(1e-3, 0.8, 0.9, 1e-6, 3, 5), (2e-3, 0.8, 0.9, 1e-6, 4, 6)]
+
+
+def _bad_device_hypers(torch):
+    # the structure alone, without the bytes that the library uses behind it; one byte short; strided
+    return [torch.zeros(C.sizeof(b.AdamWHyper), dtype=torch.uint8), torch.zeros(b.ADAMW_HYPER_BYTES - 1, dtype=torch.uint8), torch.zeros(15, dtype=torch.float64),
+            torch.zeros(2 * b.ADAMW_HYPER_BYTES, dtype=torch.uint8)[::2]]
+
+
+def test_adamw_checks_device_hyperparameters(monkeypatch):
+    torch = pytest.importorskip("torch")
+    handle, _, calls = _handle(monkeypatch)
+    for bad in _bad_device_hypers(torch):
+        with pytest.raises(ValueError, match="d_hyper"):
+            handle.step(1e-3, 1, d_hyper=bad)
+    assert not calls
+    good = torch.zeros(b.ADAMW_HYPER_BYTES, dtype=torch.uint8)
+    handle.step(1e-3, 1, d_hyper=good)
+    assert good.data_ptr() in calls[0]
+
+
+def test_stage_step_checks_its_tensors(monkeypatch):
+    torch = pytest.importorskip("torch")
+    from types import SimpleNamespace
+    calls = []
+    monkeypatch.setattr(b, "lib", lambda: SimpleNamespace(chimera_stage_adamw_step=lambda *a: calls.append(a) or b.OK))
+    stage = SimpleNamespace(torch=torch, handle=1, weights=torch.zeros(8), adamw_state=torch.zeros(8), adamw_bits=32)
+    for bad in _bad_device_hypers(torch):
+        with pytest.raises(ValueError, match="d_hyper"):
+            b.Stage.adamw_step(stage, 1e-3, 1, d_hyper=bad)
+    for bad in (torch.zeros(1, dtype=torch.float64), torch.zeros(2), torch.zeros(0)):
+        with pytest.raises(ValueError, match="grad_scale"):
+            b.Stage.adamw_step(stage, 1e-3, 1, grad_scale=bad)
+    elsewhere = SimpleNamespace(get_device=lambda: 3)
+    for bad in (dict(grad_scale=elsewhere), dict(d_hyper=elsewhere)):
+        with pytest.raises(ValueError, match="GPU"):
+            b.Stage.adamw_step(stage, 1e-3, 1, **bad)
+    assert not calls
+    b.Stage.adamw_step(stage, 1e-3, 1, grad_scale=torch.ones(1), d_hyper=torch.zeros(b.ADAMW_HYPER_BYTES, dtype=torch.uint8))
+    assert len(calls) == 1
