@@ -294,6 +294,9 @@ class Stage:
         n = lib().chimera_stage_adamw_state_bytes(self.handle, state_bits)
         self.adamw_state = self.torch.empty(n, dtype=self.torch.uint8, device=self.device)
         self.adamw_bits = state_bits
+        # the current stream hands out the memory and may still be writing the weights; the stage's stream takes it from there
+        self.stream.wait_stream(self.torch.cuda.current_stream(self.device))
+        self.adamw_state.record_stream(self.stream)
         check(lib().chimera_stage_adamw_init(self.handle, _ptr(self.weights), _ptr(self.adamw_state), state_bits))
 
     def adamw_step(self, lr, step, beta1=0.9, beta2=0.95, eps=1e-8, decay=0.0, seed=0, grad_scale=None, d_hyper=None):

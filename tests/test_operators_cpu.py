@@ -278,3 +278,16 @@ def test_stage_step_checks_its_tensors(monkeypatch):
     assert not calls
     b.Stage.adamw_step(stage, 1e-3, 1, grad_scale=torch.ones(1), d_hyper=torch.zeros(b.ADAMW_HYPER_BYTES, dtype=torch.uint8))
     assert len(calls) == 1
+
+
+def test_stage_state_is_initialised_behind_what_holds_its_memory(monkeypatch):
+    """On a stage with a stream of its own: the state's memory comes from the current stream, whose work on it may not be done."""
+    from types import SimpleNamespace
+    did = []
+    state = SimpleNamespace(record_stream=lambda s: did.append(("record", s)), data_ptr=lambda: 256)
+    stream = SimpleNamespace(wait_stream=lambda s: did.append(("wait", s)))
+    torch = SimpleNamespace(empty=lambda *a, **k: did.append("empty") or state, uint8=None, cuda=SimpleNamespace(current_stream=lambda d: "current"))
+    monkeypatch.setattr(b, "lib", lambda: SimpleNamespace(chimera_stage_adamw_state_bytes=lambda *a: 64, chimera_stage_adamw_init=lambda *a: did.append("init") or b.OK))
+    stage = SimpleNamespace(torch=torch, handle=1, weights=SimpleNamespace(data_ptr=lambda: 0), device="cuda:0", stream=stream)
+    b.Stage.adamw_init(stage, 8)
+    assert did.index("empty") < did.index(("wait", "current")) < did.index("init") and ("record", stream) in did
