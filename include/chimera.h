@@ -552,8 +552,8 @@ int chimera_op_grad_norm(int count, const int64_t* h_n, const float* const* h_gr
  *   p = p (1 - lr decay) - lr / (1 - beta1^step) m / (sqrt(v) / sqrt(1 - beta2^step) + eps),
  * factor = d_grad_scale[0] (NULL: 1); where that is not finite the call changes nothing, so a step behind a gradient norm that overflowed is left out.
  * h_param: the weights in `dtype`.  CHIMERA_BF16: h_master holds them in float as well; the step updates those and rounds.  h_grad: float.
- * h_decay: one float per tensor (NULL: none decays).  Weights, master weights or moments of two tensors must not
- * overlap (EINVAL).
+ * h_decay: one float per tensor (NULL: none decays).  What is written (weights, master weights, moments, scales) must overlap neither itself nor a
+ * gradient (EINVAL); gradients may share memory.
  * state_bits 32: h_m, h_v point to floats, the moments above; h_scale is not used.
  * state_bits 8: h_m and h_v point to one byte per element, e4m3 numbers (4 exponent bits, bias 7, 3 of mantissa, no infinities) that hold m and
  * sqrt(v) as multiples of a float scale for each 256 elements of a tensor; h_scale to the pairs (m's, sqrt(v)'s), ceil(n / 256) of them.  Zeros are the

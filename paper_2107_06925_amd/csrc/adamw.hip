@@ -288,6 +288,28 @@ int check_hyper(const chimera_adamw_hyper& h) {
     return CHIMERA_OK;
 }
 
+// Spans of memory by kind, the last kind only read: whether what is written shares a byte with anything else.  One walk over all kinds in the order
+// of addresses, each of which usually comes sorted.
+struct Span {
+    uintptr_t begin, end;
+    bool operator<(const Span& o) const { return begin < o.begin; }
+};
+template <int KINDS> bool written_twice(std::vector<Span> (&spans)[KINDS]) {
+    size_t at[KINDS] = {};
+    for (auto& v : spans)
+        if (!std::is_sorted(v.begin(), v.end())) std::sort(v.begin(), v.end());
+    uintptr_t written = 0, read = 0;                          // ends of what has been passed
+    for (;;) {
+        int k = -1;
+        for (int i = 0; i < KINDS; ++i)
+            if (at[i] < spans[i].size() && (k < 0 || spans[i][at[i]] < spans[k][at[k]])) k = i;
+        if (k < 0) return false;
+        const Span s = spans[k][at[k]++];
+        if (s.begin < written || (k < KINDS - 1 && s.begin < read)) return true;
+        (k < KINDS - 1 ? written : read) = std::max(k < KINDS - 1 ? written : read, s.end);
+    }
+}
+
 }  // namespace
 
 int adamw_step(int dtype, int bits, int count, const AdamwTensor* t, const chimera_adamw_hyper* h_hyper, void* d_hyper, const float* d_factor, void* stream) {
@@ -398,7 +420,7 @@ int chimera_op_adamw(int dtype, int state_bits, int count, const int64_t* h_n, v
     const size_t e = dtype == CHIMERA_F32 ? 4 : 2;
     try {
         std::vector<AdamwTensor> t((size_t)count);
-        std::vector<std::pair<uintptr_t, uintptr_t>> spans[4];                // of what is written: weights, master weights, moments
+        std::vector<Span> spans[6];                                           // weights, master weights, moments, scales; gradients
         for (auto& v : spans) v.reserve((size_t)count);
         for (int i = 0; i < count; ++i) {
             if (h_n[i] < 0 || h_n[i] > 1ll << 32) return fail(CHIMERA_EINVAL, "tensor %d of %lld values", i, (long long)h_n[i]);
@@ -412,16 +434,15 @@ int chimera_op_adamw(int dtype, int state_bits, int count, const int64_t* h_n, v
                 return fail(CHIMERA_EINVAL, "tensor %d is not aligned to its elements", i);
             if (!(q.decay >= 0) || !std::isfinite(q.decay)) return fail(CHIMERA_EINVAL, "weight decay of tensor %d must be finite and not negative", i);
             const size_t moment = (size_t)h_n[i] * (state_bits == 32 ? 4 : 1);
-            spans[0].push_back({(uintptr_t)q.p, (uintptr_t)q.p + (size_t)h_n[i] * e});
-            if (q.master) spans[1].push_back({(uintptr_t)q.master, (uintptr_t)q.master + (size_t)h_n[i] * 4});
-            spans[2].push_back({(uintptr_t)q.m, (uintptr_t)q.m + moment});
-            spans[3].push_back({(uintptr_t)q.v, (uintptr_t)q.v + moment});
+            auto take = [&](int kind, const void* p, size_t bytes) { if (p) spans[kind].push_back({(uintptr_t)p, (uintptr_t)p + bytes}); };
+            take(0, q.p, (size_t)h_n[i] * e);
+            take(1, q.master, (size_t)h_n[i] * 4);
+            take(2, q.m, moment);
+            take(3, q.v, moment);
+            take(4, q.scale, (size_t)(h_n[i] + MOMENT_BLOCK - 1) / MOMENT_BLOCK * 8);
+            take(5, q.g, (size_t)h_n[i] * 4);
         }
-        for (auto& v : spans) {
-            if (!std::is_sorted(v.begin(), v.end())) std::sort(v.begin(), v.end());
-            for (size_t i = 1; i < v.size(); ++i)
-                if (v[i].first < v[i - 1].second) return fail(CHIMERA_EINVAL, "weights or moments of two tensors overlap");
-        }
+        if (written_twice(spans)) return fail(CHIMERA_EINVAL, "what the step writes overlaps: weights, master weights, moments, scales or gradients of its tensors");
         return adamw_step(dtype, state_bits, count, t.data(), h_hyper, d_hyper, d_grad_scale, hip_stream);
     } catch (const std::bad_alloc&) {
         return fail(CHIMERA_ENOMEM, "out of host memory");

@@ -291,3 +291,16 @@ def test_stage_state_is_initialised_behind_what_holds_its_memory(monkeypatch):
     stage = SimpleNamespace(torch=torch, handle=1, weights=SimpleNamespace(data_ptr=lambda: 0), device="cuda:0", stream=stream)
     b.Stage.adamw_init(stage, 8)
     assert did.index("empty") < did.index(("wait", "current")) < did.index("init") and ("record", stream) in did
+
+
+def test_adamw_refuses_overlaps_between_kinds():
+    """What is written, tensor by tensor and kind by kind, shares no byte with anything else; 300 values a tensor, two blocks of 8-bit moments."""
+    at = lambda k: P + 0x1000 * k  # noqa: E731
+    good = dict(n=(300, 300), param=(at(0), at(1)), master=(at(2), at(3)), grad=(at(4), at(5)), m=(at(6), at(7)), v=(at(8), at(9)))
+    scales = (at(10), at(11))
+    for bits, bad in ((32, dict(v=(at(6), at(9)))), (32, dict(v=(at(8), at(6) + 1196))), (32, dict(m=(at(2) + 4, at(7)))), (32, dict(param=(at(0), at(9) + 1198))),
+                      (32, dict(grad=(at(0), at(5)))), (32, dict(grad=(at(4), at(3) - 1196))), (32, dict(master=(at(2), at(5)))), (8, dict(m=(at(6), at(6) + 299))),
+                      (8, dict(v=(at(6), at(9)))), (8, dict(scale=(at(10), at(10) + 12))), (8, dict(scale=(at(6) + 296, at(11)))), (8, dict(scale=(at(10), at(4) - 12)))):
+        args = dict(good, bits=bits, scale=scales if bits == 8 else None)
+        args.update(bad)
+        assert adamw(**args) == b.EINVAL and "overlaps" in b.last_error(), (bits, bad, b.last_error())
