@@ -743,6 +743,7 @@ StepState step_state(const chimera_stage* st, int bits) {
 int check_step(const chimera_stage* st, const void* d_weights, const void* d_state, int bits) {
     if (!st) return fail(CHIMERA_EINVAL, "stage is NULL");
     if (!st->bound) return fail(CHIMERA_ESTATE, "stage is not bound");
+    if (!st->keep) return fail(CHIMERA_ESTATE, "a forward-only stage forms no gradients: step the stage whose weights it shares");
     if (bits != 32 && bits != 8) return fail(CHIMERA_EINVAL, "moments of %d bits (8 or 32)", bits);
     if (!d_weights || !d_state) return fail(CHIMERA_EINVAL, "a device buffer is NULL");
     if (((uintptr_t)d_weights | (uintptr_t)d_state) & 255) return fail(CHIMERA_EINVAL, "device buffers must be 256-byte aligned");

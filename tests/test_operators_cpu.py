@@ -304,3 +304,17 @@ def test_adamw_refuses_overlaps_between_kinds():
         args = dict(good, bits=bits, scale=scales if bits == 8 else None)
         args.update(bad)
         assert adamw(**args) == b.EINVAL and "overlaps" in b.last_error(), (bits, bad, b.last_error())
+
+
+def test_forward_only_stage_is_not_stepped():
+    """It may be bound to the weights and gradients of another stage, and has none of its own."""
+    l = b.lib()
+    for bits in (32, 8):
+        st = l.chimera_stage_create(2, 64, 4, 16, 2, b.BF16)
+        for option in (b.OPT_KEEP, b.OPT_OVERLAP):
+            b.check(l.chimera_stage_set_option(st, option, 0))
+        b.check(l.chimera_stage_bind(st, P, P, P, 1, P, None))
+        h = b.AdamWHyper(1e-3, 0.9, 0.95, 1e-8, 1, 0)
+        for rc in (l.chimera_stage_adamw_init(st, 2 * P, 4 * P, bits), l.chimera_stage_adamw_step(st, 2 * P, 4 * P, bits, 0.0, C.byref(h), None, None)):
+            assert rc == b.ESTATE and "forward-only" in b.last_error()
+        l.chimera_stage_destroy(st)
