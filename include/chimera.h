@@ -572,7 +572,8 @@ int chimera_op_adamw(int dtype, int state_bits, int count, const int64_t* h_n, v
                      const float* const* h_grad, void* const* h_m, void* const* h_v, float* const* h_scale, const float* h_decay,
                      const chimera_adamw_hyper* h_hyper, void* d_hyper, const float* d_grad_scale, void* hip_stream);
 /* The same for a stage: d_weights (the buffer the stage is bound to, or another in its layout) from the stage's gradients, on the stage's stream.
- * d_state: chimera_stage_adamw_state_bytes bytes, 256-byte aligned, laid out by chimera_stage_adamw_init (master weights from d_weights, moments zero).
+ * d_state: chimera_stage_adamw_state_bytes bytes, 256-byte aligned, laid out by chimera_stage_adamw_init (master weights from d_weights, moments zero);
+ * weights, state and gradients must not overlap (EINVAL).
  * `decay` applies to the four matrices of a block, not to biases and LayerNorm parameters.  ESTATE: stage not bound or forward-only (it forms no
  * gradients), or micro-batches of it in flight (their backward reads the weights; other stages bound to the same weights are the caller's to finish first). */
 size_t chimera_stage_adamw_state_bytes(const chimera_stage* st, int state_bits);

@@ -747,6 +747,12 @@ int check_step(const chimera_stage* st, const void* d_weights, const void* d_sta
     if (bits != 32 && bits != 8) return fail(CHIMERA_EINVAL, "moments of %d bits (8 or 32)", bits);
     if (!d_weights || !d_state) return fail(CHIMERA_EINVAL, "a device buffer is NULL");
     if (((uintptr_t)d_weights | (uintptr_t)d_state) & 255) return fail(CHIMERA_EINVAL, "device buffers must be 256-byte aligned");
+    const size_t params = st->layer_params * st->L;
+    const std::pair<uintptr_t, size_t> held[] = {{(uintptr_t)d_weights, params * st->esz}, {(uintptr_t)d_state, step_state(st, bits).total}, {(uintptr_t)st->grads, params * 4}};
+    for (int i = 1; i < 3; ++i)
+        for (int j = 0; j < i; ++j)
+            if (held[i].first < held[j].first + held[j].second && held[j].first < held[i].first + held[i].second)
+                return fail(CHIMERA_EINVAL, "weights, state and gradients overlap");
     return CHIMERA_OK;
 }
 __global__ __launch_bounds__(256) void widen_kernel(const __bf16* __restrict__ from, float* __restrict__ to, size_t n) {

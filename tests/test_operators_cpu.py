@@ -318,3 +318,20 @@ def test_forward_only_stage_is_not_stepped():
         for rc in (l.chimera_stage_adamw_init(st, 2 * P, 4 * P, bits), l.chimera_stage_adamw_step(st, 2 * P, 4 * P, bits, 0.0, C.byref(h), None, None)):
             assert rc == b.ESTATE and "forward-only" in b.last_error()
         l.chimera_stage_destroy(st)
+
+
+def test_stage_step_refuses_overlapping_buffers():
+    l = b.lib()
+    params = 2 * (12 * 64 * 64 + 13 * 64)
+    up = lambda n: (n + 255) // 256 * 256  # noqa: E731
+    h = b.AdamWHyper(1e-3, 0.9, 0.95, 1e-8, 1, 0)
+    for dtype, e in ((b.F32, 4), (b.BF16, 2)):
+        for bits in (32, 8):
+            st = l.chimera_stage_create(2, 64, 4, 16, 2, dtype)
+            b.check(l.chimera_stage_set_option(st, b.OPT_OVERLAP, 0))
+            far, state = 1 << 24, up(l.chimera_stage_adamw_state_bytes(st, bits))
+            b.check(l.chimera_stage_bind(st, P, far, P, 1, P, None))
+            for w, s in ((P, P), (P, P + up(params * e) - 256), (P + state - 256, P), (P, far), (P, far + up(params * 4) - 256), (P, far - state + 256), (far, P)):
+                for rc in (l.chimera_stage_adamw_init(st, w, s, bits), l.chimera_stage_adamw_step(st, w, s, bits, 0.0, C.byref(h), None, None)):
+                    assert rc == b.EINVAL and "overlap" in b.last_error(), (dtype, bits, w, s)
+            l.chimera_stage_destroy(st)
