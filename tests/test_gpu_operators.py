@@ -643,3 +643,102 @@ def test_tensors_elsewhere_are_refused():
     step = b.AdamW([z(4)], [z(4)], [z(4)], [z(4)])
     with pytest.raises(ValueError, match="current GPU"):
         step.step(1e-3, 1, grad_scale=z(1, at="cpu"))
+
+
+# ------------------------------------------------- 8-bit moments, bit for bit
+def _random_bits(number, step, seed):
+    """32 bits for each value, from its number in the call (CPU, integers modulo 2^32)."""
+    mask = 0xFFFFFFFF
+    key = (seed & mask) * 0x243F6A89 + (step & mask) * 0xB7E15163
+    x = ((number & mask) * 0x9E3779B1 + (number >> 32) * 0x6A09E667 + (key & mask)) & mask
+    x = ((x ^ (x >> 15)) * 0x6A09E667) & mask
+    x = ((x ^ (x >> 13)) * 0xBB67AE85) & mask
+    return x ^ (x >> 16)
+
+
+def _codes(x, bits16, stays):
+    """[blocks, 256] floats -> e4m3 codes and scales, from the formula: up or down by 16 random bits; what `stays` does not fall to zero.  Each operation rounded by itself."""
+    torch = _torch()
+    top = x.abs().amax(1, keepdim=True)
+    some = top > 1e-30
+    y = x.abs() * torch.where(some, (1.0 / top) * 448.0, torch.zeros_like(top))
+    code = (((y * 2.0 ** -120).view(torch.int32) + bits16.to(torch.int32) * 16 + 8) >> 20).clamp(max=126)
+    if stays:
+        code = torch.where((x > 0) & some, code.clamp(min=1), code)
+    code = torch.where(x < 0, code | 128, code).to(torch.uint8)
+    return code, torch.where(some, top * (torch.ones(1) / 448.0), torch.zeros_like(top))
+
+
+def _eight_bit_step(s, factor, step, seed):
+    """Codes and scales of all tensors after a step, on the CPU."""
+    torch = _torch()
+    out, block = [], 0
+    for i, g in enumerate(s["grads"]):
+        n = g.numel()
+        blocks = (n + 255) // 256
+        if not n:
+            out.append(None)
+            continue
+        pad = lambda x: torch.nn.functional.pad(x.cpu(), (0, blocks * 256 - n)).view(blocks, 256)  # noqa: E731
+        scale = s["scales"][i].cpu().view(-1, 2)
+        m, r = pad(s["ms"][i].float()) * scale[:, :1], pad(s["vs"][i].float()) * scale[:, 1:]
+        x = pad(g) * factor
+        m, v = m * H["beta1"] + x * (1.0 - H["beta1"]), (r * r) * H["beta2"] + (x * x) * (1.0 - H["beta2"])
+        bits = _random_bits(torch.arange(blocks * 256) + block * 256, step, seed).view(blocks, 256)
+        (cm, sm), (cv, sv) = _codes(m, bits & 0xFFFF, False), _codes(v.sqrt(), bits >> 16, True)
+        out.append((cm.view(-1)[:n], cv.view(-1)[:n], torch.cat((sm, sv), 1).view(-1)))
+        block += blocks
+    return out
+
+
+@pytest.mark.parametrize("sizes", [[1], [255, 1, 257], [4096, 4095, 0, 4097, 3], [64, 300, 1] * 40, [300_001, 12, 0, 70_000]], ids=lambda s: "%dx%d" % (len(s), max(s)))
+@pytest.mark.parametrize("dtype", [b.F32, b.BF16])
+def test_adamw_eight_bit_codes_bit_for_bit(dtype, sizes):
+    torch = _torch()
+    print("adamw codes", dtype, len(sizes), max(sizes), flush=True)
+    s = _tensors(dtype, sizes, 8, seed=len(sizes))
+    handle = b.AdamW(**H, **s)
+    factor = torch.tensor([0.4])
+    for step, seed in ((1, 0), (2, 77), (70_000, 2 ** 32 - 1)):
+        want = _eight_bit_step(s, factor, step, seed)
+        handle.step(lr=1e-3, step=step, seed=seed, grad_scale=factor.cuda())
+        for i, w in enumerate(want):
+            if w is not None:
+                assert torch.equal(s["ms"][i].view(torch.uint8).cpu(), w[0]) and torch.equal(s["vs"][i].view(torch.uint8).cpu(), w[1]), (i, step)
+                assert torch.equal(s["scales"][i].cpu(), w[2]), (i, step)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("dtype", [b.F32, b.BF16])
+def test_stage_steps_as_its_tensors_do(dtype, bits):
+    """A stage's step and the step over the same tensors leave the same bits, master weights among them."""
+    torch = _torch()
+    from paper_2107_06925_amd import synth
+    from gpu_util import make_stage
+    print("stage as tensors", dtype, bits, flush=True)
+    L, hidden, seq, mb = 2, 72, 24, 3
+    st, _ = make_stage(L, hidden, 4, seq, mb, dtype, 0)
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    x, dy = (torch.randn((seq * mb, hidden), device="cuda", generator=gen).to(_dtype(dtype)) for _ in range(2))
+    st.set_io(0, x, dy)
+    shapes = list(synth.param_shapes(hidden).values()) * L
+    sizes = [math.prod(q) for q in shapes]
+    params = [t.clone() for t in st.weights.split(sizes)]
+    masters = [t.float() for t in params] if dtype == b.BF16 else None
+    moment = lambda: [torch.zeros(n, device="cuda", dtype=torch.float32 if bits == 32 else torch.uint8) for n in sizes]  # noqa: E731
+    scales = None if bits == 32 else [torch.zeros(2 * ((n + 255) // 256), device="cuda") for n in sizes]
+    handle = b.AdamW(params, list(st.grads.split(sizes)), moment(), moment(), masters=masters, scales=scales, decay=[0.1 if len(q) == 2 else 0.0 for q in shapes])
+    st.adamw_init(bits)
+    norm = torch.empty(2, device="cuda")
+    start = st.weights.clone()
+    for step in range(1, 4):
+        st.zero_grads()
+        st.fwd(0)
+        st.bwd(0)
+        b.chimera_op_grad_norm([st.grads], 0.05, norm)
+        handle.step(3e-3, step, seed=5, grad_scale=norm[1:])
+        st.adamw_step(3e-3, step, decay=0.1, seed=5, grad_scale=norm[1:])
+        assert torch.equal(st.weights, torch.cat(params)), step
+        if masters:
+            assert torch.equal(st.adamw_state[:4 * st.weights.numel()].view(torch.float32), torch.cat(masters)), step
+    assert not torch.equal(st.weights, start)
