@@ -685,7 +685,8 @@ def _eight_bit_step(s, factor, step, seed):
         x = pad(g) * factor
         m, v = m * H["beta1"] + x * (1.0 - H["beta1"]), (r * r) * H["beta2"] + (x * x) * (1.0 - H["beta2"])
         bits = _random_bits(torch.arange(blocks * 256) + block * 256, step, seed).view(blocks, 256)
-        (cm, sm), (cv, sv) = _codes(m, bits & 0xFFFF, False), _codes(v.sqrt(), bits >> 16, True)
+        root = v.double().sqrt().float()              # correctly rounded (53 bits hold a float's root to twice its bits and more); torch's own float root is not, everywhere
+        (cm, sm), (cv, sv) = _codes(m, bits & 0xFFFF, False), _codes(root, bits >> 16, True)
         out.append((cm.view(-1)[:n], cv.view(-1)[:n], torch.cat((sm, sv), 1).view(-1)))
         block += blocks
     return out
