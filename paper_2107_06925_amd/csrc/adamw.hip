@@ -38,7 +38,8 @@ __host__ __device__ Scalars scalars_of(const chimera_adamw_hyper& h) {
     s.eps = (float)h.eps; s.lr = (float)h.lr;
     s.rate = (float)(h.lr / (1.0 - pow(h.beta1, (double)h.step)));
     s.root = (float)(1.0 / sqrt(1.0 - pow(h.beta2, (double)h.step)));
-    s.key = (unsigned)h.seed * 0x243F6A89u + (unsigned)h.step * 0xB7E15163u;     // (pi and e, as odd numbers; below the golden ratio and the roots of 2 and 3)
+    // all 64 bits of both.  (Odd numbers from pi and e, and from the roots of 11 and 17; below from the golden ratio and the roots of 2 and 3.)
+    s.key = (unsigned)h.seed * 0x243F6A89u + (unsigned)h.step * 0xB7E15163u + (unsigned)(h.seed >> 32) * 0x510E527Fu + (unsigned)((uint64_t)h.step >> 32) * 0x1F83D9ABu;
     return s;
 }
 struct DeviceHyper { chimera_adamw_hyper given; Scalars derived; };

@@ -743,3 +743,16 @@ def test_stage_steps_as_its_tensors_do(dtype, bits):
         if masters:
             assert torch.equal(st.adamw_state[:4 * st.weights.numel()].view(torch.float32), torch.cat(masters)), step
     assert not torch.equal(st.weights, start)
+
+
+def test_adamw_rounds_by_all_of_the_seed_and_the_step():
+    # workers that take rank << 32 | seed must not round alike; numbers below 2^32 keep the bits of the formula above
+    torch = _torch()
+    seen = []
+    for seed, step in ((9, 3), (1 << 32 | 9, 3), (2 << 32 | 9, 3), (9, 1 << 32 | 3), (1 << 63 | 9, 3)):
+        s = _tensors(b.BF16, [5000, 333], 8)
+        b.AdamW(**H, **s).step(lr=1e-3, step=step, seed=seed)
+        seen.append(torch.cat([t.view(torch.uint8) for t in s["ms"] + s["vs"]]))
+    for i in range(len(seen)):
+        for j in range(i):
+            assert float((seen[i] != seen[j]).float().mean()) > 0.2, (i, j)
