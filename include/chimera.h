@@ -556,7 +556,8 @@ int chimera_op_grad_norm(int count, const int64_t* h_n, const float* const* h_gr
  * gradient (EINVAL); gradients may share memory.
  * state_bits 32: h_m, h_v point to floats, the moments above; h_scale is not used.
  * state_bits 8: h_m and h_v point to one byte per element, e4m3 numbers (4 exponent bits, bias 7, 3 of mantissa, no infinities) that hold m and
- * sqrt(v) as multiples of a float scale for each 256 elements of a tensor; h_scale to the pairs (m's, sqrt(v)'s), ceil(n / 256) of them.  Zeros are the
+ * sqrt(v) as multiples of a float scale for each 256 elements of a tensor; h_scale to the pairs (m's, sqrt(v)'s), ceil(n / 256) of them.  An element
+ * whose m or v is infinite has that moment kept as not a number; the rest of its block is as without it.  Zeros are the
  * state before the first step in either width.  Codes are rounded up or down at random, with the right mean, by a hash of seed, step and the
  * element's number in the call (tensors counted in whole blocks of 256): the same call on the same state gives the same bits.
  * Tensors are aligned to their elements.  lr >= 0, beta1 and beta2 in [0, 1), eps in [2^-126, 1], decay >= 0, step >= 1.  d_hyper (may be NULL): device memory of CHIMERA_ADAMW_HYPER_BYTES bytes, 16-byte aligned, that begins with a

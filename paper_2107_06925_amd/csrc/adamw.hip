@@ -13,6 +13,7 @@
 #include "device.h"
 
 #include <algorithm>
+#include <cfloat>
 #include <climits>
 #include <cmath>
 #include <new>
@@ -85,7 +86,7 @@ __device__ __forceinline__ unsigned mixed(unsigned x) {
 __device__ __forceinline__ unsigned encode(float x, float inv, unsigned bits16, bool keep) {
 #pragma clang fp contract(off)
     const float y = fabsf(x) * inv;
-    if (y != y) return 0x7f;                                  // not a number stays one
+    if (!(y <= FLT_MAX)) return 0x7f;                         // not a number stays one, and e4m3 has no infinities
     unsigned code = min((__float_as_uint(y * 0x1p-120f) + bits16 * 16u + 8u) >> 20, 126u);
     if (keep && x > 0.f) code = max(code, 1u);
     return x < 0.f ? code | 0x80u : code;
@@ -194,6 +195,17 @@ __global__ __launch_bounds__(STEP_THREADS) void adamw_kernel(StepLaunch L) {
                 if (e < have) { tm = fmaxf(tm, fabsf(m[e])); tv = fmaxf(tv, r[e]); }
             tm = wave_max(tm);
             tv = wave_max(tv);
+            if (!(fmaxf(tm, tv) <= FLT_MAX)) {                // an infinite moment is not its block's scale, which would leave the others no value
+                auto largest = [&](const f4_t& x) {
+                    float top = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (e < have && fabsf(x[e]) <= FLT_MAX) top = fmaxf(top, fabsf(x[e]));
+                    return wave_max(top);
+                };
+                tm = largest(m);
+                tv = largest(r);
+            }
             const float im = tm > CODE_LEAST ? __fdiv_rn(1.0f, tm) * CODE_TOP : 0.f, iv = tv > CODE_LEAST ? __fdiv_rn(1.0f, tv) * CODE_TOP : 0.f;
             unsigned qm = 0, qv = 0;
             const unsigned start = random_start((unsigned long long)(t.block0 * MOMENT_BLOCK + i), s.key);

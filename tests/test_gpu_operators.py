@@ -756,3 +756,32 @@ def test_adamw_rounds_by_all_of_the_seed_and_the_step():
     for i in range(len(seen)):
         for j in range(i):
             assert float((seen[i] != seen[j]).float().mean()) > 0.2, (i, j)
+
+
+@pytest.mark.parametrize("bad", [float("inf"), -float("inf"), 1e25, float("nan")])
+def test_adamw_eight_bit_infinities_stay_in_their_value(bad):
+    """1e25 is finite and its square is not: v alone becomes infinite.  The block's other values step as if the gradient were zero there."""
+    torch = _torch()
+    s, calm = _tensors(b.BF16, [600], 8, seed=2), _tensors(b.BF16, [600], 8, seed=2)
+    at = 300                                                              # in the second block
+    for q in (s, calm):                                                   # not its largest, whatever the gradient
+        q["ms"][0].view(torch.uint8)[at] = 0
+        q["vs"][0].view(torch.uint8)[at] = 8
+    s["grads"][0][at], calm["grads"][0][at] = bad, 0.0
+    others = torch.arange(600, device="cuda") != at
+    if bad == 1e25:                                                       # its m is finite, and the block's largest
+        others &= (torch.arange(600, device="cuda") < 256) | (torch.arange(600, device="cuda") >= 512)
+    handles = [b.AdamW(**H, **q) for q in (s, calm)]
+    for step in (1, 2):
+        for h in handles:
+            h.step(lr=1e-3, step=step, seed=4)
+        for k in ("params", "masters", "ms", "vs"):
+            x, y = (q[k][0].view(torch.uint8).view(600, -1)[others] for q in (s, calm))
+            assert torch.equal(x, y), (step, k)
+        m, v = _moments(s, 0)
+        assert torch.isnan(v[at]) and (bad == 1e25 or torch.isnan(m[at]))
+        keep = torch.arange(600, device="cuda") != at
+        assert torch.isfinite(m[keep]).all() and torch.isfinite(v[keep]).all() and torch.isfinite(s["masters"][0][keep]).all()
+        if bad != 1e25:
+            assert torch.equal(s["scales"][0], calm["scales"][0])
+        s["grads"][0][at] = 0.0                                           # once
