@@ -522,7 +522,9 @@ int chimera_head_loss(int dtype, int tokens, int hidden, int vocab, const void* 
  *   += h^T dz, or = with overwrite != 0.  Either may be NULL, not both.  z is formed again, `piece` columns of the vocabulary at a time (rounded up to
  *   a multiple of 256; 0: the library's choice); the workspace grows with it.
  * bf16: dh is formed from dz in 11 bits, dW from dz in 22, so that it is as exact as a sum of floats; the products' sums are float.
- * All sums have a fixed order.  Calls that overlap in time need workspaces of their own; kernels run on the current device, which holds all tensors.  ENOMEM if the workspace is too small (a function of the same sizes; 0 for sizes that the calls refuse). */
+ * All sums have a fixed order.  Calls that overlap in time need workspaces of their own; kernels run on the current device, which holds all tensors.
+ * Results and workspace must share no memory with each other or with an operand (EINVAL); d_dh alone may lie on d_h.
+ * ENOMEM if the workspace is too small (a function of the same sizes; 0 for sizes that the calls refuse). */
 size_t chimera_op_linear_xent_fwd_workspace_bytes(int dtype, int tokens, int hidden, int vocab);
 int chimera_op_linear_xent_fwd(int dtype, int tokens, int hidden, int vocab, const void* d_h, int ldh, const void* d_w, int ldw,
                                const int32_t* d_targets, float scale, float* d_loss_rows, float* d_lse, float* d_loss,
@@ -532,7 +534,8 @@ int chimera_op_linear_xent_bwd(int dtype, int tokens, int hidden, int vocab, con
                                const int32_t* d_targets, const float* d_lse, float scale, const float* d_dloss, void* d_dh, int lddh,
                                float* d_dw, int lddw, int overwrite, int piece, void* d_workspace, size_t workspace_bytes, void* hip_stream);
 /* chimera_head_loss on these two: the same results (tokens whose target lies outside [0, vocab) do not count here; their rows of y
- * still have to be finite) without its [tokens, vocab] workspace, for any vocab.  d_w_head and d_dw_head have rows ldw apart.  It forms z twice and dW from a
+ * still have to be finite) without its [tokens, vocab] workspace, for any vocab.  d_w_head and d_dw_head have rows ldw apart; d_dy may be d_y itself, nothing else that is written
+ * may share memory with anything (EINVAL).  It forms z twice and dW from a
  * finer dz, two thirds more work on the matrix cores: bf16 2048 x 1600 x 50304 1.69 ms in 276 MB, chimera_head_loss 1.22 in 344; float 128 x 128 x 50304 0.14 against 0.28. */
 size_t chimera_head_pieces_workspace_bytes(int dtype, int tokens, int hidden, int vocab, int piece);
 int chimera_head_loss_pieces(int dtype, int tokens, int hidden, int vocab, const void* d_y, const int32_t* d_targets, const void* d_lnf_g,

@@ -21,6 +21,8 @@
 #include <climits>
 #include <cmath>
 #include <cstdlib>
+#include <initializer_list>
+#include <utility>
 
 namespace chimera {
 namespace {
@@ -770,6 +772,34 @@ int check_xent(int dtype, int tokens, int hidden, int vocab, int ldh, int ldw) {
     return CHIMERA_OK;
 }
 
+// Rows of memory `pitch` bytes apart, of which `width` bytes are read or written (at 0: none)
+struct Rows { const void* at; size_t rows, width, pitch; };
+Rows matrix(const void* p, size_t rows, size_t cols, size_t ld, size_t element) { return {p, rows, cols * element, ld * element}; }
+Rows plain(const void* p, size_t bytes) { return {p, 1, bytes, bytes}; }
+// Whether two of them share a byte.  Where their extents meet, rows of either may still lie between the other's.
+bool meet(Rows a, Rows b) {
+    if (a.rows > b.rows) std::swap(a, b);
+    const uintptr_t pa = (uintptr_t)a.at, pb = (uintptr_t)b.at;
+    if (!pa || !pb || pa + (a.rows - 1) * a.pitch + a.width <= pb || pb + (b.rows - 1) * b.pitch + b.width <= pa) return false;
+    for (size_t i = 0; i < a.rows; ++i) {
+        const uintptr_t x = pa + i * a.pitch, end = x + a.width;
+        if (end <= pb) continue;
+        const size_t last = std::min((size_t)(end - 1 - pb) / b.pitch, b.rows - 1);          // b's last row that begins before this one ends
+        if (pb + last * b.pitch + b.width > x) return true;
+    }
+    return false;
+}
+// What a call writes must share nothing with what it reads, nor with what else it writes.
+int check_apart(std::initializer_list<Rows> reads, std::initializer_list<Rows> writes) {
+    for (const Rows* w = writes.begin(); w != writes.end(); ++w) {
+        for (const Rows& r : reads)
+            if (meet(*w, r)) return fail(CHIMERA_EINVAL, "a result or the workspace overlaps an operand");
+        for (const Rows* v = writes.begin(); v != w; ++v)
+            if (meet(*w, *v)) return fail(CHIMERA_EINVAL, "results or the workspace overlap");
+    }
+    return CHIMERA_OK;
+}
+
 template <typename R> R raster_of(int tile, int rows, int cols, int k, bool bands = true) {
     R r{(rows + tile - 1) / tile, (cols + tile - 1) / tile, 1, 0};
     if (bands) r.band = raster_band(r.tiles_m, r.tiles_n, NUM_CUS, (size_t)cols * k * 2);
@@ -932,6 +962,9 @@ int chimera_op_linear_xent_fwd(int dtype, int tokens, int hidden, int vocab, con
     if (((uintptr_t)d_workspace & 255) || (((uintptr_t)d_h | (uintptr_t)d_w) & 15)) return fail(CHIMERA_EINVAL, "workspace must be 256-byte aligned, tensors 16-byte aligned");
     const FwdLayout l = fwd_layout(dtype, tokens, hidden, vocab);
     if (workspace_bytes < l.total) return fail(CHIMERA_ENOMEM, "workspace holds %zu bytes, need %zu", workspace_bytes, l.total);
+    const size_t e = dtype == CHIMERA_F32 ? 4 : 2, m = (size_t)tokens;
+    XENT_TRY(check_apart({matrix(d_h, m, hidden, ldh, e), matrix(d_w, hidden, vocab, ldw, e), plain(d_targets, m * 4)},
+                         {plain(d_loss_rows, m * 4), plain(d_lse, m * 4), plain(d_loss, 4), plain(d_workspace, l.total)}));
     char* ws = (char*)d_workspace;
     float2* stats = (float2*)(ws + l.stats);
     float* at_target = (float*)(ws + l.at_target);
@@ -964,6 +997,11 @@ int chimera_op_linear_xent_bwd(int dtype, int tokens, int hidden, int vocab, con
         return fail(CHIMERA_EINVAL, "workspace must be 256-byte aligned, tensors 16-byte aligned");
     const BwdLayout l = bwd_layout(dtype, tokens, hidden, vocab, piece);
     if (workspace_bytes < l.total) return fail(CHIMERA_ENOMEM, "workspace holds %zu bytes, need %zu", workspace_bytes, l.total);
+    const size_t e = dtype == CHIMERA_F32 ? 4 : 2, m = (size_t)tokens;
+    const Rows dh = matrix(d_dh, m, hidden, lddh, e), dw = matrix(d_dw, hidden, vocab, lddw, 4), h = matrix(d_h, m, hidden, ldh, e), rest = plain(d_workspace, l.total);
+    // (dh is written when h has been read for the last time, and may take its place)
+    for (const Rows& r : {matrix(d_w, hidden, vocab, ldw, e), plain(d_targets, m * 4), plain(d_lse, m * 4), plain(d_dloss, m * 4)}) XENT_TRY(check_apart({r}, {dh, dw, rest}));
+    XENT_TRY(check_apart({h}, {dw, rest}));
     char* ws = (char*)d_workspace;
     if (dtype == CHIMERA_F32)
         return xent_bwd_f32(tokens, hidden, vocab, (const float*)d_h, ldh, (const float*)d_w, ldw, d_targets, d_lse, scale, d_dloss, (float*)d_dh, lddh, d_dw, lddw,
@@ -988,6 +1026,12 @@ int chimera_head_loss_pieces(int dtype, int tokens, int hidden, int vocab, const
         return fail(CHIMERA_EINVAL, "workspace must be 256-byte aligned, tensors 16-byte aligned");
     const HeadLayout l = head_layout(dtype, tokens, hidden, vocab, piece);
     if (workspace_bytes < l.total) return fail(CHIMERA_ENOMEM, "workspace holds %zu bytes, need %zu", workspace_bytes, l.total);
+    const size_t e = dtype == CHIMERA_F32 ? 4 : 2, m = (size_t)tokens, v = (size_t)hidden;
+    const Rows dy = plain(d_dy, m * v * e), dg = plain(d_dlnf_g, v * 4), db = plain(d_dlnf_b, v * 4), dw = matrix(d_dw_head, v, vocab, ldw, 4), loss = plain(d_loss, 4),
+               rest = plain(d_workspace, l.total);
+    // (dy is written last, where each row of y has just been read, and may be y itself)
+    XENT_TRY(check_apart({matrix(d_w_head, v, vocab, ldw, e), plain(d_targets, m * 4), plain(d_lnf_g, v * e), plain(d_lnf_b, v * e)}, {dy, dg, db, dw, loss, rest}));
+    XENT_TRY(check_apart({plain(d_y, m * v * e)}, {d_dy == d_y ? plain(nullptr, 1) : dy, dg, db, dw, loss, rest}));
     char* ws = (char*)d_workspace;
     void *h = ws + l.h, *dh = ws + l.dh;
     float *mean = (float*)(ws + l.mean), *rstd = (float*)(ws + l.rstd), *rows = (float*)(ws + l.loss_rows), *lse = (float*)(ws + l.lse);

@@ -785,3 +785,41 @@ def test_adamw_eight_bit_infinities_stay_in_their_value(bad):
         if bad != 1e25:
             assert torch.equal(s["scales"][0], calm["scales"][0])
         s["grads"][0][at] = 0.0                                           # once
+
+
+# ------------------------------------------------------------- shared memory
+@pytest.mark.parametrize("dtype", [b.F32, b.BF16])
+@pytest.mark.parametrize("tokens,hidden,vocab,piece", [(150, 136, 1027, 512), (40, 64, 300, 0)])
+def test_linear_xent_dh_in_the_place_of_h_and_beside_it(dtype, tokens, hidden, vocab, piece):
+    torch = _torch()
+    h, w, targets = _case(dtype, tokens, hidden, vocab, seed=2)
+    _, lse, _ = _forward(h, w, targets, 1.0)
+    dh, dw, _ = _backward(dtype, h, w, targets, lse, 0.1, piece=piece, overwrite=True)
+    place = h.clone()                                                     # on h
+    dw2 = torch.zeros((hidden, (vocab + 7) // 8 * 8), device="cuda")
+    b.chimera_op_linear_xent_bwd(place, w, targets, lse, 0.1, place, dw2[:, :vocab], overwrite=True, piece=piece)
+    assert torch.equal(place, dh) and torch.equal(dw2[:, :vocab], dw)
+    both = torch.cat((h, torch.zeros_like(h)), 1)                         # rows of dh between those of h
+    b.chimera_op_linear_xent_bwd(both[:, :hidden], w, targets, lse, 0.1, both[:, hidden:], dw2[:, :vocab], overwrite=True, piece=piece)
+    assert torch.equal(both[:, hidden:], dh) and torch.equal(both[:, :hidden], h) and torch.equal(dw2[:, :vocab], dw)
+
+
+@pytest.mark.parametrize("dtype", [b.F32, b.BF16])
+@pytest.mark.parametrize("tokens,hidden", [(130, 256), (67, 1600)])
+def test_head_in_pieces_dy_in_the_place_of_y(dtype, tokens, hidden):
+    torch = _torch()
+    vocab, t = 1001, _dtype(dtype)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    rnd = lambda *s: torch.randn(s, device="cuda", generator=gen)  # noqa: E731
+    y, g, be = rnd(tokens, hidden).to(t), (1 + 0.1 * rnd(hidden)).to(t), (0.1 * rnd(hidden)).to(t)
+    w = (rnd(hidden, 1008) / math.sqrt(hidden)).to(t)
+    targets = torch.randint(0, vocab, (tokens,), device="cuda", generator=gen, dtype=torch.int32)
+    runs = []
+    for place in (False, True):
+        x = y.clone()
+        dy = x if place else torch.zeros_like(y)
+        rest = [torch.zeros(hidden, device="cuda"), torch.zeros(hidden, device="cuda"), torch.zeros((hidden, 1008), device="cuda"), torch.zeros(1, device="cuda")]
+        b.chimera_head_loss_pieces(x, targets, g, be, w[:, :vocab], 1.0 / tokens, dy, *rest)
+        runs.append([dy] + rest)
+    for a, c in zip(*runs):
+        assert torch.equal(a, c)

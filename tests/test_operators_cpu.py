@@ -335,3 +335,52 @@ def test_stage_step_refuses_overlapping_buffers():
                 for rc in (l.chimera_stage_adamw_init(st, w, s, bits), l.chimera_stage_adamw_step(st, w, s, bits, 0.0, C.byref(h), None, None)):
                     assert rc == b.EINVAL and "overlap" in b.last_error(), (dtype, bits, w, s)
             l.chimera_stage_destroy(st)
+
+
+FAR = 1 << 40                                   # places that are far apart, whatever lies at them
+
+
+def test_linear_xent_refuses_overlaps():
+    """4 tokens of 64, 100 words in rows of 104: every result over every operand and every other result, at its last bytes."""
+    l = b.lib()
+    for dtype, e in ((b.F32, 4), (b.BF16, 2)):
+        at = {k: FAR * (i + 1) for i, k in enumerate(("h", "w", "targets", "rows", "lse", "loss", "ws"))}
+        size = dict(h=4 * 64 * e, w=(63 * 104 + 100) * e, targets=16, rows=16, lse=16, loss=4, ws=l.chimera_op_linear_xent_fwd_workspace_bytes(dtype, 4, 64, 100))
+        align = dict(h=16, w=16, targets=4, rows=4, lse=4, loss=4, ws=256)
+        for out in ("rows", "lse", "loss", "ws"):
+            for other in set(at) - {out}:
+                first, second = (out, other) if align[out] > align[other] else (other, out)            # the second begins inside the first
+                inside = at[first] + (size[first] - 1) // align[second] * align[second]
+                assert fwd(dtype=dtype, **dict(at, **{second: inside})) == b.EINVAL and "overlap" in b.last_error(), (dtype, first, second)
+        at = {k: FAR * (i + 1) for i, k in enumerate(("h", "w", "targets", "lse", "dloss", "dh", "dw", "ws"))}
+        size = dict(h=4 * 64 * e, w=(63 * 104 + 100) * e, targets=16, lse=16, dloss=16, dh=4 * 64 * e, dw=(63 * 104 + 100) * 4,
+                    ws=l.chimera_op_linear_xent_bwd_workspace_bytes(dtype, 4, 64, 100, 0))
+        align = dict(h=16, w=16, targets=4, lse=4, dloss=4, dh=16, dw=16, ws=256)
+        for out in ("dh", "dw", "ws"):
+            for other in set(at) - {out}:
+                if (out, other) == ("dh", "h"):
+                    continue
+                first, second = (out, other) if align[out] > align[other] else (other, out)
+                inside = at[first] + (size[first] - 1) // align[second] * align[second]
+                assert bwd(dtype=dtype, **dict(at, **{second: inside})) == b.EINVAL and "overlap" in b.last_error(), (dtype, first, second)
+    # rows of dh between those of w, and on them: 64 rows of w, 512 bytes apart, hold 100 words; 4 rows of dh begin 256 bytes behind one of them
+    at = dict(h=FAR, w=2 * FAR, targets=3 * FAR, lse=4 * FAR, dw=5 * FAR, ws=6 * FAR)
+    assert bwd(dtype=b.BF16, ldw=256, dh=2 * FAR + 512 * 9 + 192, lddh=256, **at) == b.EINVAL and "overlap" in b.last_error()
+    assert bwd(dtype=b.BF16, ldw=256, dh=2 * FAR + 512 * 62 + 192, lddh=512, **at) == b.EINVAL and "overlap" in b.last_error()
+
+
+def test_head_loss_pieces_refuses_overlaps():
+    l = b.lib()
+    names = ("y", "t", "g", "be", "w", "dy", "dg", "db", "dw", "loss", "ws")
+    for dtype, e in ((b.F32, 4), (b.BF16, 2)):
+        size = dict(y=4 * 64 * e, t=16, g=64 * e, be=64 * e, w=(63 * 104 + 100) * e, dy=4 * 64 * e, dg=256, db=256, dw=(63 * 104 + 100) * 4, loss=4,
+                    ws=l.chimera_head_pieces_workspace_bytes(dtype, 4, 64, 100, 0))
+        align = {k: 256 if k == "ws" else 16 if k in ("y", "w", "dy", "dw") else 4 for k in names}
+        for out in ("dy", "dg", "db", "dw", "loss", "ws"):
+            for other in set(names) - {out}:
+                at = {k: FAR * (i + 1) for i, k in enumerate(names)}
+                first, second = (out, other) if align[out] > align[other] else (other, out)
+                at[second] = at[first] + (size[first] - 1) // align[second] * align[second]
+                rc = l.chimera_head_loss_pieces(dtype, 4, 64, 100, at["y"], at["t"], at["g"], at["be"], at["w"], 104, 1.0, at["dy"], at["dg"], at["db"], at["dw"],
+                                                at["loss"], 0, at["ws"], U64, None)
+                assert rc == b.EINVAL and "overlap" in b.last_error(), (dtype, first, second)
