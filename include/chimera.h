@@ -545,7 +545,8 @@ int chimera_head_loss_pieces(int dtype, int tokens, int hidden, int vocab, const
 /* ------------------------------------------------------- from gradients to weights
  * Norm of `count` float gradient tensors taken as one vector: d_out[0] = sqrt(sum of all squares), d_out[1] = the factor that brings it down to
  * max_norm, min(1, max_norm / norm); NaN where the norm is no finite float.  Squares are summed in double, in a fixed order.  h_n: element
- * counts (0 is fine), h_grad: device pointers; both host arrays, read before the call returns, as below.  The workspace is 8-byte aligned. */
+ * counts (0 is fine), h_grad: device pointers; both host arrays, read before the call returns, as below.  The workspace is 8-byte aligned.  Result and workspace
+ * must share no memory with a gradient or with one another (EINVAL). */
 size_t chimera_op_grad_norm_workspace_bytes(int count);
 int chimera_op_grad_norm(int count, const int64_t* h_n, const float* const* h_grad, float max_norm, float* d_out,
                          void* d_workspace, size_t workspace_bytes, void* hip_stream);

@@ -399,6 +399,14 @@ int chimera_op_grad_norm(int count, const int64_t* h_n, const float* const* h_gr
     for (int i = 0; i < count; ++i)
         if (h_n[i] && (!h_grad[i] || ((uintptr_t)h_grad[i] & 3))) return fail(CHIMERA_EINVAL, "gradient %d is NULL or not aligned to floats", i);
     if (workspace_bytes < norm_bytes(count)) return fail(CHIMERA_ENOMEM, "workspace holds %zu bytes, need %zu", workspace_bytes, norm_bytes(count));
+    const Span out{(uintptr_t)d_out, (uintptr_t)d_out + 8}, rest{(uintptr_t)d_workspace, (uintptr_t)d_workspace + norm_bytes(count)};
+    auto meet = [](const Span& a, const Span& b) { return a.begin < b.end && b.begin < a.end; };
+    bool apart = !meet(out, rest);
+    for (int i = 0; i < count; ++i) {
+        const Span g{(uintptr_t)h_grad[i], (uintptr_t)h_grad[i] + (size_t)h_n[i] * 4};
+        apart = apart && !(h_n[i] && (meet(g, out) || meet(g, rest)));
+    }
+    if (!apart) return fail(CHIMERA_EINVAL, "the result or the workspace overlaps a gradient, or one another");
     hipStream_t s = (hipStream_t)hip_stream;
     NormLaunch L{};
     L.chunk = chunk;

@@ -384,3 +384,11 @@ def test_head_loss_pieces_refuses_overlaps():
                 rc = l.chimera_head_loss_pieces(dtype, 4, 64, 100, at["y"], at["t"], at["g"], at["be"], at["w"], 104, 1.0, at["dy"], at["dg"], at["db"], at["dw"],
                                                 at["loss"], 0, at["ws"], U64, None)
                 assert rc == b.EINVAL and "overlap" in b.last_error(), (dtype, first, second)
+
+
+def test_grad_norm_refuses_overlaps():
+    need = b.lib().chimera_op_grad_norm_workspace_bytes(3)
+    for bad in (dict(out=FAR + 28), dict(out=3 * FAR + 16), dict(out=FAR - 4), dict(ws=FAR + 24), dict(ws=FAR - need + 8), dict(out=5 * FAR + need - 4), dict(ws=3 * FAR - need + 16)):
+        args = dict(n=(8, 0, 5), grads=(FAR, None, 3 * FAR), out=4 * FAR, ws=5 * FAR)
+        args.update(bad)
+        assert norm(**args) == b.EINVAL and "overlaps" in b.last_error(), bad
