@@ -556,8 +556,8 @@ int chimera_op_grad_norm(int count, const int64_t* h_n, const float* const* h_gr
  *   p = p (1 - lr decay) - lr / (1 - beta1^step) m / (sqrt(v) / sqrt(1 - beta2^step) + eps),
  * factor = d_grad_scale[0] (NULL: 1); where that is not finite the call changes nothing, so a step behind a gradient norm that overflowed is left out.
  * h_param: the weights in `dtype`.  CHIMERA_BF16: h_master holds them in float as well; the step updates those and rounds.  h_grad: float.
- * h_decay: one float per tensor (NULL: none decays).  What is written (weights, master weights, moments, scales) must overlap neither itself nor a
- * gradient (EINVAL); gradients may share memory.
+ * h_decay: one float per tensor (NULL: none decays).  What is written (weights, master weights, moments, scales, d_hyper) must overlap neither itself nor a
+ * gradient or d_grad_scale (EINVAL); gradients may share memory.
  * state_bits 32: h_m, h_v point to floats, the moments above; h_scale is not used.
  * state_bits 8: h_m and h_v point to one byte per element, e4m3 numbers (4 exponent bits, bias 7, 3 of mantissa, no infinities) that hold m and
  * sqrt(v) as multiples of a float scale for each 256 elements of a tensor; h_scale to the pairs (m's, sqrt(v)'s), ceil(n / 256) of them.  An element
@@ -578,7 +578,7 @@ int chimera_op_adamw(int dtype, int state_bits, int count, const int64_t* h_n, v
                      const chimera_adamw_hyper* h_hyper, void* d_hyper, const float* d_grad_scale, void* hip_stream);
 /* The same for a stage: d_weights (the buffer the stage is bound to, or another in its layout) from the stage's gradients, on the stage's stream.
  * d_state: chimera_stage_adamw_state_bytes bytes, 256-byte aligned, laid out by chimera_stage_adamw_init (master weights from d_weights, moments zero);
- * weights, state and gradients must not overlap (EINVAL).
+ * weights, state, gradients, d_hyper and d_grad_scale must not overlap (EINVAL).
  * `decay` applies to the four matrices of a block, not to biases and LayerNorm parameters.  ESTATE: stage not bound or forward-only (it forms no
  * gradients), or micro-batches of it in flight (their backward reads the weights; other stages bound to the same weights are the caller's to finish first). */
 size_t chimera_stage_adamw_state_bytes(const chimera_stage* st, int state_bits);

@@ -441,7 +441,7 @@ int chimera_op_adamw(int dtype, int state_bits, int count, const int64_t* h_n, v
     const size_t e = dtype == CHIMERA_F32 ? 4 : 2;
     try {
         std::vector<AdamwTensor> t((size_t)count);
-        std::vector<Span> spans[6];                                           // weights, master weights, moments, scales; gradients
+        std::vector<Span> spans[7];                                           // weights, master weights, moments, scales, hyperparameters; what is read
         for (auto& v : spans) v.reserve((size_t)count);
         for (int i = 0; i < count; ++i) {
             if (h_n[i] < 0 || h_n[i] > 1ll << 32) return fail(CHIMERA_EINVAL, "tensor %d of %lld values", i, (long long)h_n[i]);
@@ -461,9 +461,11 @@ int chimera_op_adamw(int dtype, int state_bits, int count, const int64_t* h_n, v
             take(2, q.m, moment);
             take(3, q.v, moment);
             take(4, q.scale, (size_t)(h_n[i] + MOMENT_BLOCK - 1) / MOMENT_BLOCK * 8);
-            take(5, q.g, (size_t)h_n[i] * 4);
+            take(6, q.g, (size_t)h_n[i] * 4);
         }
-        if (written_twice(spans)) return fail(CHIMERA_EINVAL, "what the step writes overlaps: weights, master weights, moments, scales or gradients of its tensors");
+        if (d_hyper) spans[5].push_back({(uintptr_t)d_hyper, (uintptr_t)d_hyper + CHIMERA_ADAMW_HYPER_BYTES});
+        if (d_grad_scale) spans[6].push_back({(uintptr_t)d_grad_scale, (uintptr_t)d_grad_scale + 4});
+        if (written_twice(spans)) return fail(CHIMERA_EINVAL, "what the step writes overlaps: weights, master weights, moments, scales, hyperparameters, or a gradient or factor with one of these");
         return adamw_step(dtype, state_bits, count, t.data(), h_hyper, d_hyper, d_grad_scale, hip_stream);
     } catch (const std::bad_alloc&) {
         return fail(CHIMERA_ENOMEM, "out of host memory");

@@ -740,7 +740,7 @@ StepState step_state(const chimera_stage* st, int bits) {
     s.total = b;
     return s;
 }
-int check_step(const chimera_stage* st, const void* d_weights, const void* d_state, int bits) {
+int check_step(const chimera_stage* st, const void* d_weights, const void* d_state, int bits, const void* d_hyper = nullptr, const float* d_factor = nullptr) {
     if (!st) return fail(CHIMERA_EINVAL, "stage is NULL");
     if (!st->bound) return fail(CHIMERA_ESTATE, "stage is not bound");
     if (!st->keep) return fail(CHIMERA_ESTATE, "a forward-only stage forms no gradients: step the stage whose weights it shares");
@@ -748,11 +748,12 @@ int check_step(const chimera_stage* st, const void* d_weights, const void* d_sta
     if (!d_weights || !d_state) return fail(CHIMERA_EINVAL, "a device buffer is NULL");
     if (((uintptr_t)d_weights | (uintptr_t)d_state) & 255) return fail(CHIMERA_EINVAL, "device buffers must be 256-byte aligned");
     const size_t params = st->layer_params * st->L;
-    const std::pair<uintptr_t, size_t> held[] = {{(uintptr_t)d_weights, params * st->esz}, {(uintptr_t)d_state, step_state(st, bits).total}, {(uintptr_t)st->grads, params * 4}};
-    for (int i = 1; i < 3; ++i)
+    const std::pair<uintptr_t, size_t> held[] = {{(uintptr_t)d_weights, params * st->esz}, {(uintptr_t)d_state, step_state(st, bits).total}, {(uintptr_t)st->grads, params * 4},
+                                                 {(uintptr_t)d_hyper, CHIMERA_ADAMW_HYPER_BYTES}, {(uintptr_t)d_factor, 4}};
+    for (int i = 1; i < 5; ++i)
         for (int j = 0; j < i; ++j)
-            if (held[i].first < held[j].first + held[j].second && held[j].first < held[i].first + held[i].second)
-                return fail(CHIMERA_EINVAL, "weights, state and gradients overlap");
+            if (held[i].first && held[j].first && held[i].first < held[j].first + held[j].second && held[j].first < held[i].first + held[i].second)
+                return fail(CHIMERA_EINVAL, "weights, state, gradients, hyperparameters or factor overlap");
     return CHIMERA_OK;
 }
 __global__ __launch_bounds__(256) void widen_kernel(const __bf16* __restrict__ from, float* __restrict__ to, size_t n) {
@@ -961,7 +962,7 @@ int chimera_stage_adamw_init(chimera_stage* st, const void* d_weights, void* d_s
 
 int chimera_stage_adamw_step(chimera_stage* st, void* d_weights, void* d_state, int state_bits, float decay, const chimera_adamw_hyper* h_hyper,
                              void* d_hyper, const float* d_grad_scale) {
-    TRY(check_step(st, d_weights, d_state, state_bits));
+    TRY(check_step(st, d_weights, d_state, state_bits, d_hyper, d_grad_scale));
     TRY(adamw_check(st->dtype, state_bits, h_hyper, d_hyper));
     if (!(decay >= 0 && decay <= 3e38f)) return fail(CHIMERA_EINVAL, "weight decay must be finite and not negative");
     if (!st->in_flight.empty()) return fail(CHIMERA_ESTATE, "micro-batches are in flight");

@@ -392,3 +392,19 @@ def test_grad_norm_refuses_overlaps():
         args = dict(n=(8, 0, 5), grads=(FAR, None, 3 * FAR), out=4 * FAR, ws=5 * FAR)
         args.update(bad)
         assert norm(**args) == b.EINVAL and "overlaps" in b.last_error(), bad
+
+
+def test_adamw_refuses_factors_and_device_hyperparameters_in_what_it_writes():
+    at = lambda k: P + 0x1000 * k  # noqa: E731
+    l, h = b.lib(), b.AdamWHyper(1e-3, 0.9, 0.95, 1e-8, 1, 0)
+    two = lambda k: (C.c_void_p * 2)(at(k), at(k + 1))  # noqa: E731
+    for device, factor in ((None, at(1) + 596), (None, at(3)), (None, at(6) + 1196), (at(8) + 1184, None), (at(2) - 112, None), (at(4) + 16, None),
+                           (FAR, FAR + b.ADAMW_HYPER_BYTES - 4)):
+        rc = l.chimera_op_adamw(b.BF16, 32, 2, (C.c_int64 * 2)(300, 300), two(0), two(2), two(4), two(6), two(8), None, None, C.byref(h), device, factor, None)
+        assert rc == b.EINVAL and "overlaps" in b.last_error(), (device, factor, b.last_error())
+    st = l.chimera_stage_create(2, 64, 4, 16, 2, b.BF16)
+    b.check(l.chimera_stage_set_option(st, b.OPT_OVERLAP, 0))
+    b.check(l.chimera_stage_bind(st, FAR, 2 * FAR, P, 1, P, None))
+    for device, factor in ((FAR - 112, None), (None, FAR + 4), (None, 2 * FAR), (2 * FAR + 16, None), (None, 3 * FAR), (3 * FAR + 256, None), (4 * FAR, 4 * FAR + 48)):
+        assert l.chimera_stage_adamw_step(st, FAR, 3 * FAR, 8, 0.0, C.byref(h), device, factor) == b.EINVAL and "overlap" in b.last_error(), (device, factor)
+    l.chimera_stage_destroy(st)
