@@ -521,7 +521,9 @@ int chimera_head_loss(int dtype, int tokens, int hidden, int vocab, const void* 
  *   d_dh [tokens, hidden] (dtype, rows lddh apart) = dz W^T,  d_dw [hidden, vocab] (float, rows lddw apart, columns from vocab on left as they are)
  *   += h^T dz, or = with overwrite != 0.  Either may be NULL, not both.  z is formed again, `piece` columns of the vocabulary at a time (rounded up to
  *   a multiple of 256; 0: the library's choice); the workspace grows with it.
- * bf16: dh is formed from dz in 11 bits, dW from dz in 22, so that it is as exact as a sum of floats; the products' sums are float.
+ * bf16: dh is formed from dz in 11 bits, dW from dz in 22; the products' sums are float.  Both hold dz as fp16 numbers under a power of two for each token, so
+ * exp(z[t, v] - d_lse[t]) must stay below 3.9: d_lse is the logsumexp of the row as the forward leaves it, or of more words than these, or larger.  Where it is
+ * smaller the token's row of d_dh, and d_dw, are infinite or not numbers (float follows the formula).
  * All sums have a fixed order.  Calls that overlap in time need workspaces of their own; kernels run on the current device, which holds all tensors.
  * Results and workspace must share no memory with each other or with an operand (EINVAL); d_dh alone may lie on d_h.
  * ENOMEM if the workspace is too small (a function of the same sizes; 0 for sizes that the calls refuse). */

@@ -580,7 +580,8 @@ def chimera_op_linear_xent_fwd(h, w, targets, scale, loss_rows, lse, loss=None, 
 
 
 def chimera_op_linear_xent_bwd(h, w, targets, lse, scale, dh=None, dw=None, dloss=None, overwrite=False, piece=0, workspace=None):
-    """dh [tokens, hidden] (type of h) and dw [hidden, vocab] (float) are tensors to be filled, or None; dloss float [tokens] or None."""
+    """dh [tokens, hidden] (type of h) and dw [hidden, vocab] (float) are tensors to be filled, or None; dloss float [tokens] or None.  lse: what the forward
+    left, or the logsumexp over more words than w holds; bfloat16 holds exp(logit - lse) up to 3.9."""
     import torch
     (tokens, hidden), vocab = h.shape, w.shape[1]
     if workspace is None:

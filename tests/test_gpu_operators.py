@@ -823,3 +823,28 @@ def test_head_in_pieces_dy_in_the_place_of_y(dtype, tokens, hidden):
         runs.append([dy] + rest)
     for a, c in zip(*runs):
         assert torch.equal(a, c)
+
+
+# ------------------------------------------------ logsumexps of other rows
+@pytest.mark.parametrize("dtype", [b.F32, b.BF16])
+def test_linear_xent_bwd_with_other_logsumexps(dtype):
+    torch = _torch()
+    h, w, targets = _case(dtype, 70, 64, 1001, seed=3)
+    z = h.double() @ w.double()
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    dloss = torch.rand(70, device="cuda", generator=gen) + 0.5
+    # over twice as many words; much larger; as small as bf16 takes: the largest probability 3.9
+    for lse in ((torch.logsumexp(z, 1) + math.log(2)).float(), (torch.logsumexp(z, 1) + 30).float(), (z.amax(1) - math.log(3.9)).float()):
+        dh, dw, dw0 = _backward(dtype, h, w, targets, lse, 0.01, dloss, overwrite=True, piece=512)
+        _check_backward(dtype, h, w, targets, lse, 0.01, dloss, dh, dw, torch.zeros_like(dw0))
+    # smaller than that for some tokens: float follows the formula, bf16 leaves no finite number, and the other tokens' rows as they are
+    less = lse.clone()
+    less[::7] -= 3.0
+    valid = (targets >= 0) & (targets < 1001)
+    dh2, dw, dw0 = _backward(dtype, h, w, targets, less, 0.01, dloss, overwrite=True, piece=512)
+    if dtype == b.F32:
+        _check_backward(dtype, h, w, targets, less, 0.01, dloss, dh2, dw, torch.zeros_like(dw0))
+    else:
+        low = torch.zeros(70, dtype=torch.bool, device="cuda")
+        low[::7] = True
+        assert not torch.isfinite(dh2[low & valid]).any() and torch.equal(dh2[~low], dh[~low])
