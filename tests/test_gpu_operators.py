@@ -157,8 +157,8 @@ def _check_backward(dtype, h, w, targets, lse, scale, dloss, dh, dw, dw0):
         assert ((got - want).abs() <= tol + E24 * dw0.double().abs()).all(), float(((got - want).abs() / tol).max())
 
 
-# (tokens, hidden, vocab, ldw, piece): one piece and several, the last a few columns or ending inside a group of 8; tiles of 256 for dz
-# (1024 x 9300), dh (4100 x 2304: more 256x256 tiles than 128x128 ones pay for) and dW (1000 x 9473)
+# (tokens, hidden, vocab, ldw, piece): one piece and several, the last a few columns or ending inside a group of 8; dW cut along the tokens, on
+# 256x256 tiles (3000 x 256 x 30001, 9000 x 136 x 2051) and on 128x128 ones (6100 x 72 x 1100); uncut on 256x256 tiles: BWD_LARGE, below
 BWD = [(1, 8, 1, 8, 0), (1, 64, 7, 16, 0), (2, 8, 8, 8, 0), (3, 16, 9, 24, 0), (24, 256, 1000, 1000, 0), (33, 72, 257, 264, 256), (130, 136, 1027, 1088, 256),
        (260, 264, 771, 776, 512), (60, 512, 8000, 8000, 0), (1024, 64, 9300, 9304, 0), (40, 1000, 9473, 9480, 4864), (2200, 128, 2001, 2008, 0),
        (4100, 2304, 1031, 1032, 512), (3000, 256, 30001, 30008, 0), (100, 320, 20011, 20024, 4608),
@@ -848,3 +848,100 @@ def test_linear_xent_bwd_with_other_logsumexps(dtype):
         low = torch.zeros(70, dtype=torch.bool, device="cuda")
         low[::7] = True
         assert not torch.isfinite(dh2[low & valid]).any() and torch.equal(dh2[~low], dh[~low])
+
+
+# ------------------------------------------------------ the dispatch of large calls
+def _wide(tokens, hidden, vocab):
+    """Columns of a bf16 forward on 256x256 tiles, from its workspace: a (maximum, sum) pair for each token and tile column, and a float a token."""
+    need = b.lib().chimera_op_linear_xent_fwd_workspace_bytes(b.BF16, tokens, hidden, vocab)
+    columns = (need - (4 * tokens + 255) // 256 * 256) // (8 * tokens)
+    return 256 * ((vocab + 127) // 128 - columns)                         # each 256 wide tile is one column fewer
+
+
+# whole rounds of 256x256 tiles and 128x128 ones behind them: a few of those and many, one round and several, in bands where W (164 MB) does not stay in the
+# memory-side cache, rows that end inside a tile; and 256x256 tiles alone, several rounds of them
+@pytest.mark.parametrize("tokens,hidden,vocab,ldw,mixed", [(400, 512, 33001, 33008, True), (300, 256, 33001, 33064, True), (2048, 72, 50257, 50264, True),
+                                                           (1100, 192, 20001, 20008, True), (700, 320, 45001, 45008, True), (2100, 2048, 40001, 40008, True), (2048, 256, 32765, 32768, False)])
+def test_linear_xent_fwd_of_two_tile_sizes(tokens, hidden, vocab, ldw, mixed):
+    _torch()
+    print("linear xent fwd, large", tokens, hidden, vocab, ldw, flush=True)
+    wide = _wide(tokens, hidden, vocab)
+    assert (0 < wide < vocab) if mixed else wide >= vocab
+    h, w, targets = _case(b.BF16, tokens, hidden, vocab, ldw, hidden + 8, seed=tokens + vocab)
+    ends = [0, 255, 256, vocab - 1] + ([wide - 1, wide, wide + 127, wide + 128] if mixed else [])       # words beside the seams
+    for i, word in enumerate(ends):
+        targets[i], targets[tokens - 1 - i] = min(word, vocab - 1), min(word, vocab - 1)
+    rows, lse, loss = _forward(h, w, targets, 0.25)
+    _check_forward(b.BF16, h, w, targets, 0.25, rows, lse, loss)
+
+
+# bf16, dW in 256x256 tiles (from 128 of them on) over an undivided contraction, straight into the caller's matrix: rows of tokens beside them of 256 (more
+# than 128 tokens) or of 128; several pieces, the last one of a few columns, several rounds of tiles
+BWD_LARGE = [(300, 2048, 20001, 20008, 0), (300, 1024, 20003, 20016, 9984), (130, 1600, 21001, 21008, 20992), (1500, 1600, 12007, 12008, 0),
+             (100, 2048, 32001, 32008, 0), (16, 1024, 50257, 50264, 0), (1, 1600, 50257, 50304, 0), (128, 2048, 20485, 20488, 10240)]
+
+
+@pytest.mark.parametrize("tokens,hidden,vocab,ldw,piece", BWD_LARGE)
+def test_linear_xent_bwd_large(tokens, hidden, vocab, ldw, piece):
+    test_linear_xent_bwd(b.BF16, tokens, hidden, vocab, ldw, piece)
+
+
+@pytest.mark.parametrize("dtype", [b.F32, b.BF16])
+@pytest.mark.parametrize("tokens,hidden,vocab,ldw,piece", [(700, 512, 20001, 20008, 0), (2100, 256, 5003, 5008, 1024), (160, 2048, 16400, 16400, 0)])
+def test_head_in_pieces_large(dtype, tokens, hidden, vocab, ldw, piece):
+    """Several tiles of every product, against 64 bits through autograd.  Logits of deviation 1, whose rounded operands move dy and dW by less than the
+    rounding of h and of dh to the type, half of the bar each; a quarter of the tokens does not count."""
+    torch = _torch()
+    print("head pieces, large", dtype, tokens, hidden, vocab, flush=True)
+    t = _dtype(dtype)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    rnd = lambda *s: torch.randn(s, device="cuda", generator=gen)  # noqa: E731
+    y, g, be = rnd(tokens, hidden).to(t), (1 + 0.1 * rnd(hidden)).to(t), (0.1 * rnd(hidden)).to(t)
+    w = torch.full((hidden, ldw), float("nan"), device="cuda", dtype=t)
+    w[:, :vocab] = (rnd(hidden, vocab) / math.sqrt(hidden)).to(t)
+    targets = torch.randint(0, vocab, (tokens,), device="cuda", generator=gen, dtype=torch.int32)
+    targets[::4] = -1
+    got = [torch.full((tokens, hidden), 9.0, device="cuda", dtype=t), torch.full((hidden,), 0.5, device="cuda"), torch.full((hidden,), -0.5, device="cuda"),
+           torch.full((hidden, ldw), 0.25, device="cuda"), torch.full((1,), 2.0, device="cuda")]
+    b.chimera_head_loss_pieces(y, targets, g, be, w[:, :vocab], 1.0 / tokens, *got, piece=piece)
+    p = [x.double().requires_grad_() for x in (y, g, be, w[:, :vocab])]
+    h = torch.nn.functional.layer_norm(p[0], (hidden,), p[1], p[2], 1e-5)
+    loss = torch.nn.functional.cross_entropy(h @ p[3], targets.long(), ignore_index=-1, reduction="sum") / tokens
+    loss.backward()
+    tol = 2e-2 if dtype == b.BF16 else 1e-4
+    for name, a, q in zip(("dy", "dg", "db", "dw"), [got[0].double(), got[1].double() - 0.5, got[2].double() + 0.5, got[3][:, :vocab].double() - 0.25], [x.grad for x in p]):
+        err = float((a - q).abs().max() / q.abs().max())
+        assert err <= tol, (name, err)
+    assert (got[3][:, vocab:] == 0.25).all() and (got[0][::4] == 0).all()
+    assert abs(float(got[4]) - 2.0 - float(loss.detach())) <= tol * float(loss.detach())
+
+
+@pytest.mark.parametrize("dtype,piece", [(b.F32, 0), (b.BF16, 0), (b.BF16, 65536)])
+def test_linear_xent_beyond_2_31_logits(dtype, piece):
+    """40000 x 65536: rows and columns at both ends and on both sides of the 2^31st logit, against 64 bits."""
+    torch = _torch()
+    print("linear xent, 2.6e9 logits", dtype, piece, flush=True)
+    tokens, hidden, vocab, scale = 40000, 64, 65536, 0.01
+    h, w, targets = _case(dtype, tokens, hidden, vocab, seed=1)
+    few = torch.cat([torch.arange(a, a + 12) for a in (0, 16378, 32762, 39988)]).cuda()
+    targets[few[::3]] = (few[::3] * 331 % vocab).to(torch.int32)
+    rows, lse, loss = _forward(h, w, targets, scale)
+    _check_forward(dtype, h[few], w, targets[few], scale, rows[few], lse[few], float(rows[few].double().sum()) + 0.5)
+    total = float(rows.double().sum()) + 0.5
+    assert abs(float(loss) - total) <= (tokens + 8) * E24 * (float(rows.double().abs().sum()) + 0.5)
+    dh, dw, _ = _backward(dtype, h, w, targets, lse, scale, overwrite=True, piece=piece)
+    _check_backward(dtype, h[few], w, targets[few], lse[few], scale, None, dh[few], None, None)
+    cols = torch.cat([torch.arange(0, 8).cuda(), targets[few[::3]].long(), torch.arange(vocab - 8, vocab).cuda(), torch.arange(32764, 32772).cuda()])
+    wc = w[:, cols]
+    z, off = _logits(h, wc, dtype)
+    x = z - lse.double()[:, None]
+    p = x.exp()
+    p_off = p * (off + 3 * E24 * (x.abs() + z.abs()) + E22) + E23 * (p + 1)
+    valid = ((targets >= 0) & (targets < vocab)).double()
+    dz = scale * valid[:, None] * (p - (targets.long()[:, None] == cols[None, :]).double())
+    dz_off = scale * valid[:, None] * p_off + 2 * E24 * dz.abs()
+    hd = h.double()
+    want, mag = hd.t() @ dz, hd.abs().t() @ dz.abs()
+    top = scale * float(hd.abs().max())
+    tol = hd.abs().t() @ dz_off + (E22 + (2 * tokens + 80) * E24) * mag + tokens * 2.0 ** -36 * top + E24 * want.abs() + 1e-38
+    assert ((dw[:, cols].double() - want).abs() <= tol).all()
