@@ -511,7 +511,8 @@ int chimera_head_loss(int dtype, int tokens, int hidden, int vocab, const void* 
 
 /* The vocabulary projection and its cross-entropy without the logits: nothing of size [tokens, vocab] is kept or
  * written.  h [tokens, hidden] with rows ldh apart, W [hidden, vocab] with rows ldw apart (ldw >= vocab; the columns between may hold anything), both
- * in the given dtype; z = h W.  vocab is any number; hidden and the leading dimensions are multiples of 8, leading dimensions below 2^23, tokens up
+ * in the given dtype; z = h W.  The last row of W, too, is readable up to vocab rounded up to 8 columns (float, and d_dw: to 4), as it is in every matrix of whole rows
+ * and in every part of one that is aligned as below.  vocab is any number; hidden and the leading dimensions are multiples of 8, leading dimensions below 2^23, tokens up
  * to 2^22, hidden to 2^15, vocab to 2^22, tokens * vocab to 2^38; tensors 16-byte, the workspace 256-byte aligned.  A target outside [0, vocab) marks a token that does
  * not count (padding): its loss is 0 and it takes no part in any gradient, whatever its hidden state holds.
  *

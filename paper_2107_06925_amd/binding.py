@@ -540,10 +540,16 @@ def chimera_head_loss(y, targets, lnf_g, lnf_b, w_head, scale, dy, dlnf_g, dlnf_
 
 
 def _rows(t, dtype, what):
-    """Rows of a matrix whose rows are contiguous: how far they are apart."""
-    if t.dim() != 2 or t.dtype != dtype or (t.shape[1] > 1 and t.stride(1) != 1):
+    """Rows of a matrix whose rows are contiguous: how far they are apart.  The library reads whole pieces of 16 bytes, of the last row too."""
+    shape = t.shape
+    if len(shape) != 2 or t.dtype != dtype or (shape[1] > 1 and t.stride(1) != 1):
         raise ValueError("%s: a matrix of %s with contiguous rows expected" % (what, dtype))
-    return t.stride(0) if t.shape[0] > 1 else (t.shape[1] + 7) // 8 * 8
+    rows, cols = shape
+    ld = t.stride(0) if rows > 1 else (cols + 7) // 8 * 8
+    more = -cols % (16 // dtype.itemsize)
+    if more and rows and (t.storage_offset() + (rows - 1) * t.stride(0) + cols + more) * dtype.itemsize > t.untyped_storage().nbytes():
+        raise ValueError("%s: the memory of its last row ends inside a piece of 16 bytes" % what)
+    return ld
 
 
 def _vector(t, dtype, n, what):

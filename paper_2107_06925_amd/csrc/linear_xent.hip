@@ -829,7 +829,7 @@ int launch_dh_sum(const float* slabs, int splits, const T* dz, int ldz, const T*
 
 int xent_fwd_f32(int m, int hidden, int vocab, const float* h, int ldh, const float* w, int ldw, const int* targets, const FwdLayout& l, char* ws, void* stream) {
     for (int v0 = 0, p = 0; v0 < vocab; v0 += l.piece, ++p) {
-        const int cols = std::min(l.piece, vocab - v0), ld = round_up(cols, 8);
+        const int cols = std::min(l.piece, vocab - v0), ld = round_up(cols, 4);      // (a row of W ends no sooner: 16-byte alignment, leading dimensions in multiples of 8)
         GemmArgs g{};
         g.m = m; g.n = ld; g.k = hidden; g.a = h; g.lda = ldh; g.a_kc = 1; g.b = w + v0; g.ldb = ldw; g.b_kc = 0; g.c = ws + l.z; g.epilogue = EPI_NONE;
         XENT_TRY(gemm_f32(g, stream));
@@ -849,7 +849,7 @@ int xent_bwd_f32(int m, int hidden, int vocab, const float* h, int ldh, const fl
     CHIMERA_LAUNCH_CHECK("linear cross-entropy");
     int slabs = 0;
     for (int v0 = 0; v0 < vocab; v0 += l.piece) {
-        const int cols = std::min(l.piece, vocab - v0), ld = round_up(cols, 8), whole = cols & ~7;
+        const int cols = std::min(l.piece, vocab - v0), ld = round_up(cols, 4), whole = cols & ~7;
         GemmArgs g{};
         g.m = m; g.n = ld; g.k = hidden; g.a = h; g.lda = ldh; g.a_kc = 1; g.b = w + v0; g.ldb = ldw; g.b_kc = 0; g.c = z;
         g.epilogue = EPI_XENT; g.bias = info; g.gelu_erf = v0;

@@ -945,3 +945,26 @@ def test_linear_xent_beyond_2_31_logits(dtype, piece):
     top = scale * float(hd.abs().max())
     tol = hd.abs().t() @ dz_off + (E22 + (2 * tokens + 80) * E24) * mag + tokens * 2.0 ** -36 * top + E24 * want.abs() + 1e-38
     assert ((dw[:, cols].double() - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("dtype", [b.F32, b.BF16])
+@pytest.mark.parametrize("tokens,hidden,first,vocab,piece", [(40, 64, 4, 1012, 256), (33, 72, 12, 1001, 0), (130, 136, 8, 1008, 512), (9, 16, 4, 3, 0)])
+def test_linear_xent_of_the_last_columns_of_a_matrix(dtype, tokens, hidden, first, vocab, piece):
+    """W and dW as the columns behind `first` of wider matrices: nothing behind the last row is there, nor asked for."""
+    torch = _torch()
+    first = first if dtype == b.F32 else (first + 7) // 8 * 8                 # 16 bytes
+    wide = (first + vocab + 7) // 8 * 8
+    print("linear xent, last columns", dtype, tokens, hidden, first, vocab, wide, flush=True)
+    h, w, targets = _case(dtype, tokens, hidden, vocab, seed=7)
+    full = torch.full((hidden, wide), float("nan"), device="cuda", dtype=_dtype(dtype))
+    full[:, first:first + vocab] = w
+    part = full[:, first:first + vocab]
+    rows, lse, loss = _forward(h, part, targets, 0.25)
+    _check_forward(dtype, h, w, targets, 0.25, rows, lse, loss)
+    dfull = torch.full((hidden, wide), 0.5, device="cuda")
+    dpart, dh = dfull[:, first:first + vocab], torch.zeros_like(h)
+    for overwrite in (True, False):
+        b.chimera_op_linear_xent_bwd(h, part, targets, lse, 0.25, dh, dpart, overwrite=overwrite, piece=piece)
+        _check_backward(dtype, h, w, targets, lse, 0.25, None, dh, dpart, torch.zeros_like(dpart) if overwrite else before)
+        before = dpart.clone()
+    assert (dfull[:, :first] == 0.5).all() and (dfull[:, first + vocab:] == 0.5).all()

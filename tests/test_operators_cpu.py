@@ -408,3 +408,21 @@ def test_adamw_refuses_factors_and_device_hyperparameters_in_what_it_writes():
     for device, factor in ((FAR - 112, None), (None, FAR + 4), (None, 2 * FAR), (2 * FAR + 16, None), (None, 3 * FAR), (3 * FAR + 256, None), (4 * FAR, 4 * FAR + 48)):
         assert l.chimera_stage_adamw_step(st, FAR, 3 * FAR, 8, 0.0, C.byref(h), device, factor) == b.EINVAL and "overlap" in b.last_error(), (device, factor)
     l.chimera_stage_destroy(st)
+
+
+def test_binding_refuses_matrices_whose_memory_ends_too_soon():
+    """8 columns of bf16, 4 of float are read at a time, in the last row too, where no further row follows."""
+    torch = pytest.importorskip("torch")
+    for dtype, step in ((torch.float32, 4), (torch.bfloat16, 8)):
+        for short in range(1, step):
+            n = 24 - step + short                                             # columns; the last piece of 16 bytes holds `short` of them
+            assert b._rows(torch.zeros(16 * 24, dtype=dtype).as_strided((16, n), (24, 1)), dtype, "w") == 24
+            memory = torch.zeros(15 * 24 + n, dtype=dtype)
+            with pytest.raises(ValueError, match="16 bytes"):
+                b._rows(memory.as_strided((16, n), (24, 1)), dtype, "w")
+            z = lambda *s, d=torch.float32: torch.zeros(s, dtype=d)  # noqa: E731
+            with pytest.raises(ValueError, match="16 bytes"):
+                b.chimera_op_linear_xent_fwd(z(3, 16, d=dtype), memory.as_strided((16, n), (24, 1)), z(3, d=torch.int32), 1.0, z(3), z(3), workspace=z(8, d=torch.uint8))
+    # a part of a wider matrix that begins at a multiple of 16 bytes is whole
+    assert b._rows(torch.zeros((16, 24))[:, 4:23], torch.float32, "w") == 24
+    assert b._rows(torch.zeros((16, 24), dtype=torch.bfloat16)[:, 8:23], torch.bfloat16, "w") == 24
