@@ -308,19 +308,25 @@ struct Span {
     bool operator<(const Span& o) const { return begin < o.begin; }
 };
 template <int KINDS> bool written_twice(std::vector<Span> (&spans)[KINDS]) {
-    size_t at[KINDS] = {};
-    for (auto& v : spans)
+    struct Kind { const Span *at, *end; bool read; } kinds[KINDS];
+    int n = 0;
+    for (int i = 0; i < KINDS; ++i) {
+        auto& v = spans[i];
         if (!std::is_sorted(v.begin(), v.end())) std::sort(v.begin(), v.end());
-    uintptr_t written = 0, read = 0;                          // ends of what has been passed
-    for (;;) {
-        int k = -1;
-        for (int i = 0; i < KINDS; ++i)
-            if (at[i] < spans[i].size() && (k < 0 || spans[i][at[i]] < spans[k][at[k]])) k = i;
-        if (k < 0) return false;
-        const Span s = spans[k][at[k]++];
-        if (s.begin < written || (k < KINDS - 1 && s.begin < read)) return true;
-        (k < KINDS - 1 ? written : read) = std::max(k < KINDS - 1 ? written : read, s.end);
+        if (!v.empty()) kinds[n++] = {v.data(), v.data() + v.size(), i == KINDS - 1};
     }
+    uintptr_t written = 0, read = 0;                          // ends of what has been passed
+    while (n) {
+        int k = 0;
+        for (int i = 1; i < n; ++i)
+            if (*kinds[i].at < *kinds[k].at) k = i;
+        const Span s = *kinds[k].at++;
+        if (s.begin < written || (!kinds[k].read && s.begin < read)) return true;
+        uintptr_t& end = kinds[k].read ? read : written;
+        end = std::max(end, s.end);
+        if (kinds[k].at == kinds[k].end) kinds[k] = kinds[--n];
+    }
+    return false;
 }
 
 }  // namespace
