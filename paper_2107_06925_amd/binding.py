@@ -692,12 +692,11 @@ class AdamW:
         self.n, self.param, self.grad, self.m, self.v = _counts(params), _pointers(params), _pointers(grads), _pointers(ms), _pointers(vs)
         self.master, self.scale = _pointers(masters), _pointers(scales)
         self.decay = None if decay is None else (C.c_float * len(decay))(*decay)
-        self.beta1, self.beta2, self.eps = beta1, beta2, eps
+        self.beta1, self.beta2, self.eps, self.float32 = beta1, beta2, eps, torch.float32
 
     def step(self, lr, step, seed=0, grad_scale=None, d_hyper=None):
         """grad_scale: device float or None; d_hyper: device copy of an AdamWHyper in ADAMW_HYPER_BYTES bytes, used in place of lr, step and seed."""
-        import torch
         h = AdamWHyper(lr, self.beta1, self.beta2, self.eps, step, seed)      # the call's own: threads may step at the same time
         check(lib().chimera_op_adamw(self.dtype, self.bits, self.count, self.n, self.param, self.master, self.grad, self.m, self.v, self.scale,
-                                     self.decay, C.byref(h), _device_hyper(d_hyper), _vector(grad_scale, torch.float32, 1, "grad_scale"),
+                                     self.decay, C.byref(h), _device_hyper(d_hyper), _vector(grad_scale, self.float32, 1, "grad_scale"),
                                      _stream_of(self.tensors[0][0], grad_scale, d_hyper)))

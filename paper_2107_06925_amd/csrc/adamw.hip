@@ -448,7 +448,7 @@ int chimera_op_adamw(int dtype, int state_bits, int count, const int64_t* h_n, v
     try {
         std::vector<AdamwTensor> t((size_t)count);
         std::vector<Span> spans[7];                                           // weights, master weights, moments, scales, hyperparameters; what is read
-        for (auto& v : spans) v.reserve((size_t)count);
+        for (int k : {0, 2, 3, 6}) spans[k].reserve((size_t)count + 1);
         for (int i = 0; i < count; ++i) {
             if (h_n[i] < 0 || h_n[i] > 1ll << 32) return fail(CHIMERA_EINVAL, "tensor %d of %lld values", i, (long long)h_n[i]);
             t[i] = {h_param[i], h_m[i], h_v[i], dtype == CHIMERA_BF16 ? h_master[i] : nullptr, state_bits == 8 ? h_scale[i] : nullptr, h_grad[i], h_n[i],
