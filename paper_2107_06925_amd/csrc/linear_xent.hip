@@ -627,13 +627,16 @@ size_t aligned(size_t b) { return (b + 255) / 256 * 256; }
 int round_up(int v, int a) { return (v + a - 1) / a * a; }
 long tiles_of(int m, int n, int tile) { return (long)((m + tile - 1) / tile) * ((n + tile - 1) / tile); }
 
-// Columns of the forward's product on 256x256 tiles: whole rounds of them, and the rest too where it fills most of one (the rest on 128x128 tiles takes
-// 0.38 of a round's time for up to 64 of the large).  A small product has none.
+// Columns of the forward's product on 256x256 tiles: whole rounds of them, and the rest too where it fills more than half of one; otherwise the rest, which is four
+// times as many 128x128 tiles, takes up to two rounds of these, 0.38 each of a large one's time.  2048 tokens, hidden 1600, us with the rest on large tiles and on small:
+// 64 tiles over one round 75.8, 57.5; 128 74.6, 69.8; 136 76.4, 81.2; 160 75.5, 80.1; 64 tiles in all 37.2, 18.8; 128 36.1, 32.2; 136 37.5, 43.9; 224 41.3, 56.4;
+// and over four rounds 64 191.7, 173.9; 144 191.7, 197.1.  Up to 128 tokens a large tile's step, 2048 clocks of matrix instructions whatever its rows hold, is half
+// idle: 128 x 1600 x 20001 38.1, 22.6; x 50257 43.3, 42.7; but 128 x 256 x 50257 18.7, 21.9; and from 129 on 129 x 1600 x 50257 46.7, 70.6.
 int wide_columns(int m, int n) {
     const int tm = (m + 255) / 256, tn = (n + 255) / 256;
     const long tiles = (long)tm * tn, over = tiles % NUM_CUS;
-    if (tiles < 144 || m <= 128) return 0;                   // (few tokens: a step of a large tile is 2048 clocks of matrix instructions whatever its rows hold)
-    if (over >= 144 || over == 0) return tn * 256;
+    if (tiles <= NUM_CUS / 2 || m <= 128) return 0;
+    if (over > NUM_CUS / 2 || over == 0) return tn * 256;
     return (int)((tiles - over) / tm) * 256;
 }
 

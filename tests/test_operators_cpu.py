@@ -426,3 +426,12 @@ def test_binding_refuses_matrices_whose_memory_ends_too_soon():
     # a part of a wider matrix that begins at a multiple of 16 bytes is whole
     assert b._rows(torch.zeros((16, 24))[:, 4:23], torch.float32, "w") == 24
     assert b._rows(torch.zeros((16, 24), dtype=torch.bfloat16)[:, 8:23], torch.bfloat16, "w") == 24
+
+
+@pytest.mark.parametrize("tokens,vocab,wide", [(2048, 4096, 0), (2048, 4352, 4352), (2048, 12288, 8192), (2048, 12544, 12544), (2048, 32768, 32768), (2048, 50257, 49152),
+                                               (128, 50257, 0), (129, 50257, 50432), (256, 32768, 0), (256, 33025, 33280)])
+def test_linear_xent_forward_takes_large_tiles_from_half_a_round_on(tokens, vocab, wide):
+    """Read off the workspace: 8 bytes for each token and tile column, 4 more a token."""
+    need = b.lib().chimera_op_linear_xent_fwd_workspace_bytes(b.BF16, tokens, 64, vocab)
+    columns = wide // 256 + max(0, -(-(vocab - wide) // 128))
+    assert need == -(-8 * tokens * columns // 256) * 256 + -(-4 * tokens // 256) * 256
