@@ -640,26 +640,27 @@ int wide_columns(int m, int n) {
     return (int)((tiles - over) / tm) * 256;
 }
 
-// Columns of the vocabulary per piece where the caller leaves it open: 8192, more where their buffers stay small, fewer where they get large, in equal pieces.
-// Beside 8192 a piece whose dW just fills the chip's rounds of 256x256 tiles is taken as it is, unless that leaves a last one of less than a tenth, a pass
-// for little: 8192 x 2048 x 65536 in 8192 6990 -> 6600 us, 4096 x 1600 x 50304 in 9216 2463 -> 2344, 4096 x 2560 in 6400 3445 -> 3375; but 4096 x 2304 in seven of 7168 and
-// 128 columns 3104 -> 3199, 2048 x 1536 x 65536 in six of 10752 and 1024 1591 -> 1616.
+// Columns of the vocabulary per piece where the caller leaves it open: 8192, more where a piece's buffers (dz, and bf16 W) stay below 128 MB, fewer where they would
+// pass 512 MB, in equal pieces.  There are two sets of them, and dW's parts, where its contraction is cut, come on top.
+// From 2048 tokens on, a piece of 8192 columns or somewhat more whose dW just fills the chip's rounds of 256x256 tiles is taken as it is, up to 768 MB, unless that
+// leaves a last one of less than a tenth, a pass for little.  Equal pieces -> this, 32 sizes each of hidden 1536 to 2048 and vocabulary 20001 to 128000: 2048 tokens
+// 5 % faster to 4 % slower (2048 x 1600 x 50257 1274 -> 1246 us, x 20001 540 -> 558), 4096 8 % to -2 % (4096 x 1600 x 50257 2360 -> 2231), 8192 6 % to -3 %; but 1024
+// tokens, where dW is less of the whole, 3 % to -13 % (1024 x 1600 x 65536 900 -> 1035).  Filled pieces below 8192 lose (2048 x 2304 x 65536 in 7168 2100 -> 2266,
+// 2048 x 2560 in 6400 2237 -> 2440; but 4096 x 2560 x 50257 3338 -> 3288), beyond 10752 they do from 8192 tokens on (8192 x 1280 x 65536 in 13056 4345 -> 4652, x 1024 in 16384 3493 -> 3627).  Last pieces:
+// 2048 x 1600 x 37120 (256 columns behind four of 9216) 936 -> 977, 2048 x 1536 x 44032 (1024 behind four of 10752) 1044 -> 1031.
 constexpr size_t PIECE_BYTES_MIN = (size_t)128 << 20, PIECE_BYTES_MAX = (size_t)512 << 20, PIECE_BYTES_FILLED = (size_t)768 << 20;
-constexpr int PIECE_STEP = 256, PIECE_USUAL = 8192, PIECE_FILLED_MIN = 6144, PIECE_FILLED_MAX = 10752;
+constexpr int PIECE_STEP = 256, PIECE_USUAL = 8192, PIECE_FILLED_MAX = 10752, PIECE_FILLED_TOKENS = 2048;
 int filled_piece(int hidden) {
     const int rows = (hidden + 255) / 256;
-    int best = 0;
-    for (int rounds = 1; NUM_CUS * rounds / rows * 256 <= PIECE_FILLED_MAX; ++rounds) {
-        const int p = NUM_CUS * rounds / rows * 256;
-        if (p >= PIECE_FILLED_MIN && std::abs(p - PIECE_USUAL) <= std::abs(best - PIECE_USUAL)) best = p;
-    }
-    return best;
+    int p = 0;
+    for (int rounds = 1; p < PIECE_USUAL; ++rounds) p = NUM_CUS * rounds / rows * 256;
+    return p <= PIECE_FILLED_MAX ? p : 0;
 }
 int default_piece(int dtype, int m, int hidden, int vocab) {
     const int all = round_up(vocab, PIECE_STEP);
     const size_t column = dtype == CHIMERA_F32 ? (size_t)m * 4 : (size_t)round_up(m, TOKEN_PAD) * 8 + (size_t)hidden * 4;
     const size_t usual = std::max(PIECE_BYTES_MIN / column, std::min<size_t>(PIECE_USUAL, PIECE_BYTES_MAX / column));
-    const int filled = dtype == CHIMERA_BF16 && usual <= PIECE_USUAL ? filled_piece(hidden) : 0;
+    const int filled = dtype == CHIMERA_BF16 && m >= PIECE_FILLED_TOKENS && usual <= PIECE_USUAL ? filled_piece(hidden) : 0;
     if (filled && filled < vocab && filled * column <= PIECE_BYTES_FILLED && (vocab % filled == 0 || vocab % filled >= filled / 10)) return filled;
     const int most = (int)std::min<size_t>(all, std::max<size_t>(usual / PIECE_STEP * PIECE_STEP, PIECE_STEP));
     return round_up((vocab + (vocab + most - 1) / most - 1) / ((vocab + most - 1) / most), PIECE_STEP);        // equal pieces

@@ -435,3 +435,12 @@ def test_linear_xent_forward_takes_large_tiles_from_half_a_round_on(tokens, voca
     need = b.lib().chimera_op_linear_xent_fwd_workspace_bytes(b.BF16, tokens, 64, vocab)
     columns = wide // 256 + max(0, -(-(vocab - wide) // 128))
     assert need == -(-8 * tokens * columns // 256) * 256 + -(-4 * tokens // 256) * 256
+
+
+@pytest.mark.parametrize("tokens,hidden,vocab,piece", [(2048, 1600, 50257, 9216), (1024, 1600, 65536, 8192), (2048, 2304, 65536, 8192), (2048, 2560, 65536, 8192),
+                                                       (8192, 2048, 65536, 8192), (4096, 1536, 50257, 10752), (8192, 1280, 65536, 7424), (2048, 1600, 37120, 7424),
+                                                       (2048, 1536, 44032, 7424)])
+def test_linear_xent_pieces_that_the_library_chooses(tokens, hidden, vocab, piece):
+    """Without a piece the workspace is that of the piece of this size; and no other multiple of 256 near it has the same."""
+    need = lambda p: b.lib().chimera_op_linear_xent_bwd_workspace_bytes(b.BF16, tokens, hidden, vocab, p)  # noqa: E731
+    assert need(0) == need(piece) and need(0) not in (need(piece - 256), need(piece + 256))
