@@ -665,8 +665,11 @@ int default_piece(int dtype, int m, int hidden, int vocab) {
     const int most = (int)std::min<size_t>(all, std::max<size_t>(usual / PIECE_STEP * PIECE_STEP, PIECE_STEP));
     return round_up((vocab + (vocab + most - 1) / most - 1) / ((vocab + most - 1) / most), PIECE_STEP);        // equal pieces
 }
-// The launches' tiles, and where contractions are cut.  256x256 tiles where the products of a piece fill the chip with them; rows of 128 for
-// up to 128 tokens.  dh's tiles are cut along the vocabulary
+// The launches' tiles, and where contractions are cut.  dW on 256x256 tiles where it has half a round of them, or it and dz together a round and a quarter: 64 x 1024, us
+// on 128x128 and on 256x256 tiles, 16 columns of large tiles (64 in all) 33.1, 32.4; 30 39.5, 33.5; 34 40.5, 34.0; 300 x 1024, 16 columns 40, 56; 34 61, 63; 40 65, 67; 512 x 256, 120 tiles of both 37.6, 50.4; 1024 x 256, 280 73.8, 71.2; 480 108.7, 85.9;
+// 1536 x 256, 280 76.3, 88.0; 336 85.3, 97.3; 504 108.6, 104.3; 672 147.6, 119.4.  Tokens in tiles of 128 up to 128 of them, us beside tiles of 256: 128 x 1600 x 50257
+// 285, 320; 128 x 512 x 50257 102, 104; 129 x 512 x 50257 119, 108; 400 x 1600 472, 458; but 129 x 1600 312, 332; 256 x 2048 x 20001 168, 203.
+// dh's tiles are cut along the vocabulary
 // to half of what a CU has to do in all, or 32 steps, whichever is more (a third and a quarter: 1380 -> 1400 us at 2048 x 1600 x 50256, 360 -> 388 at 512 x 1024,
 // every part is read and written once a piece).  dW's are cut along the tokens, to what a CU has to do in all, where one would outlast that by a fifth, as many
 // tokens on few columns of h do; their parts are added a pass later (8192 x 256 x 50304 3012 -> 1320 us, 1407 in shorter parts, 1537 uncut in 128x128 tiles;
