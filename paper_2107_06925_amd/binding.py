@@ -552,6 +552,13 @@ def _rows(t, dtype, what):
     return ld
 
 
+def _projection(h, w):
+    """tokens, hidden and vocab of h [tokens, hidden] times w [hidden, vocab]."""
+    if h.dim() != 2 or w.dim() != 2 or h.shape[1] != w.shape[0]:
+        raise ValueError("w has a row for each column of h")
+    return h.shape[0], h.shape[1], w.shape[1]
+
+
 def _vector(t, dtype, n, what):
     if t is not None and (t.dtype != dtype or t.numel() != n or not t.is_contiguous()):
         raise ValueError("%s: %d contiguous values of %s expected" % (what, n, dtype))
@@ -574,7 +581,7 @@ def chimera_op_linear_xent_fwd(h, w, targets, scale, loss_rows, lse, loss=None, 
     """h [tokens, hidden], w [hidden, vocab] (rows may lie further apart than they are long), targets int32; fills loss_rows and lse
     (float, [tokens]) and adds to loss.  Allocates the workspace (a torch uint8 tensor) unless one is given, and returns it."""
     import torch
-    (tokens, hidden), vocab = h.shape, w.shape[1]
+    tokens, hidden, vocab = _projection(h, w)
     if workspace is None:
         workspace = torch.empty(lib().chimera_op_linear_xent_fwd_workspace_bytes(_dt(h), tokens, hidden, vocab), dtype=torch.uint8, device=h.device)
     f = torch.float32
@@ -589,7 +596,7 @@ def chimera_op_linear_xent_bwd(h, w, targets, lse, scale, dh=None, dw=None, dlos
     """dh [tokens, hidden] (type of h) and dw [hidden, vocab] (float) are tensors to be filled, or None; dloss float [tokens] or None.  lse: what the forward
     left, or the logsumexp over more words than w holds; bfloat16 holds exp(logit - lse) up to 3.9."""
     import torch
-    (tokens, hidden), vocab = h.shape, w.shape[1]
+    tokens, hidden, vocab = _projection(h, w)
     if workspace is None:
         workspace = torch.empty(lib().chimera_op_linear_xent_bwd_workspace_bytes(_dt(h), tokens, hidden, vocab, piece), dtype=torch.uint8, device=h.device)
     f = torch.float32
@@ -606,7 +613,7 @@ def chimera_op_linear_xent_bwd(h, w, targets, lse, scale, dh=None, dw=None, dlos
 def chimera_head_loss_pieces(y, targets, lnf_g, lnf_b, w_head, scale, dy, dlnf_g, dlnf_b, dw_head, loss, piece=0, workspace=None):
     """w_head [hidden, vocab]; dw_head has the same row stride.  Allocates the workspace unless one is given, and returns it."""
     import torch
-    tokens, hidden, vocab = y.shape[0], y.shape[1], w_head.shape[1]
+    tokens, hidden, vocab = _projection(y, w_head)
     ldw = _rows(w_head, y.dtype, "w_head")
     if _rows(dw_head, torch.float32, "dw_head") != ldw or dw_head.shape[0] != hidden or dw_head.shape[1] < vocab:
         raise ValueError("dw_head has the rows of w_head, as far apart")

@@ -444,3 +444,17 @@ def test_linear_xent_pieces_that_the_library_chooses(tokens, hidden, vocab, piec
     """Without a piece the workspace is that of the piece of this size; and no other multiple of 256 near it has the same."""
     need = lambda p: b.lib().chimera_op_linear_xent_bwd_workspace_bytes(b.BF16, tokens, hidden, vocab, p)  # noqa: E731
     assert need(0) == need(piece) and need(0) not in (need(piece - 256), need(piece + 256))
+
+
+@pytest.mark.parametrize("rows", [8, 24])
+def test_binding_refuses_a_matrix_of_other_rows(rows):
+    """The library reads (and writes) as many rows of w (and dw) as h has columns, whether the tensors hold them or not."""
+    torch = pytest.importorskip("torch")
+    z = lambda *s, d=torch.float32: torch.zeros(s, dtype=d)  # noqa: E731
+    i32, ws = torch.int32, z(8, d=torch.uint8)
+    for h, w in ((z(3, 16), z(rows, 24)), (z(3, 16), z(16, 24, 1)), (z(16), z(16, 24)), (z(1, 3, 16), z(16, 24))):
+        for call in (lambda: b.chimera_op_linear_xent_fwd(h, w, z(3, d=i32), 1.0, z(3), z(3), workspace=ws),
+                     lambda: b.chimera_op_linear_xent_bwd(h, w, z(3, d=i32), z(3), 1.0, dh=z(*h.shape), dw=z(*w.shape), workspace=ws),
+                     lambda: b.chimera_head_loss_pieces(h, z(3, d=i32), z(16), z(16), w, 1.0, z(*h.shape), z(16), z(16), z(16, 24), z(1), workspace=ws)):
+            with pytest.raises(ValueError, match="a row for each column"):
+                call()
