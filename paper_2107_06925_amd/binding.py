@@ -656,8 +656,8 @@ def _counts(tensors):
 def chimera_op_grad_norm(grads, max_norm, out, workspace=None):
     """grads: float tensors (contiguous); out: float [2], the norm and the factor that brings it down to max_norm."""
     import torch
-    if any(g.dtype != torch.float32 or not g.is_contiguous() for g in grads) or out.dtype != torch.float32 or out.numel() != 2:
-        raise ValueError("contiguous float32 gradients and two float32 results expected")
+    if any(g.dtype != torch.float32 or not g.is_contiguous() for g in grads) or out.dtype != torch.float32 or out.numel() != 2 or not out.is_contiguous():
+        raise ValueError("contiguous float32 gradients and two contiguous float32 results expected")
     n = _counts(grads)
     if workspace is None:
         workspace = torch.empty(lib().chimera_op_grad_norm_workspace_bytes(len(grads)), dtype=torch.uint8, device=out.device)

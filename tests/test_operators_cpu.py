@@ -458,3 +458,13 @@ def test_binding_refuses_a_matrix_of_other_rows(rows):
                      lambda: b.chimera_head_loss_pieces(h, z(3, d=i32), z(16), z(16), w, 1.0, z(*h.shape), z(16), z(16), z(16, 24), z(1), workspace=ws)):
             with pytest.raises(ValueError, match="a row for each column"):
                 call()
+
+
+def test_grad_norm_refuses_results_that_lie_apart(monkeypatch):
+    torch = pytest.importorskip("torch")
+    calls = []
+    monkeypatch.setattr(b, "_stream_of", lambda *tensors: 0)
+    monkeypatch.setattr(b, "lib", lambda: type("Library", (), {"chimera_op_grad_norm": staticmethod(lambda *a: calls.append(a) or b.OK)}))
+    with pytest.raises(ValueError, match="contiguous"):
+        b.chimera_op_grad_norm([torch.zeros(4)], 1.0, torch.zeros(4)[::2], workspace=torch.zeros(8, dtype=torch.uint8))
+    assert not calls
