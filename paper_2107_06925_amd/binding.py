@@ -556,6 +556,9 @@ def _projection(h, w):
     """tokens, hidden and vocab of h [tokens, hidden] times w [hidden, vocab]."""
     if h.dim() != 2 or w.dim() != 2 or h.shape[1] != w.shape[0]:
         raise ValueError("w has a row for each column of h")
+    import torch
+    if h.dtype != torch.float32 and h.dtype != torch.bfloat16:
+        raise ValueError("float32 or bfloat16 expected")
     return h.shape[0], h.shape[1], w.shape[1]
 
 

@@ -468,3 +468,17 @@ def test_grad_norm_refuses_results_that_lie_apart(monkeypatch):
     with pytest.raises(ValueError, match="contiguous"):
         b.chimera_op_grad_norm([torch.zeros(4)], 1.0, torch.zeros(4)[::2], workspace=torch.zeros(8, dtype=torch.uint8))
     assert not calls
+
+
+@pytest.mark.parametrize("dtype", ["float16", "float64", "int16", "uint8"])
+def test_binding_refuses_other_types(dtype):
+    """Two bytes that are not bfloat16 would be taken for it."""
+    torch = pytest.importorskip("torch")
+    d = getattr(torch, dtype)
+    z = lambda *s, d=torch.float32: torch.zeros(s, dtype=d)  # noqa: E731
+    i32, ws, h, w = torch.int32, z(8, d=torch.uint8), z(3, 16, d=d), z(16, 24, d=d)
+    for call in (lambda: b.chimera_op_linear_xent_fwd(h, w, z(3, d=i32), 1.0, z(3), z(3), workspace=ws),
+                 lambda: b.chimera_op_linear_xent_bwd(h, w, z(3, d=i32), z(3), 1.0, dh=z(3, 16, d=d), dw=z(16, 24), workspace=ws),
+                 lambda: b.chimera_head_loss_pieces(h, z(3, d=i32), z(16, d=d), z(16, d=d), w, 1.0, z(3, 16, d=d), z(16), z(16), z(16, 24), z(1), workspace=ws)):
+        with pytest.raises(ValueError, match="float32 or bfloat16"):
+            call()
