@@ -221,6 +221,8 @@ def _ptr(t):
 class Stage:
     """Owns the device buffers (torch tensors) a chimera_stage borrows."""
 
+    adamw_state, adamw_bits = None, 32                     # until adamw_init
+
     def __init__(self, layers, hidden, heads, seq, microbatch, dtype, causal=True, gelu_erf=False,
                  reference_kernels=False, stash_slots=1, stream=None, device="cuda:0", overlap=True, keep=True,
                  share_weights_of=None):

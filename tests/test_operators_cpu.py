@@ -482,3 +482,17 @@ def test_binding_refuses_other_types(dtype):
                  lambda: b.chimera_head_loss_pieces(h, z(3, d=i32), z(16, d=d), z(16, d=d), w, 1.0, z(3, 16, d=d), z(16), z(16), z(16, 24), z(1), workspace=ws)):
         with pytest.raises(ValueError, match="float32 or bfloat16"):
             call()
+
+
+def test_stage_step_without_its_state_is_the_librarys_error(monkeypatch):
+    """Refused like any other missing buffer, not by an attribute that is not there."""
+    torch = pytest.importorskip("torch")
+    stage = b.Stage.__new__(b.Stage)
+    stage.torch, stage.weights = torch, torch.zeros(64)
+    stage.handle = b.lib().chimera_stage_create(1, 64, 4, 16, 2, b.BF16)
+    b.check(b.lib().chimera_stage_set_option(stage.handle, b.OPT_OVERLAP, 0))
+    b.check(b.lib().chimera_stage_bind(stage.handle, P, P, P, 1, P, None))
+    with pytest.raises(b.ChimeraError, match="NULL") as e:
+        stage.adamw_step(1e-3, 1)
+    assert e.value.code == b.EINVAL
+    stage.close()
