@@ -301,33 +301,44 @@ int check_hyper(const chimera_adamw_hyper& h) {
     return CHIMERA_OK;
 }
 
-// Spans of memory by kind, the last kind only read: whether what is written shares a byte with anything else.  One walk over all kinds in the order
-// of addresses, each of which usually comes sorted.
+// Spans of memory by kind, each kind `room` of them at most, the last only read: whether what is written shares a byte with anything else.  One walk over all in the
+// order of addresses, of each kind, which usually lies sorted in a range of its own, as many as come before the next kind's.
 struct Span {
     uintptr_t begin, end;
     bool operator<(const Span& o) const { return begin < o.begin; }
 };
-template <int KINDS> bool written_twice(std::vector<Span> (&spans)[KINDS]) {
-    struct Kind { const Span *at, *end; bool read; } kinds[KINDS];
-    int n = 0;
-    for (int i = 0; i < KINDS; ++i) {
-        auto& v = spans[i];
-        if (!std::is_sorted(v.begin(), v.end())) std::sort(v.begin(), v.end());
-        if (!v.empty()) kinds[n++] = {v.data(), v.data() + v.size(), i == KINDS - 1};
+template <int KINDS> struct Spans {
+    std::vector<Span> all;
+    size_t room, count[KINDS] = {};
+    explicit Spans(size_t room) : all(room * KINDS), room(room) {}
+    void add(int kind, const void* p, size_t bytes) { if (p) all[kind * room + count[kind]++] = {(uintptr_t)p, (uintptr_t)p + bytes}; }
+    bool written_twice() {
+        struct Kind { Span *at, *end; bool read; } kinds[KINDS];
+        int n = 0;
+        for (int i = 0; i < KINDS; ++i) {
+            Span *first = all.data() + i * room, *last = first + count[i];
+            if (!std::is_sorted(first, last)) std::sort(first, last);
+            if (first != last) kinds[n++] = {first, last, i == KINDS - 1};
+        }
+        uintptr_t written = 0, read = 0;                      // ends of what has been passed
+        while (n) {
+            int k = 0;
+            for (int i = 1; i < n; ++i)
+                if (*kinds[i].at < *kinds[k].at) k = i;
+            Kind& next = kinds[k];
+            uintptr_t others = UINTPTR_MAX;
+            for (int i = 0; i < n; ++i)
+                if (i != k) others = std::min(others, kinds[i].at->begin);
+            do {
+                if (next.at->begin < written || (!next.read && next.at->begin < read)) return true;
+                uintptr_t& end = next.read ? read : written;
+                end = std::max(end, next.at->end);
+            } while (++next.at != next.end && next.at->begin <= others);
+            if (next.at == next.end) next = kinds[--n];
+        }
+        return false;
     }
-    uintptr_t written = 0, read = 0;                          // ends of what has been passed
-    while (n) {
-        int k = 0;
-        for (int i = 1; i < n; ++i)
-            if (*kinds[i].at < *kinds[k].at) k = i;
-        const Span s = *kinds[k].at++;
-        if (s.begin < written || (!kinds[k].read && s.begin < read)) return true;
-        uintptr_t& end = kinds[k].read ? read : written;
-        end = std::max(end, s.end);
-        if (kinds[k].at == kinds[k].end) kinds[k] = kinds[--n];
-    }
-    return false;
-}
+};
 
 }  // namespace
 
@@ -447,8 +458,7 @@ int chimera_op_adamw(int dtype, int state_bits, int count, const int64_t* h_n, v
     const size_t e = dtype == CHIMERA_F32 ? 4 : 2;
     try {
         std::vector<AdamwTensor> t((size_t)count);
-        std::vector<Span> spans[7];                                           // weights, master weights, moments, scales, hyperparameters; what is read
-        for (int k : {0, 2, 3, 6}) spans[k].reserve((size_t)count + 1);
+        Spans<7> spans((size_t)count + 1);                                    // weights, master weights, moments, scales, hyperparameters; what is read
         for (int i = 0; i < count; ++i) {
             if (h_n[i] < 0 || h_n[i] > 1ll << 32) return fail(CHIMERA_EINVAL, "tensor %d of %lld values", i, (long long)h_n[i]);
             t[i] = {h_param[i], h_m[i], h_v[i], dtype == CHIMERA_BF16 ? h_master[i] : nullptr, state_bits == 8 ? h_scale[i] : nullptr, h_grad[i], h_n[i],
@@ -461,17 +471,16 @@ int chimera_op_adamw(int dtype, int state_bits, int count, const int64_t* h_n, v
                 return fail(CHIMERA_EINVAL, "tensor %d is not aligned to its elements", i);
             if (!(q.decay >= 0) || !std::isfinite(q.decay)) return fail(CHIMERA_EINVAL, "weight decay of tensor %d must be finite and not negative", i);
             const size_t moment = (size_t)h_n[i] * (state_bits == 32 ? 4 : 1);
-            auto take = [&](int kind, const void* p, size_t bytes) { if (p) spans[kind].push_back({(uintptr_t)p, (uintptr_t)p + bytes}); };
-            take(0, q.p, (size_t)h_n[i] * e);
-            take(1, q.master, (size_t)h_n[i] * 4);
-            take(2, q.m, moment);
-            take(3, q.v, moment);
-            take(4, q.scale, (size_t)(h_n[i] + MOMENT_BLOCK - 1) / MOMENT_BLOCK * 8);
-            take(6, q.g, (size_t)h_n[i] * 4);
+            spans.add(0, q.p, (size_t)h_n[i] * e);
+            spans.add(1, q.master, (size_t)h_n[i] * 4);
+            spans.add(2, q.m, moment);
+            spans.add(3, q.v, moment);
+            spans.add(4, q.scale, (size_t)(h_n[i] + MOMENT_BLOCK - 1) / MOMENT_BLOCK * 8);
+            spans.add(6, q.g, (size_t)h_n[i] * 4);
         }
-        if (d_hyper) spans[5].push_back({(uintptr_t)d_hyper, (uintptr_t)d_hyper + CHIMERA_ADAMW_HYPER_BYTES});
-        if (d_grad_scale) spans[6].push_back({(uintptr_t)d_grad_scale, (uintptr_t)d_grad_scale + 4});
-        if (written_twice(spans)) return fail(CHIMERA_EINVAL, "what the step writes overlaps: weights, master weights, moments, scales, hyperparameters, or a gradient or factor with one of these");
+        spans.add(5, d_hyper, CHIMERA_ADAMW_HYPER_BYTES);
+        spans.add(6, d_grad_scale, 4);
+        if (spans.written_twice()) return fail(CHIMERA_EINVAL, "what the step writes overlaps: weights, master weights, moments, scales, hyperparameters, or a gradient or factor with one of these");
         return adamw_step(dtype, state_bits, count, t.data(), h_hyper, d_hyper, d_grad_scale, hip_stream);
     } catch (const std::bad_alloc&) {
         return fail(CHIMERA_ENOMEM, "out of host memory");
