@@ -555,13 +555,14 @@ def _rows(t, dtype, what):
 
 
 def _projection(h, w):
-    """tokens, hidden and vocab of h [tokens, hidden] times w [hidden, vocab]."""
-    if h.dim() != 2 or w.dim() != 2 or h.shape[1] != w.shape[0]:
-        raise ValueError("w has a row for each column of h")
+    """Type, tokens, hidden and vocab of h [tokens, hidden] times w [hidden, vocab]."""
     import torch
-    if h.dtype != torch.float32 and h.dtype != torch.bfloat16:
+    a, c, t = h.shape, w.shape, h.dtype
+    if len(a) != 2 or len(c) != 2 or a[1] != c[0]:
+        raise ValueError("w has a row for each column of h")
+    if t != torch.float32 and t != torch.bfloat16:
         raise ValueError("float32 or bfloat16 expected")
-    return h.shape[0], h.shape[1], w.shape[1]
+    return F32 if t == torch.float32 else BF16, a[0], a[1], c[1]
 
 
 def _vector(t, dtype, n, what):
@@ -586,11 +587,11 @@ def chimera_op_linear_xent_fwd(h, w, targets, scale, loss_rows, lse, loss=None, 
     """h [tokens, hidden], w [hidden, vocab] (rows may lie further apart than they are long), targets int32; fills loss_rows and lse
     (float, [tokens]) and adds to loss.  Allocates the workspace (a torch uint8 tensor) unless one is given, and returns it."""
     import torch
-    tokens, hidden, vocab = _projection(h, w)
+    dt, tokens, hidden, vocab = _projection(h, w)
     if workspace is None:
-        workspace = torch.empty(lib().chimera_op_linear_xent_fwd_workspace_bytes(_dt(h), tokens, hidden, vocab), dtype=torch.uint8, device=h.device)
+        workspace = torch.empty(lib().chimera_op_linear_xent_fwd_workspace_bytes(dt, tokens, hidden, vocab), dtype=torch.uint8, device=h.device)
     f = torch.float32
-    check(lib().chimera_op_linear_xent_fwd(_dt(h), tokens, hidden, vocab, h.data_ptr(), _rows(h, h.dtype, "h"), w.data_ptr(), _rows(w, h.dtype, "w"),
+    check(lib().chimera_op_linear_xent_fwd(dt, tokens, hidden, vocab, h.data_ptr(), _rows(h, h.dtype, "h"), w.data_ptr(), _rows(w, h.dtype, "w"),
                                            _vector(targets, torch.int32, tokens, "targets"), scale, _vector(loss_rows, f, tokens, "loss_rows"),
                                            _vector(lse, f, tokens, "lse"), _vector(loss, f, 1, "loss"), workspace.data_ptr(), workspace.numel(),
                                            _stream_of(h, w, targets, loss_rows, lse, loss, workspace)))
@@ -601,16 +602,17 @@ def chimera_op_linear_xent_bwd(h, w, targets, lse, scale, dh=None, dw=None, dlos
     """dh [tokens, hidden] (type of h) and dw [hidden, vocab] (float) are tensors to be filled, or None; dloss float [tokens] or None.  lse: what the forward
     left, or the logsumexp over more words than w holds; bfloat16 holds exp(logit - lse) up to 3.9."""
     import torch
-    tokens, hidden, vocab = _projection(h, w)
+    dt, tokens, hidden, vocab = _projection(h, w)
     if workspace is None:
-        workspace = torch.empty(lib().chimera_op_linear_xent_bwd_workspace_bytes(_dt(h), tokens, hidden, vocab, piece), dtype=torch.uint8, device=h.device)
+        workspace = torch.empty(lib().chimera_op_linear_xent_bwd_workspace_bytes(dt, tokens, hidden, vocab, piece), dtype=torch.uint8, device=h.device)
     f = torch.float32
     if (dh is not None and dh.shape != h.shape) or (dw is not None and dw.shape != w.shape):
         raise ValueError("dh and dw have the shapes of h and w")
-    check(lib().chimera_op_linear_xent_bwd(_dt(h), tokens, hidden, vocab, h.data_ptr(), _rows(h, h.dtype, "h"), w.data_ptr(), _rows(w, h.dtype, "w"),
+    check(lib().chimera_op_linear_xent_bwd(dt, tokens, hidden, vocab, h.data_ptr(), _rows(h, h.dtype, "h"), w.data_ptr(), _rows(w, h.dtype, "w"),
                                            _vector(targets, torch.int32, tokens, "targets"), _vector(lse, f, tokens, "lse"), scale,
                                            _vector(dloss, f, tokens, "dloss"), None if dh is None else dh.data_ptr(),
-                                           0 if dh is None else _rows(dh, h.dtype, "dh"), None if dw is None else dw.data_ptr(), 0 if dw is None else _rows(dw, f, "dw"), int(overwrite), piece, workspace.data_ptr(), workspace.numel(),
+                                           0 if dh is None else _rows(dh, h.dtype, "dh"), None if dw is None else dw.data_ptr(),
+                                           0 if dw is None else _rows(dw, f, "dw"), int(overwrite), piece, workspace.data_ptr(), workspace.numel(),
                                            _stream_of(h, w, targets, lse, dh, dw, dloss, workspace)))
     return workspace
 
@@ -618,7 +620,7 @@ def chimera_op_linear_xent_bwd(h, w, targets, lse, scale, dh=None, dw=None, dlos
 def chimera_head_loss_pieces(y, targets, lnf_g, lnf_b, w_head, scale, dy, dlnf_g, dlnf_b, dw_head, loss, piece=0, workspace=None):
     """w_head [hidden, vocab]; dw_head has the same row stride.  Allocates the workspace unless one is given, and returns it."""
     import torch
-    tokens, hidden, vocab = _projection(y, w_head)
+    dt, tokens, hidden, vocab = _projection(y, w_head)
     ldw = _rows(w_head, y.dtype, "w_head")
     if _rows(dw_head, torch.float32, "dw_head") != ldw or dw_head.shape[0] != hidden or dw_head.shape[1] < vocab:
         raise ValueError("dw_head has the rows of w_head, as far apart")
@@ -626,8 +628,8 @@ def chimera_head_loss_pieces(y, targets, lnf_g, lnf_b, w_head, scale, dy, dlnf_g
         raise ValueError("y and dy: contiguous, of one shape and type")
     f = torch.float32
     if workspace is None:
-        workspace = torch.empty(lib().chimera_head_pieces_workspace_bytes(_dt(y), tokens, hidden, vocab, piece), dtype=torch.uint8, device=y.device)
-    check(lib().chimera_head_loss_pieces(_dt(y), tokens, hidden, vocab, y.data_ptr(), _vector(targets, torch.int32, tokens, "targets"),
+        workspace = torch.empty(lib().chimera_head_pieces_workspace_bytes(dt, tokens, hidden, vocab, piece), dtype=torch.uint8, device=y.device)
+    check(lib().chimera_head_loss_pieces(dt, tokens, hidden, vocab, y.data_ptr(), _vector(targets, torch.int32, tokens, "targets"),
                                          _vector(lnf_g, y.dtype, hidden, "lnf_g"), _vector(lnf_b, y.dtype, hidden, "lnf_b"), w_head.data_ptr(), ldw, scale, dy.data_ptr(),
                                          _vector(dlnf_g, f, hidden, "dlnf_g"), _vector(dlnf_b, f, hidden, "dlnf_b"), dw_head.data_ptr(), _vector(loss, f, 1, "loss"), piece,
                                          workspace.data_ptr(), workspace.numel(),
