@@ -509,8 +509,9 @@ int chimera_head_loss(int dtype, int tokens, int hidden, int vocab, const void* 
                       float* d_dlnf_b, float* d_dw_head, float* d_loss, void* d_workspace,
                       size_t workspace_bytes, void* hip_stream);
 
-/* The vocabulary projection and its cross-entropy without the logits: nothing of size [tokens, vocab] is kept or
- * written.  h [tokens, hidden] with rows ldh apart, W [hidden, vocab] with rows ldw apart (ldw >= vocab; the columns between may hold anything), both
+/* The vocabulary projection and its cross-entropy without keeping the logits: the bf16 forward keeps a pair of floats for each token and 128 or 256 columns, all else
+ * works on a piece of the vocabulary at a time.  Left to the library, a piece is the whole vocabulary while its buffers stay below 128 MB.
+ * h [tokens, hidden] with rows ldh apart, W [hidden, vocab] with rows ldw apart (ldw >= vocab; the columns between may hold anything), both
  * in the given dtype; z = h W.  The last row of W, too, is readable up to vocab rounded up to 8 columns (float, and d_dw: to 4), as it is in every matrix of whole rows
  * and in every part of one that is aligned as below.  vocab is any number; hidden and the leading dimensions are multiples of 8, leading dimensions below 2^23, tokens up
  * to 2^22, hidden to 2^15, vocab to 2^22, tokens * vocab to 2^38; tensors 16-byte, the workspace 256-byte aligned.  A target outside [0, vocab) marks a token that does
@@ -521,9 +522,11 @@ int chimera_head_loss(int dtype, int tokens, int hidden, int vocab, const void* 
  * Backward, given d_lse, with coef[t] = scale * d_dloss[t] (d_dloss NULL: scale), dz[t, v] = coef[t] * (exp(z[t, v] - d_lse[t]) - [v == target[t]]):
  *   d_dh [tokens, hidden] (dtype, rows lddh apart) = dz W^T,  d_dw [hidden, vocab] (float, rows lddw apart, columns from vocab on left as they are)
  *   += h^T dz, or = with overwrite != 0.  Either may be NULL, not both.  z is formed again, `piece` columns of the vocabulary at a time (rounded up to
- *   a multiple of 256; 0: the library's choice); the workspace grows with it.
- * bf16: dh is formed from dz in 11 bits, dW from dz in 22; the products' sums are float.  Both hold dz as fp16 numbers under a power of two for each token, so
- * exp(z[t, v] - d_lse[t]) must stay below 3.9: d_lse is the logsumexp of the row as the forward leaves it, or of more words than these, or larger.  Where it is
+ *   a multiple of 256; 0: the library's choice, for speed); the workspace grows with it: of each column it holds dz (float: 4 bytes a token, bf16: 8, in two sets where
+ *   there are several pieces) and in bf16 an fp16 copy of W, which for few tokens is more than the logits would be.
+ * bf16: dh is formed from dz in 11 bits, dW from dz in 22; the products' sums are float.  Their operands are fp16 numbers under powers of two, which have a smallest
+ * step: dz 2^-37 of its token's coef, in dh W 2^-38 of the largest of its row in the piece, in dW coef[t] h[t] 2^-38 of the largest of all tokens.  Of dz there is a
+ * largest number too: exp(z[t, v] - d_lse[t]) must stay below 3.9: d_lse is the logsumexp of the row as the forward leaves it, or of more words than these, or larger.  Where it is
  * smaller the token's row of d_dh, and d_dw, are infinite or not numbers (float follows the formula).
  * All sums have a fixed order.  Calls that overlap in time need workspaces of their own; kernels run on the current device, which holds all tensors.
  * Results and workspace must share no memory with each other or with an operand (EINVAL); d_dh alone may lie on d_h.
@@ -537,9 +540,11 @@ int chimera_op_linear_xent_bwd(int dtype, int tokens, int hidden, int vocab, con
                                const int32_t* d_targets, const float* d_lse, float scale, const float* d_dloss, void* d_dh, int lddh,
                                float* d_dw, int lddw, int overwrite, int piece, void* d_workspace, size_t workspace_bytes, void* hip_stream);
 /* chimera_head_loss on these two: the same results (tokens whose target lies outside [0, vocab) do not count here; their rows of y
- * still have to be finite) without its [tokens, vocab] workspace, for any vocab.  d_w_head and d_dw_head have rows ldw apart; d_dy may be d_y itself, nothing else that is written
+ * still have to be finite), for any vocab, with the logits a piece at a time.  d_w_head and d_dw_head have rows ldw apart; d_dy may be d_y itself, nothing else that is written
  * may share memory with anything (EINVAL).  It forms z twice and dW from a
- * finer dz, two thirds more work on the matrix cores: bf16 2048 x 1600 x 50304 1.69 ms in 276 MB, chimera_head_loss 1.22 in 344; float 128 x 128 x 50304 0.14 against 0.28. */
+ * finer dz, two thirds more work on the matrix cores.  ms and MB of workspace, this and chimera_head_loss: bf16 2048 x 1600 x 50304 1.57 in 276 (1.95 in 86 with a piece of
+ * 2048), 1.12 in 344; 8192 x 2048 x 65536 8.07 in 805, 5.63 in 1175; 512 x 1024 x 50304 0.45 in 126, 0.29 in 71; float 2048 x 1024 x 50304 5.07 in 143, 3.78 in 433;
+ * 128 x 128 x 50304 0.12 in 30, 0.27 in 26. */
 size_t chimera_head_pieces_workspace_bytes(int dtype, int tokens, int hidden, int vocab, int piece);
 int chimera_head_loss_pieces(int dtype, int tokens, int hidden, int vocab, const void* d_y, const int32_t* d_targets, const void* d_lnf_g,
                              const void* d_lnf_b, const void* d_w_head, int ldw, float scale, void* d_dy, float* d_dlnf_g, float* d_dlnf_b,
@@ -565,8 +570,9 @@ int chimera_op_grad_norm(int count, const int64_t* h_n, const float* const* h_gr
  * state_bits 8: h_m and h_v point to one byte per element, e4m3 numbers (4 exponent bits, bias 7, 3 of mantissa, no infinities) that hold m and
  * sqrt(v) as multiples of a float scale for each 256 elements of a tensor; h_scale to the pairs (m's, sqrt(v)'s), ceil(n / 256) of them.  An element
  * whose m or v is infinite has that moment kept as not a number; the rest of its block is as without it.  Zeros are the
- * state before the first step in either width.  Codes are rounded up or down at random, with the right mean, by a hash of seed, step and the
- * element's number in the call (tensors counted in whole blocks of 256): the same call on the same state gives the same bits.
+ * state before the first step in either width.  Codes are rounded up or down at random, so that m and sqrt(v) keep their means, by a hash of seed, step and the
+ * element's number in the call (tensors counted in whole blocks of 256): the same call on the same state gives the same bits.  (v, the square of what is held, is larger
+ * by sqrt(v)'s variance: of gradients that do not change in size 2.5 % at beta2 = 0.95, 5.5 % at 0.999, with a deviation of sqrt(v) of 11 to 17 %.)
  * Tensors are aligned to their elements.  lr >= 0, beta1 and beta2 in [0, 1), eps in [2^-126, 1], decay >= 0, step >= 1.  d_hyper (may be NULL): device memory of CHIMERA_ADAMW_HYPER_BYTES bytes, 16-byte aligned, that begins with a
  * chimera_adamw_hyper to be used in place of h_hyper, so that a recorded call can be replayed for further steps; its values are the caller's to
  * check, the bytes behind the struct the call's, and calls that overlap need one each. */
