@@ -968,3 +968,48 @@ def test_linear_xent_of_the_last_columns_of_a_matrix(dtype, tokens, hidden, firs
         _check_backward(dtype, h, w, targets, lse, 0.25, None, dh, dpart, torch.zeros_like(dpart) if overwrite else before)
         before = dpart.clone()
     assert (dfull[:, :first] == 0.5).all() and (dfull[:, first + vocab:] == 0.5).all()
+
+
+# ------------------------------------------------ beyond 2^31 values in a tensor
+def test_grad_norm_beyond_2_31_values():
+    torch = _torch()
+    n = 2 ** 31 + 4099
+    print("grad norm", n, flush=True)
+    g = torch.zeros(n, device="cuda")
+    at = torch.tensor([0, 2 ** 30, 2 ** 31 - 1, 2 ** 31, 2 ** 31 + 1, n - 1], device="cuda")
+    g[at] = torch.tensor([1.0, 2.0, 4.0, 8.0, 16.0, 32.0], device="cuda")
+    out = torch.empty(2, device="cuda")
+    b.chimera_op_grad_norm([g, g[n - 1:]], 1e9, out)
+    assert abs(float(out[0]) - math.sqrt(1365 + 1024)) <= 2 * E24 * float(out[0]) and float(out[1]) == 1.0
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_beyond_2_31_values(bits):
+    """Windows at both ends and across the 2^31st value: the weights are those of a step over the window alone, codes those of the formula."""
+    torch = _torch()
+    n = 2 ** 31 + 70_003
+    print("adamw", bits, n, flush=True)
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    long = lambda d=torch.float32, m=n: torch.zeros(m, device="cuda", dtype=d)  # noqa: E731
+    p, g, small = long(), long(), torch.float32 if bits == 32 else torch.uint8
+    m, v, scale = long(small), long(small), None if bits == 32 else long(m=2 * ((n + 255) // 256))
+    windows = [(0, 5000), (2 ** 31 - 2560, 2 ** 31 + 2560), (n // 256 * 256 - 2560, n)]
+    for a, z in windows:
+        p[a:z], g[a:z] = torch.randn(z - a, device="cuda", generator=gen), torch.randn(z - a, device="cuda", generator=gen)
+    parts = [dict(params=[p[a:z].clone()], grads=[g[a:z]], ms=[torch.zeros(z - a, device="cuda", dtype=small)], vs=[torch.zeros(z - a, device="cuda", dtype=small)],
+                  scales=None if bits == 32 else [torch.zeros(2 * ((z - a + 255) // 256), device="cuda")]) for a, z in windows]
+    b.AdamW([p], [g], [m], [v], scales=None if bits == 32 else [scale], decay=[0.1], **H).step(lr=1e-2, step=1, seed=3)
+    for (a, z), q in zip(windows, parts):
+        b.AdamW(decay=[0.1], **q, **H).step(lr=1e-2, step=1, seed=3)
+        assert torch.equal(p[a:z], q["params"][0]), a
+        if bits == 32:
+            assert torch.equal(m[a:z], q["ms"][0]) and torch.equal(v[a:z], q["vs"][0]), a
+            continue
+        assert torch.equal(scale[a // 256 * 2:(z + 255) // 256 * 2][:q["scales"][0].numel() - 2], q["scales"][0][:-2]), a
+        blocks = (z - a) // 256                                           # (windows begin at a block; a last one that is not whole is left out)
+        x = g[a:a + blocks * 256].cpu().view(blocks, 256)
+        r = _random_bits(torch.arange(blocks * 256) + a, 1, 3).view(blocks, 256)
+        cm, _ = _codes(x * (1.0 - H["beta1"]), r & 0xFFFF, False)
+        cv, _ = _codes(((x * x) * (1.0 - H["beta2"])).double().sqrt().float(), r >> 16, True)
+        assert torch.equal(m[a:a + blocks * 256].cpu(), cm.view(-1)) and torch.equal(v[a:a + blocks * 256].cpu(), cv.view(-1)), a
+    assert not p[6000:2 ** 31 - 3000].any() and not m[6000:2 ** 31 - 3000].any()
