@@ -550,6 +550,71 @@ int chimera_head_loss_pieces(int dtype, int tokens, int hidden, int vocab, const
                              const void* d_lnf_b, const void* d_w_head, int ldw, float scale, void* d_dy, float* d_dlnf_g, float* d_dlnf_b,
                              float* d_dw_head, float* d_loss, int piece, void* d_workspace, size_t workspace_bytes, void* hip_stream);
 
+/* ------------------------------------------------- blocks over packed sequences
+ * What blocks with rotary positions, grouped heads and norms around their branches need besides the operators above; sequences of different lengths lie
+ * behind one another in one tensor.  All kernels run on the current device, which holds all tensors; all sums have a fixed order (no atomics).
+ *
+ * Rotary positions.  Of every head the first `rot` columns are rot/2 pairs (a, b): columns i and rot/2 + i (CHIMERA_ROTARY_HALF), or 2i and 2i + 1
+ * (CHIMERA_ROTARY_INTERLEAVED), i = 0, 1, ...  With the angle t = position * freq[i]
+ *   a' = magnitude (a cos t - b sin t),  b' = magnitude (a sin t + b cos t);  columns from rot on are passed on.
+ * transpose != 0: with -t, which takes the gradient of y to that of x. */
+enum { CHIMERA_ROTARY_HALF = 0, CHIMERA_ROTARY_INTERLEAVED = 1 };
+enum {
+    CHIMERA_ROTARY_PLAIN = 0,   /* f = base^(-2i/rot)                                                                       */
+    CHIMERA_ROTARY_LINEAR = 1,  /* f / factor: positions of a context that is `factor` times as long, moved together         */
+    CHIMERA_ROTARY_BASE = 2,    /* base * factor^(rot/(rot-2)) in place of base: the slowest pair as above, the fastest kept */
+    CHIMERA_ROTARY_BLEND = 3    /* w f + (1 - w) f / factor, w = (turns - low) / (high - low) held to [0, 1], with           */
+                                /* turns = context f / 2 pi, what the pair makes over the context it was trained on          */
+};
+/* h_freq[rot/2], host memory, in radians per position; computed once and copied to the device by the caller, who may as well use others.  rot: even, 2 to 256.
+ * factor >= 1; context, low and high are read for CHIMERA_ROTARY_BLEND only (factor for all but PLAIN). */
+int chimera_rotary_frequencies(int rot, double base, int scaling, double factor, double context, double low, double high, double* h_freq);
+/* y = the turned x, both [tokens, heads, head_dim] in the given dtype with rows (tokens) ldx and ldy elements apart, of any alignment; heads lie side by side.  d_positions
+ * int32 [tokens] (NULL: 0, 1, 2, ...), d_freq double [rot/2].  Angles are formed in double and off by at most 2^-51 of themselves.  y may be x itself (then
+ * columns from rot on are not touched), and must share nothing with an operand otherwise (EINVAL).  heads * head_dim up to 65536. */
+int chimera_op_rotary(int dtype, int tokens, int heads, int head_dim, int rot, int layout, int transpose, float magnitude, const int32_t* d_positions,
+                      const double* d_freq, const void* d_x, int ldx, void* d_y, int ldy, void* hip_stream);
+
+/* Attention over packed sequences with grouped heads.  d_offsets int32 [seqs + 1], ascending, in [0, tokens]: sequence i owns rows d_offsets[i] to d_offsets[i+1] - 1
+ * of all tensors (none is fine).  q, ctx and their gradients [tokens, heads, head_dim], k, v and theirs [tokens, kv_heads, head_dim], rows (tokens) ld*
+ * elements apart, heads side by side; query head j reads key and value head j / (heads / kv_heads).  In each sequence and head
+ *   ctx = softmax(scale q k^T [+ causal mask]) v,   d_lse[head, token] = log-sum-exp of the scaled scores (float [heads, tokens]).
+ * Rows that no sequence owns are neither read nor written, in results as in operands.  Offsets are read on the device; those that are not as above give meaningless
+ * results but no access outside the tensors.  head_dim is a multiple of 8 (float: 4) up to 128, so are leading dimensions; tensors are 16-byte aligned, heads
+ * up to 65536 / head_dim; scale is positive.  Results must share no memory with operands or one another (EINVAL); operands may (k = v).  Values are expected to be finite: a NaN or an
+ * infinity may also reach rows that the mask keeps it from, up to 127 positions away, but no other sequence or group of heads. */
+int chimera_op_attention_packed_fwd(int dtype, int seqs, int tokens, int heads, int kv_heads, int head_dim, int causal, float scale,
+                                    const int32_t* d_offsets, const void* d_q, int ldq, const void* d_k, int ldk, const void* d_v, int ldv,
+                                    void* d_ctx, int ldctx, float* d_lse, void* hip_stream);
+/* dq, dk, dv from dctx; dk and dv of a head are the sums over the query heads that read it.  d_workspace: ..._workspace_bytes bytes (0 for sizes that the calls
+ * refuse), 256-byte aligned; ENOMEM if it is too small.  Calls that overlap in time need workspaces of their own. */
+size_t chimera_op_attention_packed_bwd_workspace_bytes(int dtype, int seqs, int tokens, int heads, int kv_heads, int head_dim);
+int chimera_op_attention_packed_bwd(int dtype, int seqs, int tokens, int heads, int kv_heads, int head_dim, int causal, float scale,
+                                    const int32_t* d_offsets, const void* d_q, int ldq, const void* d_k, int ldk, const void* d_v, int ldv,
+                                    const void* d_ctx, int ldctx, const float* d_lse, const void* d_dctx, int lddctx, void* d_dq, int lddq,
+                                    void* d_dk, int lddk, void* d_dv, int lddv, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* What joins a branch (attention, MLP) to the residual stream: the norm behind the branch, its gate, the scaled sum, and the norm in front of the next branch.
+ *   u = post(f),   y = alpha x + beta gate u,   h = pre(y)
+ * f, h [rows, cols] in `dtype`; the stream x, y in `stream_dtype`, dtype or float.  post, pre: none (u = f; no h), LayerNorm ((v - mean) rstd gain + bias, biased
+ * variance + eps) or RMSNorm (v rstd gain + bias, rstd = 1 / sqrt(mean square + eps)); gains [cols] in dtype, biases too or NULL.  gate [gate_rows, cols] in dtype: row t of the
+ * tensors takes row t / (rows / gate_rows), so 1 is a gate per channel, the number of sequences a gate of each, rows one of each token; NULL: none.  x NULL:
+ * y = beta gate u.  h is the norm of y before its rounding.  d_stats float [4, rows]: mean (LayerNorm) and rstd of post, of pre, for the backward; what a call does not have
+ * is not written.  cols is a multiple of 8 up to 8192, rows up to 2^28; tensors are contiguous and 16-byte aligned.  y may be x itself and h may be f;
+ * results must share nothing else with operands or one another (EINVAL). */
+enum { CHIMERA_NORM_NONE = 0, CHIMERA_NORM_LAYER = 1, CHIMERA_NORM_RMS = 2 };
+int chimera_op_branch_norm_fwd(int dtype, int stream_dtype, int rows, int cols, int post, int pre, float eps, float alpha, float beta, const void* d_f,
+                               const void* d_x, const void* d_gate, int gate_rows, const void* d_post_gain, const void* d_post_bias, const void* d_pre_gain,
+                               const void* d_pre_bias, void* d_y, void* d_h, float* d_stats, void* hip_stream);
+/* Gradients from dy (stream_dtype; NULL: zero, needs pre) and dh (dtype, with pre): dx (stream_dtype, NULL: not wanted), df (dtype), and those of gains, biases and gate, floats
+ * of the parameters' shapes that are added to, or overwritten; NULL where not wanted.  y (with pre) and d_stats as the forward left them.  dx may be dy itself, df may be dh.
+ * The workspace depends on the same sizes (gate_rows 0 without a gate), 256-byte aligned; calls that overlap in time need one each. */
+size_t chimera_op_branch_norm_bwd_workspace_bytes(int rows, int cols, int gate_rows);
+int chimera_op_branch_norm_bwd(int dtype, int stream_dtype, int rows, int cols, int post, int pre, float alpha, float beta, const void* d_f, const void* d_y,
+                               const void* d_gate, int gate_rows, const void* d_post_gain, const void* d_post_bias, const void* d_pre_gain, const float* d_stats,
+                               const void* d_dy, const void* d_dh, void* d_dx, void* d_df, float* d_dpost_gain, float* d_dpost_bias, float* d_dpre_gain,
+                               float* d_dpre_bias, float* d_dgate, int overwrite, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
 /* ------------------------------------------------------- from gradients to weights
  * Norm of `count` float gradient tensors taken as one vector: d_out[0] = sqrt(sum of all squares), d_out[1] = the factor that brings it down to
  * max_norm, min(1, max_norm / norm); NaN where the norm is no finite float.  Squares are summed in double, in a fixed order.  h_n: element

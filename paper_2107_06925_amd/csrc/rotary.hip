@@ -1,0 +1,181 @@
+// Rotary positions: of every head the first `rot` columns, taken as rot / 2 pairs (a, b), are turned by an angle that grows with the token's position,
+//
+//   a' = magnitude (a cos t - b sin t),   b' = magnitude (a sin t + b cos t),   t = position * frequency[pair],
+//
+// and the rest is passed on.  The gradient takes the transposed matrix, the same with -t.
+//
+// The kernel moves 2 x tokens x heads x head_dim elements and computes little: what bounds it is memory.  An angle is the same for all heads of a token, so
+// a workgroup forms the sines and cosines of its tokens once, in LDS, and every thread then takes pieces of 16 bytes of the heads' rows from there.  The angle
+// is formed in double, in turns, of which only the fraction goes on in float: a float angle at position 10^5 would be off by 0.004.
+#include "device.h"
+#include "spans.h"
+
+#include <cmath>
+
+namespace chimera {
+
+namespace {
+
+constexpr int RT = 256;                 // threads
+constexpr int RT_TOKENS = 16;           // tokens of a workgroup at most
+constexpr int ROT_MAX = 256;
+
+struct RotaryArgs {
+    const void* x;
+    void* y;
+    const int* positions;
+    const double* freq;
+    long long ldx, ldy;
+    int tokens, heads, d, rot, per_group;           // per_group: tokens of a workgroup
+    int turned, items;                              // pieces of a head's row that are turned, and all of them
+    unsigned by_items, by_heads;                    // 2^31 / n, rounded up: quotients of numbers up to 2^16 by n up to 2^15
+    float magnitude, sign;
+};
+
+// n consecutive elements from an address that need not be aligned to more than an element
+template <typename T, int V> __device__ __forceinline__ void load_any(const T* p, int n, T* out) {
+    if (n == V) __builtin_memcpy(out, p, V * sizeof(T));
+    else
+#pragma unroll
+        for (int i = 0; i < V; ++i) out[i] = i < n ? p[i] : (T)0.f;
+}
+template <typename T, int V> __device__ __forceinline__ void store_any(T* p, int n, const T* v) {
+    if (n == V) __builtin_memcpy(p, v, V * sizeof(T));
+    else
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i < n) p[i] = v[i];
+}
+
+template <typename T, bool HALF>
+__global__ __launch_bounds__(RT) void rotary_kernel(RotaryArgs a) {
+    constexpr int V = Elem<T>::VEC;
+    __shared__ float2 turn[RT_TOKENS * ROT_MAX / 2];
+    const int tid = threadIdx.x, pairs = a.rot / 2;
+    const int token0 = (int)blockIdx.x * a.per_group, here = min(a.per_group, a.tokens - token0);
+    for (int i = tid; i < here * pairs; i += RT) {
+        const int t = i / pairs, p = i % pairs;
+        const double turns = (double)(a.positions ? a.positions[token0 + t] : token0 + t) * (a.freq[p] * 0.15915494309189533577);      // 1 / 2 pi
+        float s, c;
+        sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
+        turn[i] = make_float2(c * a.magnitude, s * a.magnitude * a.sign);
+    }
+    __syncthreads();
+    const int total = here * a.heads * a.items;
+    for (int i = tid; i < total; i += RT) {
+        const int row = (int)((unsigned long long)i * a.by_items >> 31), j = i - row * a.items;
+        const int t = (int)((unsigned long long)row * a.by_heads >> 31), h = row - t * a.heads;
+        const T* x = (const T*)a.x + (long long)(token0 + t) * a.ldx + h * a.d;
+        T* y = (T*)a.y + (long long)(token0 + t) * a.ldy + h * a.d;
+        const float2* w = turn + t * pairs;
+        if (j >= a.turned) {                                    // behind the turned columns
+            const int c = a.rot + (j - a.turned) * V, n = min(V, a.d - c);
+            T v[V];
+            load_any<T, V>(x + c, n, v);
+            store_any<T, V>(y + c, n, v);
+        } else if constexpr (HALF) {                            // pairs lie rot / 2 columns apart
+            const int c = j * V, n = min(V, pairs - c);
+            T u[V], v[V];
+            load_any<T, V>(x + c, n, u);
+            load_any<T, V>(x + pairs + c, n, v);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float2 cs = w[min(c + e, pairs - 1)];
+                const float p = Elem<T>::to_f(u[e]), q = Elem<T>::to_f(v[e]);
+                u[e] = Elem<T>::from_f(p * cs.x - q * cs.y);
+                v[e] = Elem<T>::from_f(p * cs.y + q * cs.x);
+            }
+            store_any<T, V>(y + c, n, u);
+            store_any<T, V>(y + pairs + c, n, v);
+        } else {                                                // pairs are neighbours
+            const int c = j * V, n = min(V, a.rot - c);
+            T v[V];
+            load_any<T, V>(x + c, n, v);
+#pragma unroll
+            for (int e = 0; e < V; e += 2) {
+                const float2 cs = w[min((c + e) / 2, pairs - 1)];
+                const float p = Elem<T>::to_f(v[e]), q = Elem<T>::to_f(v[e + 1]);
+                v[e] = Elem<T>::from_f(p * cs.x - q * cs.y);
+                v[e + 1] = Elem<T>::from_f(p * cs.y + q * cs.x);
+            }
+            store_any<T, V>(y + c, n, v);
+        }
+    }
+}
+
+}  // namespace
+
+}  // namespace chimera
+
+using namespace chimera;
+
+extern "C" {
+
+int chimera_rotary_frequencies(int rot, double base, int scaling, double factor, double context, double low, double high, double* h_freq) {
+    if (rot < 2 || rot > ROT_MAX || rot % 2) return fail(CHIMERA_EINVAL, "rot=%d must be even, 2 to %d", rot, ROT_MAX);
+    if (!h_freq) return fail(CHIMERA_EINVAL, "h_freq is NULL");
+    if (!(base > 1) || !std::isfinite(base)) return fail(CHIMERA_EINVAL, "base must be a number above 1");
+    if (scaling < CHIMERA_ROTARY_PLAIN || scaling > CHIMERA_ROTARY_BLEND) return fail(CHIMERA_EINVAL, "unknown scaling %d", scaling);
+    if (scaling != CHIMERA_ROTARY_PLAIN && (!(factor >= 1) || !std::isfinite(factor))) return fail(CHIMERA_EINVAL, "factor must be a number of at least 1");
+    if (scaling == CHIMERA_ROTARY_BASE) {
+        if (rot == 2) return fail(CHIMERA_EINVAL, "one pair has no base to scale");
+        base *= std::pow(factor, (double)rot / (rot - 2));
+    }
+    if (scaling == CHIMERA_ROTARY_BLEND && (!(context > 0) || !std::isfinite(context) || !(low >= 0) || !(high > low) || !std::isfinite(high)))
+        return fail(CHIMERA_EINVAL, "blending needs a positive context and 0 <= low < high");
+    for (int i = 0; i < rot / 2; ++i) {
+        double f = std::pow(base, -2.0 * i / rot);
+        if (scaling == CHIMERA_ROTARY_LINEAR) f /= factor;
+        if (scaling == CHIMERA_ROTARY_BLEND) {
+            const double turns = context * f * 0.15915494309189533577;
+            const double keep = std::min(1.0, std::max(0.0, (turns - low) / (high - low)));
+            f = keep * f + (1 - keep) * f / factor;
+        }
+        h_freq[i] = f;
+    }
+    return CHIMERA_OK;
+}
+
+int chimera_op_rotary(int dtype, int tokens, int heads, int head_dim, int rot, int layout, int transpose, float magnitude, const int32_t* d_positions,
+                      const double* d_freq, const void* d_x, int ldx, void* d_y, int ldy, void* hip_stream) {
+    if (dtype != CHIMERA_F32 && dtype != CHIMERA_BF16) return fail(CHIMERA_EINVAL, "unknown dtype %d", dtype);
+    if (tokens < 1 || heads < 1 || head_dim < 1) return fail(CHIMERA_EINVAL, "sizes must be positive");
+    if (rot < 2 || rot > ROT_MAX || rot % 2 || rot > head_dim) return fail(CHIMERA_EINVAL, "rot=%d must be even, 2 to %d and at most head_dim=%d", rot, ROT_MAX, head_dim);
+    if (layout != CHIMERA_ROTARY_HALF && layout != CHIMERA_ROTARY_INTERLEAVED) return fail(CHIMERA_EINVAL, "unknown layout %d", layout);
+    if (!std::isfinite(magnitude)) return fail(CHIMERA_EINVAL, "magnitude must be finite");
+    if (!d_freq || !d_x || !d_y) return fail(CHIMERA_EINVAL, "NULL operand");
+    if (tokens > 1 << 28 || (long long)heads * head_dim > 1 << 16) return fail(CHIMERA_EINVAL, "more than 2^28 tokens or 2^16 columns");
+    const int cols = heads * head_dim;
+    if (ldx < cols || ldy < cols) return fail(CHIMERA_EINVAL, "leading dimension too small");
+    const size_t e = dtype == CHIMERA_F32 ? 4 : 2;
+    if ((((uintptr_t)d_x | (uintptr_t)d_y) & (e - 1)) || ((uintptr_t)d_freq & 7) || ((uintptr_t)d_positions & 3)) return fail(CHIMERA_EINVAL, "a tensor is not aligned to its elements");
+    const bool in_place = d_x == d_y && ldx == ldy;
+    const Rows x = matrix(d_x, tokens, cols, ldx, e), y = matrix(d_y, tokens, cols, ldy, e);
+    const Rows f = plain(d_freq, (size_t)rot * 4), p = plain(d_positions, (size_t)tokens * 4);
+    if (int rc = in_place ? check_apart({f, p}, {y}) : check_apart({x, f, p}, {y})) return rc;
+    RotaryArgs a{};
+    const int v = dtype == CHIMERA_F32 ? 4 : 8;
+    a.x = d_x; a.y = d_y; a.positions = d_positions; a.freq = d_freq; a.ldx = ldx; a.ldy = ldy;
+    a.tokens = tokens; a.heads = heads; a.d = head_dim; a.rot = rot; a.magnitude = magnitude; a.sign = transpose ? -1.0f : 1.0f;
+    a.turned = layout == CHIMERA_ROTARY_HALF ? (rot / 2 + v - 1) / v : (rot + v - 1) / v;
+    a.items = a.turned + (in_place ? 0 : (head_dim - rot + v - 1) / v);
+    // three pieces a thread, but no fewer than 512 workgroups where there are tokens for them
+    const int row_items = heads * a.items;
+    a.per_group = std::max(1, std::min({RT_TOKENS, (3 * RT + row_items - 1) / row_items, (tokens + 511) / 512}));
+    a.by_items = (unsigned)(((1u << 31) + a.items - 1) / a.items);
+    a.by_heads = (unsigned)(((1u << 31) + heads - 1) / heads);
+    const dim3 grid((unsigned)((tokens + a.per_group - 1) / a.per_group)), block(RT);
+    hipStream_t s = (hipStream_t)hip_stream;
+    const bool half = layout == CHIMERA_ROTARY_HALF;
+    if (dtype == CHIMERA_F32) {
+        if (half) hipLaunchKernelGGL((rotary_kernel<float, true>), grid, block, 0, s, a);
+        else hipLaunchKernelGGL((rotary_kernel<float, false>), grid, block, 0, s, a);
+    } else {
+        if (half) hipLaunchKernelGGL((rotary_kernel<bf16_t, true>), grid, block, 0, s, a);
+        else hipLaunchKernelGGL((rotary_kernel<bf16_t, false>), grid, block, 0, s, a);
+    }
+    CHIMERA_LAUNCH_CHECK("rotary positions");
+    return CHIMERA_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,188 @@
+"""What rotary positions, attention over packed sequences and the norms around a branch refuse, their sizes and host-side tables: no launch is made."""
+import math
+
+import pytest
+
+from paper_2107_06925_amd import binding as b
+
+NAN, INF = float("nan"), float("inf")
+U64 = 1 << 62
+
+
+def at(i):
+    """Addresses far apart, aligned; no call below follows them."""
+    return (i + 1) << 40
+
+
+def rotary(dtype=b.BF16, tokens=10, heads=4, dim=64, rot=64, layout=0, magnitude=1.0, pos=at(0), freq=at(1), x=at(2), ldx=256, y=at(3), ldy=256):
+    return b.lib().chimera_op_rotary(dtype, tokens, heads, dim, rot, layout, 0, magnitude, pos, freq, x, ldx, y, ldy, None)
+
+
+@pytest.mark.parametrize("bad", [dict(dtype=2), dict(tokens=0), dict(tokens=-1), dict(tokens=(1 << 28) + 1), dict(heads=0), dict(dim=0), dict(dim=62), dict(rot=0), dict(rot=63), dict(rot=66),
+                                 dict(dim=300, rot=258, ldx=1200, ldy=1200), dict(layout=2), dict(layout=-1), dict(magnitude=NAN), dict(magnitude=INF), dict(freq=None), dict(x=None), dict(y=None),
+                                 dict(ldx=255), dict(ldy=255), dict(heads=2048, ldx=1 << 20, ldy=1 << 20), dict(x=at(2) + 1), dict(y=at(3) + 1), dict(freq=at(1) + 4), dict(pos=at(0) + 2),
+                                 dict(y=at(2) + 2), dict(y=at(2), ldy=264), dict(y=at(2) + 512 * 9), dict(y=at(1)), dict(y=at(0)), dict(x=at(1), y=at(1))], ids=str)
+def test_rotary_refuses(bad):
+    assert rotary(**bad) == b.EINVAL
+    assert b.last_error()
+
+
+def test_rotary_frequencies():
+    plain = b.chimera_rotary_frequencies(64, 10000.0)
+    assert plain.shape == (32,)
+    for i, f in enumerate(plain.tolist()):
+        assert abs(f - 10000.0 ** (-2.0 * i / 64)) <= 4e-16 * f
+    linear = b.chimera_rotary_frequencies(64, 10000.0, b.ROTARY_LINEAR, 4.0)
+    assert ((linear - plain / 4).abs() <= 4e-16 * plain).all()
+    base = b.chimera_rotary_frequencies(64, 10000.0, b.ROTARY_BASE, 4.0)
+    assert float(base[0]) == 1.0 and abs(float(base[-1] / plain[-1]) - 0.25) < 1e-12        # the slowest pair as with positions divided, the fastest kept
+    blend = b.chimera_rotary_frequencies(64, 10000.0, b.ROTARY_BLEND, 8.0, context=2048, low=1.0, high=32.0)
+    for f, g in zip(plain.tolist(), blend.tolist()):
+        w = min(1.0, max(0.0, (2048 * f / (2 * math.pi) - 1.0) / 31.0))
+        assert abs(g - (w * f + (1 - w) * f / 8)) <= 1e-14 * f
+    assert float(blend[0]) == 1.0 and abs(float(blend[-1] * 8 / plain[-1]) - 1) < 1e-14
+    assert b.chimera_rotary_frequencies(2).tolist() == [1.0]
+
+
+@pytest.mark.parametrize("bad", [dict(rot=0), dict(rot=-2), dict(rot=7), dict(rot=258), dict(base=1.0), dict(base=NAN), dict(base=INF), dict(scaling=4), dict(scaling=-1),
+                                 dict(scaling=1, factor=0.5), dict(scaling=1, factor=NAN), dict(scaling=2, factor=INF), dict(scaling=2, rot=2), dict(scaling=3, context=0.0),
+                                 dict(scaling=3, context=NAN), dict(scaling=3, context=2048.0, low=-1.0), dict(scaling=3, context=2048.0, low=2.0, high=2.0),
+                                 dict(scaling=3, context=2048.0, high=INF), dict(scaling=3, context=2048.0, high=NAN)], ids=str)
+def test_rotary_frequencies_refuses(bad):
+    with pytest.raises(b.ChimeraError) as e:
+        b.chimera_rotary_frequencies(**{**dict(rot=64, factor=2.0), **bad})
+    assert e.value.code == b.EINVAL
+
+
+NAMES = ("q", "k", "v", "ctx", "dctx", "dq", "dk", "dv")
+
+
+def packed(back, **o):
+    a = dict(dtype=b.BF16, seqs=3, tokens=100, heads=8, kv=2, dim=64, scale=0.125, offsets=at(8), lse=at(9), ws=at(10), size=U64)
+    a.update({n: at(i) for i, n in enumerate(NAMES)})
+    a.update({"ld" + n: 128 if n in ("k", "v", "dk", "dv") else 512 for n in NAMES})
+    a.update(o)
+    head = (a["dtype"], a["seqs"], a["tokens"], a["heads"], a["kv"], a["dim"], 1, a["scale"], a["offsets"], a["q"], a["ldq"], a["k"], a["ldk"], a["v"], a["ldv"], a["ctx"], a["ldctx"], a["lse"])
+    if not back:
+        return b.lib().chimera_op_attention_packed_fwd(*head, None)
+    return b.lib().chimera_op_attention_packed_bwd(*head, a["dctx"], a["lddctx"], a["dq"], a["lddq"], a["dk"], a["lddk"], a["dv"], a["lddv"], a["ws"], a["size"], None)
+
+
+PACKED_BAD = [dict(dtype=2), dict(seqs=0), dict(seqs=-1), dict(tokens=0), dict(tokens=(1 << 28) + 1), dict(heads=0), dict(kv=0), dict(kv=3), dict(heads=4, kv=8), dict(dim=0), dict(dim=60), dict(dim=4),
+              dict(dim=136, ldq=2048, ldk=512, ldv=512, ldctx=2048), dict(heads=1026, ldq=1 << 17, ldctx=1 << 17, kv=2), dict(tokens=1 << 28, heads=1024, dim=64, ldq=1 << 16, ldctx=1 << 16),
+              dict(scale=0.0), dict(scale=-1.0), dict(scale=NAN), dict(scale=INF), dict(offsets=None), dict(offsets=at(8) + 2), dict(lse=None), dict(lse=at(9) + 1),
+              dict(q=None), dict(k=None), dict(v=None), dict(ctx=None), dict(q=at(0) + 8), dict(k=at(1) + 2), dict(v=at(2) + 4), dict(ctx=at(3) + 8), dict(ldq=504), dict(ldk=120), dict(ldv=132),
+              dict(ldctx=516), dict(dtype=b.F32, dim=66), dict(dtype=b.F32, ldq=514)]
+
+
+@pytest.mark.parametrize("bad", PACKED_BAD + [dict(ctx=at(0)), dict(ctx=at(0) + 1024), dict(lse=at(3)), dict(lse=at(8)), dict(ctx=at(2) + 16)], ids=str)
+def test_attention_packed_fwd_refuses(bad):
+    assert packed(False, **bad) == b.EINVAL
+    assert b.last_error()
+
+
+@pytest.mark.parametrize("bad", PACKED_BAD + [dict(dctx=None), dict(dq=None), dict(dk=None), dict(dv=None), dict(ws=None), dict(ws=at(10) + 128), dict(dq=at(0)), dict(dk=at(6) + 8), dict(lddv=120),
+                                              dict(lddq=508), dict(dq=at(3)), dict(dq=at(4)), dict(dv=at(6)), dict(ws=at(9)), dict(dk=at(8)), dict(dk=at(5) + 128, lddk=512)], ids=str)
+def test_attention_packed_bwd_refuses(bad):
+    assert packed(True, **bad) == b.EINVAL
+    assert b.last_error()
+
+
+@pytest.mark.parametrize("dtype", [b.F32, b.BF16])
+@pytest.mark.parametrize("seqs,tokens,heads,kv,dim", [(1, 1, 1, 1, 8), (5, 1000, 25, 5, 64), (3, 16384, 16, 2, 128), (70, 300, 8, 8, 40)])
+def test_attention_packed_workspaces(dtype, seqs, tokens, heads, kv, dim):
+    need = b.lib().chimera_op_attention_packed_bwd_workspace_bytes(dtype, seqs, tokens, heads, kv, dim)
+    assert heads * tokens * 4 <= need <= heads * tokens * 4 + 256 + 8 * heads * tokens * dim       # the deltas, and at most a float dk and dv of each query head
+    lds = {"ld" + n: (kv if n in ("k", "v", "dk", "dv") else heads) * dim for n in NAMES}
+    assert packed(True, dtype=dtype, seqs=seqs, tokens=tokens, heads=heads, kv=kv, dim=dim, size=need - 1, **lds) == b.ENOMEM
+
+
+def test_attention_packed_workspace_of_refused_sizes_is_zero():
+    f = b.lib().chimera_op_attention_packed_bwd_workspace_bytes
+    for args in ((3, 1, 8, 2, 2, 64), (b.BF16, 0, 8, 2, 2, 64), (b.BF16, 1, 0, 2, 2, 64), (b.BF16, 1, 8, 3, 2, 64), (b.BF16, 1, 8, 2, 2, 12), (b.BF16, 1, 8, 2, 2, 136)):
+        assert f(*args) == 0
+
+
+FWD = ("f", "x", "gate", "g1", "b1", "g2", "b2", "y", "h", "stats")
+
+
+def join_fwd(**o):
+    a = dict(dtype=b.BF16, st=b.F32, rows=12, cols=64, post=1, pre=2, eps=1e-5, alpha=1.0, beta=1.0, gates=3)
+    a.update({n: at(i) for i, n in enumerate(FWD)})
+    a.update(o)
+    return b.lib().chimera_op_branch_norm_fwd(a["dtype"], a["st"], a["rows"], a["cols"], a["post"], a["pre"], a["eps"], a["alpha"], a["beta"], a["f"], a["x"], a["gate"], a["gates"],
+                                              a["g1"], a["b1"], a["g2"], a["b2"], a["y"], a["h"], a["stats"], None)
+
+
+JOIN_BAD = [dict(dtype=2), dict(st=2), dict(dtype=b.F32, st=b.BF16), dict(rows=0), dict(rows=(1 << 28) + 1), dict(cols=0), dict(cols=60), dict(cols=8200), dict(gates=5), dict(gates=0), dict(gates=-3),
+            dict(post=3), dict(post=-1), dict(pre=3), dict(alpha=NAN), dict(beta=INF), dict(f=None), dict(g1=None), dict(g2=None), dict(stats=None), dict(stats=at(9) + 2),
+            dict(f=at(0) + 8), dict(gate=at(2) + 2), dict(g1=at(3) + 8), dict(y=at(7) + 8), dict(y=None)]
+
+
+@pytest.mark.parametrize("bad", JOIN_BAD + [dict(eps=-1e-5), dict(eps=NAN), dict(h=None), dict(x=at(1) + 8), dict(b2=at(6) + 4), dict(y=at(0)), dict(y=at(1) + 16), dict(y=at(2)), dict(h=at(1)),
+                                            dict(h=at(7) + 64), dict(h=at(0) + 16), dict(stats=at(8)), dict(stats=at(3)), dict(h=at(5))], ids=str)
+def test_branch_norm_fwd_refuses(bad):
+    assert join_fwd(**bad) == b.EINVAL
+    assert b.last_error()
+
+
+BWD = ("f", "y", "gate", "g1", "b1", "g2", "stats", "dy", "dh", "dx", "df", "dg1", "db1", "dg2", "db2", "dgate", "ws")
+
+
+def join_bwd(**o):
+    a = dict(dtype=b.BF16, st=b.F32, rows=12, cols=64, post=1, pre=2, alpha=1.0, beta=1.0, gates=3, size=U64)
+    a.update({n: at(i) for i, n in enumerate(BWD)})
+    a.update(o)
+    return b.lib().chimera_op_branch_norm_bwd(a["dtype"], a["st"], a["rows"], a["cols"], a["post"], a["pre"], a["alpha"], a["beta"], a["f"], a["y"], a["gate"], a["gates"], a["g1"], a["b1"],
+                                              a["g2"], a["stats"], a["dy"], a["dh"], a["dx"], a["df"], a["dg1"], a["db1"], a["dg2"], a["db2"], a["dgate"], 0, a["ws"], a["size"], None)
+
+
+@pytest.mark.parametrize("bad", [dict(x, **({"stats": at(6) + 2} if "stats" in x and x["stats"] else {})) for x in JOIN_BAD if "y" not in x or x["y"] is None] +
+                         [dict(dh=None), dict(df=None), dict(ws=None), dict(ws=at(16) + 16), dict(y=at(1) + 8), dict(dy=at(7) + 4), dict(dgate=at(15) + 8), dict(dx=at(0)), dict(df=at(0)), dict(df=at(7)),
+                          dict(dx=at(8)), dict(dx=at(7) + 16), dict(dg1=at(12)), dict(ws=at(8)), dict(dgate=at(2)), dict(db2=at(6)), dict(pre=0), dict(post=0), dict(gate=None),
+                          dict(pre=0, dg2=None, db2=None, dy=None), dict(dg1=at(9) + 16)], ids=str)
+def test_branch_norm_bwd_refuses(bad):
+    assert join_bwd(**bad) == b.EINVAL
+    assert b.last_error()
+
+
+@pytest.mark.parametrize("rows,cols,gates", [(1, 8, 0), (60, 512, 1), (8192, 1600, 8), (30000, 64, 30000), (4096, 8192, 2), (7, 4104, 7)])
+def test_branch_norm_workspace(rows, cols, gates):
+    need = b.lib().chimera_op_branch_norm_bwd_workspace_bytes(rows, cols, gates)
+    assert 0 < need <= 1100 * 5 * cols * 4
+    assert join_bwd(rows=rows, cols=cols, gates=gates, gate=at(2) if gates else None, dgate=at(15) if gates else None, size=need - 1) == b.ENOMEM
+
+
+def test_branch_norm_workspace_of_refused_sizes_is_zero():
+    f = b.lib().chimera_op_branch_norm_bwd_workspace_bytes
+    for args in ((0, 64, 0), (4, 60, 0), (4, 8200, 0), (4, 64, 3), (4, 64, -1)):
+        assert f(*args) == 0
+
+
+def test_bindings_refuse_tensors_that_do_not_fit():
+    torch = pytest.importorskip("torch")
+    t = lambda *s, d=torch.float32: torch.zeros(s, dtype=d)  # noqa: E731
+    f8, i32 = t(8, d=torch.float64), t(3, d=torch.int32)
+    for call in (lambda: b.chimera_op_rotary(t(3, 2, 16), t(3, 2, 8), f8), lambda: b.chimera_op_rotary(t(3, 32), t(3, 32), f8), lambda: b.chimera_op_rotary(t(3, 2, 16), t(3, 2, 16), f8.float()),
+                 lambda: b.chimera_op_rotary(t(3, 2, 16), t(3, 2, 16), f8, positions=t(3)), lambda: b.chimera_op_rotary(t(3, 2, 16), t(3, 2, 16), f8, positions=t(4, d=torch.int32)),
+                 lambda: b.chimera_op_rotary(t(3, 16, 2).transpose(1, 2), t(3, 2, 16), f8), lambda: b.chimera_op_rotary(t(3, 4, 16)[:, ::2], t(3, 2, 16), f8),
+                 lambda: b.chimera_op_rotary(t(3, 2, 16, d=torch.float16), t(3, 2, 16, d=torch.float16), f8), lambda: b.chimera_op_rotary(t(3, 2, 16), t(3, 2, 16, d=torch.bfloat16), f8),
+                 lambda: b.chimera_op_rotary(t(3, 2, 16), t(3, 2, 16), f8)):                       # (the last: tensors of the host)
+        with pytest.raises(ValueError):
+            call()
+    q, k = t(5, 4, 8), t(5, 2, 8)
+    good = dict(q=q, k=k, v=k, offsets=i32, ctx=t(5, 4, 8), lse=t(4, 5))
+    for bad in (dict(k=t(4, 2, 8)), dict(k=t(5, 2, 16)), dict(v=t(5, 1, 8)), dict(q=t(5, 32)), dict(offsets=t(3)), dict(lse=t(4, 4)), dict(ctx=t(5, 4, 4)), dict(ctx=t(5, 4, 8, d=torch.bfloat16)),
+                dict(lse=t(5, 4).t().double()), {}):
+        with pytest.raises(ValueError):
+            b.chimera_op_attention_packed_fwd(**{**good, **bad})
+    for bad in (dict(dq=k), dict(dk=q), dict(dctx=k), dict(dv=t(5, 2, 8, d=torch.bfloat16)), {}):
+        with pytest.raises(ValueError):
+            b.chimera_op_attention_packed_bwd(**{**good, **dict(dctx=t(5, 4, 8), dq=t(5, 4, 8), dk=t(5, 2, 8), dv=t(5, 2, 8)), **bad})
+    m = t(4, 16)
+    for bad in (dict(f=t(16)), dict(x=t(4, 8)), dict(y=t(8, 16)[::2]), dict(gate=t(16)), dict(gate=t(2, 8)), dict(post_gain=t(8)), dict(stats=t(4, 5)), dict(h=t(4, 16, d=torch.bfloat16)), {}):
+        with pytest.raises(ValueError):
+            b.chimera_op_branch_norm_fwd(**{**dict(f=m, x=m, y=t(4, 16)), **bad})
+    for bad in (dict(dgate=t(16), gate=t(1, 16)), dict(dpost_gain=t(8)), dict(stats=t(4, 3)), dict(dx=t(4, 8)), {}):
+        with pytest.raises(ValueError):
+            b.chimera_op_branch_norm_bwd(**{**dict(f=m, y=m, stats=t(4, 4), dy=m, dh=None, dx=t(4, 16), df=t(4, 16)), **bad})
