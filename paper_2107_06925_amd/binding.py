@@ -659,12 +659,12 @@ def chimera_rotary_frequencies(rot, base=10000.0, scaling=ROTARY_PLAIN, factor=1
     return freq
 
 
-def _heads(t, dtype, what):
-    """Of a tensor [tokens, heads, head_dim] whose heads lie side by side: how far its rows are apart."""
-    shape = t.shape
-    if len(shape) != 3 or t.dtype != dtype or (shape[2] > 1 and t.stride(2) != 1) or (shape[1] > 1 and t.stride(1) != shape[2]):
-        raise ValueError("%s: [tokens, heads, head_dim] of %s with its heads side by side expected" % (what, dtype))
-    return t.stride(0) if shape[0] > 1 else shape[1] * shape[2]
+def _heads(t, shape, dtype, what):
+    """How far the rows of a tensor [tokens, heads, head_dim] are apart, whose heads lie side by side."""
+    stride = t.stride()
+    if t.shape != shape or t.dtype != dtype or len(stride) != 3 or (stride[2] != 1 and shape[2] > 1) or (stride[1] != shape[2] and shape[1] > 1):
+        raise ValueError("%s: %s of %s with its heads side by side expected" % (what, tuple(shape), dtype))
+    return stride[0] if shape[0] > 1 else shape[1] * shape[2]
 
 
 def _float_type(t):
@@ -677,79 +677,82 @@ def _float_type(t):
 def chimera_op_rotary(x, y, freq, positions=None, layout=ROTARY_HALF, magnitude=1.0, transpose=False):
     """x, y [tokens, heads, head_dim] of one type (rows may lie further apart; y may be x); freq: float64 [rot / 2]; positions int32 [tokens], or 0, 1, 2, ..."""
     import torch
-    dt = _float_type(x)
-    if x.shape != y.shape:
-        raise ValueError("x and y have one shape")
-    ldx, ldy = _heads(x, x.dtype, "x"), _heads(y, x.dtype, "y")
-    tokens, heads, dim = x.shape
-    check(lib().chimera_op_rotary(dt, tokens, heads, dim, 2 * freq.numel(), layout, int(transpose), magnitude, _vector(positions, torch.int32, tokens, "positions"),
-                                  _vector(freq, torch.float64, freq.numel(), "freq"), x.data_ptr(), ldx, y.data_ptr(), ldy, _stream_of(x, y, freq, positions)))
+    dt, t, shape = _float_type(x), x.dtype, x.shape
+    ldx, ldy = _heads(x, shape, t, "x"), _heads(y, shape, t, "y")
+    tokens, heads, dim = shape
+    pairs = freq.numel()
+    check(lib().chimera_op_rotary(dt, tokens, heads, dim, 2 * pairs, layout, int(transpose), magnitude, _vector(positions, torch.int32, tokens, "positions"),
+                                  _vector(freq, torch.float64, pairs, "freq"), x.data_ptr(), ldx, y.data_ptr(), ldy, _stream_of(x, y, freq, positions)))
 
 
-def _packed(q, k, v, offsets, lse):
-    """Type, sequences, tokens, heads, key and value heads, head size of packed attention, and what its calls have in common."""
+def _packed(q, k, v, offsets, ctx, lse):
+    """Of packed attention: type, sequences, tokens, heads, key and value heads, head size; the operands as the library takes them; ctx and lse."""
     import torch
-    dt = _float_type(q)
-    if len(q.shape) != 3 or len(k.shape) != 3 or k.shape != v.shape or q.shape[0] != k.shape[0] or q.shape[2] != k.shape[2]:
+    dt, t, wide, narrow = _float_type(q), q.dtype, q.shape, k.shape
+    if len(wide) != 3 or len(narrow) != 3 or wide[0] != narrow[0] or wide[2] != narrow[2]:
         raise ValueError("q [tokens, heads, head_dim], k and v [tokens, kv_heads, head_dim] expected")
-    tokens, heads, dim = q.shape
+    tokens, heads, dim = wide
     seqs = offsets.numel() - 1
-    return (dt, seqs, tokens, heads, k.shape[1], dim), (_vector(offsets, torch.int32, seqs + 1, "offsets"), q.data_ptr(), _heads(q, q.dtype, "q"), k.data_ptr(),
-                                                        _heads(k, q.dtype, "k"), v.data_ptr(), _heads(v, q.dtype, "v")), _vector(lse, torch.float32, heads * tokens, "lse")
+    return ((dt, seqs, tokens, heads, narrow[1], dim),
+            (_vector(offsets, torch.int32, seqs + 1, "offsets"), q.data_ptr(), _heads(q, wide, t, "q"), k.data_ptr(), _heads(k, narrow, t, "k"), v.data_ptr(), _heads(v, narrow, t, "v")),
+            (ctx.data_ptr(), _heads(ctx, wide, t, "ctx"), _vector(lse, torch.float32, heads * tokens, "lse")))
 
 
 def chimera_op_attention_packed_fwd(q, k, v, offsets, ctx, lse, causal=True, scale=None):
     """q, ctx [tokens, heads, head_dim], k, v [tokens, kv_heads, head_dim] (rows may lie further apart than they are long), offsets int32 [sequences + 1],
     lse float [heads, tokens]; scale None: 1 / sqrt(head_dim)."""
-    sizes, operands, lse_at = _packed(q, k, v, offsets, lse)
-    if ctx.shape != q.shape:
-        raise ValueError("ctx has the shape of q")
-    check(lib().chimera_op_attention_packed_fwd(*sizes, int(causal), sizes[5] ** -0.5 if scale is None else scale, *operands, ctx.data_ptr(), _heads(ctx, q.dtype, "ctx"),
-                                                lse_at, _stream_of(q, k, v, offsets, ctx, lse)))
+    sizes, operands, results = _packed(q, k, v, offsets, ctx, lse)
+    check(lib().chimera_op_attention_packed_fwd(*sizes, int(causal), sizes[5] ** -0.5 if scale is None else scale, *operands, *results,
+                                                _stream_of(q, k, v, offsets, ctx, lse)))
 
 
 def chimera_op_attention_packed_bwd(q, k, v, offsets, ctx, lse, dctx, dq, dk, dv, causal=True, scale=None, workspace=None):
     """dq, dk, dv: tensors of the shapes of q, k, v to be filled (views of one buffer are fine).  Allocates the workspace unless one is given, and returns it."""
     import torch
-    sizes, operands, lse_at = _packed(q, k, v, offsets, lse)
-    if ctx.shape != q.shape or dctx.shape != q.shape or dq.shape != q.shape or dk.shape != k.shape or dv.shape != k.shape:
-        raise ValueError("ctx, dctx and dq have the shape of q, dk and dv that of k")
+    sizes, operands, kept = _packed(q, k, v, offsets, ctx, lse)
+    t, wide, narrow = q.dtype, q.shape, k.shape
     if workspace is None:
         workspace = torch.empty(lib().chimera_op_attention_packed_bwd_workspace_bytes(*sizes), dtype=torch.uint8, device=q.device)
-    t = q.dtype
-    check(lib().chimera_op_attention_packed_bwd(*sizes, int(causal), sizes[5] ** -0.5 if scale is None else scale, *operands, ctx.data_ptr(), _heads(ctx, t, "ctx"),
-                                                lse_at, dctx.data_ptr(), _heads(dctx, t, "dctx"), dq.data_ptr(), _heads(dq, t, "dq"), dk.data_ptr(),
-                                                _heads(dk, t, "dk"), dv.data_ptr(), _heads(dv, t, "dv"), workspace.data_ptr(), workspace.numel(),
-                                                _stream_of(q, k, v, offsets, ctx, lse, dctx, dq, dk, dv, workspace)))
+    check(lib().chimera_op_attention_packed_bwd(*sizes, int(causal), sizes[5] ** -0.5 if scale is None else scale, *operands, *kept,
+                                                dctx.data_ptr(), _heads(dctx, wide, t, "dctx"), dq.data_ptr(), _heads(dq, wide, t, "dq"),
+                                                dk.data_ptr(), _heads(dk, narrow, t, "dk"), dv.data_ptr(), _heads(dv, narrow, t, "dv"),
+                                                workspace.data_ptr(), workspace.numel(), _stream_of(q, k, v, offsets, ctx, lse, dctx, dq, dk, dv, workspace)))
     return workspace
 
 
 def _matrix(t, dtype, shape, what):
-    if t is not None and (t.dtype != dtype or t.shape != shape or not t.is_contiguous()):
+    if t is None:
+        return None
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError("%s: contiguous %s of %s expected" % (what, tuple(shape), dtype))
-    return None if t is None else t.data_ptr()
+    return t.data_ptr()
 
 
 def _join(f, stream, gate):
-    """Types and sizes of f [rows, cols] and its stream, rows of the gate."""
-    if len(f.shape) != 2:
+    """Types and sizes of f [rows, cols] and its stream; the gate, and its rows."""
+    n, t = f.shape, f.dtype
+    if len(n) != 2:
         raise ValueError("f: [rows, cols] expected")
-    if gate is not None and (len(gate.shape) != 2 or gate.shape[0] < 1 or gate.shape[1] != f.shape[1]):
+    dt = _float_type(f)
+    sizes = (dt, dt if stream.dtype == t else _float_type(stream), n[0], n[1])
+    if gate is None:
+        return sizes, None, 0
+    if len(gate.shape) != 2 or gate.shape[0] < 1 or gate.shape[1] != n[1]:
         raise ValueError("gate: [gate_rows, cols] expected")
-    return _float_type(f), _float_type(stream), f.shape[0], f.shape[1], 0 if gate is None else gate.shape[0]
+    return sizes, _matrix(gate, t, gate.shape, "gate"), gate.shape[0]
 
 
 def chimera_op_branch_norm_fwd(f, x, y, h=None, stats=None, post=NORM_NONE, post_gain=None, post_bias=None, pre=NORM_NONE, pre_gain=None, pre_bias=None,
                                gate=None, alpha=1.0, beta=1.0, eps=1e-5):
     """y = alpha x + beta gate post(f), h = pre(y).  f, h [rows, cols], x (or None) and y of the stream's type, gate [gate_rows, cols]; stats float [4, rows]."""
     import torch
-    dt, st, rows, cols, gates = _join(f, y, gate)
+    sizes, gate_at, gates = _join(f, y, gate)
     t, ts, n = f.dtype, y.dtype, f.shape
-    check(lib().chimera_op_branch_norm_fwd(dt, st, rows, cols, post, pre, eps, alpha, beta, _matrix(f, t, n, "f"), _matrix(x, ts, n, "x"),
-                                           None if gate is None else _matrix(gate, t, gate.shape, "gate"), gates, _vector(post_gain, t, cols, "post_gain"),
-                                           _vector(post_bias, t, cols, "post_bias"), _vector(pre_gain, t, cols, "pre_gain"), _vector(pre_bias, t, cols, "pre_bias"),
-                                           _matrix(y, ts, n, "y"), _matrix(h, t, n, "h"), _vector(stats, torch.float32, 4 * rows, "stats"),
-                                           _stream_of(f, x, y, h, stats, post_gain, post_bias, pre_gain, pre_bias, gate)))
+    cols = sizes[3]
+    check(lib().chimera_op_branch_norm_fwd(*sizes, post, pre, eps, alpha, beta, _matrix(f, t, n, "f"), _matrix(x, ts, n, "x"), gate_at, gates,
+                                           _vector(post_gain, t, cols, "post_gain"), _vector(post_bias, t, cols, "post_bias"), _vector(pre_gain, t, cols, "pre_gain"),
+                                           _vector(pre_bias, t, cols, "pre_bias"), _matrix(y, ts, n, "y"), _matrix(h, t, n, "h"),
+                                           _vector(stats, torch.float32, 4 * n[0], "stats"), _stream_of(f, x, y, h, stats, post_gain, post_bias, pre_gain, pre_bias, gate)))
 
 
 def chimera_op_branch_norm_bwd(f, y, stats, dy, dh, dx, df, post=NORM_NONE, post_gain=None, post_bias=None, pre=NORM_NONE, pre_gain=None, gate=None, alpha=1.0,
@@ -757,18 +760,18 @@ def chimera_op_branch_norm_bwd(f, y, stats, dy, dh, dx, df, post=NORM_NONE, post
     """dx (or None) and df are filled; the parameters' gradients (float, of their shapes, or None) are added to, or overwritten.  y: needed with `pre`; dy (or None)
     and dx of the stream's type.  Allocates the workspace unless one is given, and returns it."""
     import torch
-    stream = next((v for v in (dy, dx, y) if v is not None), f)
-    dt, st, rows, cols, gates = _join(f, stream, gate)
+    stream = dy if dy is not None else dx if dx is not None else y if y is not None else f
+    sizes, gate_at, gates = _join(f, stream, gate)
     t, ts, n, w = f.dtype, stream.dtype, f.shape, torch.float32
+    rows, cols = n
     if workspace is None:
         workspace = torch.empty(lib().chimera_op_branch_norm_bwd_workspace_bytes(rows, cols, gates), dtype=torch.uint8, device=f.device)
-    check(lib().chimera_op_branch_norm_bwd(dt, st, rows, cols, post, pre, alpha, beta, _matrix(f, t, n, "f"), _matrix(y, ts, n, "y"),
-                                           None if gate is None else _matrix(gate, t, gate.shape, "gate"), gates, _vector(post_gain, t, cols, "post_gain"),
-                                           _vector(post_bias, t, cols, "post_bias"), _vector(pre_gain, t, cols, "pre_gain"), _vector(stats, w, 4 * rows, "stats"),
-                                           _matrix(dy, ts, n, "dy"), _matrix(dh, t, n, "dh"), _matrix(dx, ts, n, "dx"), _matrix(df, t, n, "df"),
-                                           _vector(dpost_gain, w, cols, "dpost_gain"), _vector(dpost_bias, w, cols, "dpost_bias"),
+    check(lib().chimera_op_branch_norm_bwd(*sizes, post, pre, alpha, beta, _matrix(f, t, n, "f"), _matrix(y, ts, n, "y"), gate_at, gates,
+                                           _vector(post_gain, t, cols, "post_gain"), _vector(post_bias, t, cols, "post_bias"), _vector(pre_gain, t, cols, "pre_gain"),
+                                           _vector(stats, w, 4 * rows, "stats"), _matrix(dy, ts, n, "dy"), _matrix(dh, t, n, "dh"), _matrix(dx, ts, n, "dx"),
+                                           _matrix(df, t, n, "df"), _vector(dpost_gain, w, cols, "dpost_gain"), _vector(dpost_bias, w, cols, "dpost_bias"),
                                            _vector(dpre_gain, w, cols, "dpre_gain"), _vector(dpre_bias, w, cols, "dpre_bias"),
-                                           None if dgate is None else _matrix(dgate, w, (gates, cols), "dgate"), int(overwrite), workspace.data_ptr(),
+                                           None if dgate is None else _matrix(dgate, w, gate.shape if gates else n, "dgate"), int(overwrite), workspace.data_ptr(),
                                            workspace.numel(), _stream_of(f, y, stats, dy, dh, dx, df, post_gain, post_bias, pre_gain, gate, dpost_gain, dpost_bias,
                                                                          dpre_gain, dpre_bias, dgate, workspace)))
     return workspace

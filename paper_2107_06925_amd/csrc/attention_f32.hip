@@ -45,6 +45,76 @@ __device__ __forceinline__ bool tile_of(int bid, const Shape& sh, int& rank, int
     return p < pairs;
 }
 
+// One row's share of a lane, over the head dimension: columns 8i + 4g .. +3.
+template <int D> struct RowFrag {
+    f32x4 v[D / 8];
+    __device__ __forceinline__ void load(const float* __restrict__ row, int d, int g, bool zero_beyond) {
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) {
+            const int c = 8 * i + 4 * g;
+            v[i] = *reinterpret_cast<const f32x4*>(row + min(c, d - 4));
+            if (zero_beyond && c >= d) v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+    }
+};
+// acc[row of a][row of b] += sum over the head dimension
+template <int D> __device__ __forceinline__ f32x16 dot_rows(const RowFrag<D>& a, const RowFrag<D>& b) {
+    f32x16 acc;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[r] = 0.f;
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[i][j], b.v[i][j], acc, 0, 0, 0);
+    return acc;
+}
+// The transposed operand: lane's column c = 32t + l32 of the 16 rows that its lane group contracts.
+template <int D> struct ColFrag {
+    float v[D / 32][16];
+    __device__ __forceinline__ void load(const float* __restrict__ base, int ld, int row0, int last, int d, int l32, int g) {
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                v[t][r] = base[(size_t)min(row0 + 8 * (r >> 2) + 4 * g + (r & 3), last) * ld + min(t * 32 + l32, d - 1)];
+    }
+};
+template <int D> __device__ __forceinline__ void add_outer(f32x16 (&acc)[D / 32], const ColFrag<D>& a, const f32x16& p) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t) acc[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[t][r], p[r], acc[t], 0, 0, 0);
+}
+
+// Sum of the wavefronts' accumulators [D columns][32 rows], in wavefront order; wavefront w receives
+// the 4 columns 32t + 8w + 4g .. +3 of row l32 in out[t].
+template <int D>
+__device__ __forceinline__ void combine(float* lds, const f32x16 (&acc)[D / 32], f32x4 (&out)[D / 32], int wave, int lane) {
+    constexpr int OT = D / 32;
+#pragma unroll
+    for (int t = 0; t < OT; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) lds[((wave * OT + t) * 16 + r) * WAVE + lane] = acc[t][r];
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < OT; ++t)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            float s = 0.f;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) s += lds[((w * OT + t) * 16 + wave * 4 + c) * WAVE + lane];
+            out[t][c] = s;
+        }
+}
+template <int D>
+__device__ __forceinline__ void store_rows(float* __restrict__ row, const f32x4 (&v)[D / 32], float scale, int d, int wave, int g) {
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t) {
+        const int c = t * 32 + 8 * wave + 4 * g;
+        if (c < d) *reinterpret_cast<f32x4*>(row + c) = v[t] * scale;
+    }
+}
+
 template <int D, bool CAUSAL>
 __global__ __launch_bounds__(NT) void attn_fwd_f32_kernel(const float* __restrict__ qkv, float* __restrict__ ctx,
                                                           float* __restrict__ lse, Shape sh, float scale_log2e) {

@@ -97,29 +97,31 @@ __device__ __forceinline__ bool packed_tile(const int* __restrict__ offsets, int
     return false;
 }
 
-// Workgroup -> slot and unit (a head, or a part of a group).  Workgroups go round-robin over the 8 XCDs; where units divide among them, neighbouring
-// ones, which read the same keys and values, share an XCD and its L2.
-__device__ __forceinline__ void slot_of(int bid, int units, int& slot, int& unit) {
+// Workgroup -> slot and unit (a head, or a part of a group).  Workgroups go round-robin over the 8 XCDs.  Where units divide among them an XCD takes neighbouring
+// ones of every slot; otherwise the `group` units of a slot that read the same keys and values go to one XCD, the next ones to the next.
+__device__ __forceinline__ void slot_of(int bid, int units, int group, int& slot, int& unit) {
+    const int x = bid & 7, j = bid >> 3;
     if (units & 7) {
-        slot = bid / units;
-        unit = bid % units;
+        const int n = j / group * 8 + x, groups = units / group;
+        slot = n / groups;
+        unit = n % groups * group + j % group;
     } else {
-        const int per = units >> 3, j = bid >> 3;
+        const int per = units >> 3;
         slot = j / per;
-        unit = (bid & 7) * per + j % per;
+        unit = x * per + j % per;
     }
 }
 
 // ------------------------------------------------------------------ bf16 forward
 template <int D, bool CAUSAL>
-__global__ __launch_bounds__(NT) void packed_fwd_kernel(PackedArgs a) {
+__global__ __launch_bounds__(NT, D == 64 ? 4 : 2) void packed_fwd_kernel(PackedArgs a) {
     constexpr int KS = D / 16, OT = D / 32;
     __shared__ __attribute__((aligned(16))) bf16_t Ks[2][64 * D];
     __shared__ __attribute__((aligned(16))) bf16_t Vs[2][64 * D];
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, g = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int slot, h, begin, S, at;
-    slot_of((int)blockIdx.x, a.heads, slot, h);
+    slot_of((int)blockIdx.x, a.heads, a.group, slot, h);
     if (!packed_tile<128, CAUSAL>(a.offsets, a.seqs, a.tokens, slot, lane, begin, S, at)) return;
     const int q0 = at * 128, d = a.d;
     const bf16_t* Qg = (const bf16_t*)a.q + (size_t)begin * a.ldq + h * d;
@@ -233,24 +235,36 @@ __global__ __launch_bounds__(NT) void packed_fwd_kernel(PackedArgs a) {
 }
 
 // ----------------------------------------------------------------- bf16 backward
+// A query that sees one key has the probability 1 whatever its score is: its dS is zero, where dP - delta leaves the difference of two sums' roundings.
+template <bool CAUSAL> __device__ __forceinline__ bool sees_one(int S, int query) { return S == 1 || (CAUSAL && query == 0); }
+
 // LDS of one workgroup: two tensors x two stages of [64][D] tiles, and (dK/dV) the statistics of a tile's 64 queries.
 template <int D> struct PackedBwdLds {
     bf16_t t0[2][64 * D], t1[2][64 * D];
     float lse2[2][64], dl[2][64];
 };
 
+// FINE: P and dS, which go into products as bf16, go in as two bf16 numbers, the rounded one and what the rounding took off.  One leaves each term of a sum off by half a
+// step of bf16, as much as the result's own rounding; of many terms and rows that is 1.4 times the error of the rounding alone, of few it can be twice.  It costs half as
+// many matrix instructions again (16384 tokens of 25 heads of 64 in 3 sequences 1526 -> 2038 us), and is taken for few rows (see the host).
+__device__ __forceinline__ bf16x8 pack8_rest(const f32x16& v, int first, const bf16x8& rounded) {
+    bf16x8 o;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = (bf16_t)(v[first + i] - (float)rounded[i]);
+    return o;
+}
+
 // dQ of 128 queries (32 per wavefront), looping over 64-key tiles; forms delta of its queries and leaves it for the dK/dV kernel.
 //   S^T = K Q^T (keys x queries)   P = exp2(S^T c - lse2)   dP^T = V dO^T
 //   dS^T = P (dP^T - delta)        dQ^T += K^T dS^T (then * scale)
-template <int D, bool CAUSAL>
-__global__ __launch_bounds__(NT) void packed_dq_kernel(PackedArgs a) {
+template <int D, bool CAUSAL, bool FORM_DELTA, bool FINE>
+__device__ __forceinline__ void packed_dq(PackedBwdLds<D>& sm, int bid, const PackedArgs& a) {
     constexpr int KS = D / 16, OT = D / 32;
     constexpr unsigned TILE_BYTES = 64 * D * 2;
-    __shared__ __attribute__((aligned(16))) PackedBwdLds<D> sm;
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, g = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int slot, h, begin, S, at;
-    slot_of((int)blockIdx.x, a.heads, slot, h);
+    slot_of(bid, a.heads, a.group, slot, h);
     if (!packed_tile<128, CAUSAL>(a.offsets, a.seqs, a.tokens, slot, lane, begin, S, at)) return;
     const int q0 = at * 128, d = a.d;
     const bf16_t* Qg = (const bf16_t*)a.q + (size_t)begin * a.ldq + h * d;
@@ -278,13 +292,19 @@ __global__ __launch_bounds__(NT) void packed_dq_kernel(PackedArgs a) {
         const bool ok = qrow < S && kk * 16 + g * 8 < d;
         qf[kk] = load_frag(Qg + (size_t)qrow * a.ldq + kk * 16 + g * 8, ok);
         of[kk] = load_frag(dOg + (size_t)qrow * a.lddctx + kk * 16 + g * 8, ok);
-        const bf16x8 cf = load_frag(Og + (size_t)qrow * a.ldctx + kk * 16 + g * 8, ok);
+        if constexpr (FORM_DELTA) {
+            const bf16x8 cf = load_frag(Og + (size_t)qrow * a.ldctx + kk * 16 + g * 8, ok);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) my_dl += (float)of[kk][e] * (float)cf[e];
+            for (int e = 0; e < 8; ++e) my_dl += (float)of[kk][e] * (float)cf[e];
+        }
     }
     const float my_lse2 = qrow < S ? a.lse[stat0 + qrow] * LOG2E : 0.f;
-    my_dl = sum32(my_dl);                                   // lanes l and l ^ 32 hold the whole row
-    if (g == 0 && qrow < S) a.delta[stat0 + qrow] = my_dl;
+    if constexpr (FORM_DELTA) {
+        my_dl = sum32(my_dl);                               // lanes l and l ^ 32 hold the whole row
+        if (g == 0 && qrow < S) a.delta[stat0 + qrow] = my_dl;
+    } else {
+        my_dl = qrow < S ? a.delta[stat0 + qrow] : 0.f;
+    }
     f32x16 dq[OT];
 #pragma unroll
     for (int t = 0; t < OT; ++t)
@@ -318,7 +338,7 @@ __global__ __launch_bounds__(NT) void packed_dq_kernel(PackedArgs a) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int key = k0 + kt * 32 + 8 * (r >> 2) + 4 * g + (r & 3);
-                    if (key >= S || (CAUSAL && key > qrow)) p[r] = 0.f;
+                    if (key >= S || (CAUSAL && key > qrow) || sees_one<CAUSAL>(S, qrow)) p[r] = 0.f;
                 }
             }
 #pragma unroll
@@ -329,6 +349,12 @@ __global__ __launch_bounds__(NT) void packed_dq_kernel(PackedArgs a) {
 #pragma unroll
                 for (int t2 = 0; t2 < OT; ++t2)
                     dq[t2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_ut<D>(Kt, t2 * 32, kt * 2 + j, lane), dsf, dq[t2], 0, 0, 0);
+                if constexpr (FINE) {
+                    const bf16x8 rest = pack8_rest(dp, j * 8, dsf);
+#pragma unroll
+                    for (int t2 = 0; t2 < OT; ++t2)
+                        dq[t2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_ut<D>(Kt, t2 * 32, kt * 2 + j, lane), rest, dq[t2], 0, 0, 0);
+                }
             }
         }
     };
@@ -353,18 +379,17 @@ __global__ __launch_bounds__(NT) void packed_dq_kernel(PackedArgs a) {
 // dK, dV of 128 keys (32 per wavefront), looping over the heads of the group (of this workgroup's part of it) and, in each, over 64-query tiles.
 //   S = Q K^T (queries x keys)   P = exp2(S c - lse2)     dP = dO V^T, started at -delta
 //   dS = P dP                    dV^T += dO^T P           dK^T += Q^T dS (then * scale)
-template <int D, bool CAUSAL>
-__global__ __launch_bounds__(NT) void packed_dkv_kernel(PackedArgs a) {
+template <int D, bool CAUSAL, bool FINE>
+__device__ __forceinline__ void packed_dkv(PackedBwdLds<D>& sm, int bid, const PackedArgs& a) {
     constexpr int KS = D / 16, OT = D / 32;
     constexpr unsigned TILE_BYTES = 64 * D * 2;
-    __shared__ __attribute__((aligned(16))) PackedBwdLds<D> sm;
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, g = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int slot, unit, begin, S, at;
-    slot_of((int)blockIdx.x, a.kv_heads * a.splits, slot, unit);
+    slot_of(bid, a.kv_heads * a.splits, 1, slot, unit);
     if (!packed_tile<128, CAUSAL>(a.offsets, a.seqs, a.tokens, slot, lane, begin, S, at)) return;
     const int kvh = unit / a.splits, part = unit % a.splits, d = a.d;
-    const int h0 = kvh * a.group + part * (a.group / a.splits), hn = a.group / a.splits;
+    const int h0 = kvh * a.group + part * a.group / a.splits, hn = kvh * a.group + (part + 1) * a.group / a.splits - h0;
     const int j0 = ((S + 127) / 128 - 1 - at) * 128;        // the first keys meet the most queries
     const bf16_t* Kg = (const bf16_t*)a.k + (size_t)begin * a.ldk + kvh * d;
     const bf16_t* Vg = (const bf16_t*)a.v + (size_t)begin * a.ldv + kvh * d;
@@ -418,7 +443,7 @@ __global__ __launch_bounds__(NT) void packed_dkv_kernel(PackedArgs a) {
         if (i + 1 < steps) fetch(buf ^ 1);
         const bf16_t* Qt = sm.t0[buf];
         const bf16_t* Ot = sm.t1[buf];
-        if (wj0 >= S || (CAUSAL && i0 + 63 < wj0)) return;           // wavefront-uniform: no key, or none that some query sees
+        if (wj0 >= S || (CAUSAL && i0 + 63 < wj0)) return;       // wavefront-uniform: no key, or none that some query sees
         const bool edge = (i0 + 63 >= S) || (CAUSAL && i0 < wj0 + 31);
 #pragma unroll
         for (int it = 0; it < 2; ++it) {
@@ -451,6 +476,10 @@ __global__ __launch_bounds__(NT) void packed_dkv_kernel(PackedArgs a) {
             }
 #pragma unroll
             for (int r = 0; r < 16; ++r) dp[r] *= p[r];
+            if (edge)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (sees_one<CAUSAL>(S, i0 + it * 32 + 8 * (r >> 2) + 4 * g + (r & 3))) dp[r] = 0.f;
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const int J = it * 2 + j;
@@ -460,6 +489,15 @@ __global__ __launch_bounds__(NT) void packed_dkv_kernel(PackedArgs a) {
                 for (int t2 = 0; t2 < OT; ++t2) {
                     dv[t2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_ut<D>(Ot, t2 * 32, J, lane), pf, dv[t2], 0, 0, 0);
                     dk[t2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_ut<D>(Qt, t2 * 32, J, lane), dsf, dk[t2], 0, 0, 0);
+                }
+                if constexpr (FINE) {
+                    const bf16x8 pr = pack8_rest(p, j * 8, pf);
+                    const bf16x8 dsr = pack8_rest(dp, j * 8, dsf);
+#pragma unroll
+                    for (int t2 = 0; t2 < OT; ++t2) {
+                        dv[t2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_ut<D>(Ot, t2 * 32, J, lane), pr, dv[t2], 0, 0, 0);
+                        dk[t2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_ut<D>(Qt, t2 * 32, J, lane), dsr, dk[t2], 0, 0, 0);
+                    }
                 }
             }
         }
@@ -501,6 +539,49 @@ __global__ __launch_bounds__(NT) void packed_dkv_kernel(PackedArgs a) {
         }
 }
 
+// delta[head, token] = rowsum(dctx ctx), for the two roles in one launch: sixteen lanes take a row of a head, 16 bytes each at a time.
+template <typename T>
+__global__ __launch_bounds__(NT) void packed_delta_kernel(PackedArgs a) {
+    constexpr int V = Elem<T>::VEC;
+    const int first = min(max(a.offsets[0], 0), a.tokens), end = min(max(a.offsets[a.seqs], 0), a.tokens);
+    const size_t n = ((size_t)blockIdx.x * NT + threadIdx.x) / 16, row = n / a.heads;
+    const int h = (int)(n % a.heads), lane = threadIdx.x % 16;
+    const bool live = row >= (size_t)first && row < (size_t)end;
+    float v = 0.f;
+    if (live)
+        for (int c = lane * V; c < a.d; c += 16 * V) {
+            float x[V], y[V];
+            load_vec<T>((const T*)a.ctx + row * a.ldctx + h * a.d + c, x);
+            load_vec<T>((const T*)a.dctx + row * a.lddctx + h * a.d + c, y);
+#pragma unroll
+            for (int e = 0; e < V; ++e) v += x[e] * y[e];
+        }
+    v += dpp<0x128>(v);
+    v += dpp<0x124>(v);
+    v += dpp<0x4e>(v);
+    v += dpp<0xb1>(v);
+    if (live && lane == 0) a.delta[(size_t)h * a.tokens + row] = v;
+}
+
+// The two roles in one launch, dK/dV, whose workgroups last longest, first: the others fill what they leave.
+template <int D, bool CAUSAL, bool FINE>
+__global__ __launch_bounds__(NT) void packed_bwd_kernel(PackedArgs a, int dkv) {
+    __shared__ __attribute__((aligned(16))) PackedBwdLds<D> sm;
+    const int bid = (int)blockIdx.x;
+    if (bid < dkv) packed_dkv<D, CAUSAL, FINE>(sm, bid, a);
+    else packed_dq<D, CAUSAL, false, FINE>(sm, bid - dkv, a);
+}
+template <int D, bool CAUSAL>
+__global__ __launch_bounds__(NT) void packed_dq_kernel(PackedArgs a) {
+    __shared__ __attribute__((aligned(16))) PackedBwdLds<D> sm;
+    packed_dq<D, CAUSAL, true, false>(sm, (int)blockIdx.x, a);
+}
+template <int D, bool CAUSAL>
+__global__ __launch_bounds__(NT) void packed_dkv_kernel(PackedArgs a) {
+    __shared__ __attribute__((aligned(16))) PackedBwdLds<D> sm;
+    packed_dkv<D, CAUSAL, false>(sm, (int)blockIdx.x, a);
+}
+
 // dk, dv = the sums of the parts' slabs, in the order of the parts, over the rows that sequences own.  A thread takes 4 columns of a row.
 template <typename T>
 __global__ __launch_bounds__(NT) void packed_join_kernel(PackedArgs a) {
@@ -524,233 +605,534 @@ __global__ __launch_bounds__(NT) void packed_join_kernel(PackedArgs a) {
     }
 }
 
+// ------------------------------------------------------------------ float tiles
+// v_mfma_f32_16x16x4_f32 takes a float per lane and operand: row (or column) l%16, contraction index l/16, and leaves lane l column l%16 and rows 4 (l/16) + r.  A wavefront
+// holds 16 rows of its own side, a workgroup 64; the other side's tiles of 32 rows lie in LDS, asked for one step ahead.  As in bf16 scores are computed with the
+// tile's rows as result rows, so register r of the four lane groups holds rows {r, 4 + r, 8 + r, 12 + r}, the operand of the next product.  For products over the
+// head dimension lane group g reads columns 16 i + 4 g .. + 3 at once and instruction j contracts {16 i + 4 g + j}.  (With 32 rows a wavefront, 32x32x2 instructions and
+// operands straight from memory the backward had no registers for two wavefronts a SIMD and spilled at head dim 128.)
+// The 16-byte chunk c of row r lies at c ^ (r mod 16), c ^ (r/2 mod 8) in rows of 128 bytes: sixteen rows at one chunk, and four rows at four neighbouring chunks, meet
+// all banks (in rows of 128 bytes the latter meet half of them twice).
+// Compiled for head dims 32, 64, 96 and 128; rows of 96 columns lie 128 apart.
+constexpr int FT = 32;                  // rows of a tile
+template <int D> constexpr int FLD = D > 64 ? 128 : D;
+template <int D> __device__ __forceinline__ int fsw(int row, int chunk) { return D == 32 ? chunk ^ ((row >> 1) & 7) : chunk ^ (row & 15); }
+template <int D>
+__device__ __forceinline__ void dma_ftile(const float* __restrict__ x, int ld, int row0, int row_last, int d, unsigned lds_base, int wave, int lane) {
+    constexpr int CPR = FLD<D> / 4;
+#pragma unroll
+    for (int n0 = 0; n0 < FT * CPR / WAVE; n0 += NW) {
+        const int n = n0 + wave, i = n * WAVE + lane, row = i / CPR;
+        const int col = min(fsw<D>(row, i % CPR), d / 4 - 1) * 4;
+        lds_dma16(x + (size_t)min(row0 + row, row_last) * ld + col, lds_base + n * 1024);
+    }
+}
+// own rows, held in registers: zeros beyond the head's columns
+template <int D> __device__ __forceinline__ void own_rows(f32x4 (&v)[D / 16], const float* __restrict__ row, bool ok, int d, int g) {
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+        v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (ok && 16 * i + 4 * g < d) v[i] = *reinterpret_cast<const f32x4*>(row + 16 * i + 4 * g);
+    }
+}
+// acc[tile's row][own row] += products over the head dimension; the tile's two halves are two chains
+template <int D> __device__ __forceinline__ void over_columns(const float* tile, const f32x4 (&own)[D / 16], f32x4 (&acc)[2], int l16, int g) {
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(tile + l16 * FLD<D> + fsw<D>(l16, 4 * i + g) * 4);
+        const f32x4 y = *reinterpret_cast<const f32x4*>(tile + (16 + l16) * FLD<D> + fsw<D>(16 + l16, 4 * i + g) * 4);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            acc[0] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[j], own[i][j], acc[0], 0, 0, 0);
+            acc[1] = __builtin_amdgcn_mfma_f32_16x16x4f32(y[j], own[i][j], acc[1], 0, 0, 0);
+        }
+    }
+}
+// acc[column][own row] += products over the tile's 16 rows from row0 on
+template <int D> __device__ __forceinline__ void over_rows(const float* tile, int row0, const f32x4& p, f32x4 (&acc)[D / 16], int l16, int g) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int row = row0 + 4 * g + r;
+#pragma unroll
+        for (int t = 0; t < D / 16; ++t) {
+            const int c = 16 * t + l16;
+            acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(tile[row * FLD<D> + fsw<D>(row, c >> 2) * 4 + (c & 3)], p[r], acc[t], 0, 0, 0);
+        }
+    }
+}
+template <int D> __device__ __forceinline__ void store_own(float* __restrict__ row, const f32x4 (&v)[D / 16], float scale, int d, int g) {
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t)
+        if (16 * t + 4 * g < d) *reinterpret_cast<f32x4*>(row + 16 * t + 4 * g) = v[t] * scale;
+}
+// f over lanes l, l ^ 16, l ^ 32, l ^ 48
+template <typename F> __device__ __forceinline__ float fold_groups(float v, F f) {
+    v = fold32(v, f);
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+template <int D> struct PackedLdsF32 {
+    float t0[2][FT * FLD<D>], t1[2][FT * FLD<D>];
+    float lse[2][FT], dl[2][FT];
+};
+
 // ----------------------------------------------------------------- float forward
 template <int D, bool CAUSAL>
 __global__ __launch_bounds__(NT) void packed_fwd_f32_kernel(PackedArgs a) {
-    constexpr int OT = D / 32;
-    __shared__ float lds[NW * OT * 16 * WAVE];
-    __shared__ float stat[2][NW][32];
-    const int lane = threadIdx.x & 63, l32 = lane & 31, g = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    constexpr int KS = D / 16;
+    constexpr unsigned TILE_BYTES = FT * FLD<D> * 4;
+    __shared__ __attribute__((aligned(16))) PackedLdsF32<D> sm;
+    const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int slot, h, begin, S, at;
-    slot_of((int)blockIdx.x, a.heads, slot, h);
-    if (!packed_tile<TILE, CAUSAL>(a.offsets, a.seqs, a.tokens, slot, lane, begin, S, at)) return;
-    const int q0 = at * TILE, d = a.d;
+    slot_of((int)blockIdx.x, a.heads, a.group, slot, h);
+    if (!packed_tile<64, CAUSAL>(a.offsets, a.seqs, a.tokens, slot, lane, begin, S, at)) return;
+    const int q0 = at * 64, d = a.d, wq0 = q0 + wave * 16, qrow = wq0 + l16;
     const float* Qg = (const float*)a.q + (size_t)begin * a.ldq + h * d;
     const float* Kg = (const float*)a.k + (size_t)begin * a.ldk + h / a.group * d;
     const float* Vg = (const float*)a.v + (size_t)begin * a.ldv + h / a.group * d;
     const float scale_log2e = a.scale * LOG2E;
-    const int qrow = q0 + l32;
-    RowFrag<D> q;
-    q.load(Qg + (size_t)min(qrow, S - 1) * a.ldq, d, g, true);
-    f32x16 o[OT];
+    const unsigned ks0 = lds_address(sm.t0), vs0 = lds_address(sm.t1);
+    const int ntiles = ((CAUSAL ? min(S, q0 + 64) : S) + FT - 1) / FT;
+    auto fetch = [&](int t, int buf) {
+        dma_ftile<D>(Kg, a.ldk, t * FT, S - 1, d, ks0 + buf * TILE_BYTES, wave, lane);
+        dma_ftile<D>(Vg, a.ldv, t * FT, S - 1, d, vs0 + buf * TILE_BYTES, wave, lane);
+    };
+    fetch(0, 0);
+    f32x4 q[KS], o[KS];
+    own_rows<D>(q, Qg + (size_t)qrow * a.ldq, qrow < S, d, g);
 #pragma unroll
-    for (int t = 0; t < OT; ++t)
+    for (int t = 0; t < KS; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = NEG_BIG, lsum = 0.f;                              // lsum: over this lane's quarter of the keys
+    auto step = [&](int t, auto buf_c) {
+        constexpr int buf = decltype(buf_c)::value;
+        const int k0 = t * FT;
+        wait_vmcnt<0>();
+        __syncthreads();
+        if (t + 1 < ntiles) fetch(t + 1, buf ^ 1);
+        if (wq0 >= S || (CAUSAL && k0 > wq0 + 15)) return;
+        f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+        over_columns<D>(sm.t0[buf], q, s, l16, g);
+        if (k0 + FT > S || (CAUSAL && k0 + FT - 1 > wq0)) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) o[t][r] = 0.f;
-    float m = NEG_BIG, lsum = 0.f;
-    const int kend = CAUSAL ? min(S, q0 + TILE) : S;
-    for (int k0 = wave * TILE; k0 < kend; k0 += NW * TILE) {
-        RowFrag<D> k;
-        ColFrag<D> v;
-        k.load(Kg + (size_t)min(k0 + l32, S - 1) * a.ldk, d, g, false);
-        v.load(Vg, a.ldv, k0, S - 1, d, l32, g);
-        f32x16 s = dot_rows<D>(k, q);
-        if (k0 + TILE > S || (CAUSAL && k0 + TILE - 1 > q0)) {
+            for (int rt = 0; rt < 2; ++rt)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int key = k0 + 8 * (r >> 2) + 4 * g + (r & 3);
-                if (key >= S || (CAUSAL && key > qrow)) s[r] = NEG_BIG;
+                for (int r = 0; r < 4; ++r) {
+                    const int key = k0 + rt * 16 + 4 * g + r;
+                    if (key >= S || (CAUSAL && key > qrow)) s[rt][r] = NEG_BIG;
+                }
+        }
+        float mx = NEG_BIG;
+#pragma unroll
+        for (int rt = 0; rt < 2; ++rt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) mx = fmaxf(mx, s[rt][r]);
+        const float m_new = fmaxf(m, fold_groups(mx, [](float x, float y) { return fmaxf(x, y); }) * scale_log2e), alpha = __builtin_amdgcn_exp2f(m - m_new);
+        lsum *= alpha;
+#pragma unroll
+        for (int rt = 0; rt < 2; ++rt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                s[rt][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][r], scale_log2e, -m_new));
+                lsum += s[rt][r];
             }
-        }
-        float mx = s[0];
-#pragma unroll
-        for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
-        mx = max32(mx) * scale_log2e;
-        const float m_new = fmaxf(m, mx), alpha = __builtin_amdgcn_exp2f(m - m_new);
-        float rs = 0.f;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], scale_log2e, -m_new));
-            rs += s[r];
-        }
-        lsum = lsum * alpha + sum32(rs);
         m = m_new;
 #pragma unroll
-        for (int t = 0; t < OT; ++t)
+        for (int t2 = 0; t2 < KS; ++t2) o[t2] *= alpha;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) o[t][r] *= alpha;
-        add_outer<D>(o, v, s);
+        for (int rt = 0; rt < 2; ++rt) over_rows<D>(sm.t1[buf], rt * 16, s[rt], o, l16, g);
+    };
+    for (int t = 0; t < ntiles; t += 2) {
+        step(t, std::integral_constant<int, 0>{});
+        if (t + 1 < ntiles) step(t + 1, std::integral_constant<int, 1>{});
     }
-    // the wavefronts' partial softmaxes: common maximum, rescaled sums
-    if (g == 0) { stat[0][wave][l32] = m; stat[1][wave][l32] = lsum; }
-    __syncthreads();
-    float M = stat[0][0][l32];
-#pragma unroll
-    for (int w = 1; w < NW; ++w) M = fmaxf(M, stat[0][w][l32]);
-    float total = 0.f;
-#pragma unroll
-    for (int w = 0; w < NW; ++w) total += stat[1][w][l32] * __builtin_amdgcn_exp2f(stat[0][w][l32] - M);
-    const float mine = __builtin_amdgcn_exp2f(m - M);           // 0 for a wavefront that saw no key
-#pragma unroll
-    for (int t = 0; t < OT; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[t][r] *= mine;
-    f32x4 out[OT];
-    combine<D>(lds, o, out, wave, lane);
-    if (qrow < S) {
-        store_rows<D>((float*)a.ctx + (size_t)(begin + qrow) * a.ldctx + h * d, out, 1.0f / total, d, wave, g);
-        if (wave == 0 && g == 0) a.lse[(size_t)h * a.tokens + begin + qrow] = __builtin_fmaf(M, LN2, __builtin_fmaf(M, LN2_LOW, logf(total)));
-    }
+    lsum = fold_groups(lsum, [](float x, float y) { return x + y; });
+    if (qrow >= S) return;
+    store_own<D>((float*)a.ctx + (size_t)(begin + qrow) * a.ldctx + h * d, o, 1.0f / lsum, d, g);
+    if (g == 0) a.lse[(size_t)h * a.tokens + begin + qrow] = __builtin_fmaf(m, LN2, __builtin_fmaf(m, LN2_LOW, logf(lsum)));
 }
 
 // ---------------------------------------------------------------- float backward
-// dQ of 32 queries; delta = rowsum(dO * O) of the queries on the way.
+// dQ of 64 queries, looping over 32-key tiles.
 template <int D, bool CAUSAL>
-__device__ __forceinline__ void packed_dq_f32(float* lds, int bid, const PackedArgs& a) {
-    constexpr int OT = D / 32;
-    const int lane = threadIdx.x & 63, l32 = lane & 31, g = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+__device__ __forceinline__ void packed_dq_f32(PackedLdsF32<D>& sm, int bid, const PackedArgs& a) {
+    constexpr int KS = D / 16;
+    constexpr unsigned TILE_BYTES = FT * FLD<D> * 4;
+    const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int slot, h, begin, S, at;
-    slot_of(bid, a.heads, slot, h);
-    if (!packed_tile<TILE, CAUSAL>(a.offsets, a.seqs, a.tokens, slot, lane, begin, S, at)) return;
-    const int q0 = at * TILE, d = a.d;
+    slot_of(bid, a.heads, a.group, slot, h);
+    if (!packed_tile<64, CAUSAL>(a.offsets, a.seqs, a.tokens, slot, lane, begin, S, at)) return;
+    const int q0 = at * 64, d = a.d, wq0 = q0 + wave * 16, qrow = wq0 + l16;
     const float* Kg = (const float*)a.k + (size_t)begin * a.ldk + h / a.group * d;
     const float* Vg = (const float*)a.v + (size_t)begin * a.ldv + h / a.group * d;
-    const int qrow = q0 + l32;
-    const size_t qr = (size_t)begin + min(qrow, S - 1);
-    RowFrag<D> q, dO, o;
-    q.load((const float*)a.q + qr * a.ldq + h * d, d, g, true);
-    dO.load((const float*)a.dctx + qr * a.lddctx + h * d, d, g, true);
-    o.load((const float*)a.ctx + qr * a.ldctx + h * d, d, g, true);
-    const float my_lse = a.lse[(size_t)h * a.tokens + qr];
-    float delta = 0.f;
+    const unsigned ks0 = lds_address(sm.t0), vs0 = lds_address(sm.t1);
+    const int ntiles = ((CAUSAL ? min(S, q0 + 64) : S) + FT - 1) / FT;
+    auto fetch = [&](int t, int buf) {
+        dma_ftile<D>(Kg, a.ldk, t * FT, S - 1, d, ks0 + buf * TILE_BYTES, wave, lane);
+        dma_ftile<D>(Vg, a.ldv, t * FT, S - 1, d, vs0 + buf * TILE_BYTES, wave, lane);
+    };
+    fetch(0, 0);
+    const size_t row = (size_t)begin + min(qrow, S - 1), stat = (size_t)h * a.tokens + row;
+    f32x4 q[KS], dO[KS], dq[KS];
+    own_rows<D>(q, (const float*)a.q + row * a.ldq + h * d, qrow < S, d, g);
+    own_rows<D>(dO, (const float*)a.dctx + row * a.lddctx + h * d, qrow < S, d, g);
+    const float my_lse = a.lse[stat], my_dl = -a.delta[stat];
 #pragma unroll
-    for (int i = 0; i < D / 8; ++i)
+    for (int t = 0; t < KS; ++t) dq[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto step = [&](int t, auto buf_c) {
+        constexpr int buf = decltype(buf_c)::value;
+        const int k0 = t * FT;
+        wait_vmcnt<0>();
+        __syncthreads();
+        if (t + 1 < ntiles) fetch(t + 1, buf ^ 1);
+        if (wq0 >= S || (CAUSAL && k0 > wq0 + 15)) return;
+        const bool edge = k0 + FT > S || (CAUSAL && k0 + FT - 1 > wq0);
+        f32x4 p[2], dp[2];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) delta += dO.v[i][j] * o.v[i][j];
-    delta = sum32(delta);
-    f32x16 dq[OT];
+        for (int rt = 0; rt < 2; ++rt) { p[rt] = f32x4{0.f, 0.f, 0.f, 0.f}; dp[rt] = f32x4{my_dl, my_dl, my_dl, my_dl}; }
+        over_columns<D>(sm.t0[buf], q, p, l16, g);
+        over_columns<D>(sm.t1[buf], dO, dp, l16, g);
 #pragma unroll
-    for (int t = 0; t < OT; ++t)
+        for (int rt = 0; rt < 2; ++rt) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) dq[t][r] = 0.f;
-    const int kend = CAUSAL ? min(S, q0 + TILE) : S;
-    for (int k0 = wave * TILE; k0 < kend; k0 += NW * TILE) {
-        RowFrag<D> k, v;
-        ColFrag<D> kt;
-        const size_t kr = (size_t)min(k0 + l32, S - 1);
-        k.load(Kg + kr * a.ldk, d, g, false);
-        v.load(Vg + kr * a.ldv, d, g, false);
-        kt.load(Kg, a.ldk, k0, S - 1, d, l32, g);
-        f32x16 p = dot_rows<D>(k, q), dp = dot_rows<D>(v, dO);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) p[r] = prob(p[r], a.scale, my_lse);
-        if (k0 + TILE > S || (CAUSAL && k0 + TILE - 1 > q0)) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int key = k0 + 8 * (r >> 2) + 4 * g + (r & 3);
-                if (key >= S || (CAUSAL && key > qrow)) p[r] = 0.f;
+            for (int r = 0; r < 4; ++r) {
+                const int key = k0 + rt * 16 + 4 * g + r;
+                float v = prob(p[rt][r], a.scale, my_lse);
+                if (edge && (key >= S || (CAUSAL && key > qrow) || sees_one<CAUSAL>(S, qrow))) v = 0.f;
+                dp[rt][r] *= v;
             }
+            over_rows<D>(sm.t0[buf], rt * 16, dp[rt], dq, l16, g);
         }
-#pragma unroll
-        for (int r = 0; r < 16; ++r) dp[r] = p[r] * (dp[r] - delta);
-        add_outer<D>(dq, kt, dp);
+    };
+    for (int t = 0; t < ntiles; t += 2) {
+        step(t, std::integral_constant<int, 0>{});
+        if (t + 1 < ntiles) step(t + 1, std::integral_constant<int, 1>{});
     }
-    f32x4 out[OT];
-    combine<D>(lds, dq, out, wave, lane);
-    if (qrow < S) store_rows<D>((float*)a.dq + qr * a.lddq + h * d, out, a.scale, d, wave, g);
+    if (qrow < S) store_own<D>((float*)a.dq + row * a.lddq + h * d, dq, a.scale, d, g);
 }
 
-// dK, dV of 32 keys; the wavefronts deal the (head, tile of queries) pairs of the part among themselves.
+// dK, dV of 64 keys, looping over the heads of the part and, in each, over 32-query tiles.
 template <int D, bool CAUSAL>
-__device__ __forceinline__ void packed_dkv_f32(float* lds, int bid, const PackedArgs& a) {
-    constexpr int OT = D / 32;
-    const int lane = threadIdx.x & 63, l32 = lane & 31, g = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+__device__ __forceinline__ void packed_dkv_f32(PackedLdsF32<D>& sm, int bid, const PackedArgs& a) {
+    constexpr int KS = D / 16;
+    constexpr unsigned TILE_BYTES = FT * FLD<D> * 4;
+    const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int slot, unit, begin, S, at;
-    slot_of(bid, a.kv_heads * a.splits, slot, unit);
-    if (!packed_tile<TILE, CAUSAL>(a.offsets, a.seqs, a.tokens, slot, lane, begin, S, at)) return;
+    slot_of(bid, a.kv_heads * a.splits, 1, slot, unit);
+    if (!packed_tile<64, CAUSAL>(a.offsets, a.seqs, a.tokens, slot, lane, begin, S, at)) return;
     const int kvh = unit / a.splits, part = unit % a.splits, d = a.d;
-    const int h0 = kvh * a.group + part * (a.group / a.splits), hn = a.group / a.splits;
-    const int j0 = ((S + TILE - 1) / TILE - 1 - at) * TILE;          // the first keys meet the most queries
-    const int jrow = j0 + l32;
-    const size_t jr = (size_t)begin + min(jrow, S - 1);
-    RowFrag<D> k, v;
-    k.load((const float*)a.k + jr * a.ldk + kvh * d, d, g, true);
-    v.load((const float*)a.v + jr * a.ldv + kvh * d, d, g, true);
-    f32x16 dk[OT], dv[OT];
-#pragma unroll
-    for (int t = 0; t < OT; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) { dk[t][r] = 0.f; dv[t][r] = 0.f; }
-    const int first = CAUSAL ? j0 : 0, tiles = (S - first + TILE - 1) / TILE;
-    int h = h0, i0 = first + wave * TILE;
-    for (int n = wave; n < tiles * hn; n += NW, i0 += NW * TILE) {
-        while (i0 >= first + tiles * TILE) { i0 -= tiles * TILE; ++h; }
-        const int ir = min(i0 + l32, S - 1);
-        const size_t qr = (size_t)begin + ir;
-        RowFrag<D> q, dO, o;
-        ColFrag<D> qt, dOt;
-        q.load((const float*)a.q + qr * a.ldq + h * d, d, g, false);
-        dO.load((const float*)a.dctx + qr * a.lddctx + h * d, d, g, true);
-        o.load((const float*)a.ctx + qr * a.ldctx + h * d, d, g, true);
-        dOt.load((const float*)a.dctx + (size_t)begin * a.lddctx + h * d, a.lddctx, i0, S - 1, d, l32, g);
-        qt.load((const float*)a.q + (size_t)begin * a.ldq + h * d, a.ldq, i0, S - 1, d, l32, g);
-        const float my_lse = a.lse[(size_t)h * a.tokens + qr];
-        float delta = 0.f;                       // of row l32; the rows of the score registers fetch theirs from its lane
-#pragma unroll
-        for (int i = 0; i < D / 8; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) delta += dO.v[i][j] * o.v[i][j];
-        delta = sum32(delta);
-        f32x16 p = dot_rows<D>(q, k), dp = dot_rows<D>(dO, v);
-        const bool edge = i0 + TILE > S || (CAUSAL && i0 < j0 + TILE - 1);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int ii = 8 * (r >> 2) + 4 * g + (r & 3);
-            p[r] = prob(p[r], a.scale, __shfl(my_lse, ii, WAVE));
-            if (edge && (i0 + ii >= S || (CAUSAL && i0 + ii < jrow))) p[r] = 0.f;
-            dp[r] = p[r] * (dp[r] - __shfl(delta, ii, WAVE));
+    const int h0 = kvh * a.group + part * a.group / a.splits, hn = kvh * a.group + (part + 1) * a.group / a.splits - h0;
+    const int j0 = ((S + 63) / 64 - 1 - at) * 64;               // the first keys meet the most queries
+    const int wj0 = j0 + wave * 16, jrow = wj0 + l16;
+    const float* Qg = (const float*)a.q + (size_t)begin * a.ldq + h0 * d;
+    const float* dOg = (const float*)a.dctx + (size_t)begin * a.lddctx + h0 * d;
+    const float* lse = a.lse + (size_t)h0 * a.tokens + begin;
+    const float* delta = a.delta + (size_t)h0 * a.tokens + begin;
+    const unsigned qs0 = lds_address(sm.t0), os0 = lds_address(sm.t1);
+    const int qt0 = CAUSAL ? j0 / FT : 0, qtn = (S + FT - 1) / FT, steps = (qtn - qt0) * hn;
+    float stat = 0.f;                      // lse (threads 0..31) or -delta (threads 32..63) of the next tile
+    int next_t = qt0, next_h = 0;          // the tile to be fetched
+    auto fetch = [&](int buf) {
+        const int i0 = next_t * FT;
+        dma_ftile<D>(Qg + next_h * d, a.ldq, i0, S - 1, d, qs0 + buf * TILE_BYTES, wave, lane);
+        dma_ftile<D>(dOg + next_h * d, a.lddctx, i0, S - 1, d, os0 + buf * TILE_BYTES, wave, lane);
+        if (tid < 2 * FT) {
+            const int i = i0 + (tid & (FT - 1));
+            const size_t s = (size_t)next_h * a.tokens + i;
+            stat = i < S ? (tid < FT ? lse[s] : -delta[s]) : 0.f;
         }
-        add_outer<D>(dv, dOt, p);
-        add_outer<D>(dk, qt, dp);
+        if (++next_t == qtn) { next_t = qt0; ++next_h; }
+    };
+    fetch(0);
+    const size_t row = (size_t)begin + min(jrow, S - 1);
+    f32x4 k[KS], v[KS], dk[KS], dv[KS];
+    own_rows<D>(k, (const float*)a.k + row * a.ldk + kvh * d, jrow < S, d, g);
+    own_rows<D>(v, (const float*)a.v + row * a.ldv + kvh * d, jrow < S, d, g);
+#pragma unroll
+    for (int t = 0; t < KS; ++t) { dk[t] = f32x4{0.f, 0.f, 0.f, 0.f}; dv[t] = dk[t]; }
+    int t = qt0;                           // the tile of the step
+    auto step = [&](int i, auto buf_c) {
+        constexpr int buf = decltype(buf_c)::value;
+        const int i0 = t * FT;
+        if (++t == qtn) t = qt0;
+        wait_vmcnt<0>();
+        if (tid < FT) sm.lse[buf][tid] = stat;
+        else if (tid < 2 * FT) sm.dl[buf][tid - FT] = stat;
+        __syncthreads();
+        if (i + 1 < steps) fetch(buf ^ 1);
+        if (wj0 >= S || (CAUSAL && i0 + FT - 1 < wj0)) return;
+        const bool edge = i0 + FT > S || (CAUSAL && i0 < wj0 + 15);
+        f32x4 p[2], dp[2];
+#pragma unroll
+        for (int rt = 0; rt < 2; ++rt) { p[rt] = f32x4{0.f, 0.f, 0.f, 0.f}; dp[rt] = *reinterpret_cast<const f32x4*>(&sm.dl[buf][rt * 16 + 4 * g]); }
+        over_columns<D>(sm.t0[buf], k, p, l16, g);
+        over_columns<D>(sm.t1[buf], v, dp, l16, g);
+#pragma unroll
+        for (int rt = 0; rt < 2; ++rt) {
+            const f32x4 l = *reinterpret_cast<const f32x4*>(&sm.lse[buf][rt * 16 + 4 * g]);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int q = i0 + rt * 16 + 4 * g + r;
+                p[rt][r] = prob(p[rt][r], a.scale, l[r]);
+                if (edge && (q >= S || (CAUSAL && q < jrow))) p[rt][r] = 0.f;
+                dp[rt][r] *= edge && sees_one<CAUSAL>(S, q) ? 0.f : p[rt][r];
+            }
+            over_rows<D>(sm.t1[buf], rt * 16, p[rt], dv, l16, g);
+            over_rows<D>(sm.t0[buf], rt * 16, dp[rt], dk, l16, g);
+        }
+    };
+    for (int i = 0; i < steps; i += 2) {
+        step(i, std::integral_constant<int, 0>{});
+        if (i + 1 < steps) step(i + 1, std::integral_constant<int, 1>{});
     }
+    if (jrow >= S) return;
     const size_t width = (size_t)a.kv_heads * d, slab = (size_t)a.tokens * width;
-    float* dko = a.splits > 1 ? a.slabs + (size_t)part * 2 * slab + jr * width + kvh * d : (float*)a.dk + jr * a.lddk + kvh * d;
-    float* dvo = a.splits > 1 ? a.slabs + (size_t)part * 2 * slab + slab + jr * width + kvh * d : (float*)a.dv + jr * a.lddv + kvh * d;
-    f32x4 out[OT];
-    combine<D>(lds, dv, out, wave, lane);
-    if (jrow < S) store_rows<D>(dvo, out, 1.0f, d, wave, g);
-    __syncthreads();                             // everyone has read the dV sums
-    combine<D>(lds, dk, out, wave, lane);
-    if (jrow < S) store_rows<D>(dko, out, a.scale, d, wave, g);
+    store_own<D>(a.splits > 1 ? a.slabs + (size_t)part * 2 * slab + row * width + kvh * d : (float*)a.dk + row * a.lddk + kvh * d, dk, a.scale, d, g);
+    store_own<D>(a.splits > 1 ? a.slabs + (size_t)part * 2 * slab + slab + row * width + kvh * d : (float*)a.dv + row * a.lddv + kvh * d, dv, 1.0f, d, g);
 }
 
-// Both roles in one launch, the longer one first; each forms the delta it needs.
 template <int D, bool CAUSAL>
 __global__ __launch_bounds__(NT) void packed_bwd_f32_kernel(PackedArgs a, int dkv) {
-    __shared__ float lds[NW * (D / 32) * 16 * WAVE];
+    __shared__ __attribute__((aligned(16))) PackedLdsF32<D> sm;
     const int bid = (int)blockIdx.x;
-    if (bid < dkv) packed_dkv_f32<D, CAUSAL>(lds, bid, a);
-    else packed_dq_f32<D, CAUSAL>(lds, bid - dkv, a);
+    if (bid < dkv) packed_dkv_f32<D, CAUSAL>(sm, bid, a);
+    else packed_dq_f32<D, CAUSAL>(sm, bid - dkv, a);
+}
+
+// ------------------------------------------------------- float, few workgroups
+// Where 64 own rows a workgroup leave CUs without one, the four wavefronts share 16 own rows and deal the other side's tiles among themselves, each with a place in LDS of its
+// own and no barrier in the loop; their sums meet at the end, in their order.
+template <int D> struct PackedFewLds {
+    float t0[NW][FT * FLD<D>], t1[NW][FT * FLD<D>];
+    float stat[2][NW][16];
+};
+template <int D>
+__device__ __forceinline__ void dma_few(const float* __restrict__ x, int ld, int row0, int row_last, int d, unsigned lds_base, int lane) {
+    constexpr int CPR = FLD<D> / 4;
+#pragma unroll
+    for (int n = 0; n < FT * CPR / WAVE; ++n) {
+        const int i = n * WAVE + lane, row = i / CPR;
+        const int col = min(fsw<D>(row, i % CPR), d / 4 - 1) * 4;
+        lds_dma16(x + (size_t)min(row0 + row, row_last) * ld + col, lds_base + n * 1024);
+    }
+}
+// the wavefront's reads of its last tile are done before the next one is asked for
+__device__ __forceinline__ void wait_lds_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+// Sums over the wavefronts, in their order, of acc; wavefront w stores columns 16 t .. + 15 with t mod 4 = w.  `lds`: 4 x D x 16 floats that nobody reads any more.
+template <int D> __device__ __forceinline__ void store_few(float* lds, const f32x4 (&acc)[D / 16], float* __restrict__ row, bool ok, float scale, int d, int wave, int lane) {
+    constexpr int KS = D / 16;
+#pragma unroll
+    for (int t = 0; t < KS; ++t) *reinterpret_cast<f32x4*>(lds + ((wave * KS + t) * WAVE + lane) * 4) = acc[t];
+    __syncthreads();
+    const int g = lane >> 4;
+#pragma unroll
+    for (int t0 = 0; t0 < KS; t0 += NW) {
+        const int t = t0 + wave;
+        if (t >= KS || !ok || 16 * t + 4 * g >= d) continue;
+        f32x4 v = *reinterpret_cast<const f32x4*>(lds + (t * WAVE + lane) * 4);
+#pragma unroll
+        for (int w = 1; w < NW; ++w) v += *reinterpret_cast<const f32x4*>(lds + ((w * KS + t) * WAVE + lane) * 4);
+        *reinterpret_cast<f32x4*>(row + 16 * t + 4 * g) = v * scale;
+    }
+}
+
+template <int D, bool CAUSAL>
+__global__ __launch_bounds__(NT) void packed_fwd_few_kernel(PackedArgs a) {
+    constexpr int KS = D / 16;
+    __shared__ __attribute__((aligned(16))) PackedFewLds<D> sm;
+    const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int slot, h, begin, S, at;
+    slot_of((int)blockIdx.x, a.heads, a.group, slot, h);
+    if (!packed_tile<16, CAUSAL>(a.offsets, a.seqs, a.tokens, slot, lane, begin, S, at)) return;
+    const int q0 = at * 16, d = a.d, qrow = q0 + l16;
+    const float* Kg = (const float*)a.k + (size_t)begin * a.ldk + h / a.group * d;
+    const float* Vg = (const float*)a.v + (size_t)begin * a.ldv + h / a.group * d;
+    const float scale_log2e = a.scale * LOG2E;
+    const unsigned ks0 = lds_address(sm.t0[wave]), vs0 = lds_address(sm.t1[wave]);
+    const size_t row = (size_t)begin + min(qrow, S - 1);
+    f32x4 q[KS], o[KS];
+    own_rows<D>(q, (const float*)a.q + row * a.ldq + h * d, qrow < S, d, g);
+#pragma unroll
+    for (int t = 0; t < KS; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = NEG_BIG, lsum = 0.f;
+    const int kend = CAUSAL ? min(S, q0 + 16) : S;
+    for (int k0 = wave * FT; k0 < kend; k0 += NW * FT) {
+        wait_lds_reads();
+        dma_few<D>(Kg, a.ldk, k0, S - 1, d, ks0, lane);
+        dma_few<D>(Vg, a.ldv, k0, S - 1, d, vs0, lane);
+        wait_vmcnt<0>();
+        f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+        over_columns<D>(sm.t0[wave], q, s, l16, g);
+        float mx = NEG_BIG;
+#pragma unroll
+        for (int rt = 0; rt < 2; ++rt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int key = k0 + rt * 16 + 4 * g + r;
+                if (key >= S || (CAUSAL && key > qrow)) s[rt][r] = NEG_BIG;
+                mx = fmaxf(mx, s[rt][r]);
+            }
+        const float m_new = fmaxf(m, fold_groups(mx, [](float x, float y) { return fmaxf(x, y); }) * scale_log2e), alpha = __builtin_amdgcn_exp2f(m - m_new);
+        lsum *= alpha;
+#pragma unroll
+        for (int rt = 0; rt < 2; ++rt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                s[rt][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][r], scale_log2e, -m_new));
+                lsum += s[rt][r];
+            }
+        m = m_new;
+#pragma unroll
+        for (int t2 = 0; t2 < KS; ++t2) o[t2] *= alpha;
+#pragma unroll
+        for (int rt = 0; rt < 2; ++rt) over_rows<D>(sm.t1[wave], rt * 16, s[rt], o, l16, g);
+    }
+    // the wavefronts' partial softmaxes: common maximum, rescaled sums
+    lsum = fold_groups(lsum, [](float x, float y) { return x + y; });
+    if (g == 0) { sm.stat[0][wave][l16] = m; sm.stat[1][wave][l16] = lsum; }
+    __syncthreads();                                            // (and every tile has been read)
+    float M = sm.stat[0][0][l16];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) M = fmaxf(M, sm.stat[0][w][l16]);
+    float total = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) total += sm.stat[1][w][l16] * __builtin_amdgcn_exp2f(sm.stat[0][w][l16] - M);
+    const float mine = __builtin_amdgcn_exp2f(m - M);           // 0 for a wavefront that saw no key
+#pragma unroll
+    for (int t = 0; t < KS; ++t) o[t] *= mine;
+    store_few<D>(sm.t0[0], o, (float*)a.ctx + row * a.ldctx + h * d, qrow < S, 1.0f / total, d, wave, lane);
+    if (wave == 0 && g == 0 && qrow < S) a.lse[(size_t)h * a.tokens + row] = __builtin_fmaf(M, LN2, __builtin_fmaf(M, LN2_LOW, logf(total)));
+}
+
+template <int D, bool CAUSAL>
+__device__ __forceinline__ void packed_dq_few(PackedFewLds<D>& sm, int bid, const PackedArgs& a) {
+    constexpr int KS = D / 16;
+    const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int slot, h, begin, S, at;
+    slot_of(bid, a.heads, a.group, slot, h);
+    if (!packed_tile<16, CAUSAL>(a.offsets, a.seqs, a.tokens, slot, lane, begin, S, at)) return;
+    const int q0 = at * 16, d = a.d, qrow = q0 + l16;
+    const float* Kg = (const float*)a.k + (size_t)begin * a.ldk + h / a.group * d;
+    const float* Vg = (const float*)a.v + (size_t)begin * a.ldv + h / a.group * d;
+    const unsigned ks0 = lds_address(sm.t0[wave]), vs0 = lds_address(sm.t1[wave]);
+    const size_t row = (size_t)begin + min(qrow, S - 1), stat = (size_t)h * a.tokens + row;
+    f32x4 q[KS], dO[KS], dq[KS];
+    own_rows<D>(q, (const float*)a.q + row * a.ldq + h * d, qrow < S, d, g);
+    own_rows<D>(dO, (const float*)a.dctx + row * a.lddctx + h * d, qrow < S, d, g);
+    const float my_lse = a.lse[stat], my_dl = -a.delta[stat];
+#pragma unroll
+    for (int t = 0; t < KS; ++t) dq[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int kend = CAUSAL ? min(S, q0 + 16) : S;
+    for (int k0 = wave * FT; k0 < kend; k0 += NW * FT) {
+        wait_lds_reads();
+        dma_few<D>(Kg, a.ldk, k0, S - 1, d, ks0, lane);
+        dma_few<D>(Vg, a.ldv, k0, S - 1, d, vs0, lane);
+        wait_vmcnt<0>();
+        f32x4 p[2], dp[2];
+#pragma unroll
+        for (int rt = 0; rt < 2; ++rt) { p[rt] = f32x4{0.f, 0.f, 0.f, 0.f}; dp[rt] = f32x4{my_dl, my_dl, my_dl, my_dl}; }
+        over_columns<D>(sm.t0[wave], q, p, l16, g);
+        over_columns<D>(sm.t1[wave], dO, dp, l16, g);
+#pragma unroll
+        for (int rt = 0; rt < 2; ++rt) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int key = k0 + rt * 16 + 4 * g + r;
+                dp[rt][r] *= key >= S || (CAUSAL && key > qrow) || sees_one<CAUSAL>(S, qrow) ? 0.f : prob(p[rt][r], a.scale, my_lse);
+            }
+            over_rows<D>(sm.t0[wave], rt * 16, dp[rt], dq, l16, g);
+        }
+    }
+    __syncthreads();                                            // every tile has been read
+    store_few<D>(sm.t0[0], dq, (float*)a.dq + row * a.lddq + h * d, qrow < S, a.scale, d, wave, lane);
+}
+
+template <int D, bool CAUSAL>
+__device__ __forceinline__ void packed_dkv_few(PackedFewLds<D>& sm, int bid, const PackedArgs& a) {
+    constexpr int KS = D / 16;
+    const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int slot, unit, begin, S, at;
+    slot_of(bid, a.kv_heads * a.splits, 1, slot, unit);
+    if (!packed_tile<16, CAUSAL>(a.offsets, a.seqs, a.tokens, slot, lane, begin, S, at)) return;
+    const int kvh = unit / a.splits, part = unit % a.splits, d = a.d;
+    const int h0 = kvh * a.group + part * a.group / a.splits, hn = kvh * a.group + (part + 1) * a.group / a.splits - h0;
+    const int j0 = ((S + 15) / 16 - 1 - at) * 16, jrow = j0 + l16;
+    const float* Qg = (const float*)a.q + (size_t)begin * a.ldq + h0 * d;
+    const float* dOg = (const float*)a.dctx + (size_t)begin * a.lddctx + h0 * d;
+    const float* lse = a.lse + (size_t)h0 * a.tokens + begin;
+    const float* delta = a.delta + (size_t)h0 * a.tokens + begin;
+    const unsigned qs0 = lds_address(sm.t0[wave]), os0 = lds_address(sm.t1[wave]);
+    const size_t row = (size_t)begin + min(jrow, S - 1);
+    f32x4 k[KS], v[KS], dk[KS], dv[KS];
+    own_rows<D>(k, (const float*)a.k + row * a.ldk + kvh * d, jrow < S, d, g);
+    own_rows<D>(v, (const float*)a.v + row * a.ldv + kvh * d, jrow < S, d, g);
+#pragma unroll
+    for (int t = 0; t < KS; ++t) { dk[t] = f32x4{0.f, 0.f, 0.f, 0.f}; dv[t] = dk[t]; }
+    const int qt0 = CAUSAL ? j0 / FT : 0, tiles = (S + FT - 1) / FT - qt0;
+    for (int n = wave; n < tiles * hn; n += NW) {
+        const int h = n / tiles, i0 = (qt0 + n % tiles) * FT;
+        wait_lds_reads();
+        dma_few<D>(Qg + h * d, a.ldq, i0, S - 1, d, qs0, lane);
+        dma_few<D>(dOg + h * d, a.lddctx, i0, S - 1, d, os0, lane);
+        f32x4 p[2], dp[2], l[2];
+#pragma unroll
+        for (int rt = 0; rt < 2; ++rt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const size_t s = (size_t)h * a.tokens + min(i0 + rt * 16 + 4 * g + r, S - 1);
+                p[rt][r] = 0.f; dp[rt][r] = -delta[s]; l[rt][r] = lse[s];
+            }
+        wait_vmcnt<0>();
+        over_columns<D>(sm.t0[wave], k, p, l16, g);
+        over_columns<D>(sm.t1[wave], v, dp, l16, g);
+#pragma unroll
+        for (int rt = 0; rt < 2; ++rt) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int q = i0 + rt * 16 + 4 * g + r;
+                p[rt][r] = q >= S || (CAUSAL && q < jrow) ? 0.f : prob(p[rt][r], a.scale, l[rt][r]);
+                dp[rt][r] *= sees_one<CAUSAL>(S, q) ? 0.f : p[rt][r];
+            }
+            over_rows<D>(sm.t1[wave], rt * 16, p[rt], dv, l16, g);
+            over_rows<D>(sm.t0[wave], rt * 16, dp[rt], dk, l16, g);
+        }
+    }
+    const size_t width = (size_t)a.kv_heads * d, slab = (size_t)a.tokens * width;
+    __syncthreads();                                            // every tile has been read
+    store_few<D>(sm.t0[0], dk, a.splits > 1 ? a.slabs + (size_t)part * 2 * slab + row * width + kvh * d : (float*)a.dk + row * a.lddk + kvh * d, jrow < S, a.scale, d, wave, lane);
+    store_few<D>(sm.t1[0], dv, a.splits > 1 ? a.slabs + (size_t)part * 2 * slab + slab + row * width + kvh * d : (float*)a.dv + row * a.lddv + kvh * d, jrow < S, 1.0f, d, wave, lane);
+}
+
+template <int D, bool CAUSAL>
+__global__ __launch_bounds__(NT) void packed_bwd_few_kernel(PackedArgs a, int dkv) {
+    __shared__ __attribute__((aligned(16))) PackedFewLds<D> sm;
+    const int bid = (int)blockIdx.x;
+    if (bid < dkv) packed_dkv_few<D, CAUSAL>(sm, bid, a);
+    else packed_dq_few<D, CAUSAL>(sm, bid - dkv, a);
 }
 
 // ------------------------------------------------------------------------- host
-int tile_rows(int dtype) { return dtype == CHIMERA_F32 ? TILE : 128; }
+// Rows of a workgroup's tile.  Float tiles of 64 rows that are fewer than 256 for all heads go on 16 rows (632 tokens of 8 heads of 80 in 3 sequences, forward 28.0 -> 22.9 us, backward
+// 72.6 -> 57.4; but 3000 tokens of 8 heads of 128, 376 tiles, 400 -> 454 and 1359 -> 1693).
+int tile_rows(int dtype, int tokens, int heads) { return dtype != CHIMERA_F32 ? 128 : (size_t)heads * ((tokens + 63) / 64) < 256 ? 16 : 64; }
 
 // Slots for every tile that `tokens` rows in `seqs` sequences can have: a full one for each tile's rows, one more that is not full for each sequence
-size_t slots(int dtype, int seqs, int tokens) { return (size_t)tokens / tile_rows(dtype) + (size_t)std::min(seqs, tokens); }
+size_t slots(int rows, int seqs, int tokens) { return (size_t)tokens / rows + (size_t)std::min(seqs, tokens); }
 
-// Parts of a group's heads: the fewest that give dK and dV 600 workgroups
-int group_parts(int dtype, int tokens, int kv_heads, int group) {
-    const size_t some = (size_t)kv_heads * ((tokens + tile_rows(dtype) - 1) / tile_rows(dtype));
-    for (int s = 1; s < group; ++s)
-        if (group % s == 0 && some * s >= 600) return s;
-    return group;
+// Parts of a group's heads: the fewest that give dK and dV 450 workgroups, so that the longest, which start first, end with the rest.  Each part costs a slab of floats, written
+// and read.  8192 causal tokens, 16 heads of 128 over 2 in 2 sequences: one part 1529 us, 4 588, 8 625; 25 of 64 over 5 in 21 sequences one 185, 2 138, 5 141.
+int group_parts(int rows, int tokens, int kv_heads, int group) {
+    const long some = (long)kv_heads * ((tokens + rows - 1) / rows);
+    return (int)std::min<long>(group, (449 + some) / some);
 }
+
+// Workgroups for all slots of `units` units, as slot_of deals them
+size_t workgroups(size_t slots, int units, int group) { return units & 7 ? (slots * (units / group) + 7) / 8 * 8 * group : slots * units; }
 
 struct BwdLayout { size_t delta, slabs, total; int splits; };
 BwdLayout bwd_layout(int dtype, int tokens, int heads, int kv_heads, int d) {
     BwdLayout l{};
-    l.splits = group_parts(dtype, tokens, kv_heads, heads / kv_heads);
+    l.splits = group_parts(tile_rows(dtype, tokens, heads), tokens, kv_heads, heads / kv_heads);
     l.slabs = ((size_t)heads * tokens * 4 + 255) & ~(size_t)255;
     l.total = l.slabs + (l.splits > 1 ? (size_t)l.splits * 2 * tokens * kv_heads * d * 4 : 0);
     return l;
@@ -763,7 +1145,7 @@ int check_packed(int dtype, int seqs, int tokens, int heads, int kv_heads, int d
     const int unit = dtype == CHIMERA_F32 ? 4 : 8;
     if (d < unit || d > 128 || d % unit) return fail(CHIMERA_EINVAL, "head_dim=%d must be a multiple of %d up to 128", d, unit);
     if ((long)heads * d > 1 << 16) return fail(CHIMERA_EINVAL, "more than 2^16 columns of query heads");
-    if (tokens > 1 << 28 || seqs > 1 << 28 || (size_t)heads * (slots(dtype, seqs, tokens) + 8) >= (size_t)1 << 30)
+    if (tokens > 1 << 28 || seqs > 1 << 28 || (size_t)heads * (slots(tile_rows(dtype, tokens, heads), seqs, tokens) + 8) >= (size_t)1 << 30)
         return fail(CHIMERA_EINVAL, "more than 2^28 tokens, or 2^30 tiles of all heads");
     return CHIMERA_OK;
 }
@@ -777,10 +1159,12 @@ int check_rows(const char* what, const void* p, int ld, int cols, int dtype) {
 }
 
 #define PACKED_TRY(expr) do { int rc__ = (expr); if (rc__) return rc__; } while (0)
-#define PACKED_GO(KERNEL, D, GRID, ...)                                                                              \
+#define PACKED_GO(KERNEL, D, GRID, ...) PACKED_LAUNCH((KERNEL<D, true>), (KERNEL<D, false>), GRID, __VA_ARGS__)
+#define PACKED_GO_BWD(D, F) PACKED_LAUNCH((packed_bwd_kernel<D, true, F>), (packed_bwd_kernel<D, false, F>), dq_grid + dkv_grid, a, (int)dkv_grid)
+#define PACKED_LAUNCH(CAUSAL, FULL, GRID, ...)                                                                       \
     do {                                                                                                             \
-        if (causal) hipLaunchKernelGGL((KERNEL<D, true>), dim3((unsigned)(GRID)), dim3(NT), 0, s, __VA_ARGS__);       \
-        else hipLaunchKernelGGL((KERNEL<D, false>), dim3((unsigned)(GRID)), dim3(NT), 0, s, __VA_ARGS__);             \
+        if (causal) hipLaunchKernelGGL(CAUSAL, dim3((unsigned)(GRID)), dim3(NT), 0, s, __VA_ARGS__);                  \
+        else hipLaunchKernelGGL(FULL, dim3((unsigned)(GRID)), dim3(NT), 0, s, __VA_ARGS__);                           \
         CHIMERA_LAUNCH_CHECK("attention over packed sequences");                                                     \
     } while (0)
 
@@ -814,10 +1198,17 @@ int chimera_op_attention_packed_fwd(int dtype, int seqs, int tokens, int heads, 
     a.offsets = d_offsets; a.seqs = seqs; a.tokens = tokens; a.heads = heads; a.kv_heads = kv_heads; a.group = heads / kv_heads; a.d = head_dim; a.scale = scale;
     a.q = d_q; a.k = d_k; a.v = d_v; a.ldq = ldq; a.ldk = ldk; a.ldv = ldv; a.ctx = d_ctx; a.ldctx = ldctx; a.lse = d_lse;
     hipStream_t s = (hipStream_t)hip_stream;
-    const size_t grid = slots(dtype, seqs, tokens) * heads;
-    if (dtype == CHIMERA_F32) {
+    const int rows = tile_rows(dtype, tokens, heads);
+    const size_t grid = workgroups(slots(rows, seqs, tokens), heads, a.group);
+    if (dtype == CHIMERA_F32 && rows == 16) {
+        if (head_dim <= 32) PACKED_GO(packed_fwd_few_kernel, 32, grid, a);
+        else if (head_dim <= 64) PACKED_GO(packed_fwd_few_kernel, 64, grid, a);
+        else if (head_dim <= 96) PACKED_GO(packed_fwd_few_kernel, 96, grid, a);
+        else PACKED_GO(packed_fwd_few_kernel, 128, grid, a);
+    } else if (dtype == CHIMERA_F32) {
         if (head_dim <= 32) PACKED_GO(packed_fwd_f32_kernel, 32, grid, a);
         else if (head_dim <= 64) PACKED_GO(packed_fwd_f32_kernel, 64, grid, a);
+        else if (head_dim <= 96) PACKED_GO(packed_fwd_f32_kernel, 96, grid, a);
         else PACKED_GO(packed_fwd_f32_kernel, 128, grid, a);
     } else {
         if (head_dim <= 64) PACKED_GO(packed_fwd_kernel, 64, grid, a);
@@ -855,17 +1246,40 @@ int chimera_op_attention_packed_bwd(int dtype, int seqs, int tokens, int heads, 
     a.dctx = d_dctx; a.lddctx = lddctx; a.dq = d_dq; a.dk = d_dk; a.dv = d_dv; a.lddq = lddq; a.lddk = lddk; a.lddv = lddv;
     a.delta = (float*)d_workspace; a.slabs = (float*)((char*)d_workspace + l.slabs); a.splits = l.splits;
     hipStream_t s = (hipStream_t)hip_stream;
-    const size_t dq_grid = slots(dtype, seqs, tokens) * heads, dkv_grid = slots(dtype, seqs, tokens) * kv_heads * l.splits;
-    if (dtype == CHIMERA_F32) {
+    const int rows = tile_rows(dtype, tokens, heads);
+    const size_t dq_grid = workgroups(slots(rows, seqs, tokens), heads, a.group), dkv_grid = workgroups(slots(rows, seqs, tokens), kv_heads * l.splits, 1);
+    // Both roles in one launch, behind one for the deltas, or, at head dims above 64 with many workgroups, dQ (which forms them) and dK/dV apart: there a SIMD holds two
+    // wavefronts of dQ and one of dK/dV, or of both in one launch.  8192 causal tokens of 16 heads of 128 in 2 sequences 588 us apart, 617 together; 16384 in 4 1655 and
+    // 1756; 2048 in 2 107 and 84; head dim 64: 8192 tokens of 25 heads in 21 sequences 173 and 140, 16384 in 3 1949 and 1595.  Without a mask what is
+    // left at the end of each launch is more: 8192 tokens of 16 heads of 128 over 2 in 2 sequences 1396 and 1289.
+    const bool apart = dtype == CHIMERA_BF16 && head_dim > 64 && dq_grid >= 1024 && (causal || l.splits == 1);
+    // Few rows: few terms set the error, and the launch waits for latency (1000 tokens of 16 heads in 3 sequences 45.4 -> 48.3 us at head dim 128, 32.7 -> 36.9 at 64)
+    const bool fine = (size_t)tokens * heads <= 16384;
+    if (!apart) {
+        const dim3 grid((unsigned)(((size_t)tokens * heads * 16 + NT - 1) / NT));
+        if (dtype == CHIMERA_F32) hipLaunchKernelGGL(packed_delta_kernel<float>, grid, dim3(NT), 0, s, a);
+        else hipLaunchKernelGGL(packed_delta_kernel<bf16_t>, grid, dim3(NT), 0, s, a);
+        CHIMERA_LAUNCH_CHECK("attention over packed sequences");
+    }
+    if (dtype == CHIMERA_F32 && rows == 16) {
+        if (head_dim <= 32) PACKED_GO(packed_bwd_few_kernel, 32, dq_grid + dkv_grid, a, (int)dkv_grid);
+        else if (head_dim <= 64) PACKED_GO(packed_bwd_few_kernel, 64, dq_grid + dkv_grid, a, (int)dkv_grid);
+        else if (head_dim <= 96) PACKED_GO(packed_bwd_few_kernel, 96, dq_grid + dkv_grid, a, (int)dkv_grid);
+        else PACKED_GO(packed_bwd_few_kernel, 128, dq_grid + dkv_grid, a, (int)dkv_grid);
+    } else if (dtype == CHIMERA_F32) {
         if (head_dim <= 32) PACKED_GO(packed_bwd_f32_kernel, 32, dq_grid + dkv_grid, a, (int)dkv_grid);
         else if (head_dim <= 64) PACKED_GO(packed_bwd_f32_kernel, 64, dq_grid + dkv_grid, a, (int)dkv_grid);
+        else if (head_dim <= 96) PACKED_GO(packed_bwd_f32_kernel, 96, dq_grid + dkv_grid, a, (int)dkv_grid);
         else PACKED_GO(packed_bwd_f32_kernel, 128, dq_grid + dkv_grid, a, (int)dkv_grid);
-    } else if (head_dim <= 64) {
-        PACKED_GO(packed_dq_kernel, 64, dq_grid, a);
-        PACKED_GO(packed_dkv_kernel, 64, dkv_grid, a);
-    } else {
+    } else if (apart) {
         PACKED_GO(packed_dq_kernel, 128, dq_grid, a);
         PACKED_GO(packed_dkv_kernel, 128, dkv_grid, a);
+    } else if (head_dim <= 64) {
+        if (fine) PACKED_GO_BWD(64, true);
+        else PACKED_GO_BWD(64, false);
+    } else {
+        if (fine) PACKED_GO_BWD(128, true);
+        else PACKED_GO_BWD(128, false);
     }
     if (l.splits > 1) {
         const size_t chunks = (size_t)tokens * narrow / 4;

@@ -21,6 +21,7 @@ namespace {
 
 constexpr int V = 8;                     // columns of a chunk
 constexpr int BN_COLS = 8192;
+constexpr int ROW_GROUPS = 512;          // workgroups of the backward
 
 // A chunk as it comes from memory
 template <typename T> struct Chunk {
@@ -34,6 +35,21 @@ template <typename T> struct Chunk {
         for (int i = 0; i < V / Elem<T>::VEC; ++i) load_vec<T>(reinterpret_cast<const T*>(&q[i]), out + i * Elem<T>::VEC);
     }
 };
+
+// A chunk of a result, stored past the caches' order of use, where its lines push out what is still to be read (8192 x 2048, float stream, forward 44.2 -> 41.4 us; 8192 x 1600
+// backward 51.5 -> 49.9)
+template <typename T> __device__ __forceinline__ void store_chunk(T* p, const float* v) {
+    typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int i = 0; i < V; i += Elem<T>::VEC) {
+        T w[Elem<T>::VEC];
+#pragma unroll
+        for (int e = 0; e < Elem<T>::VEC; ++e) w[e] = Elem<T>::from_f(v[i + e]);
+        u32x4 q;
+        __builtin_memcpy(&q, w, sizeof(q));
+        __builtin_nontemporal_store(q, reinterpret_cast<u32x4*>(p + i));
+    }
+}
 
 struct JoinArgs {
     int rows, cols, run;                 // run: rows that share a row of the gate
@@ -55,13 +71,13 @@ struct JoinArgs {
 };
 enum { SUM_GAIN1, SUM_BIAS1, SUM_GAIN2, SUM_BIAS2, SUM_GATE, SUMS };
 
-// Sums of N numbers over the TPR threads that share a row; `lds` holds N floats for each wavefront of the workgroup.  Every thread of the workgroup comes here.
+// Sums of N numbers over the TPR threads that share a row; `lds` holds N floats for each wavefront of the workgroup.  Every thread of the workgroup comes here, and
+// a call's `lds` is not used again by the next one: one barrier each is then enough.
 template <int TPR, int N> __device__ __forceinline__ void row_sums(float (&v)[N], float* lds, int wave, int lane) {
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
     if constexpr (TPR > WAVE) {
         constexpr int PER = TPR / WAVE;
-        __syncthreads();                 // the last sums have been read
         if (lane == 0)
 #pragma unroll
             for (int i = 0; i < N; ++i) lds[wave * N + i] = v[i];
@@ -80,11 +96,11 @@ template <int TPR, int N> __device__ __forceinline__ void row_sums(float (&v)[N]
 template <typename T, typename TS, int TPR, int MAXT>
 __global__ __launch_bounds__(256) void join_fwd_kernel(JoinArgs a) {
     constexpr int LANES = 256 / TPR;                        // rows side by side
-    __shared__ float lds[8];
+    __shared__ float lds[2][4][4];
     const int tid = threadIdx.x, lane = tid % WAVE, wave = tid / WAVE, c0 = tid % TPR, cols = a.cols, nchunk = cols / V;
     const float inv_cols = 1.0f / (float)cols;
     const int first = blockIdx.x * a.per_group, last = min(a.rows, first + a.per_group);
-    for (int base = first; base < last; base += LANES) {    // the same count for every thread
+    for (int base = first, odd = 0; base < last; base += LANES, odd ^= 1) {    // the same count for every thread
         const int row = min(base + tid / TPR, last - 1);
         const bool mine = base + tid / TPR < last;
         const size_t at = (size_t)row * cols;
@@ -108,7 +124,7 @@ __global__ __launch_bounds__(256) void join_fwd_kernel(JoinArgs a) {
                     if (c0 + t * TPR < nchunk)
 #pragma unroll
                         for (int e = 0; e < V; ++e) s[0] += u[t][e];
-                row_sums<TPR>(s, lds, wave, lane);
+                row_sums<TPR>(s, lds[odd][0], wave, lane);
                 mean = s[0] * inv_cols;
                 s[0] = 0.f;
             }
@@ -119,7 +135,7 @@ __global__ __launch_bounds__(256) void join_fwd_kernel(JoinArgs a) {
                     u[t][e] -= mean;
                     if (c0 + t * TPR < nchunk) s[0] += u[t][e] * u[t][e];
                 }
-            row_sums<TPR>(s, lds, wave, lane);
+            row_sums<TPR>(s, lds[odd][1], wave, lane);
             const float rstd = 1.0f / sqrtf(s[0] * inv_cols + a.eps);
             if (mine && c0 == 0) { a.stats[row] = mean; a.stats[(size_t)a.rows + row] = rstd; }
 #pragma unroll
@@ -146,12 +162,12 @@ __global__ __launch_bounds__(256) void join_fwd_kernel(JoinArgs a) {
                 if (a.x) u[t][e] += a.alpha * x[e];
                 if (c0 + t * TPR < nchunk) s[0] += u[t][e];
             }
-            if (mine && c0 + t * TPR < nchunk) store_elems<TS, V>((TS*)a.y + at + c, u[t]);
+            if (mine && c0 + t * TPR < nchunk) store_chunk<TS>((TS*)a.y + at + c, u[t]);
         }
         if (a.pre) {
             float mean = 0.f;
             if (a.pre == CHIMERA_NORM_LAYER) {
-                row_sums<TPR>(s, lds, wave, lane);
+                row_sums<TPR>(s, lds[odd][2], wave, lane);
                 mean = s[0] * inv_cols;
             }
             s[0] = 0.f;
@@ -162,7 +178,7 @@ __global__ __launch_bounds__(256) void join_fwd_kernel(JoinArgs a) {
                     u[t][e] -= mean;
                     if (c0 + t * TPR < nchunk) s[0] += u[t][e] * u[t][e];
                 }
-            row_sums<TPR>(s, lds, wave, lane);
+            row_sums<TPR>(s, lds[odd][3], wave, lane);
             const float rstd = 1.0f / sqrtf(s[0] * inv_cols + a.eps);
             if (mine && c0 == 0) { a.stats[2 * (size_t)a.rows + row] = mean; a.stats[3 * (size_t)a.rows + row] = rstd; }
 #pragma unroll
@@ -173,21 +189,25 @@ __global__ __launch_bounds__(256) void join_fwd_kernel(JoinArgs a) {
                 if (a.pre_bias) load_elems<T, V>((const T*)a.pre_bias + c, b);
 #pragma unroll
                 for (int e = 0; e < V; ++e) u[t][e] = u[t][e] * rstd * g[e] + (a.pre_bias ? b[e] : 0.f);
-                if (mine && c0 + t * TPR < nchunk) store_elems<T, V>((T*)a.h + at + c, u[t]);
+                if (mine && c0 + t * TPR < nchunk) store_chunk<T>((T*)a.h + at + c, u[t]);
             }
         }
     }
 }
 
 // --------------------------------------------------------------------- backward
-// A workgroup of 512 threads takes `per_group` rows, 512 / TPR of them side by side.  A thread's columns are the same in every row, so its share of the column sums
+// A workgroup takes `per_group` rows, as many side by side as it has threads for.  A thread's columns are the same in every row, so its share of the column sums
 // stays in registers; at the end the rows side by side meet in LDS, in their order, and the workgroup's sums leave for join_sum_kernel (or are final
 // where there is one workgroup).  dgate's sums end where a run of the gate ends: either a run holds whole workgroups, or a workgroup holds whole runs, and then
 // each of the rows side by side belongs to a run of its own.
+// A row is a chain of loads and two sums over its threads: the next row is asked for before the sums of this one, and small workgroups, two on a CU, fill one another's
+// waits (8192 x 1600 bf16, all sums: 512 workgroups of 256 threads 50 us, 256 of 512 54; two rows at a time in each take the registers of the second
+// workgroup, 71).
+constexpr int bwd_threads(int threads_a_row) { return threads_a_row > 256 ? threads_a_row : 256; }
 template <typename T, typename TS, int TPR, int MAXT>
-__global__ __launch_bounds__(512) void join_bwd_kernel(JoinArgs a) {
-    constexpr int LANES = 512 / TPR;
-    __shared__ float lds[2 * 8];
+__global__ __launch_bounds__(bwd_threads(TPR)) void join_bwd_kernel(JoinArgs a) {
+    constexpr int LANES = bwd_threads(TPR) / TPR;           // rows side by side
+    __shared__ float lds[2][2][2 * 8];
     extern __shared__ float meet_at[];                      // [LANES][cols], where LANES > 1
     const int tid = threadIdx.x, lane = tid % WAVE, wave = tid / WAVE, c0 = tid % TPR, rl = tid / TPR, cols = a.cols, nchunk = cols / V;
     const float inv_cols = 1.0f / (float)cols;
@@ -202,9 +222,29 @@ __global__ __launch_bounds__(512) void join_bwd_kernel(JoinArgs a) {
         last = min((run + 1) * a.run, first + a.per_group);
     }
     // of those, a lane takes every LANES-th, or (whole runs) neighbouring ones that are whole runs too
-    const int runs = a.whole_runs ? (last - first) / a.run : 0;
-    const int own = a.whole_runs ? (runs + LANES - 1) / LANES * a.run : 0;
+    const int own = a.whole_runs ? ((last - first) / a.run + LANES - 1) / LANES * a.run : 0;
     const int steps = a.whole_runs ? own : (last - first + LANES - 1) / LANES;
+    auto row_of = [&](int i) { return a.whole_runs ? first + rl * own + i : first + i * LANES + rl; };
+    int at[MAXT];                                           // the thread's columns; beyond the last ones: none
+    bool live[MAXT];
+    float gain1[MAXT][V], bias1[MAXT][V], gain2[MAXT][V], gate[MAXT][V];
+#pragma unroll
+    for (int t = 0; t < MAXT; ++t) {
+        live[t] = c0 + t * TPR < nchunk;
+        at[t] = live[t] ? (c0 + t * TPR) * V : 0;
+#pragma unroll
+        for (int e = 0; e < V; ++e) { gain1[t][e] = 1.f; bias1[t][e] = 0.f; gain2[t][e] = 0.f; gate[t][e] = 1.f; }
+    }
+    auto parameters = [&] {
+#pragma unroll
+        for (int t = 0; t < MAXT; ++t) {
+            if (a.post) load_elems<T, V>((const T*)a.post_gain + at[t], gain1[t]);
+            if (a.post_bias) load_elems<T, V>((const T*)a.post_bias + at[t], bias1[t]);
+            if (a.pre) load_elems<T, V>((const T*)a.pre_gain + at[t], gain2[t]);
+            if (a.gate && !a.whole_runs) load_elems<T, V>((const T*)a.gate + (size_t)(first / a.run) * cols + at[t], gate[t]);
+        }
+    };
+    if constexpr (MAXT == 1) parameters();                  // (two chunks have no registers for them from row to row)
     float sum[SUMS][MAXT][V];
 #pragma unroll
     for (int k = 0; k < SUMS; ++k)
@@ -212,128 +252,117 @@ __global__ __launch_bounds__(512) void join_bwd_kernel(JoinArgs a) {
         for (int t = 0; t < MAXT; ++t)
 #pragma unroll
             for (int e = 0; e < V; ++e) sum[k][t][e] = 0.f;
-    for (int i = 0; i < steps; ++i) {
-        const int want = a.whole_runs ? first + rl * own + i : first + i * LANES + rl;
-        const bool mine = want < last;
-        const int row = min(want, last - 1);
-        const size_t at = (size_t)row * cols;
-        Chunk<T> rf[MAXT], rdh[MAXT];
-        Chunk<TS> ry[MAXT], rdy[MAXT];
+    Chunk<T> rf[MAXT], rdh[MAXT], rg[MAXT];
+    Chunk<TS> ry[MAXT], rdy[MAXT];
+    float mean1 = 0.f, rstd1 = 1.f, mean2 = 0.f, rstd2 = 0.f;
+    auto load = [&](int i) {
+        const int row = min(row_of(i), last - 1);
 #pragma unroll
         for (int t = 0; t < MAXT; ++t) {
-            const size_t c = at + min(c0 + t * TPR, nchunk - 1) * V;
+            const size_t c = (size_t)row * cols + at[t];
             if (a.dy) rdy[t].load((const TS*)a.dy + c);
             if (a.pre) {
                 rdh[t].load((const T*)a.dh + c);
                 ry[t].load((const TS*)a.y + c);
             }
             rf[t].load((const T*)a.f + c);
+            if (a.whole_runs) rg[t].load((const T*)a.gate + (size_t)(row / a.run) * cols + at[t]);
         }
-        float d[MAXT][V];
+        if (a.pre == CHIMERA_NORM_LAYER) mean2 = a.stats[2 * (size_t)a.rows + row];
+        if (a.pre) rstd2 = a.stats[3 * (size_t)a.rows + row];
+        if (a.post == CHIMERA_NORM_LAYER) mean1 = a.stats[row];
+        if (a.post) rstd1 = a.stats[(size_t)a.rows + row];
+    };
+    load(0);
+    for (int i = 0; i < steps; ++i) {
+        const int row = row_of(i);
+        const bool mine = row < last;                       // the same for the threads of a row
+        const float m1 = mean1, r1 = rstd1, m2 = mean2, r2 = rstd2;
+        float d[MAXT][V], hat1[MAXT][V], hat2[MAXT][V], dg[MAXT][V];
+        if constexpr (MAXT > 1) parameters();
 #pragma unroll
         for (int t = 0; t < MAXT; ++t) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) { d[t][e] = 0.f; hat2[t][e] = 0.f; dg[t][e] = 0.f; }
             if (a.dy) rdy[t].unpack(d[t]);
-            else
-#pragma unroll
-                for (int e = 0; e < V; ++e) d[t][e] = 0.f;
-        }
-        if (a.pre) {
-            const float mean = a.pre == CHIMERA_NORM_LAYER ? a.stats[2 * (size_t)a.rows + row] : 0.f, rstd = a.stats[3 * (size_t)a.rows + row];
-            float s[2] = {0.f, 0.f}, dg[MAXT][V], hat[MAXT][V];
-#pragma unroll
-            for (int t = 0; t < MAXT; ++t) {
-                float g[V], dh[V];
-                load_elems<T, V>((const T*)a.pre_gain + min(c0 + t * TPR, nchunk - 1) * V, g);
-                rdh[t].unpack(dh);
-                ry[t].unpack(hat[t]);
-                if (!mine || c0 + t * TPR >= nchunk)
-#pragma unroll
-                    for (int e = 0; e < V; ++e) dh[e] = 0.f;
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    hat[t][e] = (hat[t][e] - mean) * rstd;
-                    sum[SUM_GAIN2][t][e] += mine && c0 + t * TPR < nchunk ? dh[e] * hat[t][e] : 0.f;
-                    sum[SUM_BIAS2][t][e] += dh[e];
-                    dg[t][e] = dh[e] * g[e];
-                    s[0] += dg[t][e];
-                    s[1] += mine && c0 + t * TPR < nchunk ? dg[t][e] * hat[t][e] : 0.f;
-                }
+            if (a.pre) {
+                rdh[t].unpack(dg[t]);
+                ry[t].unpack(hat2[t]);
             }
-            row_sums<TPR>(s, lds, wave, lane);
-            const float m1 = a.pre == CHIMERA_NORM_LAYER ? s[0] * inv_cols : 0.f, m2 = s[1] * inv_cols;
-#pragma unroll
-            for (int t = 0; t < MAXT; ++t)
-#pragma unroll
-                for (int e = 0; e < V; ++e) d[t][e] += rstd * (dg[t][e] - m1 - hat[t][e] * m2);
+            rf[t].unpack(hat1[t]);
+            if (a.whole_runs) rg[t].unpack(gate[t]);
         }
-        if (a.dx && mine)
+        if (i + 1 < steps) load(i + 1);
+        if (a.pre) {
+            float s[2] = {0.f, 0.f};
 #pragma unroll
             for (int t = 0; t < MAXT; ++t)
-                if (c0 + t * TPR < nchunk) {
+                if (mine && live[t])
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        hat2[t][e] = (hat2[t][e] - m2) * r2;
+                        sum[SUM_GAIN2][t][e] += dg[t][e] * hat2[t][e];
+                        sum[SUM_BIAS2][t][e] += dg[t][e];
+                        dg[t][e] *= gain2[t][e];
+                        s[0] += dg[t][e];
+                        s[1] += dg[t][e] * hat2[t][e];
+                    }
+            row_sums<TPR>(s, lds[i & 1][0], wave, lane);
+            const float mean_d = a.pre == CHIMERA_NORM_LAYER ? s[0] * inv_cols : 0.f, c1 = s[1] * inv_cols;
+#pragma unroll
+            for (int t = 0; t < MAXT; ++t)
+#pragma unroll
+                for (int e = 0; e < V; ++e) d[t][e] += r2 * (dg[t][e] - mean_d - hat2[t][e] * c1);
+        }
+        float s[2] = {0.f, 0.f};
+#pragma unroll
+        for (int t = 0; t < MAXT; ++t)
+            if (mine && live[t]) {
+                if (a.dx) {
                     float o[V];
 #pragma unroll
                     for (int e = 0; e < V; ++e) o[e] = a.alpha * d[t][e];
-                    store_elems<TS, V>((TS*)a.dx + at + (c0 + t * TPR) * V, o);
+                    store_chunk<TS>((TS*)a.dx + (size_t)row * cols + at[t], o);
                 }
-        const T* gate = a.gate ? (const T*)a.gate + (size_t)(row / a.run) * cols : nullptr;
-        const float mean = a.post == CHIMERA_NORM_LAYER ? a.stats[row] : 0.f, rstd = a.post ? a.stats[(size_t)a.rows + row] : 1.f;
-        float s[2] = {0.f, 0.f}, hat[MAXT][V];
 #pragma unroll
-        for (int t = 0; t < MAXT; ++t) {
-            const int c = min(c0 + t * TPR, nchunk - 1) * V;
-            const bool live = mine && c0 + t * TPR < nchunk;
-            float g[V], b[V], w[V];
-            rf[t].unpack(hat[t]);
-            if (a.post) load_elems<T, V>((const T*)a.post_gain + c, g);
-            if (a.post && a.post_bias) load_elems<T, V>((const T*)a.post_bias + c, b);
-            if (gate) load_elems<T, V>(gate + c, w);
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                hat[t][e] = (hat[t][e] - mean) * rstd;
-                d[t][e] *= a.beta;
-                if (gate) {
-                    const float u = a.post ? hat[t][e] * g[e] + (a.post_bias ? b[e] : 0.f) : hat[t][e];
-                    sum[SUM_GATE][t][e] += live ? d[t][e] * u : 0.f;
-                    d[t][e] *= w[e];
-                }
-                if (a.post) {
-                    sum[SUM_GAIN1][t][e] += live ? d[t][e] * hat[t][e] : 0.f;
-                    sum[SUM_BIAS1][t][e] += live ? d[t][e] : 0.f;
-                    d[t][e] *= g[e];
-                    s[0] += live ? d[t][e] : 0.f;
-                    s[1] += live ? d[t][e] * hat[t][e] : 0.f;
+                for (int e = 0; e < V; ++e) {
+                    hat1[t][e] = (hat1[t][e] - m1) * r1;    // (without a norm: f itself)
+                    d[t][e] *= a.beta;
+                    sum[SUM_GATE][t][e] += d[t][e] * (hat1[t][e] * gain1[t][e] + bias1[t][e]);
+                    d[t][e] *= gate[t][e];
+                    sum[SUM_GAIN1][t][e] += d[t][e] * hat1[t][e];
+                    sum[SUM_BIAS1][t][e] += d[t][e];
+                    d[t][e] *= gain1[t][e];
+                    s[0] += d[t][e];
+                    s[1] += d[t][e] * hat1[t][e];
                 }
             }
-        }
+        if (a.whole_runs && (i + 1) % a.run == 0)                       // the end of a run: its row of dgate is this lane's
+#pragma unroll
+            for (int t = 0; t < MAXT; ++t) {
+                if (mine && live[t] && a.out[SUM_GATE]) {
+                    float* o = a.out[SUM_GATE] + (size_t)(row / a.run) * cols + at[t];
+                    float v[V];
+                    if (!a.overwrite) load_elems<float, V>(o, v);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) v[e] = a.overwrite ? sum[SUM_GATE][t][e] : v[e] + sum[SUM_GATE][t][e];
+                    store_elems<float, V>(o, v);
+                }
+#pragma unroll
+                for (int e = 0; e < V; ++e) sum[SUM_GATE][t][e] = 0.f;
+            }
         if (a.post) {
-            row_sums<TPR>(s, lds, wave, lane);
-            const float m1 = a.post == CHIMERA_NORM_LAYER ? s[0] * inv_cols : 0.f, m2 = s[1] * inv_cols;
+            row_sums<TPR>(s, lds[i & 1][1], wave, lane);
+            const float mean_d = a.post == CHIMERA_NORM_LAYER ? s[0] * inv_cols : 0.f, c1 = s[1] * inv_cols;
 #pragma unroll
             for (int t = 0; t < MAXT; ++t)
 #pragma unroll
-                for (int e = 0; e < V; ++e) d[t][e] = rstd * (d[t][e] - m1 - hat[t][e] * m2);
+                for (int e = 0; e < V; ++e) d[t][e] = r1 * (d[t][e] - mean_d - hat1[t][e] * c1);
         }
         if (mine)
 #pragma unroll
             for (int t = 0; t < MAXT; ++t)
-                if (c0 + t * TPR < nchunk) store_elems<T, V>((T*)a.df + at + (c0 + t * TPR) * V, d[t]);
-        if (a.whole_runs && (i + 1) % a.run == 0) {                     // the end of a run: its row of dgate is this lane's
-            if (mine && a.out[SUM_GATE])
-#pragma unroll
-                for (int t = 0; t < MAXT; ++t)
-                    if (c0 + t * TPR < nchunk) {
-                        float* o = a.out[SUM_GATE] + (size_t)(row / a.run) * cols + (c0 + t * TPR) * V;
-                        float v[V];
-                        if (!a.overwrite) load_elems<float, V>(o, v);
-#pragma unroll
-                        for (int e = 0; e < V; ++e) v[e] = a.overwrite ? sum[SUM_GATE][t][e] : v[e] + sum[SUM_GATE][t][e];
-                        store_elems<float, V>(o, v);
-                    }
-#pragma unroll
-            for (int t = 0; t < MAXT; ++t)
-#pragma unroll
-                for (int e = 0; e < V; ++e) sum[SUM_GATE][t][e] = 0.f;
-        }
+                if (live[t]) store_chunk<T>((T*)a.df + (size_t)row * cols + at[t], d[t]);
     }
     int slot = 0;
 #pragma unroll
@@ -343,24 +372,23 @@ __global__ __launch_bounds__(512) void join_bwd_kernel(JoinArgs a) {
             __syncthreads();
 #pragma unroll
             for (int t = 0; t < MAXT; ++t)
-                if (c0 + t * TPR < nchunk) store_elems<float, V>(meet_at + (size_t)rl * cols + (c0 + t * TPR) * V, sum[k][t]);
+                if (live[t]) store_elems<float, V>(meet_at + (size_t)rl * cols + at[t], sum[k][t]);
             __syncthreads();
         }
         if (rl == 0)
 #pragma unroll
             for (int t = 0; t < MAXT; ++t) {
-                const int c = (c0 + t * TPR) * V;
-                if (c0 + t * TPR >= nchunk) continue;
+                if (!live[t]) continue;
                 float v[V];
 #pragma unroll
                 for (int e = 0; e < V; ++e) v[e] = sum[k][t][e];
                 for (int l = 1; l < LANES; ++l) {
                     float w[V];
-                    load_elems<float, V>(meet_at + (size_t)l * cols + c, w);
+                    load_elems<float, V>(meet_at + (size_t)l * cols + at[t], w);
 #pragma unroll
                     for (int e = 0; e < V; ++e) v[e] += w[e];
                 }
-                float* o = a.partial ? a.partial + ((size_t)blockIdx.x * __builtin_popcount(a.sums) + slot) * cols + c : a.out[k] + c;
+                float* o = a.partial ? a.partial + ((size_t)blockIdx.x * __builtin_popcount(a.sums) + slot) * cols + at[t] : a.out[k] + at[t];
                 if (!a.partial && !a.overwrite) {
                     float w[V];
                     load_elems<float, V>(o, w);
@@ -373,15 +401,15 @@ __global__ __launch_bounds__(512) void join_bwd_kernel(JoinArgs a) {
     }
 }
 
-// The workgroups' sums, in their order: 8 sub-sums of every eighth workgroup, then those.  blockIdx.y: which sum; from `slots` on, rows of dgate, whose
+// The workgroups' sums, in their order: 32 sub-sums of every 32nd workgroup, then those.  blockIdx.y: which sum; from `slots` on, rows of dgate, whose
 // workgroups lie together.
 struct JoinSums {
     const float* partial;
     float* out[SUMS];                    // of the slots
     int slots, cols, groups, gate_slot, groups_per_run, overwrite;
 };
-__global__ __launch_bounds__(256) void join_sum_kernel(JoinSums a) {
-    __shared__ float red[8][32];
+__global__ __launch_bounds__(1024) void join_sum_kernel(JoinSums a) {
+    __shared__ float red[32][32];
     const int c = threadIdx.x & 31, q = threadIdx.x >> 5, i = blockIdx.x * 32 + c, y = blockIdx.y;
     const bool gate = a.gate_slot >= 0 && y >= a.gate_slot;             // the gate's sum is the last slot
     const int run = gate ? y - a.gate_slot : 0, first = gate ? run * a.groups_per_run : 0, count = gate ? a.groups_per_run : a.groups;
@@ -391,15 +419,15 @@ __global__ __launch_bounds__(256) void join_sum_kernel(JoinSums a) {
     float s = 0.f;
     if (i < a.cols) {
         int g = q;
-        for (; g + 24 < count; g += 32) s += (p[g * step] + p[(g + 8) * step]) + (p[(g + 16) * step] + p[(g + 24) * step]);
-        for (; g < count; g += 8) s += p[g * step];
+        for (; g + 96 < count; g += 128) s += (p[g * step] + p[(g + 32) * step]) + (p[(g + 64) * step] + p[(g + 96) * step]);
+        for (; g < count; g += 32) s += p[g * step];
     }
     red[q][c] = s;
     __syncthreads();
     if (q == 0 && i < a.cols) {
         float t = red[0][c];
 #pragma unroll
-        for (int k = 1; k < 8; ++k) t += red[k][c];
+        for (int k = 1; k < 32; ++k) t += red[k][c];
         float* o = a.out[slot] + (size_t)run * a.cols + i;
         *o = a.overwrite ? t : *o + t;
     }
@@ -414,8 +442,9 @@ int threads_a_row(int cols) { return cols <= 512 ? 64 : cols <= 1024 ? 128 : col
 struct BwdPlan { int per_group, groups, whole_runs, groups_per_run; };
 BwdPlan bwd_plan(int rows, int cols, int gate_rows) {
     BwdPlan p{};
-    const int lanes = 512 / threads_a_row(cols);
-    int per = (std::max((rows + 255) / 256, lanes) + lanes - 1) / lanes * lanes;
+    const int lanes = bwd_threads(threads_a_row(cols)) / threads_a_row(cols);
+    // no more than 8 rows a lane: one workgroup, whose sums are final (a launch less)
+    const int per = rows <= 8 * lanes ? rows : (std::max((rows + ROW_GROUPS - 1) / ROW_GROUPS, lanes) + lanes - 1) / lanes * lanes;
     if (!gate_rows) {
         p.per_group = per;
         p.groups = (rows + per - 1) / per;
@@ -551,16 +580,16 @@ int chimera_op_branch_norm_bwd(int dtype, int stream_dtype, int rows, int cols, 
     }
     a.partial = p.groups > 1 ? (float*)d_workspace : nullptr;
     constexpr int WIDE = 512;
-    const int lanes = 512 / threads_a_row(cols);
+    const int lanes = bwd_threads(threads_a_row(cols)) / threads_a_row(cols);
     const size_t lds = lanes > 1 ? (size_t)lanes * cols * 4 : 0;
     hipStream_t s = (hipStream_t)hip_stream;
-#define JOIN_BWD(T, TS, TPR, MAXT) hipLaunchKernelGGL((join_bwd_kernel<T, TS, TPR, MAXT>), dim3((unsigned)p.groups), dim3(512), lds, s, a)
+#define JOIN_BWD(T, TS, TPR, MAXT) hipLaunchKernelGGL((join_bwd_kernel<T, TS, TPR, MAXT>), dim3((unsigned)p.groups), dim3(bwd_threads(TPR)), lds, s, a)
     JOIN_TYPES(JOIN_BWD);
     CHIMERA_LAUNCH_CHECK("norm of a branch, backward");
     if (a.partial && r.slots) {
         r.partial = a.partial; r.cols = cols; r.groups = p.groups; r.groups_per_run = p.groups_per_run; r.overwrite = overwrite;
         const unsigned ny = (unsigned)(r.gate_slot >= 0 ? r.gate_slot + gate_rows : r.slots);
-        hipLaunchKernelGGL(join_sum_kernel, dim3((unsigned)((cols + 31) / 32), ny), dim3(256), 0, s, r);
+        hipLaunchKernelGGL(join_sum_kernel, dim3((unsigned)((cols + 31) / 32), ny), dim3(1024), 0, s, r);
         CHIMERA_LAUNCH_CHECK("norm of a branch, backward");
     }
     return CHIMERA_OK;

@@ -5,8 +5,9 @@
 // and the rest is passed on.  The gradient takes the transposed matrix, the same with -t.
 //
 // The kernel moves 2 x tokens x heads x head_dim elements and computes little: what bounds it is memory.  An angle is the same for all heads of a token, so
-// a workgroup forms the sines and cosines of its tokens once, in LDS, and every thread then takes pieces of 16 bytes of the heads' rows from there.  The angle
-// is formed in double, in turns, of which only the fraction goes on in float: a float angle at position 10^5 would be off by 0.004.
+// a workgroup forms the sines and cosines of its tokens once, in LDS, and goes through their rows in pieces of 16 bytes (in the half layout with their partners),
+// neighbouring threads on neighbouring pieces, the next ones under way while these are turned.  The angle is formed in double, in turns, of which only the
+// fraction goes on in float: a float angle at position 10^5 would be off by 0.004.
 #include "device.h"
 #include "spans.h"
 
@@ -28,9 +29,12 @@ struct RotaryArgs {
     long long ldx, ldy;
     int tokens, heads, d, rot, per_group;           // per_group: tokens of a workgroup
     int turned, items;                              // pieces of a head's row that are turned, and all of them
-    unsigned by_items, by_heads;                    // 2^31 / n, rounded up: quotients of numbers up to 2^16 by n up to 2^15
+    unsigned long long by_items, by_heads;          // 2^40 / n, rounded up
     float magnitude, sign;
 };
+
+// i / n for i up to 2^20 and n up to 2^16, from 2^40 / n rounded up
+__device__ __forceinline__ int quotient(int i, unsigned long long by) { return (int)((unsigned long long)(unsigned)i * by >> 40); }
 
 // n consecutive elements from an address that need not be aligned to more than an element
 template <typename T, int V> __device__ __forceinline__ void load_any(const T* p, int n, T* out) {
@@ -39,9 +43,16 @@ template <typename T, int V> __device__ __forceinline__ void load_any(const T* p
 #pragma unroll
         for (int i = 0; i < V; ++i) out[i] = i < n ? p[i] : (T)0.f;
 }
+// (Stored past the caches' order of use: kept there, the lines push out what is still to be read.  8192 x 18 heads of 128 19.4 -> 17.7 us, and no longer with
+// attention over the result behind it; 16384 x 30 of 64 interleaved 28.2 -> 25.1.)
 template <typename T, int V> __device__ __forceinline__ void store_any(T* p, int n, const T* v) {
-    if (n == V) __builtin_memcpy(p, v, V * sizeof(T));
-    else
+    typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+    typedef u32x4 piece_t __attribute__((aligned(2)));
+    if (n == V) {
+        u32x4 q;
+        __builtin_memcpy(&q, v, sizeof(q));
+        __builtin_nontemporal_store(q, (piece_t*)p);
+    } else
 #pragma unroll
         for (int i = 0; i < V; ++i)
             if (i < n) p[i] = v[i];
@@ -49,10 +60,38 @@ template <typename T, int V> __device__ __forceinline__ void store_any(T* p, int
 
 template <typename T, bool HALF>
 __global__ __launch_bounds__(RT) void rotary_kernel(RotaryArgs a) {
-    constexpr int V = Elem<T>::VEC;
+    constexpr int V = Elem<T>::VEC, N = HALF ? 1 : 2;               // pieces of a thread under way at a time: 32 bytes
     __shared__ float2 turn[RT_TOKENS * ROT_MAX / 2];
     const int tid = threadIdx.x, pairs = a.rot / 2;
     const int token0 = (int)blockIdx.x * a.per_group, here = min(a.per_group, a.tokens - token0);
+    const int total = here * a.heads * a.items;
+    T u[N][V], v[HALF ? N : 1][V];
+    // piece i: where it begins in x and in y, its token, its first column, and how many of its columns there are
+    struct Piece { long long x, y; int t, c, n; bool turned; };
+    auto piece = [&](int i) {
+        const int row = quotient(i, a.by_items), j = i - row * a.items;
+        const int t = quotient(row, a.by_heads), h = row - t * a.heads;
+        Piece p;
+        p.t = t;
+        p.turned = j < a.turned;
+        p.c = p.turned ? j * V : a.rot + (j - a.turned) * V;
+        p.n = min(V, (p.turned ? (HALF ? pairs : a.rot) : a.d) - p.c);
+        p.x = (token0 + t) * a.ldx + h * a.d + p.c;
+        p.y = (token0 + t) * a.ldy + h * a.d + p.c;
+        return p;
+    };
+    auto load = [&](int i0) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const int i = i0 + k * RT;
+            if (i >= total) continue;
+            const Piece p = piece(i);
+            load_any<T, V>((const T*)a.x + p.x, p.n, u[k]);
+            if constexpr (HALF)
+                if (p.turned) load_any<T, V>((const T*)a.x + p.x + pairs, p.n, v[k]);
+        }
+    };
+    load(tid);                                                  // under way while the angles are formed
     for (int i = tid; i < here * pairs; i += RT) {
         const int t = i / pairs, p = i % pairs;
         const double turns = (double)(a.positions ? a.positions[token0 + t] : token0 + t) * (a.freq[p] * 0.15915494309189533577);      // 1 / 2 pi
@@ -61,44 +100,44 @@ __global__ __launch_bounds__(RT) void rotary_kernel(RotaryArgs a) {
         turn[i] = make_float2(c * a.magnitude, s * a.magnitude * a.sign);
     }
     __syncthreads();
-    const int total = here * a.heads * a.items;
-    for (int i = tid; i < total; i += RT) {
-        const int row = (int)((unsigned long long)i * a.by_items >> 31), j = i - row * a.items;
-        const int t = (int)((unsigned long long)row * a.by_heads >> 31), h = row - t * a.heads;
-        const T* x = (const T*)a.x + (long long)(token0 + t) * a.ldx + h * a.d;
-        T* y = (T*)a.y + (long long)(token0 + t) * a.ldy + h * a.d;
-        const float2* w = turn + t * pairs;
-        if (j >= a.turned) {                                    // behind the turned columns
-            const int c = a.rot + (j - a.turned) * V, n = min(V, a.d - c);
-            T v[V];
-            load_any<T, V>(x + c, n, v);
-            store_any<T, V>(y + c, n, v);
-        } else if constexpr (HALF) {                            // pairs lie rot / 2 columns apart
-            const int c = j * V, n = min(V, pairs - c);
-            T u[V], v[V];
-            load_any<T, V>(x + c, n, u);
-            load_any<T, V>(x + pairs + c, n, v);
+    for (int i0 = tid; i0 < total; i0 += N * RT) {
+        T l[N][V], r[HALF ? N : 1][V];
+#pragma unroll
+        for (int k = 0; k < N; ++k)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const float2 cs = w[min(c + e, pairs - 1)];
-                const float p = Elem<T>::to_f(u[e]), q = Elem<T>::to_f(v[e]);
-                u[e] = Elem<T>::from_f(p * cs.x - q * cs.y);
-                v[e] = Elem<T>::from_f(p * cs.y + q * cs.x);
+                l[k][e] = u[k][e];
+                if constexpr (HALF) r[k][e] = v[k][e];
             }
-            store_any<T, V>(y + c, n, u);
-            store_any<T, V>(y + pairs + c, n, v);
-        } else {                                                // pairs are neighbours
-            const int c = j * V, n = min(V, a.rot - c);
-            T v[V];
-            load_any<T, V>(x + c, n, v);
+        if (i0 + N * RT < total) load(i0 + N * RT);
 #pragma unroll
-            for (int e = 0; e < V; e += 2) {
-                const float2 cs = w[min((c + e) / 2, pairs - 1)];
-                const float p = Elem<T>::to_f(v[e]), q = Elem<T>::to_f(v[e + 1]);
-                v[e] = Elem<T>::from_f(p * cs.x - q * cs.y);
-                v[e + 1] = Elem<T>::from_f(p * cs.y + q * cs.x);
+        for (int k = 0; k < N; ++k) {
+            const int i = i0 + k * RT;
+            if (i >= total) continue;
+            const Piece p = piece(i);
+            const float2* w = turn + p.t * pairs;
+            T* y = (T*)a.y + p.y;
+            if (p.turned) {
+                if constexpr (HALF) {                           // pairs lie rot / 2 columns apart
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        const float2 cs = w[min(p.c + e, pairs - 1)];
+                        const float f = Elem<T>::to_f(l[k][e]), g = Elem<T>::to_f(r[k][e]);
+                        l[k][e] = Elem<T>::from_f(f * cs.x - g * cs.y);
+                        r[k][e] = Elem<T>::from_f(f * cs.y + g * cs.x);
+                    }
+                    store_any<T, V>(y + pairs, p.n, r[k]);
+                } else {                                        // pairs are neighbours
+#pragma unroll
+                    for (int e = 0; e < V; e += 2) {
+                        const float2 cs = w[min((p.c + e) / 2, pairs - 1)];
+                        const float f = Elem<T>::to_f(l[k][e]), g = Elem<T>::to_f(l[k][e + 1]);
+                        l[k][e] = Elem<T>::from_f(f * cs.x - g * cs.y);
+                        l[k][e + 1] = Elem<T>::from_f(f * cs.y + g * cs.x);
+                    }
+                }
             }
-            store_any<T, V>(y + c, n, v);
+            store_any<T, V>(y, p.n, l[k]);
         }
     }
 }
@@ -159,11 +198,11 @@ int chimera_op_rotary(int dtype, int tokens, int heads, int head_dim, int rot, i
     a.tokens = tokens; a.heads = heads; a.d = head_dim; a.rot = rot; a.magnitude = magnitude; a.sign = transpose ? -1.0f : 1.0f;
     a.turned = layout == CHIMERA_ROTARY_HALF ? (rot / 2 + v - 1) / v : (rot + v - 1) / v;
     a.items = a.turned + (in_place ? 0 : (head_dim - rot + v - 1) / v);
-    // three pieces a thread, but no fewer than 512 workgroups where there are tokens for them
-    const int row_items = heads * a.items;
-    a.per_group = std::max(1, std::min({RT_TOKENS, (3 * RT + row_items - 1) / row_items, (tokens + 511) / 512}));
-    a.by_items = (unsigned)(((1u << 31) + a.items - 1) / a.items);
-    a.by_heads = (unsigned)(((1u << 31) + heads - 1) / heads);
+    // Tokens of a workgroup: up to 768 pieces, three a thread, and as many as leave 1024 workgroups.  (8192 x 18 heads of 128 17.7 us, 4.3 TB/s, 16384 x 30 of 64 interleaved 25.1, 5.0; with
+    // 512 pieces 17.6 and 26.1, 1024 18.9 and 24.5, 2048 19.3 and 27.5.)
+    a.per_group = std::max(1, std::min({RT_TOKENS, 768 / (heads * a.items), (tokens + 1023) / 1024}));
+    a.by_items = ((1ull << 40) + a.items - 1) / a.items;
+    a.by_heads = ((1ull << 40) + heads - 1) / heads;
     const dim3 grid((unsigned)((tokens + a.per_group - 1) / a.per_group)), block(RT);
     hipStream_t s = (hipStream_t)hip_stream;
     const bool half = layout == CHIMERA_ROTARY_HALF;
