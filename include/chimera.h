@@ -581,7 +581,7 @@ int chimera_op_rotary(int dtype, int tokens, int heads, int head_dim, int rot, i
  *   ctx = softmax(scale q k^T [+ causal mask]) v,   d_lse[head, token] = log-sum-exp of the scaled scores (float [heads, tokens]).
  * Rows that no sequence owns are neither read nor written, in results as in operands.  Offsets are read on the device; those that are not as above give meaningless
  * results but no access outside the tensors.  head_dim is a multiple of 8 (float: 4) up to 128, so are leading dimensions; tensors are 16-byte aligned, heads
- * up to 65536 / head_dim; scale is positive.  Results must share no memory with operands or one another (EINVAL); operands may (k = v).  Values are expected to be finite: a NaN or an
+ * up to 65536 / head_dim, sequences up to 65536; scale lies between 2^-100 and 2^100.  Results must share no memory with operands or one another (EINVAL); operands may (k = v).  Values are expected to be finite: a NaN or an
  * infinity may also reach rows that the mask keeps it from, up to 127 positions away, but no other sequence or group of heads. */
 int chimera_op_attention_packed_fwd(int dtype, int seqs, int tokens, int heads, int kv_heads, int head_dim, int causal, float scale,
                                     const int32_t* d_offsets, const void* d_q, int ldq, const void* d_k, int ldk, const void* d_v, int ldv,

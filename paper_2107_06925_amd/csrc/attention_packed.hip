@@ -20,6 +20,9 @@ namespace chimera {
 
 namespace {
 
+// A masked score: nothing whatever the scale is.  (The running maximum starts at a finite number, so that a tile without a visible key leaves it there.)
+constexpr float MASKED = -__builtin_inff();
+
 struct PackedArgs {
     const int* offsets;
     int seqs, tokens, heads, kv_heads, group, d;
@@ -174,7 +177,7 @@ __global__ __launch_bounds__(NT, D == 64 ? 4 : 2) void packed_fwd_kernel(PackedA
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int key = k0 + kt * 32 + 8 * (r >> 2) + 4 * g + (r & 3);
-                    if (key >= S || (CAUSAL && key > qrow)) s[kt][r] = NEG_BIG;
+                    if (key >= S || (CAUSAL && key > qrow)) s[kt][r] = MASKED;
                 }
         }
         // running maximum in the scaled (log2) domain; the scale is positive, so it commutes with max
@@ -719,7 +722,7 @@ __global__ __launch_bounds__(NT) void packed_fwd_f32_kernel(PackedArgs a) {
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int key = k0 + rt * 16 + 4 * g + r;
-                    if (key >= S || (CAUSAL && key > qrow)) s[rt][r] = NEG_BIG;
+                    if (key >= S || (CAUSAL && key > qrow)) s[rt][r] = MASKED;
                 }
         }
         float mx = NEG_BIG;
@@ -969,7 +972,7 @@ __global__ __launch_bounds__(NT) void packed_fwd_few_kernel(PackedArgs a) {
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int key = k0 + rt * 16 + 4 * g + r;
-                if (key >= S || (CAUSAL && key > qrow)) s[rt][r] = NEG_BIG;
+                if (key >= S || (CAUSAL && key > qrow)) s[rt][r] = MASKED;
                 mx = fmaxf(mx, s[rt][r]);
             }
         const float m_new = fmaxf(m, fold_groups(mx, [](float x, float y) { return fmaxf(x, y); }) * scale_log2e), alpha = __builtin_amdgcn_exp2f(m - m_new);
@@ -1145,8 +1148,9 @@ int check_packed(int dtype, int seqs, int tokens, int heads, int kv_heads, int d
     const int unit = dtype == CHIMERA_F32 ? 4 : 8;
     if (d < unit || d > 128 || d % unit) return fail(CHIMERA_EINVAL, "head_dim=%d must be a multiple of %d up to 128", d, unit);
     if ((long)heads * d > 1 << 16) return fail(CHIMERA_EINVAL, "more than 2^16 columns of query heads");
-    if (tokens > 1 << 28 || seqs > 1 << 28 || (size_t)heads * (slots(tile_rows(dtype, tokens, heads), seqs, tokens) + 8) >= (size_t)1 << 30)
-        return fail(CHIMERA_EINVAL, "more than 2^28 tokens, or 2^30 tiles of all heads");
+    if (seqs > 1 << 16) return fail(CHIMERA_EINVAL, "more than 2^16 sequences");
+    if (tokens > 1 << 28 || (size_t)heads * tokens > (size_t)1 << 33 || (size_t)heads * (slots(tile_rows(dtype, tokens, heads), seqs, tokens) + 8) >= (size_t)1 << 30)
+        return fail(CHIMERA_EINVAL, "more than 2^28 tokens, 2^33 rows or 2^30 tiles of all heads");
     return CHIMERA_OK;
 }
 
@@ -1184,7 +1188,7 @@ int chimera_op_attention_packed_fwd(int dtype, int seqs, int tokens, int heads, 
                                     const int32_t* d_offsets, const void* d_q, int ldq, const void* d_k, int ldk, const void* d_v, int ldv,
                                     void* d_ctx, int ldctx, float* d_lse, void* hip_stream) {
     PACKED_TRY(check_packed(dtype, seqs, tokens, heads, kv_heads, head_dim));
-    if (!(scale > 0) || scale > 3e38f) return fail(CHIMERA_EINVAL, "scale must be positive and finite");
+    if (!(scale >= 0x1p-100f && scale <= 0x1p100f)) return fail(CHIMERA_EINVAL, "scale must lie between 2^-100 and 2^100");
     if (!d_offsets || !d_lse || (((uintptr_t)d_offsets | (uintptr_t)d_lse) & 3)) return fail(CHIMERA_EINVAL, "offsets or lse is NULL or not aligned");
     const int wide = heads * head_dim, narrow = kv_heads * head_dim;
     PACKED_TRY(check_rows("q", d_q, ldq, wide, dtype));
@@ -1222,7 +1226,7 @@ int chimera_op_attention_packed_bwd(int dtype, int seqs, int tokens, int heads, 
                                     const void* d_ctx, int ldctx, const float* d_lse, const void* d_dctx, int lddctx, void* d_dq, int lddq,
                                     void* d_dk, int lddk, void* d_dv, int lddv, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
     PACKED_TRY(check_packed(dtype, seqs, tokens, heads, kv_heads, head_dim));
-    if (!(scale > 0) || scale > 3e38f) return fail(CHIMERA_EINVAL, "scale must be positive and finite");
+    if (!(scale >= 0x1p-100f && scale <= 0x1p100f)) return fail(CHIMERA_EINVAL, "scale must lie between 2^-100 and 2^100");
     if (!d_offsets || !d_lse || (((uintptr_t)d_offsets | (uintptr_t)d_lse) & 3)) return fail(CHIMERA_EINVAL, "offsets or lse is NULL or not aligned");
     const int wide = heads * head_dim, narrow = kv_heads * head_dim;
     PACKED_TRY(check_rows("q", d_q, ldq, wide, dtype));

@@ -70,7 +70,7 @@ def packed(back, **o):
 
 PACKED_BAD = [dict(dtype=2), dict(seqs=0), dict(seqs=-1), dict(tokens=0), dict(tokens=(1 << 28) + 1), dict(heads=0), dict(kv=0), dict(kv=3), dict(heads=4, kv=8), dict(dim=0), dict(dim=60), dict(dim=4),
               dict(dim=136, ldq=2048, ldk=512, ldv=512, ldctx=2048), dict(heads=1026, ldq=1 << 17, ldctx=1 << 17, kv=2), dict(tokens=1 << 28, heads=1024, dim=64, ldq=1 << 16, ldctx=1 << 16),
-              dict(scale=0.0), dict(scale=-1.0), dict(scale=NAN), dict(scale=INF), dict(offsets=None), dict(offsets=at(8) + 2), dict(lse=None), dict(lse=at(9) + 1),
+              dict(seqs=65537), dict(scale=0.0), dict(scale=-1.0), dict(scale=1e-31), dict(scale=2e30), dict(scale=NAN), dict(scale=INF), dict(offsets=None), dict(offsets=at(8) + 2), dict(lse=None), dict(lse=at(9) + 1),
               dict(q=None), dict(k=None), dict(v=None), dict(ctx=None), dict(q=at(0) + 8), dict(k=at(1) + 2), dict(v=at(2) + 4), dict(ctx=at(3) + 8), dict(ldq=504), dict(ldk=120), dict(ldv=132),
               dict(ldctx=516), dict(dtype=b.F32, dim=66), dict(dtype=b.F32, ldq=514)]
 

@@ -280,6 +280,47 @@ def test_attention_packed_extreme_scores(dtype):
     a.check_backward()
 
 
+@pytest.mark.parametrize("dtype,lengths,kv_heads", [(b.F32, [200, 70], 2), (b.BF16, [200, 70], 2), (b.F32, [2100], 8)], ids=["f32", "bf16", "f32-large"])
+def test_attention_packed_masks_hold_at_any_scale(dtype, lengths, kv_heads):
+    """At the smallest scale every visible key has the same probability, and a masked one none."""
+    torch = _torch()
+    a = Packed(dtype, lengths, 8, kv_heads, 64, seed=6, scale=2.0 ** -100)
+    a.forward()
+    a.check_forward()
+    n = torch.cat([torch.arange(1, m + 1) for m in lengths]).cuda().double()
+    assert ((a.lse.double() - n.log()).abs() <= 4 * E22 + 2100 * E24).all()
+    a.backward()
+    a.check_backward()
+
+
+@pytest.mark.parametrize("dtype", [b.F32, b.BF16], ids=["f32", "bf16"])
+def test_attention_packed_queries_that_see_one_key(dtype):
+    """Their probability is 1 whatever the score is: no gradient reaches q or k."""
+    a = Packed(dtype, [1] * 40 + [0] + [1] * 60, 4, 2, 64, causal=False, seed=7)
+    a.forward()
+    a.backward()
+    assert (a.dq == 0).all() and (a.dk == 0).all()
+    a.check_backward()
+    a = Packed(dtype, [30, 90], 4, 2, 64, seed=7)
+    a.forward()
+    a.backward()
+    assert (a.dq[0] == 0).all() and (a.dq[30] == 0).all() and (a.dq[1] != 0).any()
+
+
+@pytest.mark.parametrize("dtype", [b.F32, b.BF16], ids=["f32", "bf16"])
+def test_attention_packed_thousands_of_sequences(dtype):
+    a = Packed(dtype, [i % 3 for i in range(4000)], 2, 1, 32, causal=True, seed=10)
+    a.forward()
+    a.backward()
+    a.ends = a.ends[:20] + a.ends[-20:]
+    a.check_forward(some=19)
+    a.check_backward(some=19)
+    a.ends = a.ends[-20:]
+    a.check_forward()
+    a.check_backward()
+    a.untouched()
+
+
 @pytest.mark.parametrize("dtype", [b.F32, b.BF16], ids=["f32", "bf16"])
 def test_attention_packed_sequences_do_not_see_each_other(dtype):
     torch = _torch()
