@@ -116,13 +116,16 @@ __device__ __forceinline__ void slot_of(int bid, int units, int group, int& slot
 }
 
 // ------------------------------------------------------------------ bf16 forward
-template <int D, bool CAUSAL>
-__global__ __launch_bounds__(NT, D == 64 ? 4 : 2) void packed_fwd_kernel(PackedArgs a) {
+// TEAMS teams of four wavefronts share a workgroup's 128 queries; team i takes key tiles i, i + TEAMS, ..., and the teams' partial softmaxes are joined at the end.  Two teams
+// halve the chain of steps of a long sequence's last tile, which sets the time of a launch that the chip takes in a few rounds (see the host).
+template <int D, bool CAUSAL, int TEAMS>
+__global__ __launch_bounds__(TEAMS * NT, D == 64 ? 4 : 2) void packed_fwd_kernel(PackedArgs a) {
     constexpr int KS = D / 16, OT = D / 32;
-    __shared__ __attribute__((aligned(16))) bf16_t Ks[2][64 * D];
-    __shared__ __attribute__((aligned(16))) bf16_t Vs[2][64 * D];
+    __shared__ __attribute__((aligned(16))) bf16_t tiles[TEAMS][2][2][64 * D];          // [team][K, V][stage]
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, g = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int team = TEAMS == 1 ? 0 : __builtin_amdgcn_readfirstlane(tid / NT), wave = __builtin_amdgcn_readfirstlane(tid / WAVE % NW);
+    const bf16_t (&Ks)[2][64 * D] = tiles[team][0];
+    const bf16_t (&Vs)[2][64 * D] = tiles[team][1];
     int slot, h, begin, S, at;
     slot_of((int)blockIdx.x, a.heads, a.group, slot, h);
     if (!packed_tile<128, CAUSAL>(a.offsets, a.seqs, a.tokens, slot, lane, begin, S, at)) return;
@@ -137,8 +140,11 @@ __global__ __launch_bounds__(NT, D == 64 ? 4 : 2) void packed_fwd_kernel(PackedA
 
     const int kv_end = CAUSAL ? min(S, q0 + 128) : S;
     const int ntiles = (kv_end + 63) / 64;
-    dma_utile<D>(Kg, a.ldk, 0, S - 1, d, ks0, wave, lane);
-    dma_utile<D>(Vg, a.ldv, 0, S - 1, d, vs0, wave, lane);
+    auto fetch = [&](int t, int buf) {
+        dma_utile<D>(Kg, a.ldk, t * 64, S - 1, d, ks0 + buf * TILE_BYTES, wave, lane);
+        dma_utile<D>(Vg, a.ldv, t * 64, S - 1, d, vs0 + buf * TILE_BYTES, wave, lane);
+    };
+    if (team < ntiles) fetch(team, 0);
 
     bf16x8 qf[KS];
 #pragma unroll
@@ -156,11 +162,8 @@ __global__ __launch_bounds__(NT, D == 64 ? 4 : 2) void packed_fwd_kernel(PackedA
         const int k0 = t * 64;
         wait_vmcnt<0>();                   // this wavefront's share of tile t has landed
         __syncthreads();                   // everyone's has; and tile t-1 is consumed, so its buffer is free
-        if (t + 1 < ntiles) {
-            dma_utile<D>(Kg, a.ldk, k0 + 64, S - 1, d, ks0 + (buf ^ 1) * TILE_BYTES, wave, lane);
-            dma_utile<D>(Vg, a.ldv, k0 + 64, S - 1, d, vs0 + (buf ^ 1) * TILE_BYTES, wave, lane);
-        }
-        if (wq0 >= S || (CAUSAL && k0 > wq0 + 31)) return;           // wavefront-uniform: no query, or none that sees a key
+        if (t + TEAMS < ntiles) fetch(t + TEAMS, buf ^ 1);
+        if (t >= ntiles || wq0 >= S || (CAUSAL && k0 > wq0 + 31)) return;           // wavefront-uniform: no tile, no query, or none that sees a key
         f32x16 s[2];
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt) {
@@ -181,7 +184,7 @@ __global__ __launch_bounds__(NT, D == 64 ? 4 : 2) void packed_fwd_kernel(PackedA
                 }
         }
         // running maximum in the scaled (log2) domain; the scale is positive, so it commutes with max
-        float mx = NEG_BIG;
+        float mx = MASKED;
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
@@ -215,12 +218,36 @@ __global__ __launch_bounds__(NT, D == 64 ? 4 : 2) void packed_fwd_kernel(PackedA
                 o[t2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_ut<D>(Vs[buf], t2 * 32, J, lane), pf, o[t2], 0, 0, 0);
         }
     };
-    for (int t = 0; t < ntiles; t += 2) {
-        step(t, std::integral_constant<int, 0>{});
-        if (t + 1 < ntiles) step(t + 1, std::integral_constant<int, 1>{});
+    // (the teams meet at the same barriers: their first tiles count)
+    for (int t = 0; t < ntiles; t += 2 * TEAMS) {
+        step(t + team, std::integral_constant<int, 0>{});
+        if (t + TEAMS < ntiles) step(t + TEAMS + team, std::integral_constant<int, 1>{});
     }
 
     lsum = sum32(lsum);
+    if constexpr (TEAMS == 2) {                             // the second team's results through LDS, once every tile has been read
+        static_assert(sizeof(tiles) >= (size_t)NT * OT * 16 * 4 + 2 * NT * 4, "the place of a team's results");
+        float* at = reinterpret_cast<float*>(tiles) + (wave * OT * 16) * WAVE + lane;
+        float* stat = reinterpret_cast<float*>(tiles) + NW * OT * 16 * WAVE + wave * WAVE + lane;
+        __syncthreads();
+        if (team == 1) {
+#pragma unroll
+            for (int t2 = 0; t2 < OT; ++t2)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) at[(t2 * 16 + r) * WAVE] = o[t2][r];
+            stat[0] = m;
+            stat[NT] = lsum;
+        }
+        __syncthreads();
+        if (team == 1) return;
+        const float m1 = stat[0], m_new = fmaxf(m, m1), mine = __builtin_amdgcn_exp2f(m - m_new), other = __builtin_amdgcn_exp2f(m1 - m_new);
+        lsum = lsum * mine + stat[NT] * other;
+        m = m_new;
+#pragma unroll
+        for (int t2 = 0; t2 < OT; ++t2)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[t2][r] = o[t2][r] * mine + at[(t2 * 16 + r) * WAVE] * other;
+    }
     if (qrow < S) {
         const float inv = 1.0f / lsum;
         bf16_t* out = (bf16_t*)a.ctx + (size_t)(begin + qrow) * a.ldctx + h * d;
@@ -725,7 +752,7 @@ __global__ __launch_bounds__(NT) void packed_fwd_f32_kernel(PackedArgs a) {
                     if (key >= S || (CAUSAL && key > qrow)) s[rt][r] = MASKED;
                 }
         }
-        float mx = NEG_BIG;
+        float mx = MASKED;
 #pragma unroll
         for (int rt = 0; rt < 2; ++rt)
 #pragma unroll
@@ -966,7 +993,7 @@ __global__ __launch_bounds__(NT) void packed_fwd_few_kernel(PackedArgs a) {
         wait_vmcnt<0>();
         f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
         over_columns<D>(sm.t0[wave], q, s, l16, g);
-        float mx = NEG_BIG;
+        float mx = MASKED;
 #pragma unroll
         for (int rt = 0; rt < 2; ++rt)
 #pragma unroll
@@ -1163,12 +1190,13 @@ int check_rows(const char* what, const void* p, int ld, int cols, int dtype) {
 }
 
 #define PACKED_TRY(expr) do { int rc__ = (expr); if (rc__) return rc__; } while (0)
-#define PACKED_GO(KERNEL, D, GRID, ...) PACKED_LAUNCH((KERNEL<D, true>), (KERNEL<D, false>), GRID, __VA_ARGS__)
-#define PACKED_GO_BWD(D, F) PACKED_LAUNCH((packed_bwd_kernel<D, true, F>), (packed_bwd_kernel<D, false, F>), dq_grid + dkv_grid, a, (int)dkv_grid)
-#define PACKED_LAUNCH(CAUSAL, FULL, GRID, ...)                                                                       \
+#define PACKED_GO(KERNEL, D, GRID, ...) PACKED_LAUNCH((KERNEL<D, true>), (KERNEL<D, false>), GRID, NT, __VA_ARGS__)
+#define PACKED_GO_FWD(D, T) PACKED_LAUNCH((packed_fwd_kernel<D, true, T>), (packed_fwd_kernel<D, false, T>), grid, T * NT, a)
+#define PACKED_GO_BWD(D, F) PACKED_LAUNCH((packed_bwd_kernel<D, true, F>), (packed_bwd_kernel<D, false, F>), dq_grid + dkv_grid, NT, a, (int)dkv_grid)
+#define PACKED_LAUNCH(CAUSAL, FULL, GRID, THREADS, ...)                                                              \
     do {                                                                                                             \
-        if (causal) hipLaunchKernelGGL(CAUSAL, dim3((unsigned)(GRID)), dim3(NT), 0, s, __VA_ARGS__);                  \
-        else hipLaunchKernelGGL(FULL, dim3((unsigned)(GRID)), dim3(NT), 0, s, __VA_ARGS__);                           \
+        if (causal) hipLaunchKernelGGL(CAUSAL, dim3((unsigned)(GRID)), dim3(THREADS), 0, s, __VA_ARGS__);             \
+        else hipLaunchKernelGGL(FULL, dim3((unsigned)(GRID)), dim3(THREADS), 0, s, __VA_ARGS__);                      \
         CHIMERA_LAUNCH_CHECK("attention over packed sequences");                                                     \
     } while (0)
 
@@ -1215,8 +1243,16 @@ int chimera_op_attention_packed_fwd(int dtype, int seqs, int tokens, int heads, 
         else if (head_dim <= 96) PACKED_GO(packed_fwd_f32_kernel, 96, grid, a);
         else PACKED_GO(packed_fwd_f32_kernel, 128, grid, a);
     } else {
-        if (head_dim <= 64) PACKED_GO(packed_fwd_kernel, 64, grid, a);
-        else PACKED_GO(packed_fwd_kernel, 128, grid, a);
+        // Two teams where the chip holds all workgroups at once and sequences are not short: 2048 tokens of 16 heads of 128 in 2 sequences 31.5 -> 28.3 us, 8192 of 8 of 64 in one 120 ->
+        // 109, 12132 in 20 42.7 -> 38.0; but 4096 of 16 of 128 in 8 (640 workgroups) 31.9 -> 37.4, 4096 of 16 of 64 in 16 24.2 -> 26.3, 8192 of 25 of 64 in 21 41.7 -> 58.6.
+        const bool teams = grid <= (head_dim <= 64 ? 1024 : 512) && tokens / seqs >= 320;
+        if (head_dim <= 64) {
+            if (teams) PACKED_GO_FWD(64, 2);
+            else PACKED_GO_FWD(64, 1);
+        } else {
+            if (teams) PACKED_GO_FWD(128, 2);
+            else PACKED_GO_FWD(128, 1);
+        }
     }
     return CHIMERA_OK;
 }
