@@ -946,8 +946,10 @@ __device__ __forceinline__ void dma_few(const float* __restrict__ x, int ld, int
         lds_dma16(x + (size_t)min(row0 + row, row_last) * ld + col, lds_base + n * 1024);
     }
 }
-// the wavefront's reads of its last tile are done before the next one is asked for
+// the wavefront's reads of its last tile are done before the next one is asked for; its copies have landed before they are read (there is no barrier that would order the
+// reads behind the wait)
 __device__ __forceinline__ void wait_lds_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 // Sums over the wavefronts, in their order, of acc; wavefront w stores columns 16 t .. + 15 with t mod 4 = w.  `lds`: 4 x D x 16 floats that nobody reads any more.
 template <int D> __device__ __forceinline__ void store_few(float* lds, const f32x4 (&acc)[D / 16], float* __restrict__ row, bool ok, float scale, int d, int wave, int lane) {
     constexpr int KS = D / 16;
@@ -990,7 +992,7 @@ __global__ __launch_bounds__(NT) void packed_fwd_few_kernel(PackedArgs a) {
         wait_lds_reads();
         dma_few<D>(Kg, a.ldk, k0, S - 1, d, ks0, lane);
         dma_few<D>(Vg, a.ldv, k0, S - 1, d, vs0, lane);
-        wait_vmcnt<0>();
+        wait_copies();
         f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
         over_columns<D>(sm.t0[wave], q, s, l16, g);
         float mx = MASKED;
@@ -1057,7 +1059,7 @@ __device__ __forceinline__ void packed_dq_few(PackedFewLds<D>& sm, int bid, cons
         wait_lds_reads();
         dma_few<D>(Kg, a.ldk, k0, S - 1, d, ks0, lane);
         dma_few<D>(Vg, a.ldv, k0, S - 1, d, vs0, lane);
-        wait_vmcnt<0>();
+        wait_copies();
         f32x4 p[2], dp[2];
 #pragma unroll
         for (int rt = 0; rt < 2; ++rt) { p[rt] = f32x4{0.f, 0.f, 0.f, 0.f}; dp[rt] = f32x4{my_dl, my_dl, my_dl, my_dl}; }
@@ -1112,7 +1114,7 @@ __device__ __forceinline__ void packed_dkv_few(PackedFewLds<D>& sm, int bid, con
                 const size_t s = (size_t)h * a.tokens + min(i0 + rt * 16 + 4 * g + r, S - 1);
                 p[rt][r] = 0.f; dp[rt][r] = -delta[s]; l[rt][r] = lse[s];
             }
-        wait_vmcnt<0>();
+        wait_copies();
         over_columns<D>(sm.t0[wave], k, p, l16, g);
         over_columns<D>(sm.t1[wave], v, dp, l16, g);
 #pragma unroll

@@ -372,6 +372,42 @@ def test_attention_packed_with_equal_lengths_is_attention():
         assert rel_err(a.lse.view(heads, batch, seq).transpose(0, 1).cpu(), lse.cpu()) <= 1e-5
 
 
+@pytest.mark.parametrize("dtype", [b.F32, b.BF16], ids=["f32", "bf16"])
+def test_attention_packed_keys_that_are_values(dtype):
+    a = Packed(dtype, [150, 40], 4, 2, 64, seed=14)
+    a.v = a.k
+    a.forward()
+    a.backward()
+    a.check_forward()
+    a.check_backward()
+
+
+def test_two_calls_at_once():
+    """On two streams, with workspaces of their own, beside each other and again."""
+    torch = _torch()
+    calls = [Packed(b.BF16, [500, 300], 8, 2, 64, seed=15), Packed(b.F32, [400, 111], 4, 1, 64, seed=16)]
+    joins = [Join(b.BF16, b.F32, 900, 1024, L, R, 9, seed=17), Join(b.F32, b.F32, 1000, 520, R, L, 1, seed=18)]
+    for a in calls + joins:
+        a.forward()
+        a.backward()
+    want = [[x.clone() for x in (a.ctx, a.lse, a.drows)] for a in calls] + [[x.clone() for x in (a.y, a.h, a.dx, a.df, *a.grads.values())] for a in joins]
+    for a in calls:
+        a.results()
+    for a in joins:
+        a.reset()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for a, s in zip(calls + joins, streams * 2):
+        with torch.cuda.stream(s):
+            a.forward()
+            a.backward()
+    torch.cuda.synchronize()
+    got = [[a.ctx, a.lse, a.drows] for a in calls] + [[a.y, a.h, a.dx, a.df, *a.grads.values()] for a in joins]
+    for x, y in zip(want, got):
+        for u, v in zip(x, y):
+            assert torch.equal(u, v)
+
+
 def test_attention_packed_rows_beyond_32_bits():
     """The last rows lie more than 2^31 elements behind the first."""
     torch = _torch()
