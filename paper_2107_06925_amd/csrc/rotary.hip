@@ -43,15 +43,15 @@ template <typename T, int V> __device__ __forceinline__ void load_any(const T* p
 #pragma unroll
         for (int i = 0; i < V; ++i) out[i] = i < n ? p[i] : (T)0.f;
 }
-// (Stored past the caches' order of use: kept there, the lines push out what is still to be read.  8192 x 18 heads of 128 19.4 -> 17.7 us, and no longer with
-// attention over the result behind it; 16384 x 30 of 64 interleaved 28.2 -> 25.1.)
+// (Stores past the caches' order of use are faster alone, 8192 x 18 heads of 128 19.5 -> 18.6 us, 16384 x 30 of 64 interleaved 28.4 -> 25.8, but what is written here is read next:
+// with the projection in front and attention behind, the latter's 16384 tokens take 181 us in place of 174, 8192 of the former as long.)
 template <typename T, int V> __device__ __forceinline__ void store_any(T* p, int n, const T* v) {
     typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
     typedef u32x4 piece_t __attribute__((aligned(2)));
     if (n == V) {
         u32x4 q;
         __builtin_memcpy(&q, v, sizeof(q));
-        __builtin_nontemporal_store(q, (piece_t*)p);
+        *(piece_t*)p = q;
     } else
 #pragma unroll
         for (int i = 0; i < V; ++i)
@@ -198,8 +198,8 @@ int chimera_op_rotary(int dtype, int tokens, int heads, int head_dim, int rot, i
     a.tokens = tokens; a.heads = heads; a.d = head_dim; a.rot = rot; a.magnitude = magnitude; a.sign = transpose ? -1.0f : 1.0f;
     a.turned = layout == CHIMERA_ROTARY_HALF ? (rot / 2 + v - 1) / v : (rot + v - 1) / v;
     a.items = a.turned + (in_place ? 0 : (head_dim - rot + v - 1) / v);
-    // Tokens of a workgroup: up to 768 pieces, three a thread, and as many as leave 1024 workgroups.  (8192 x 18 heads of 128 17.7 us, 4.3 TB/s, 16384 x 30 of 64 interleaved 25.1, 5.0; with
-    // 512 pieces 17.6 and 26.1, 1024 18.9 and 24.5, 2048 19.3 and 27.5.)
+    // Tokens of a workgroup: up to 768 pieces, three a thread, and as many as leave 1024 workgroups.  (8192 x 18 heads of 128 19.5 us, 3.9 TB/s, 16384 x 30 of 64 interleaved 28.4, 4.4; with stores
+    // past the caches 768 pieces 17.7 and 25.1, 512 17.6 and 26.1, 1024 18.9 and 24.5, 2048 19.3 and 27.5.)
     a.per_group = std::max(1, std::min({RT_TOKENS, 768 / (heads * a.items), (tokens + 1023) / 1024}));
     a.by_items = ((1ull << 40) + a.items - 1) / a.items;
     a.by_heads = ((1ull << 40) + heads - 1) / heads;
