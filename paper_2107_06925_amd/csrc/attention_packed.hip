@@ -284,10 +284,10 @@ __device__ __forceinline__ bf16x8 pack8_rest(const f32x16& v, int first, const b
     return o;
 }
 
-// dQ of 128 queries (32 per wavefront), looping over 64-key tiles; forms delta of its queries and leaves it for the dK/dV kernel.
+// dQ of 128 queries (32 per wavefront), looping over 64-key tiles.  FORM_DELTA: from its queries' rows; LEAVE_DELTA: and written for the dK/dV kernel.
 //   S^T = K Q^T (keys x queries)   P = exp2(S^T c - lse2)   dP^T = V dO^T
 //   dS^T = P (dP^T - delta)        dQ^T += K^T dS^T (then * scale)
-template <int D, bool CAUSAL, bool FORM_DELTA, bool FINE>
+template <int D, bool CAUSAL, bool FORM_DELTA, bool LEAVE_DELTA, bool FINE>
 __device__ __forceinline__ void packed_dq(PackedBwdLds<D>& sm, int bid, const PackedArgs& a) {
     constexpr int KS = D / 16, OT = D / 32;
     constexpr unsigned TILE_BYTES = 64 * D * 2;
@@ -331,7 +331,7 @@ __device__ __forceinline__ void packed_dq(PackedBwdLds<D>& sm, int bid, const Pa
     const float my_lse2 = qrow < S ? a.lse[stat0 + qrow] * LOG2E : 0.f;
     if constexpr (FORM_DELTA) {
         my_dl = sum32(my_dl);                               // lanes l and l ^ 32 hold the whole row
-        if (g == 0 && qrow < S) a.delta[stat0 + qrow] = my_dl;
+        if (LEAVE_DELTA && g == 0 && qrow < S) a.delta[stat0 + qrow] = my_dl;
     } else {
         my_dl = qrow < S ? a.delta[stat0 + qrow] : 0.f;
     }
@@ -409,7 +409,7 @@ __device__ __forceinline__ void packed_dq(PackedBwdLds<D>& sm, int bid, const Pa
 // dK, dV of 128 keys (32 per wavefront), looping over the heads of the group (of this workgroup's part of it) and, in each, over 64-query tiles.
 //   S = Q K^T (queries x keys)   P = exp2(S c - lse2)     dP = dO V^T, started at -delta
 //   dS = P dP                    dV^T += dO^T P           dK^T += Q^T dS (then * scale)
-template <int D, bool CAUSAL, bool FINE>
+template <int D, bool CAUSAL, bool FORM_DELTA, bool FINE>
 __device__ __forceinline__ void packed_dkv(PackedBwdLds<D>& sm, int bid, const PackedArgs& a) {
     constexpr int KS = D / 16, OT = D / 32;
     constexpr unsigned TILE_BYTES = 64 * D * 2;
@@ -434,15 +434,29 @@ __device__ __forceinline__ void packed_dkv(PackedBwdLds<D>& sm, int bid, const P
     const int qt0 = CAUSAL ? j0 / 64 : 0;
     const int qtn = (S + 63) / 64, steps = (qtn - qt0) * hn;
     float stat = 0.f;                      // lse (threads 0..63) or -delta (threads 64..127) of the next tile
+    // FORM_DELTA: a query's delta comes from four neighbouring threads, each with a quarter of its row of dO and O
+    constexpr int DP = FORM_DELTA ? D / 32 : 1;
+    const int dl_row = tid >> 2, dl_col = (tid & 3) * (D / 4);
+    const bf16_t* Og = (const bf16_t*)a.ctx + (size_t)begin * a.ldctx + h0 * d;
+    bf16x8 od[DP], oc[DP];
     int next_t = qt0, next_h = 0;          // the tile to be fetched
     auto fetch = [&](int buf) {
         const int i0 = next_t * 64;
         dma_utile<D>(Qg + next_h * d, a.ldq, i0, S - 1, d, qs0 + buf * TILE_BYTES, wave, lane);
         dma_utile<D>(dOg + next_h * d, a.lddctx, i0, S - 1, d, os0 + buf * TILE_BYTES, wave, lane);
-        if (tid < 128) {
+        if (tid < (FORM_DELTA ? 64 : 128)) {
             const int i = i0 + (tid & 63);
             const size_t s = (size_t)next_h * a.tokens + i;
             stat = i < S ? (tid < 64 ? lse[s] * LOG2E : -delta[s]) : 0.f;
+        }
+        if constexpr (FORM_DELTA) {
+            const size_t r = (size_t)(i0 + dl_row);
+#pragma unroll
+            for (int j = 0; j < DP; ++j) {
+                const bool ok = i0 + dl_row < S && dl_col + 8 * j < d;
+                od[j] = load_frag(dOg + r * a.lddctx + next_h * d + dl_col + 8 * j, ok);
+                oc[j] = load_frag(Og + r * a.ldctx + next_h * d + dl_col + 8 * j, ok);
+            }
         }
         if (++next_t == qtn) { next_t = qt0; ++next_h; }
     };
@@ -468,7 +482,17 @@ __device__ __forceinline__ void packed_dkv(PackedBwdLds<D>& sm, int bid, const P
         if (++t == qtn) t = qt0;
         wait_vmcnt<0>();                   // this wavefront's share of the tile (and its statistics) has arrived
         if (tid < 64) sm.lse2[buf][tid] = stat;
-        else if (tid < 128) sm.dl[buf][tid - 64] = stat;
+        else if (!FORM_DELTA && tid < 128) sm.dl[buf][tid - 64] = stat;
+        if constexpr (FORM_DELTA) {
+            float v = 0.f;
+#pragma unroll
+            for (int j = 0; j < DP; ++j)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v += (float)od[j][e] * (float)oc[j][e];
+            v += dpp<0xb1>(v);
+            v += dpp<0x4e>(v);
+            if ((tid & 3) == 0) sm.dl[buf][dl_row] = -v;
+        }
         __syncthreads();                   // the tile is complete in LDS; the one before is consumed by everyone
         if (i + 1 < steps) fetch(buf ^ 1);
         const bf16_t* Qt = sm.t0[buf];
@@ -569,7 +593,7 @@ __device__ __forceinline__ void packed_dkv(PackedBwdLds<D>& sm, int bid, const P
         }
 }
 
-// delta[head, token] = rowsum(dctx ctx), for the two roles in one launch: sixteen lanes take a row of a head, 16 bytes each at a time.
+// delta[head, token] = rowsum(dctx ctx), for the two roles in one launch where they do not form it: sixteen lanes take a row of a head, 16 bytes each at a time.
 template <typename T>
 __global__ __launch_bounds__(NT) void packed_delta_kernel(PackedArgs a) {
     constexpr int V = Elem<T>::VEC;
@@ -593,23 +617,23 @@ __global__ __launch_bounds__(NT) void packed_delta_kernel(PackedArgs a) {
     if (live && lane == 0) a.delta[(size_t)h * a.tokens + row] = v;
 }
 
-// The two roles in one launch, dK/dV, whose workgroups last longest, first: the others fill what they leave.
-template <int D, bool CAUSAL, bool FINE>
+// The two roles in one launch, dK/dV, whose workgroups last longest, first: the others fill what they leave.  OWN: each forms the deltas it needs.
+template <int D, bool CAUSAL, bool OWN, bool FINE>
 __global__ __launch_bounds__(NT) void packed_bwd_kernel(PackedArgs a, int dkv) {
     __shared__ __attribute__((aligned(16))) PackedBwdLds<D> sm;
     const int bid = (int)blockIdx.x;
-    if (bid < dkv) packed_dkv<D, CAUSAL, FINE>(sm, bid, a);
-    else packed_dq<D, CAUSAL, false, FINE>(sm, bid - dkv, a);
+    if (bid < dkv) packed_dkv<D, CAUSAL, OWN, FINE>(sm, bid, a);
+    else packed_dq<D, CAUSAL, OWN, false, FINE>(sm, bid - dkv, a);
 }
 template <int D, bool CAUSAL>
 __global__ __launch_bounds__(NT) void packed_dq_kernel(PackedArgs a) {
     __shared__ __attribute__((aligned(16))) PackedBwdLds<D> sm;
-    packed_dq<D, CAUSAL, true, false>(sm, (int)blockIdx.x, a);
+    packed_dq<D, CAUSAL, true, true, false>(sm, (int)blockIdx.x, a);
 }
 template <int D, bool CAUSAL>
 __global__ __launch_bounds__(NT) void packed_dkv_kernel(PackedArgs a) {
     __shared__ __attribute__((aligned(16))) PackedBwdLds<D> sm;
-    packed_dkv<D, CAUSAL, false>(sm, (int)blockIdx.x, a);
+    packed_dkv<D, CAUSAL, false, false>(sm, (int)blockIdx.x, a);
 }
 
 // dk, dv = the sums of the parts' slabs, in the order of the parts, over the rows that sequences own.  A thread takes 4 columns of a row.
@@ -1194,7 +1218,7 @@ int check_rows(const char* what, const void* p, int ld, int cols, int dtype) {
 #define PACKED_TRY(expr) do { int rc__ = (expr); if (rc__) return rc__; } while (0)
 #define PACKED_GO(KERNEL, D, GRID, ...) PACKED_LAUNCH((KERNEL<D, true>), (KERNEL<D, false>), GRID, NT, __VA_ARGS__)
 #define PACKED_GO_FWD(D, T) PACKED_LAUNCH((packed_fwd_kernel<D, true, T>), (packed_fwd_kernel<D, false, T>), grid, T * NT, a)
-#define PACKED_GO_BWD(D, F) PACKED_LAUNCH((packed_bwd_kernel<D, true, F>), (packed_bwd_kernel<D, false, F>), dq_grid + dkv_grid, NT, a, (int)dkv_grid)
+#define PACKED_GO_BWD(D, O, F) PACKED_LAUNCH((packed_bwd_kernel<D, true, O, F>), (packed_bwd_kernel<D, false, O, F>), dq_grid + dkv_grid, NT, a, (int)dkv_grid)
 #define PACKED_LAUNCH(CAUSAL, FULL, GRID, THREADS, ...)                                                              \
     do {                                                                                                             \
         if (causal) hipLaunchKernelGGL(CAUSAL, dim3((unsigned)(GRID)), dim3(THREADS), 0, s, __VA_ARGS__);             \
@@ -1290,14 +1314,17 @@ int chimera_op_attention_packed_bwd(int dtype, int seqs, int tokens, int heads, 
     hipStream_t s = (hipStream_t)hip_stream;
     const int rows = tile_rows(dtype, tokens, heads);
     const size_t dq_grid = workgroups(slots(rows, seqs, tokens), heads, a.group), dkv_grid = workgroups(slots(rows, seqs, tokens), kv_heads * l.splits, 1);
-    // Both roles in one launch, behind one for the deltas, or, at head dims above 64 with many workgroups, dQ (which forms them) and dK/dV apart: there a SIMD holds two
+    // Both roles in one launch, behind one for the deltas (or without, below), or, at head dims above 64 with many workgroups, dQ (which forms them) and dK/dV apart: there a SIMD holds two
     // wavefronts of dQ and one of dK/dV, or of both in one launch.  8192 causal tokens of 16 heads of 128 in 2 sequences 588 us apart, 617 together; 16384 in 4 1655 and
     // 1756; 2048 in 2 107 and 84; head dim 64: 8192 tokens of 25 heads in 21 sequences 173 and 140, 16384 in 3 1949 and 1595.  Without a mask what is
     // left at the end of each launch is more: 8192 tokens of 16 heads of 128 over 2 in 2 sequences 1396 and 1289.
     const bool apart = dtype == CHIMERA_BF16 && head_dim > 64 && dq_grid >= 1024 && (causal || l.splits == 1);
     // Few rows: few terms set the error, and the launch waits for latency (1000 tokens of 16 heads in 3 sequences 45.4 -> 48.3 us at head dim 128, 32.7 -> 36.9 at 64)
     const bool fine = (size_t)tokens * heads <= 16384;
-    if (!apart) {
+    // In one launch the roles can form the deltas themselves, dK/dV a query's once per tile of keys: a launch less, which pays for short sequences (300 tokens of 8 heads of 64 in 3 20.4 -> 18.3 us,
+    // 12132 in 20 103.6 -> 99.4; but 16384 of 25 in 3 1605 -> 1736) and at head dims up to 64, where registers are left.
+    const bool own = dtype == CHIMERA_BF16 && head_dim <= 64 && tokens / seqs <= 1024;
+    if (!apart && !own) {
         const dim3 grid((unsigned)(((size_t)tokens * heads * 16 + NT - 1) / NT));
         if (dtype == CHIMERA_F32) hipLaunchKernelGGL(packed_delta_kernel<float>, grid, dim3(NT), 0, s, a);
         else hipLaunchKernelGGL(packed_delta_kernel<bf16_t>, grid, dim3(NT), 0, s, a);
@@ -1317,11 +1344,13 @@ int chimera_op_attention_packed_bwd(int dtype, int seqs, int tokens, int heads, 
         PACKED_GO(packed_dq_kernel, 128, dq_grid, a);
         PACKED_GO(packed_dkv_kernel, 128, dkv_grid, a);
     } else if (head_dim <= 64) {
-        if (fine) PACKED_GO_BWD(64, true);
-        else PACKED_GO_BWD(64, false);
+        if (own && fine) PACKED_GO_BWD(64, true, true);
+        else if (own) PACKED_GO_BWD(64, true, false);
+        else if (fine) PACKED_GO_BWD(64, false, true);
+        else PACKED_GO_BWD(64, false, false);
     } else {
-        if (fine) PACKED_GO_BWD(128, true);
-        else PACKED_GO_BWD(128, false);
+        if (fine) PACKED_GO_BWD(128, false, true);
+        else PACKED_GO_BWD(128, false, false);
     }
     if (l.splits > 1) {
         const size_t chunks = (size_t)tokens * narrow / 4;

@@ -231,7 +231,7 @@ SHORT = [0, 5, 0, 1, 64, 65, 0, 33]
 EDGES = [127, 128, 129, 32, 31]
 MANY = [(i * 37) % 23 for i in range(150)]                       # more sequences than a wavefront has lanes, some empty
 BF16_CASES = [([1], 1, 1, 8), ([1, 1, 1], 4, 4, 64), (SHORT, 6, 2, 64), (EDGES, 5, 1, 128), ([300], 8, 8, 40), (MANY, 3, 3, 64), ([0, 0, 0], 2, 1, 64), ([700, 3, 130], 16, 2, 72),
-              ([257, 511], 25, 5, 64), ([200, 90], 8, 4, 120), ([1030], 2, 1, 128)]
+              ([257, 511], 25, 5, 64), ([200, 90], 8, 4, 120), ([1030], 2, 1, 128), ([1040], 3, 1, 64), ([1200, 1000], 9, 3, 64)]
 F32_CASES = [([1], 1, 1, 4), (SHORT, 6, 2, 64), (EDGES, 5, 1, 128), ([300], 8, 8, 36), (MANY, 3, 3, 32), ([0, 0], 2, 1, 64), ([257, 40], 16, 2, 12), ([130, 90], 8, 4, 100)]
 
 
