@@ -571,7 +571,7 @@ enum {
 int chimera_rotary_frequencies(int rot, double base, int scaling, double factor, double context, double low, double high, double* h_freq);
 /* y = the turned x, both [tokens, heads, head_dim] in the given dtype with rows (tokens) ldx and ldy elements apart, of any alignment; heads lie side by side.  d_positions
  * int32 [tokens] (NULL: 0, 1, 2, ...), d_freq double [rot/2].  Angles are formed in double and off by at most 2^-51 of themselves.  y may be x itself (then
- * columns from rot on are not touched), and must share nothing with an operand otherwise (EINVAL).  heads * head_dim up to 65536. */
+ * columns from rot on are not touched), and must share nothing with an operand otherwise (EINVAL).  heads * head_dim up to 65536, tokens up to 2^28 - 16. */
 int chimera_op_rotary(int dtype, int tokens, int heads, int head_dim, int rot, int layout, int transpose, float magnitude, const int32_t* d_positions,
                       const double* d_freq, const void* d_x, int ldx, void* d_y, int ldy, void* hip_stream);
 
@@ -581,7 +581,8 @@ int chimera_op_rotary(int dtype, int tokens, int heads, int head_dim, int rot, i
  *   ctx = softmax(scale q k^T [+ causal mask]) v,   d_lse[head, token] = log-sum-exp of the scaled scores (float [heads, tokens]).
  * Rows that no sequence owns are neither read nor written, in results as in operands.  Offsets are read on the device; those that are not as above give meaningless
  * results but no access outside the tensors.  head_dim is a multiple of 8 (float: 4) up to 128, so are leading dimensions; tensors are 16-byte aligned, heads
- * up to 65536 / head_dim, sequences up to 65536; scale lies between 2^-100 and 2^100.  Results must share no memory with operands or one another (EINVAL); operands may (k = v).  Values are expected to be finite: a NaN or an
+ * up to 65536 / head_dim, sequences up to 65536, tokens up to 2^28, heads * (tokens / 128 (float: 64) + sequences + 8) below 2^23; scale lies between 2^-100 and 2^100, and scaled
+ * scores, of whose log-sum-exp a float is kept, are below 2^20 or so.  Results must share no memory with operands or one another (EINVAL); operands may (k = v).  Values are expected to be finite: a NaN or an
  * infinity may also reach rows that the mask keeps it from, up to 127 positions away, but no other sequence or group of heads. */
 int chimera_op_attention_packed_fwd(int dtype, int seqs, int tokens, int heads, int kv_heads, int head_dim, int causal, float scale,
                                     const int32_t* d_offsets, const void* d_q, int ldq, const void* d_k, int ldk, const void* d_v, int ldv,

@@ -598,11 +598,12 @@ template <typename T>
 __global__ __launch_bounds__(NT) void packed_delta_kernel(PackedArgs a) {
     constexpr int V = Elem<T>::VEC;
     const int first = min(max(a.offsets[0], 0), a.tokens), end = min(max(a.offsets[a.seqs], 0), a.tokens);
-    const size_t n = ((size_t)blockIdx.x * NT + threadIdx.x) / 16, row = n / a.heads;
-    const int h = (int)(n % a.heads), lane = threadIdx.x % 16;
-    const bool live = row >= (size_t)first && row < (size_t)end;
-    float v = 0.f;
-    if (live)
+    const int lane = threadIdx.x % 16;
+    for (size_t n = ((size_t)blockIdx.x * NT + threadIdx.x) / 16; n < (size_t)a.tokens * a.heads; n += (size_t)gridDim.x * (NT / 16)) {       // the same count for the sixteen lanes
+        const size_t row = n / a.heads;
+        const int h = (int)(n % a.heads);
+        if (row < (size_t)first || row >= (size_t)end) continue;
+        float v = 0.f;
         for (int c = lane * V; c < a.d; c += 16 * V) {
             float x[V], y[V];
             load_vec<T>((const T*)a.ctx + row * a.ldctx + h * a.d + c, x);
@@ -610,11 +611,12 @@ __global__ __launch_bounds__(NT) void packed_delta_kernel(PackedArgs a) {
 #pragma unroll
             for (int e = 0; e < V; ++e) v += x[e] * y[e];
         }
-    v += dpp<0x128>(v);
-    v += dpp<0x124>(v);
-    v += dpp<0x4e>(v);
-    v += dpp<0xb1>(v);
-    if (live && lane == 0) a.delta[(size_t)h * a.tokens + row] = v;
+        v += dpp<0x128>(v);
+        v += dpp<0x124>(v);
+        v += dpp<0x4e>(v);
+        v += dpp<0xb1>(v);
+        if (lane == 0) a.delta[(size_t)h * a.tokens + row] = v;
+    }
 }
 
 // The two roles in one launch, dK/dV, whose workgroups last longest, first: the others fill what they leave.  OWN: each forms the deltas it needs.
@@ -1202,8 +1204,9 @@ int check_packed(int dtype, int seqs, int tokens, int heads, int kv_heads, int d
     if (d < unit || d > 128 || d % unit) return fail(CHIMERA_EINVAL, "head_dim=%d must be a multiple of %d up to 128", d, unit);
     if ((long)heads * d > 1 << 16) return fail(CHIMERA_EINVAL, "more than 2^16 columns of query heads");
     if (seqs > 1 << 16) return fail(CHIMERA_EINVAL, "more than 2^16 sequences");
-    if (tokens > 1 << 28 || (size_t)heads * tokens > (size_t)1 << 33 || (size_t)heads * (slots(tile_rows(dtype, tokens, heads), seqs, tokens) + 8) >= (size_t)1 << 30)
-        return fail(CHIMERA_EINVAL, "more than 2^28 tokens, 2^33 rows or 2^30 tiles of all heads");
+    // a launch holds fewer than 2^32 threads: 2^24 workgroups of 256, both roles of the backward together
+    if (tokens > 1 << 28 || (size_t)heads * (slots(tile_rows(dtype, tokens, heads), seqs, tokens) + 8) >= (size_t)1 << 23)
+        return fail(CHIMERA_EINVAL, "more than 2^28 tokens or 2^23 tiles of all heads");
     return CHIMERA_OK;
 }
 
@@ -1325,7 +1328,7 @@ int chimera_op_attention_packed_bwd(int dtype, int seqs, int tokens, int heads, 
     // 12132 in 20 103.6 -> 99.4; but 16384 of 25 in 3 1605 -> 1736) and at head dims up to 64, where registers are left.
     const bool own = dtype == CHIMERA_BF16 && head_dim <= 64 && tokens / seqs <= 1024;
     if (!apart && !own) {
-        const dim3 grid((unsigned)(((size_t)tokens * heads * 16 + NT - 1) / NT));
+        const dim3 grid((unsigned)std::min<size_t>(((size_t)tokens * heads * 16 + NT - 1) / NT, 1 << 20));
         if (dtype == CHIMERA_F32) hipLaunchKernelGGL(packed_delta_kernel<float>, grid, dim3(NT), 0, s, a);
         else hipLaunchKernelGGL(packed_delta_kernel<bf16_t>, grid, dim3(NT), 0, s, a);
         CHIMERA_LAUNCH_CHECK("attention over packed sequences");

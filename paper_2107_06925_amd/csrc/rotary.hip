@@ -183,7 +183,8 @@ int chimera_op_rotary(int dtype, int tokens, int heads, int head_dim, int rot, i
     if (layout != CHIMERA_ROTARY_HALF && layout != CHIMERA_ROTARY_INTERLEAVED) return fail(CHIMERA_EINVAL, "unknown layout %d", layout);
     if (!std::isfinite(magnitude)) return fail(CHIMERA_EINVAL, "magnitude must be finite");
     if (!d_freq || !d_x || !d_y) return fail(CHIMERA_EINVAL, "NULL operand");
-    if (tokens > 1 << 28 || (long long)heads * head_dim > 1 << 16) return fail(CHIMERA_EINVAL, "more than 2^28 tokens or 2^16 columns");
+    constexpr int GROUPS = (1 << 24) - 1;                      // of 256 threads: a launch holds fewer than 2^32
+    if (tokens > RT_TOKENS * GROUPS || (long long)heads * head_dim > 1 << 16) return fail(CHIMERA_EINVAL, "more than %d tokens or 2^16 columns", RT_TOKENS * GROUPS);
     const int cols = heads * head_dim;
     if (ldx < cols || ldy < cols) return fail(CHIMERA_EINVAL, "leading dimension too small");
     const size_t e = dtype == CHIMERA_F32 ? 4 : 2;
@@ -200,7 +201,7 @@ int chimera_op_rotary(int dtype, int tokens, int heads, int head_dim, int rot, i
     a.items = a.turned + (in_place ? 0 : (head_dim - rot + v - 1) / v);
     // Tokens of a workgroup: up to 768 pieces, three a thread, and as many as leave 1024 workgroups.  (8192 x 18 heads of 128 19.5 us, 3.9 TB/s, 16384 x 30 of 64 interleaved 28.4, 4.4; with stores
     // past the caches 768 pieces 17.7 and 25.1, 512 17.6 and 26.1, 1024 18.9 and 24.5, 2048 19.3 and 27.5.)
-    a.per_group = std::max(1, std::min({RT_TOKENS, 768 / (heads * a.items), (tokens + 1023) / 1024}));
+    a.per_group = std::max((tokens + GROUPS - 1) / GROUPS, std::min({RT_TOKENS, 768 / (heads * a.items), (tokens + 1023) / 1024}));
     a.by_items = ((1ull << 40) + a.items - 1) / a.items;
     a.by_heads = ((1ull << 40) + heads - 1) / heads;
     const dim3 grid((unsigned)((tokens + a.per_group - 1) / a.per_group)), block(RT);

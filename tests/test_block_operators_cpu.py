@@ -103,6 +103,18 @@ def test_attention_packed_workspace_of_refused_sizes_is_zero():
         assert f(*args) == 0
 
 
+# a launch holds fewer than 2^32 threads
+@pytest.mark.parametrize("dtype,seqs,tokens,heads", [(b.BF16, 1, 1 << 27, 8), (b.F32, 1, 1 << 26, 8), (b.BF16, 1 << 16, 1 << 20, 128)])
+def test_attention_packed_refuses_more_workgroups_than_a_launch_holds(dtype, seqs, tokens, heads):
+    f = b.lib().chimera_op_attention_packed_bwd_workspace_bytes
+    assert f(dtype, seqs, tokens, heads, 2, 64) == 0 and "tiles" in b.last_error()
+    assert f(dtype, seqs, tokens, heads // 2, 2, 64) > 0
+
+
+def test_rotary_refuses_more_workgroups_than_a_launch_holds():
+    assert rotary(tokens=(1 << 28) - 15, y=at(2)) == b.EINVAL and "tokens" in b.last_error()
+
+
 FWD = ("f", "x", "gate", "g1", "b1", "g2", "b2", "y", "h", "stats")
 
 

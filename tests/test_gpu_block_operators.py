@@ -428,6 +428,30 @@ def test_attention_packed_rows_beyond_32_bits():
     a.check_backward()
 
 
+def test_attention_packed_of_more_than_2_to_the_28_rows_of_all_heads():
+    """Sixteen threads for each row of a head would be more than a launch holds."""
+    a = Packed(b.BF16, [300], 65, 13, 8, before=1 << 22, tail=2, seed=13)
+    a.forward()
+    a.backward()
+    a.check_forward()
+    a.check_backward()
+    a.untouched()
+
+
+def test_rotary_of_more_rows_than_a_launch_holds_workgroups():
+    """Where a token is enough for a workgroup, two go to each."""
+    torch = _torch()
+    tokens, heads = (1 << 24) + 100, 400
+    x = torch.zeros(tokens, heads, 2, device="cuda", dtype=torch.bfloat16)
+    x[-200:] = _randn(_gen(14), 200, heads, 2).to(torch.bfloat16)
+    last = x[-200:].clone()
+    freq = torch.full((1,), 1e-7, dtype=torch.float64, device="cuda")
+    b.chimera_op_rotary(x, x, freq)
+    want, tol = _turned(last, torch.arange(tokens - 200, tokens, device="cuda").double()[:, None] * freq, 1.0, b.ROTARY_HALF, False)
+    _within(x[-200:], want, tol + HALF[b.BF16] * want.abs(), "y")
+    assert (x[:-200] == 0).all()
+
+
 def _replayed(run, change, outputs):
     """Captures run(), replays it over inputs that change, and compares with the eager run each time."""
     torch = _torch()
